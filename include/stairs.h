@@ -41,6 +41,7 @@ extern "C" {
 
 #define STAIRS_DTYPE_FP32  0     /* matrices are float                                     */
 #define STAIRS_DTYPE_BF16  1     /* matrices are bfloat16 bit patterns (uint16_t)          */
+#define STAIRS_DTYPE_FP16  2     /* IEEE half bit patterns (operators on device buffers)   */
 
 #define STAIRS_MAX_ROWS    32    /* most rows one forward takes: k + 1 <= STAIRS_MAX_ROWS  */
 #define STAIRS_MAX_BATCH        128   /* most sequences stairs_reserve_batch makes room for          */
@@ -223,6 +224,14 @@ int draft_propose_sampled(stairs_ctx *ctx, int32_t k, float temperature, uint64_
 int stairs_verify_sampled(stairs_ctx *ctx, int32_t k, float temperature, uint64_t seed, int32_t *emitted_out,
                           int32_t *n_accepted_out, float *logits_out);
 
+/* Which tokens the sampled calls may draw (all of them after stairs_init).  A row of logits, the assistant's and the main
+ * model's alike, keeps the tokens that stairs_sample_device's top_k, top_p and min_p keep at the call's temperature, and p and q
+ * above are its probabilities over those.  top_k = 0, top_p = 1 and min_p = 0 turn a rule off; several are applied in that
+ * order.  Logits that draft_propose_sampled and stairs_verify_sampled hand out are -INFINITY at tokens not kept.
+ * Errors: EINVAL (top_k < 0, top_p outside (0, 1], min_p outside [0, 1], vocab above STAIRS_SAMPLE_MAX_VOCAB with a rule
+ * on), ESTATE (a proposal is pending). */
+int stairs_set_truncation(stairs_ctx *ctx, int32_t top_k, float top_p, float min_p);
+
 /* ---- encoder-decoder models (the model family of the paper's experiments, Sec. 2.3 / 4.3 / 4.4) -----------
  * The source text goes through the encoder once; the stair batch of Sec. 3.3 is made of prefixes of the DECODER
  * sequence, and every stair row reads the same encoder output (its per-layer cross-attention keys and values are
@@ -285,6 +294,135 @@ int32_t stairs_rel_bucket(int32_t rel, int32_t two_sided, int32_t buckets, int32
 
 /* Copy the current sequence (prompt + generated) into out[0..min(cap, len)); *len = length. */
 int stairs_get_tokens(stairs_ctx *ctx, int32_t *out, int32_t cap, int32_t *len);
+
+/* ---- operators on the caller's device buffers: paged key/value caches, drawing tokens ---------------------------------
+ * For callers that run a model's layers themselves (see stairs_gemm_device) and serve many requests from one pool of pages:
+ *   stairs_paged_plan       pages for the requests' new rows, and where each row goes
+ *   stairs_paged_append     new rows: q and k rotated, k and v into their pages
+ *   stairs_paged_attention  attention of the new rows over the pages
+ *   stairs_sample_device    a token from each row of logits
+ * A verification of k draft tokens is k + 1 new rows of a request; its rollback is a smaller `cached` in the next plan.
+ * All pointers inside the structures are DEVICE pointers the caller owns, on the device that is current and that hip_stream
+ * (a hipStream_t or NULL) belongs to; the structures themselves are host memory and may go after the call.  Calls allocate
+ * nothing, keep nothing from one call to the next, and do not wait: results are valid once the stream has reached the end of
+ * them.  All may be captured into a HIP graph.  What the device finds in index arrays is checked there: a page or slot
+ * outside the pool is neither read nor written, rows outside the buffers likewise.
+ * Errors of all of them: EINVAL (NULL, a size or type outside what is said, a pointer or stride without the alignment asked
+ * for, a stream of another device), ECAPACITY (workspace too small), EHIP. */
+
+/* The pool of one layer: n_pages pages for keys and as many for values, each holding page_size positions of n_kv_heads heads.
+ * A page is [n_kv_heads][page_size * head_dim] elements; inside a head, element (position p, dim e) of
+ *   keys   is at (((p / 16) * (head_dim / 32) + e / 32) * 64 + p % 16 + 16 * (e % 32 / 8)) * 8 + e % 8
+ *   values is at (((p / 32) * (head_dim / 16) + e / 16) * 64 + e % 16 + 16 * (p % 16 / 4)) * 8 + p % 4 + 4 * (p % 32 / 16)
+ * (the operand order of the matrix instructions: a wave reads whole tiles of 1 KiB).  Slot = page * page_size + position in it.
+ * k, v 16-byte aligned; dtype BF16 or FP16; page_size 32, 64, 128 or 256; head_dim 64 or 128; n_pages * page_size < 2^31. */
+typedef struct {
+  void *k, *v;
+  int32_t dtype, n_pages, page_size, n_kv_heads, head_dim;
+} stairs_paged_cache;
+
+#define STAIRS_PAGED_MAX_SEQS   1024
+
+/* Request b has cached[b] positions in its pages already and brings fresh[b] new rows; its pages are the first held[b]
+ * entries of block_table[b].  It needs ceil((cached + fresh) / page_size) of them.  What it holds beyond that goes back behind
+ * the *n_free free pages (request order, then block order; a request that has ended, 0 and 0, gives all back); what it lacks
+ * is taken from the end of that stack (request order).  A request whose pages, added to those of all requests in front that
+ * asked for any, exceed what is free, or that needs more than max_blocks, gets none: its seq_len is 0, its rows go
+ * nowhere, it keeps what it holds.  Requests that ask for no page always go on.  Negative counts are taken as 0.
+ *   held_out, n_free_out  pages held and free afterwards (may be held and n_free themselves)
+ *   row_start[b]          first row of request b, row_start[n_seqs] = all rows
+ *   seq_len[b]            cached + fresh
+ *   position, slot [max_rows]   of every row; -1 for rows that go nowhere and those behind the last
+ * block_table and free_pages are changed in place: entries given back stay where they were in the table, taken ones in the
+ * stack.  0 <= n_seqs <= STAIRS_PAGED_MAX_SEQS, max_blocks >= 1, max_rows >= 0; sums below 2^31. */
+typedef struct {
+  int32_t n_seqs, max_blocks, n_pages, page_size, max_rows;
+  const int32_t *cached, *fresh;   /* [n_seqs] */
+  const int32_t *held;             /* [n_seqs] */
+  const int32_t *n_free;           /* [1] */
+  int32_t *block_table;            /* [n_seqs][max_blocks] */
+  int32_t *free_pages;             /* [n_pages] */
+  int32_t *held_out, *n_free_out;
+  int32_t *row_start;              /* [n_seqs + 1] */
+  int32_t *seq_len;                /* [n_seqs] */
+  int32_t *position, *slot;        /* [max_rows] */
+} stairs_page_plan;
+int stairs_paged_plan(const stairs_page_plan *plan, void *hip_stream);
+
+/* New rows into their pages.  q [rows][n_heads][head_dim], k, v [rows][n_kv_heads][head_dim] in the cache's type, rows
+ * *_stride elements apart (slices of one projection's output, say).  With rope_theta > 0 a row's q and k are first rotated by
+ * its position: pairs (i, i + head_dim / 2) by the angle position * rope_theta^(-2 i / head_dim), formed in double.  q goes to
+ * q_out (which may be q itself with the same stride), k and v to the row's slot.  A row whose slot is outside the pool is not
+ * stored; one whose position is negative leaves q_out as it was.  n_heads = 0: k and v only.  rope_theta = 0: no rotation,
+ * position not read (q_out is written for every row, or nowhere when it is q).  Two rows of a call have different slots.
+ * Pointers 16-byte aligned, strides multiples of 8. */
+typedef struct {
+  int32_t rows, n_heads;
+  const void *q, *k, *v;
+  void *q_out;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;
+  const int32_t *position, *slot;  /* [rows] */
+  float rope_theta;
+} stairs_paged_rows;
+int stairs_paged_append(const stairs_paged_cache *cache, const stairs_paged_rows *rows, void *hip_stream);
+
+/* Attention of the new rows of n_seqs sequences over their pages (which hold the new rows' keys and values already).  Rows
+ * row_start[b] .. row_start[b + 1] - 1 are the last positions of sequence b's seq_len[b]; each sees the positions up to its own.
+ * Head h reads key head h / (n_heads / n_kv_heads).  out = softmax(scale * q . k) . v, sums and softmax in float, the
+ * probabilities rounded to the cache's type for the product with v; scale <= 0: 1 / sqrt(head_dim).  Positions whose page
+ * number lies outside the pool are not seen, and a row that sees nothing gives zeros.  Masked positions may hold anything,
+ * infinities and NaN included.  Rows of out that no sequence has are left as they were.  rows: rows of the q and out buffers;
+ * max_fresh: most rows any sequence has (only the choice of kernels depends on it).  The result does not depend on which
+ * sequences share a call only up to the last bits: the split of a long sequence follows the whole batch.
+ * workspace: stairs_paged_attention_workspace bytes (0 <= result; depends on n_heads, head_dim, n_kv_heads and max_fresh alone),
+ * 16-byte aligned, all zeros before its first use, left fit for the next call; calls that may overlap need one each.
+ * 0 <= n_seqs <= STAIRS_PAGED_MAX_SEQS; n_heads a multiple of n_kv_heads; pointers 16-byte aligned, strides multiples of 8. */
+typedef struct {
+  int32_t n_seqs, max_blocks, rows, n_heads, max_fresh;
+  const void *q;                   /* [rows][n_heads][head_dim] */
+  void *out;                       /* the same; not q */
+  int64_t q_stride, out_stride;
+  const int32_t *block_table;      /* [n_seqs][max_blocks] */
+  const int32_t *row_start;        /* [n_seqs + 1] */
+  const int32_t *seq_len;          /* [n_seqs] */
+  float scale;
+  void *workspace;
+  int64_t workspace_bytes;
+} stairs_paged_attn;
+int64_t stairs_paged_attention_workspace(const stairs_paged_cache *cache, const stairs_paged_attn *attn);
+int stairs_paged_attention(const stairs_paged_cache *cache, const stairs_paged_attn *attn, void *hip_stream);
+
+/* A token from each row of logits [rows][vocab] (FP32, BF16 or FP16; rows ld elements apart), with one uniform random number in
+ * [0, 1) a row.  Tokens are ordered by logit, larger first, equal ones by index; weight w_v = exp((x_v - max) / temperature).
+ *   1. the first top_k                       (0 or less, or vocab and more: all)
+ *   2. of these the shortest prefix that holds top_p of their weight: a token stays while the weight in front of it is below
+ *      top_p times the whole                 (1 and more: all; the first token always stays)
+ *   3. of these the tokens with w_v >= min_p (0: all; more than 1 counts as 1)
+ * and the token drawn is the lowest index at which the kept weights, summed by index, exceed uniform times their sum.
+ * Weights are formed in double and summed exactly (multiples of 2^-44 of the largest), so a row's result does not depend on the
+ * other rows or on the launch.  temperature <= 0 or NaN: the largest logit, lowest index.  Per-row arrays may be NULL: temperature 1, the
+ * rule off; uniform may be NULL only if temperature is 0 everywhere, else 0 is taken.  A NaN logit is never drawn; if a logit is +INFINITY,
+ * those alone have weight; a token whose weight is 0 in double is not kept.  A row of -INFINITY and NaN alone gives token
+ * -1, logprob -INFINITY, kept 0.  logprob (natural logarithm of the drawn token's share of the kept weight) and kept (tokens
+ * kept) may be NULL.  1 <= vocab <= STAIRS_SAMPLE_MAX_VOCAB, ld >= vocab; logits aligned to their type.
+ * workspace: stairs_sample_workspace bytes (may be 0), on the terms of stairs_paged_attention's. */
+#define STAIRS_SAMPLE_MAX_VOCAB 524288
+typedef struct {
+  int32_t dtype, rows, vocab;
+  int64_t ld;
+  const void *logits;
+  const float *temperature;        /* [rows] or NULL */
+  const int32_t *top_k;            /* [rows] or NULL */
+  const float *top_p, *min_p;      /* [rows] or NULL */
+  const float *uniform;            /* [rows] */
+  int32_t *token;                  /* [rows] */
+  float *logprob;                  /* [rows] or NULL */
+  int32_t *kept;                   /* [rows] or NULL */
+  void *workspace;
+  int64_t workspace_bytes;
+} stairs_sampling;
+int64_t stairs_sample_workspace(const stairs_sampling *sampling);
+int stairs_sample_device(const stairs_sampling *sampling, void *hip_stream);
 
 /* ---- diagnostics (kernel-level tests and roofline measurement) ------------------------ */
 

@@ -10,10 +10,10 @@ import numpy as np
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libstairs.so")
-_SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("stairs_kernels.hip", "stairs_block.hip", "stairs_api.hip")]
+_SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("stairs_kernels.hip", "stairs_block.hip", "stairs_api.hip", "stairs_paged.hip", "stairs_sampling.hip")]
 
 STAIRS_MAX_ROWS = 32
-DTYPE_FP32, DTYPE_BF16 = 0, 1
+DTYPE_FP32, DTYPE_BF16, DTYPE_FP16 = 0, 1, 2
 
 EXPORTED_SYMBOLS = [
     "stairs_strerror", "stairs_last_error", "stairs_init", "stairs_free", "stairs_prefill",
@@ -21,7 +21,9 @@ EXPORTED_SYMBOLS = [
     "stairs_get_tokens", "stairs_set_eos", "stairs_gemm_host", "stairs_gemm_device", "stairs_time_kernel", "stairs_copy_probe",
     "stairs_encdec_init", "stairs_encode", "stairs_encdec_generate",
     "stairs_decode_sampled", "stairs_generate_sampled", "draft_propose_sampled", "stairs_verify_sampled",
-    "stairs_rel_bucket",
+    "stairs_rel_bucket", "stairs_set_truncation",
+    "stairs_paged_plan", "stairs_paged_append", "stairs_paged_attention", "stairs_paged_attention_workspace",
+    "stairs_sample_device", "stairs_sample_workspace",
 ]
 
 
@@ -93,6 +95,29 @@ class StairsStats(C.Structure):
                     ms_verify=self.ms_verify, accept_hist=list(self.accept_hist))
 
 
+def _structure(name: str, doc: str, fields: str):
+    """ctypes structure of include/stairs.h: "i32 a b; ptr c" -> fields a, b, c.  Device addresses are ints (or None)."""
+    kinds = dict(i32=C.c_int32, i64=C.c_int64, f32=C.c_float, ptr=C.c_void_p)
+    members = [(n, kinds[part.split()[0]]) for part in fields.split(";") for n in part.split()[1:]]
+    return type(name, (C.Structure,), {"_fields_": members, "__doc__": doc})
+
+
+# Arguments of the operators on device buffers; build one with keyword arguments, keep it as long as its buffers stay where
+# they are.  (The buffers are the caller's: an address does not keep a tensor alive.)
+StairsPagedCache = _structure("StairsPagedCache", "stairs_paged_cache: one layer's pool of pages.",
+                              "ptr k v; i32 dtype n_pages page_size n_kv_heads head_dim")
+StairsPagePlan = _structure("StairsPagePlan", "stairs_page_plan: requests, pages and rows of a step.",
+                            "i32 n_seqs max_blocks n_pages page_size max_rows; ptr cached fresh held n_free block_table free_pages held_out "
+                            "n_free_out row_start seq_len position slot")
+StairsPagedRows = _structure("StairsPagedRows", "stairs_paged_rows: new rows to rotate and store.",
+                             "i32 rows n_heads; ptr q k v q_out; i64 q_stride k_stride v_stride q_out_stride; ptr position slot; f32 rope_theta")
+StairsPagedAttention = _structure("StairsPagedAttention", "stairs_paged_attn: attention of new rows over pages.",
+                                  "i32 n_seqs max_blocks rows n_heads max_fresh; ptr q out; i64 q_stride out_stride; ptr block_table row_start "
+                                  "seq_len; f32 scale; ptr workspace; i64 workspace_bytes")
+StairsSampling = _structure("StairsSampling", "stairs_sampling: rows of logits and the rules to draw from them.",
+                            "i32 dtype rows vocab; i64 ld; ptr logits temperature top_k top_p min_p uniform token logprob kept workspace; "
+                            "i64 workspace_bytes")
+
 _lib = None
 
 
@@ -138,9 +163,16 @@ def lib() -> C.CDLL:
     L.draft_propose_sampled.argtypes = [vp, i32, C.c_float, C.c_uint64, i32p, f32p]
     L.stairs_verify_sampled.argtypes = [vp, i32, C.c_float, C.c_uint64, i32p, i32p, f32p]
     L.stairs_encdec_generate.argtypes = [vp, i32p, i32, i32, i32, i32p, C.POINTER(StairsStats)]
+    L.stairs_set_truncation.argtypes = [vp, i32, C.c_float, C.c_float]
+    L.stairs_paged_plan.argtypes = [C.POINTER(StairsPagePlan), vp]
+    L.stairs_paged_append.argtypes = [C.POINTER(StairsPagedCache), C.POINTER(StairsPagedRows), vp]
+    L.stairs_paged_attention.argtypes = [C.POINTER(StairsPagedCache), C.POINTER(StairsPagedAttention), vp]
+    L.stairs_paged_attention_workspace.argtypes = [C.POINTER(StairsPagedCache), C.POINTER(StairsPagedAttention)]
+    L.stairs_sample_device.argtypes = [C.POINTER(StairsSampling), vp]
+    L.stairs_sample_workspace.argtypes = [C.POINTER(StairsSampling)]
     for name in EXPORTED_SYMBOLS:
         if name not in ("stairs_strerror", "stairs_last_error", "stairs_free"):
-            getattr(L, name).restype = C.c_int
+            getattr(L, name).restype = C.c_int64 if name.endswith("_workspace") else C.c_int
     _lib = L
     return L
 
@@ -329,6 +361,43 @@ def stairs_gemm_device(dtype: int, W_dev: int, X_dev: int, Y_dev: int, M: int, N
            "stairs_gemm_device")
 
 
+def stairs_paged_plan(plan: StairsPagePlan, stream: Optional[int] = None) -> None:
+    """Pages for the requests' new rows and the rows' slots; enqueued on `stream`, not waited for (as all operators on
+    device buffers)."""
+    _check(lib().stairs_paged_plan(plan, stream), "stairs_paged_plan")
+
+
+def stairs_paged_append(cache: StairsPagedCache, rows: StairsPagedRows, stream: Optional[int] = None) -> None:
+    """New rows: q and k rotated, k and v into their pages."""
+    _check(lib().stairs_paged_append(cache, rows, stream), "stairs_paged_append")
+
+
+def stairs_paged_attention(cache: StairsPagedCache, attn: StairsPagedAttention, stream: Optional[int] = None) -> None:
+    """Attention of the new rows over their sequences' pages."""
+    _check(lib().stairs_paged_attention(cache, attn, stream), "stairs_paged_attention")
+
+
+def _bytes(n: int, where: str) -> int:
+    if n < 0:
+        raise StairsError(n, where)
+    return n
+
+
+def stairs_paged_attention_workspace(cache: StairsPagedCache, attn: StairsPagedAttention) -> int:
+    """Bytes of zeroed device memory that stairs_paged_attention takes as attn.workspace."""
+    return _bytes(lib().stairs_paged_attention_workspace(cache, attn), "stairs_paged_attention_workspace")
+
+
+def stairs_sample_device(sampling: StairsSampling, stream: Optional[int] = None) -> None:
+    """A token from each row of logits."""
+    _check(lib().stairs_sample_device(sampling, stream), "stairs_sample_device")
+
+
+def stairs_sample_workspace(sampling: StairsSampling) -> int:
+    """Bytes of zeroed device memory that stairs_sample_device takes as sampling.workspace."""
+    return _bytes(lib().stairs_sample_workspace(sampling), "stairs_sample_workspace")
+
+
 def stairs_time_kernel(ctx, which: int, M: int, ctx_len: int, reps: int):
     ms, by = C.c_float(0), C.c_double(0)
     _check(lib().stairs_time_kernel(ctx, which, M, ctx_len, reps, C.byref(ms), C.byref(by)), "stairs_time_kernel", ctx)
@@ -422,6 +491,10 @@ def stairs_generate_sampled(ctx, prompt: Sequence[int], G: int, k: int, temperat
     return out[:G], st
 
 
+def stairs_set_truncation(ctx, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0):
+    _check(lib().stairs_set_truncation(ctx, top_k, top_p, min_p), "stairs_set_truncation", ctx)
+
+
 def draft_propose_sampled(ctx, k: int, temperature: float, seed: int, vocab: int = 0):
     """-> (k tokens, their logits rows [k, vocab] or None when vocab == 0)."""
     out = np.zeros(max(k, 1), np.int32)
@@ -503,6 +576,9 @@ class Stairs:
 
     def generate_sampled(self, prompt, G, k, temperature, seed):
         return stairs_generate_sampled(self.ctx, prompt, G, k, temperature, seed)
+
+    def set_truncation(self, top_k=0, top_p=1.0, min_p=0.0):
+        stairs_set_truncation(self.ctx, top_k, top_p, min_p)
 
     def propose_sampled(self, k, temperature, seed, logits=True):
         return draft_propose_sampled(self.ctx, k, temperature, seed, self.vocab if logits else 0)

@@ -107,6 +107,8 @@ struct stairs_ctx {
   SampleWs* samp_ws = nullptr;
   float *dlogits = nullptr, *lse = nullptr;
   bool pending_sampled = false;
+  int top_k = 0;               // rules of stairs_set_truncation
+  float top_p = 1.f, min_p = 0.f;
   int nchunk_cap = 0;
   int* tokens = nullptr;       // device copy of the sequence(s): [n_slots][tok_stride], capacity tok_cap each
   int tok_cap = 0, tok_stride = 0;
@@ -129,7 +131,7 @@ struct stairs_ctx {
   int pending_k = -1;          // draft length of the outstanding proposal, -1 = none
   hipEvent_t ev[16] = {};      // 0,1,2: general; 8..11, 12..15: iterations, two in flight: start / after the proposal / after
                                // validation / results on the host
-  struct IterGraph { int half, k, nch, B; hipGraphExec_t exec; };   // B = 0: the single-sequence path, -1: its sampled variant
+  struct IterGraph { int half, k, nch, B; hipGraphExec_t exec; };   // B = 0: the single-sequence path, -1: its sampled variant, -2: with truncation
   std::vector<IterGraph> graphs;   // captured iterations, see iteration_graph()
   std::vector<hipEvent_t> probe_ev;   // stairs_time_kernel(8): event pairs around one projection inside a forward
   int probe_role = -1;               // role being timed in situ, -1 = none, kProbeEmptyPair = calibration
@@ -1132,6 +1134,7 @@ int enqueue_verify(stairs_ctx* c, int k, int nch, bool in_loop) {
 
 // The two halves of a SAMPLED iteration: the assistant draws its k tokens one by one (its logits rows stay in
 // c->dlogits for the validation), then the stair batch, the rows' log-sum-exps and the keep / replace walk.
+bool truncates(const stairs_ctx* c) { return c->top_k > 0 || c->top_p < 1.f || c->min_p > 0.f; }
 int enqueue_propose_sampled(stairs_ctx* c, int k, int nch, bool embedded) {
   Model* m = &c->D;
   const int V = m->cfg.vocab;
@@ -1139,6 +1142,7 @@ int enqueue_propose_sampled(stairs_ctx* c, int k, int nch, bool embedded) {
   int rc = forward(c, m, rel_pos(c, -r1), nch, r1, 1, 0, c->dlogits, embedded);
   if (rc) return rc;
   auto decide = [&](int j) {
+    if (truncates(c)) launch_truncate(c->dlogits + (size_t)j * V, 1, V, V, c->samp, c->st);
     launch_sample(c->dlogits + (size_t)j * V, V, c->samp, 0, c->tokens, rel_pos(c, j), c->samp_ws, c->st,
                   j + 1 < k ? next_embed(c, m) : NextEmbed{});
   };
@@ -1157,6 +1161,7 @@ int enqueue_verify_sampled(stairs_ctx* c, int k, int nch, bool in_loop) {
   const int M = k + 1, V = m->cfg.vocab;
   int rc = forward(c, m, rel_pos(c, -1), nch, M, M, 0, nullptr, in_loop && k == 0);
   if (rc) return rc;
+  if (truncates(c)) launch_truncate(c->logits, M, V, V, c->samp, c->st);
   launch_row_lse(c->logits, M, c->dlogits, k, V, V, c->samp, c->lse, c->st);
   launch_accept_sampled(c->tokens, c->logits, c->dlogits, V, V, k, c->lse, c->samp, c->state, c->tgt_tok, c->samp_ws, c->st,
                         in_loop ? next_embed(c, first_model(c, k)) : NextEmbed{}, first_model_rows(c, k), host_result(c, in_loop));
@@ -1179,7 +1184,7 @@ int set_sampling(stairs_ctx* c, float temperature, uint64_t seed) {
   uint64_t z = seed + 0x9E3779B97F4A7C15ull;       // one splitmix64 step, forced odd
   z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
   z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
-  const SampleParams sp{1.0f / temperature, (z ^ (z >> 31)) | 1ull};
+  const SampleParams sp{1.0f / temperature, (z ^ (z >> 31)) | 1ull, c->top_k, c->top_p, c->min_p};
   HIPCHK(c, hipMemcpyAsync(c->samp, &sp, sizeof(sp), hipMemcpyHostToDevice, c->st));
   HIPCHK(c, hipStreamSynchronize(c->st));           // sp is on the stack
   return STAIRS_OK;
@@ -1727,7 +1732,7 @@ static int decode_loop(stairs_ctx* c, int32_t G, int32_t k, bool adaptive, int32
     if (c->use_graphs) {
       const int nch = std::min((chunks_for(L + k) + 3) / 4 * 4, c->nchunk_cap);   // never past the partial buffers
       hipGraphExec_t gp = nullptr, gv = nullptr;
-      const int gB = sampled ? -1 : 0;
+      const int gB = sampled ? (truncates(c) ? -2 : -1) : 0;
       if (k > 0 && (rc = iteration_graph(c, 0, k, nch, &gp, gB))) return rc;
       if ((rc = iteration_graph(c, 1, k, nch, &gv, gB))) return rc;
       if (k > 0) HIPCHK(c, hipGraphLaunch(gp, c->st));
@@ -1853,6 +1858,19 @@ int stairs_decode_sampled(stairs_ctx* c, int32_t G, int32_t k, float temperature
   int rc = set_sampling(c, temperature, seed);
   if (rc) return rc;
   return decode_loop(c, G, k, false, tokens_out, stats, true);
+}
+
+int stairs_set_truncation(stairs_ctx* c, int32_t top_k, float top_p, float min_p) {
+  if (!c) return STAIRS_EINVAL;
+  if (top_k < 0 || !(top_p > 0.f && top_p <= 1.f) || !(min_p >= 0.f && min_p <= 1.f))
+    return fail(c, STAIRS_EINVAL, "top_k, top_p or min_p out of range");
+  if (c->T.cfg.vocab > STAIRS_SAMPLE_MAX_VOCAB && (top_k > 0 || top_p < 1.f || min_p > 0.f))
+    return fail(c, STAIRS_EINVAL, "vocabulary too large for truncation");
+  if (c->pending_k >= 0) return fail(c, STAIRS_ESTATE, "a proposal is pending");
+  c->top_k = top_k;
+  c->top_p = top_p;
+  c->min_p = min_p;
+  return STAIRS_OK;
 }
 
 int draft_propose_sampled(stairs_ctx* c, int32_t k, float temperature, uint64_t seed, int32_t* draft_out, float* draft_logits_out) {

@@ -238,6 +238,8 @@ void launch_accept(int* tokens, const int* tgt, int k, int* state, int nslots, i
 struct SampleParams {
   float inv_temp;      // 1 / temperature
   uint64_t key;        // key of the counter-based generator (from the seed)
+  int top_k;           // rules of launch_truncate; 0, 1, 0: off
+  float top_p, min_p;
 };
 // Scratch of a draw spread over several blocks: one (score, index) per block and the ticket of the last arrival
 // (zero at allocation, zero again after every launch)
@@ -253,6 +255,8 @@ struct SampleWs {
 constexpr int kLseParts = 8;
 void launch_row_lse(const float* a, int n_a, const float* b, int n_b, int ld, int V, const SampleParams* sp, float* lse,
                     hipStream_t st);
+// -infinity at the tokens of rows [rows][ld] that the rules of *sp do not keep at its temperature (stairs_sample_device's rules)
+void launch_truncate(float* logits, int rows, int ld, int V, const SampleParams* sp, hipStream_t st);
 // tokens[o] = one draw from softmax(logits / T) by Gumbel-max with the random numbers of (o, stream), o = out_pos; next: as for
 // launch_argmax
 void launch_sample(const float* logits, int V, const SampleParams* sp, int stream, int* tokens, PosRef out_pos,
@@ -336,6 +340,9 @@ void launch_attention_flash(const float* q, const void* Kc, const void* Vc, int 
 
 // dst[0..bytes) = src[0..bytes), bytes a multiple of 16: reads `bytes` and writes `bytes` of HBM
 void launch_copy_probe(const void* src, void* dst, size_t bytes, hipStream_t st);
+
+// STAIRS_OK, or why work of the current device cannot be put on the stream: EINVAL for a stream of another one
+int check_stream(hipStream_t st);
 
 // opt in to large dynamic LDS for the kernels that need it (the first call on a device does it)
 hipError_t configure_kernels();

@@ -1,0 +1,515 @@
+"""GPU: planning pages, storing rows and attention over pages, against plain implementations in 64 bits (operators_util.py)."""
+import numpy as np
+import pytest
+
+import paper_2407_19947_amd as pkg
+import operators_util as ou
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- pages and slots -----------------------------------------------------------------------------------------------
+class Plan:
+    def __init__(self, cached, fresh, held, spare, page, max_blocks=None, max_rows=None, seed=0, n_pages=None):
+        rng = np.random.default_rng([seed, len(cached), page])
+        self.page, B = page, len(cached)
+        most = max([h for h in held] + [-(-(c + f) // page) for c, f in zip(cached, fresh)] + [1])
+        self.max_blocks = max_blocks or most
+        self.n_pages = n_pages or sum(held) + spare + 1
+        order = rng.permutation(self.n_pages)
+        self.table = np.full((B, self.max_blocks), -1, np.int32)
+        at = 0
+        for b, h in enumerate(held):
+            self.table[b, :h] = order[at:at + h]
+            at += h
+        self.free = np.full(self.n_pages, -5, np.int32)
+        self.free[:spare] = order[at:at + spare]
+        self.cached, self.fresh, self.held, self.n_free = cached, fresh, held, spare
+        self.max_rows = sum(max(f, 0) for f in fresh) + 2 if max_rows is None else max_rows
+
+    def call(self, in_place=False):
+        import torch
+        i32 = lambda v: torch.as_tensor(np.asarray(v, np.int32).reshape(-1).copy()).cuda()  # noqa: E731
+        B = len(self.cached)
+        d = dict(cached=i32(self.cached), fresh=i32(self.fresh), held=i32(self.held), n_free=i32([self.n_free]),
+                 block_table=i32(self.table), free_pages=i32(self.free), row_start=i32([-9] * (B + 1)), seq_len=i32([-9] * B),
+                 position=i32([-9] * (self.max_rows + 4)), slot=i32([-9] * (self.max_rows + 4)))
+        d["held_out"] = d["held"] if in_place else i32([-9] * B)
+        d["n_free_out"] = d["n_free"] if in_place else i32([-9])
+        p = pkg.StairsPagePlan(n_seqs=B, max_blocks=self.max_blocks, n_pages=self.n_pages, page_size=self.page, max_rows=self.max_rows,
+                               **{k: v.data_ptr() for k, v in d.items()})
+        torch.cuda.synchronize()
+        pkg.stairs_paged_plan(p, torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        return {k: v.cpu().numpy() for k, v in d.items()}
+
+    def check(self, got):
+        table, free = self.table.copy(), self.free.copy()
+        want = ou.plan_reference(self.cached, self.fresh, self.held, table, free, self.n_free, self.page, self.max_rows)
+        assert got["held_out"].tolist() == want["held"]
+        assert got["n_free_out"].tolist() == [want["n_free"]]
+        assert got["row_start"].tolist() == want["row_start"]
+        assert got["seq_len"].tolist() == want["seq_len"]
+        assert got["position"][:self.max_rows].tolist() == want["position"]
+        assert got["slot"][:self.max_rows].tolist() == want["slot"]
+        assert (got["position"][self.max_rows:] == -9).all() and (got["slot"][self.max_rows:] == -9).all()
+        assert np.array_equal(got["block_table"].reshape(table.shape), table)
+        assert np.array_equal(got["free_pages"], free)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("page", [32, 64, 128, 256])
+@pytest.mark.parametrize("B", [1, 2, 63, 64, 65, 257, 1024])
+def test_plan_of_random_requests(B, page, in_place):
+    rng = np.random.default_rng([B, page])
+    cached = rng.integers(0, 900, B)
+    fresh = np.where(rng.random(B) < 0.2, rng.integers(0, 200, B), rng.integers(0, 6, B))
+    done = rng.random(B) < 0.2
+    held = -(-rng.integers(0, 1100, B) // page)
+    cached[done] = fresh[done] = 0
+    ask = np.maximum(-(-(cached + fresh) // page) - held, 0).sum()
+    for spare in sorted({0, int(ask // 2), int(ask) + 3}):        # too few pages, half of them, enough
+        p = Plan(cached.tolist(), fresh.tolist(), held.tolist(), spare, page, seed=spare)
+        p.check(p.call(in_place))
+
+
+@pytest.mark.parametrize("cached,fresh,held,spare", [
+    ([0], [0], [0], 0), ([0], [1], [0], 1), ([0], [1], [0], 0), ([63], [1], [1], 0), ([64], [1], [1], 1), ([64], [1], [1], 0),
+    ([10, 200, 5], [3, 300, 3], [1, 4, 1], 2),                    # the middle one does not fit, the last asks for nothing
+    ([10, 200, 64], [3, 300, 3], [1, 4, 1], 3),                   # ... and the last asks for one: no overtaking
+    ([0, 100], [0, 100], [4, 2], 0),                              # what one gives back the next one takes in the same call
+    ([130], [0], [5], 1), ([-5, 7], [-3, 2], [1, 0], 2), ([1000], [5000], [16], 100)])
+def test_plan_of_chosen_requests(cached, fresh, held, spare):
+    p = Plan(cached, fresh, held, spare, 64)
+    p.check(p.call())
+
+
+def test_plan_of_no_requests_and_no_rows():
+    p = Plan([], [], [], 3, 64, max_rows=5)
+    got = p.call()
+    assert got["row_start"].tolist() == [0] and got["n_free_out"].tolist() == [3] and (got["slot"][:5] == -1).all()
+    p = Plan([5], [3], [1], 1, 64, max_rows=0)
+    p.check(p.call())
+
+
+def test_plan_of_more_rows_than_the_buffers_hold_and_more_blocks_than_the_table():
+    p = Plan([5, 70], [30, 40], [1, 2], 4, 64, max_rows=33)
+    p.check(p.call())
+    p = Plan([5, 500], [3, 40], [1, 2], 40, 64, max_blocks=4)     # the second needs 9 blocks
+    p.check(p.call())
+
+
+def test_plan_with_many_rows():
+    p = Plan([0, 5000, 17], [30000, 1, 9000], [0, 79, 1], 700, 64)
+    p.check(p.call())
+
+
+def test_plan_with_counts_that_make_no_sense_stays_in_its_buffers():
+    big = 2 ** 31 - 1
+    for cached, fresh, held, n_free in (([big, 3], [big, 2], [big, 0], 2), ([5] * 40, [big] * 40, [1] * 40, 5), ([0, 0], [1, 1], [big, big], big),
+                                        ([70, 70], [1, 1], [0, 0], -4)):
+        p = Plan([1] * len(cached), [1] * len(cached), [1] * len(cached), 4, 64, max_rows=50)
+        p.cached, p.fresh, p.held, p.n_free = cached, fresh, held, n_free
+        got = p.call()
+        assert (got["slot"] < p.n_pages * p.page).all() and 0 <= got["n_free_out"][0] <= p.n_pages
+        assert (got["position"][50:] == -9).all() and (got["slot"][50:] == -9).all()
+
+
+# ---- storing rows --------------------------------------------------------------------------------------------------
+def rotate_reference(x, position, theta):
+    """x [rows, heads, hd] in float64"""
+    hd = x.shape[-1]
+    angle = position[:, None].astype(np.float64) * theta ** (-2.0 * np.arange(hd // 2) / hd)
+    c, s = np.cos(angle)[:, None], np.sin(angle)[:, None]
+    a, b = x[..., :hd // 2], x[..., hd // 2:]
+    return np.concatenate([a * c - b * s, b * c + a * s], -1)
+
+
+def append_case(dtype, slots, Hq, Hkv, hd, page, n_pages, theta, pad=0, in_place=False, positions=None, seed=0):
+    import torch
+    dt, half = ou.torch_type(dtype), ou.HALF_STEP[dtype]
+    n = len(slots)
+    g = torch.Generator().manual_seed(seed)
+    wide = (Hq + 2 * Hkv) * hd + pad
+    qkv = torch.randn(n, wide, generator=g).to(dt)
+    K0, V0 = torch.randn(n_pages, Hkv, page * hd, generator=g).to(dt), torch.randn(n_pages, Hkv, page * hd, generator=g).to(dt)
+    pos = np.asarray(slots, np.int64) * 7 % 70000 if positions is None else np.asarray(positions, np.int64)
+    dev = dict(qkv=qkv.cuda(), k=K0.cuda(), v=V0.cuda(), pos=torch.tensor(pos, dtype=torch.int32).cuda(),
+               slot=torch.tensor(slots, dtype=torch.int32).cuda(), q_out=torch.full((n, max(Hq, 1) * hd + pad), 5.0, dtype=dt).cuda())
+    e = dev["qkv"].element_size()
+    base = dev["qkv"].data_ptr()
+    q_out, q_ld = (base, wide) if in_place else (dev["q_out"].data_ptr(), dev["q_out"].stride(0))
+    cache = pkg.StairsPagedCache(k=dev["k"].data_ptr(), v=dev["v"].data_ptr(), dtype=ou.CODE[dtype], n_pages=n_pages, page_size=page,
+                                 n_kv_heads=Hkv, head_dim=hd)
+    r = pkg.StairsPagedRows(rows=n, n_heads=Hq, q=base if Hq else None, k=base + Hq * hd * e, v=base + (Hq + Hkv) * hd * e, q_out=q_out if Hq else None,
+                            q_stride=wide, k_stride=wide, v_stride=wide, q_out_stride=q_ld, position=dev["pos"].data_ptr(),
+                            slot=dev["slot"].data_ptr(), rope_theta=theta)
+    torch.cuda.synchronize()
+    pkg.stairs_paged_append(cache, r, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+
+    x = qkv[:, :wide - pad].double().numpy()
+    q, k, v = (x[:, a * hd:b * hd].reshape(n, b - a, hd) for a, b in ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, Hq + 2 * Hkv)))
+    # rounding of the result (half of the smallest step next to 0, a subnormal half's 2^-25); the float arithmetic in front of it (sine and cosine to half a step, products and sum); the angle in
+    # double, whose power of theta has a relative error of 2^-48 (an exponent of up to 19 to 2^-53 of itself)
+    amp = lambda t: np.sqrt(t[..., :hd // 2] ** 2 + t[..., hd // 2:] ** 2)  # noqa: E731
+    far = np.abs(pos)[:, None, None] * 2.0 ** -48
+    tol = lambda t, r: half * np.abs(r) + ou.SMALLEST[dtype] + (6 * 2.0 ** -24 + far) * np.concatenate([amp(t)] * 2, -1)  # noqa: E731
+    turned = (lambda t: rotate_reference(t, pos, theta)) if theta > 0 else (lambda t: t)
+    got_q = (dev["qkv"] if in_place else dev["q_out"]).double().cpu().numpy()
+    if Hq:
+        want = turned(q)
+        gq = got_q[:, :Hq * hd].reshape(n, Hq, hd)
+        written = pos >= 0 if theta > 0 else np.ones(n, bool)
+        ou.check_close(gq[written], want[written], tol(q, want)[written])
+        assert (gq[~written] == (q[~written] if in_place else 5.0)).all()
+        if pad and not in_place:
+            assert (got_q[:, Hq * hd:] == 5.0).all()
+    K, V = K0.double().numpy(), V0.double().numpy()
+    tolK = np.zeros_like(K)
+    kt = turned(k)
+    ktol = tol(k, kt)
+    e_ = np.arange(hd)
+    for t, s in enumerate(slots):
+        if 0 <= s < n_pages * page:
+            for h in range(Hkv):
+                K[s // page, h, ou.key_at(s % page, e_, hd)] = kt[t, h]
+                tolK[s // page, h, ou.key_at(s % page, e_, hd)] = ktol[t, h] if theta > 0 else 0
+                V[s // page, h, ou.value_at(s % page, e_, hd)] = v[t, h]
+    ou.check_close(dev["k"].double().cpu().numpy(), K, tolK)
+    assert np.array_equal(dev["v"].double().cpu().numpy(), V)
+
+
+SLOT_SETS = {
+    "one": [37],
+    "run across pages": list(range(25, 25 + 77)),
+    "single rows": [5, 700, 64, 63, 31, 32, 1000, 127],
+    "backwards": list(range(90, 50, -1)),
+    "runs of all alignments": [*range(3, 9), *range(66, 67), *range(130, 147), *range(257, 262), *range(320, 384)],
+    "some nowhere": [-1, 3, 4, 5, 6, 1 << 30, 7, -2 ** 31, 40, 41, 42, 43, 2 ** 31 - 1],
+    "whole blocks": list(range(64, 64 + 128)),
+}
+
+
+@pytest.mark.parametrize("slots", SLOT_SETS, ids=lambda s: s.replace(" ", "_"))
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("Hq,Hkv,hd,page", [(4, 4, 64, 32), (8, 2, 128, 64), (3, 1, 128, 256)])
+def test_append(dtype, Hq, Hkv, hd, page, slots):
+    append_case(dtype, SLOT_SETS[slots], Hq, Hkv, hd, page, 1100 // page + 2, 10000.0)
+
+
+@pytest.mark.parametrize("theta", [0.0, 1.0, 500000.0])
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("pad", [0, 24])
+def test_append_rotations_strides_and_in_place(theta, in_place, pad):
+    append_case("bf16", SLOT_SETS["runs of all alignments"], 8, 2, 128, 64, 20, theta, pad, in_place)
+    append_case("fp16", SLOT_SETS["some nowhere"], 8, 2, 64, 32, 20, theta, pad, in_place, positions=[3, -1, 0, 5, -7, 9, 1, 2, 3, 59999, -1, 2 ** 31 - 1, 6])
+
+
+def test_append_of_keys_and_values_alone_and_of_many_heads():
+    append_case("bf16", SLOT_SETS["run across pages"], 0, 4, 128, 64, 20, 10000.0)
+    append_case("fp16", SLOT_SETS["single rows"], 96, 96, 64, 64, 20, 10000.0)
+    append_case("bf16", list(range(5, 1005)), 32, 8, 128, 128, 9, 10000.0)
+
+
+# ---- attention -----------------------------------------------------------------------------------------------------
+HEADS = [(4, 4, 64), (4, 4, 128), (8, 2, 64), (8, 2, 128), (7, 1, 128), (40, 2, 64)]
+LENS = [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200, 257]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("Hq,Hkv,hd", HEADS)
+@pytest.mark.parametrize("page", [32, 64, 256])
+def test_attention_of_single_rows_at_every_border(dtype, Hq, Hkv, hd, page):
+    a = ou.Attend(dtype, LENS, [1] * len(LENS), Hq, Hkv, hd, page)
+    a.check(a.call())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("Hq,Hkv,hd", HEADS)
+@pytest.mark.parametrize("rows", [2, 5, 9, 16, 17, 33])
+def test_attention_of_verifications(dtype, Hq, Hkv, hd, rows):
+    lens = [rows, rows + 1, 40 + rows, 100, 129, 300]
+    a = ou.Attend(dtype, lens, [rows] * len(lens), Hq, Hkv, hd, 64, seed=rows)
+    a.check(a.call())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("Hq,Hkv,hd", [(2, 2, 64), (2, 2, 128), (8, 2, 64), (8, 2, 128), (5, 1, 128)])
+@pytest.mark.parametrize("lens,fresh", [([130], [130]), ([300], [129]), ([513], [257]), ([700, 64, 333], [65, 64, 200])])
+def test_attention_of_chunks(dtype, Hq, Hkv, hd, lens, fresh):
+    a = ou.Attend(dtype, lens, fresh, Hq, Hkv, hd, 64)
+    a.check(a.call())
+
+
+@pytest.mark.parametrize("dtype,page", [("bf16", 32), ("fp16", 128)])
+def test_attention_of_a_mixed_batch(dtype, page):
+    lens = [300, 1, 77, 0, 500, 64, 33, 1000, 12, 250]
+    fresh = [200, 1, 3, 0, 1, 64, 2, 150, 0, 5]
+    a = ou.Attend(dtype, lens, fresh, 8, 2, 128, page)
+    a.check(a.call())
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,hd", [("bf16", 8, 2, 128), ("fp16", 2, 2, 64)])
+def test_attention_over_long_sequences_beside_short_ones(dtype, Hq, Hkv, hd):
+    a = ou.Attend(dtype, [20011, 3, 64, 9000, 257], [1, 3, 2, 5, 1], Hq, Hkv, hd, 128)
+    a.check(a.call())
+
+
+def test_attention_of_the_longest_sequence():
+    a = ou.Attend("fp16", [59999], [2], 2, 1, 128, 256)
+    a.check(a.call())
+
+
+def test_attention_of_many_sequences():
+    rng = np.random.default_rng(5)
+    lens = rng.integers(0, 70, 1024)
+    fresh = np.minimum(lens, rng.integers(0, 3, 1024))
+    a = ou.Attend("bf16", lens.tolist(), fresh.tolist(), 2, 1, 64, 32)
+    a.check(a.call())
+
+
+def test_attention_with_strides_scale_and_a_hint_that_is_too_small():
+    a = ou.Attend("bf16", [300, 64, 5, 900], [70, 3, 5, 300], 8, 2, 128, 64)
+    a.check(a.call(scale=0.3, q_pad=40, out_pad=8), scale=0.3)
+    for hint in (0, 1, 5000):
+        a.check(a.call(max_fresh=hint))
+
+
+@pytest.mark.parametrize("rows,lens", [(1, [40, 100, 300]), (5, [40, 100, 300]), (140, [150, 200, 300])])
+def test_rows_that_see_nothing_and_pages_that_are_none(rows, lens):
+    a = ou.Attend("bf16", lens, [rows if rows > 5 else rows] * 3, 8, 2, 128, 32)
+    a.table[0, :] = -1                                       # nothing there
+    a.table[1, 0] = a.n_pages                                # the first page is none
+    a.table[2, 1] = -2 ** 31
+    a.table[2, 3] = 2 ** 31 - 1
+    a.check(a.call())
+
+
+def test_more_rows_than_positions_and_more_positions_than_blocks():
+    a = ou.Attend("fp16", [3, 40, 200], [7, 60, 2], 8, 2, 64, 32, extra_blocks=0)
+    a.check(a.call())                                        # rows in front of position 0 see nothing
+    a = ou.Attend("fp16", [64, 100], [2, 70], 8, 2, 64, 32, extra_blocks=0)
+    a.lens = [10 ** 9, 140]                                  # behind the table's four blocks nothing is seen
+    out = a.call()
+    q, K, V = (t.double().numpy() for t in (a.q, a.K, a.V))
+    full = [128 + 2, 140]                                    # sequence 0: rows far behind everything there is; 1: positions 70 .. 139
+    ref, tol = ou.attention_reference(q, K, V, a.table, a.row_start, full, a.scale, ou.HALF_STEP["fp16"])
+    live = a.row_start[-1]
+    ou.check_close(out[:live], ref[:live], tol[:live])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("Hq,Hkv,hd,lens,fresh", [(8, 2, 128, [70, 33, 129], [5, 1, 9]), (4, 4, 64, [200, 150], [140, 150]), (8, 2, 128, [300], [130])])
+def test_masked_positions_may_hold_anything(dtype, value, Hq, Hkv, hd, lens, fresh):
+    """Behind a sequence's last position, in pages nobody has, and in later rows of the same chunk (where the row itself and
+    those behind it do see it)."""
+    import torch
+    a = ou.Attend(dtype, lens, fresh, Hq, Hkv, hd, 32)
+    for T in (a.K, a.V):
+        used = set()
+        for b, n in enumerate(lens):
+            for j in range(-(-n // 32)):
+                p = a.table[b, j]
+                used.add(int(p))
+                T[p, :, max(0, n - 32 * j):] = value
+        for p in set(range(a.n_pages)) - used:
+            T[p] = value
+    a.check(a.call())
+    for T in (a.V, a.K):
+        for b, n in enumerate(lens):
+            at = n - (fresh[b] + 1) // 2                     # the middle of the new rows
+            T[a.table[b, at // 32], 0, at % 32, 3::17] = value
+        out = a.call()
+        want, tol = a.reference()
+        for b in range(len(lens)):
+            at = fresh[b] - (fresh[b] + 1) // 2
+            early = slice(a.row_start[b], a.row_start[b] + at)
+            assert np.isfinite(out[early]).all() and (np.abs(out - want) <= tol)[early].all()
+        if T is a.V:                                         # one value that is seen makes that dimension's sums what they are
+            ok = (np.abs(out - want) <= tol) | (out == want) | (np.isnan(out) & np.isnan(want))
+            assert ok[:a.row_start[-1]].all()
+
+
+def test_scores_of_every_size():
+    """Queries that make one key win by far, scores beyond 1e4, and of one sign only."""
+    for dtype, scale in (("bf16", 300.0), ("fp16", 60.0), ("bf16", 1e-3)):
+        a = ou.Attend(dtype, [400, 65, 300], [5, 1, 140], 4, 2, 128, 64, q_scale=scale)
+        # (the float sums of scores this large move exponents: the tolerance follows from their size)
+        a.check(a.call())
+    a = ou.Attend("bf16", [300, 300], [3, 130], 4, 2, 128, 64)
+    a.q = a.q.abs() * 4
+    a.K = -a.K.abs() * 4
+    a.check(a.call())
+
+
+def test_a_cache_beyond_32_bit_offsets():
+    """Pages far into pools of more than 2^32 bytes each."""
+    import torch
+    n_pages, page, hd = 70000, 256, 128                      # 70000 x 256 x 128 x 2 bytes = 4.6 GB
+    a = ou.Attend("fp16", [600, 300], [3, 130], 2, 1, hd, page, extra_blocks=0)
+    small = a.call()
+    d = a.dev
+    K = torch.zeros(n_pages, page * hd, dtype=a.dt, device="cuda")
+    V = torch.zeros(n_pages, page * hd, dtype=a.dt, device="cuda")
+    far = n_pages - a.n_pages
+    K[far:] = d["k"].view(a.n_pages, -1)
+    V[far:] = d["v"].view(a.n_pages, -1)
+    table = torch.where(d["table"] >= 0, d["table"] + far, d["table"])
+    a.cache.k, a.cache.v, a.cache.n_pages = K.data_ptr(), V.data_ptr(), n_pages
+    a.args.block_table = table.data_ptr()
+    d["out"].fill_(7.0)
+    torch.cuda.synchronize()
+    pkg.stairs_paged_attention(a.cache, a.args, None)
+    torch.cuda.synchronize()
+    assert np.array_equal(a.result(), small)
+    rows = pkg.StairsPagedRows(rows=1, n_heads=0, k=d["q"].data_ptr(), v=d["q"].data_ptr(), k_stride=hd, v_stride=hd,
+                               slot=torch.tensor([n_pages * page - 1], dtype=torch.int32).cuda().data_ptr(), rope_theta=0.0)
+    keep = torch.tensor([n_pages * page - 1], dtype=torch.int32).cuda()
+    rows.slot = keep.data_ptr()
+    pkg.stairs_paged_append(a.cache, rows, None)
+    torch.cuda.synchronize()
+    at = torch.from_numpy(ou.key_at(page - 1, np.arange(hd), hd))
+    assert torch.equal(K[-1].cpu()[at], a.q.view(-1)[:hd])
+
+
+def test_calls_one_after_the_other_share_a_workspace_and_give_the_same_bits():
+    import torch
+    a = ou.Attend("bf16", [9000, 300, 64], [1, 5, 2], 8, 2, 128, 64)
+    b = ou.Attend("bf16", [400, 6000], [130, 300], 8, 2, 128, 64)
+    first_a, first_b = a.call(), b.call()
+    need = max(x.dev["work"].numel() for x in (a, b))
+    work = torch.zeros(need, dtype=torch.uint8).cuda()
+    for _ in range(3):
+        assert np.array_equal(a.call(workspace=work), first_a)
+        assert np.array_equal(b.call(workspace=work), first_b)
+
+
+def test_a_workspace_that_is_too_small_is_refused():
+    a = ou.Attend("bf16", [300], [1], 8, 2, 128, 64)
+    a.call()
+    need = pkg.stairs_paged_attention_workspace(a.cache, a.args)
+    if need == 0:
+        pytest.skip("no workspace needed")
+    a.args.workspace_bytes = need - 1
+    with pytest.raises(pkg.StairsError) as e:
+        pkg.stairs_paged_attention(a.cache, a.args, None)
+    assert e.value.code == -2
+    a.args.workspace_bytes, a.args.workspace = need, None
+    with pytest.raises(pkg.StairsError) as e:
+        pkg.stairs_paged_attention(a.cache, a.args, None)
+    assert e.value.code == -1
+
+
+# ---- a step as it is used --------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_iterations_of_a_server_captured_and_replayed(dtype):
+    """Plan, store, attend and draw for requests that grow by verifications, roll back, end and are replaced: every iteration
+    is one replay of a captured graph, its tensors are the program's; each result against the same steps in 64 bits."""
+    import torch
+    dt, half = ou.torch_type(dtype), ou.HALF_STEP[dtype]
+    B, Hq, Hkv, hd, page, n_pages, k, V = 5, 8, 2, 64, 32, 40, 4, 500
+    most, cap = 12, 64
+    rng = np.random.default_rng(3)
+    dev = "cuda"
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device=dev)  # noqa: E731
+    cached, fresh, held, n_free, table, free = i32(B), i32(B), i32(B), i32(1), i32(B, most), i32(n_pages)
+    free.copy_(torch.arange(n_pages, dtype=torch.int32))
+    n_free.fill_(n_pages)
+    row_start, seq_len, position, slot = i32(B + 1), i32(B), i32(cap), i32(cap)
+    qkv = torch.zeros(cap, (Hq + 2 * Hkv) * hd, dtype=dt, device=dev)
+    q_out, out = torch.zeros(cap, Hq * hd, dtype=dt, device=dev), torch.zeros(cap, Hq * hd, dtype=dt, device=dev)
+    K, Vp = torch.zeros(n_pages, Hkv, page * hd, dtype=dt, device=dev), torch.zeros(n_pages, Hkv, page * hd, dtype=dt, device=dev)
+    u, token = torch.zeros(cap, device=dev), i32(cap)
+    e, wide = qkv.element_size(), qkv.stride(0)
+    plan = pkg.StairsPagePlan(n_seqs=B, max_blocks=most, n_pages=n_pages, page_size=page, max_rows=cap, cached=cached.data_ptr(), fresh=fresh.data_ptr(),
+                              held=held.data_ptr(), n_free=n_free.data_ptr(), block_table=table.data_ptr(), free_pages=free.data_ptr(),
+                              held_out=held.data_ptr(), n_free_out=n_free.data_ptr(), row_start=row_start.data_ptr(), seq_len=seq_len.data_ptr(),
+                              position=position.data_ptr(), slot=slot.data_ptr())
+    cache = pkg.StairsPagedCache(k=K.data_ptr(), v=Vp.data_ptr(), dtype=ou.CODE[dtype], n_pages=n_pages, page_size=page, n_kv_heads=Hkv, head_dim=hd)
+    rows = pkg.StairsPagedRows(rows=cap, n_heads=Hq, q=qkv.data_ptr(), k=qkv.data_ptr() + Hq * hd * e, v=qkv.data_ptr() + (Hq + Hkv) * hd * e,
+                               q_out=q_out.data_ptr(), q_stride=wide, k_stride=wide, v_stride=wide, q_out_stride=Hq * hd,
+                               position=position.data_ptr(), slot=slot.data_ptr(), rope_theta=10000.0)
+    attn = pkg.StairsPagedAttention(n_seqs=B, max_blocks=most, rows=cap, n_heads=Hq, max_fresh=20, q=q_out.data_ptr(), out=out.data_ptr(),
+                                    q_stride=Hq * hd, out_stride=Hq * hd, block_table=table.data_ptr(), row_start=row_start.data_ptr(),
+                                    seq_len=seq_len.data_ptr(), scale=0.0)
+    work = torch.zeros(max(16, pkg.stairs_paged_attention_workspace(cache, attn)), dtype=torch.uint8, device=dev)
+    attn.workspace, attn.workspace_bytes = work.data_ptr(), work.numel()
+    draw = pkg.StairsSampling(dtype=ou.CODE[dtype], rows=cap, vocab=V, ld=Hq * hd, logits=out.data_ptr(), uniform=u.data_ptr(), token=token.data_ptr())
+    swork = torch.zeros(max(16, pkg.stairs_sample_workspace(draw)), dtype=torch.uint8, device=dev)
+    draw.workspace, draw.workspace_bytes = swork.data_ptr(), swork.numel()
+
+    def step(stream):
+        pkg.stairs_paged_plan(plan, stream)
+        pkg.stairs_paged_append(cache, rows, stream)
+        pkg.stairs_paged_attention(cache, attn, stream)
+        pkg.stairs_sample_device(draw, stream)
+
+    step(torch.cuda.current_stream().cuda_stream)                         # no requests yet: the kernels are loaded
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(torch.cuda.current_stream().cuda_stream)
+
+    history = [np.zeros((0, (Hq + 2 * Hkv) * hd)) for _ in range(B)]      # every request's rows so far, as projected
+    for it in range(14):
+        want_fresh = np.array([k + 1] * B)
+        if it == 0:
+            want_fresh[:] = rng.integers(1, 13, B)
+        if it in (5, 9):                                                  # one ends, another starts in its place later
+            history[it % B] = history[it % B][:0]
+            want_fresh[it % B] = 0
+        if it in (6, 10):
+            want_fresh[(it - 1) % B] = 11
+        have = np.array([len(h) for h in history])
+        total = int(want_fresh.sum())
+        x = torch.from_numpy(rng.standard_normal((cap, wide)).astype(np.float32)).to(dt)
+        uni = rng.random(cap).astype(np.float32)
+        qkv.copy_(x)
+        u.copy_(torch.from_numpy(uni))
+        cached.copy_(torch.from_numpy(have.astype(np.int32)))
+        fresh.copy_(torch.from_numpy(want_fresh.astype(np.int32)))
+        out.fill_(3.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        xs = x.double().numpy()
+        got = out.double().cpu().numpy().reshape(cap, Hq, hd)
+        at = 0
+        for b in range(B):
+            f = int(want_fresh[b])
+            history[b] = np.concatenate([history[b], xs[at:at + f]])
+            n = len(history[b])
+            assert int(seq_len[b]) == n
+            if f:
+                pos = np.arange(n)
+                kk = history[b][:, Hq * hd:(Hq + Hkv) * hd].reshape(n, Hkv, hd)
+                kk = torch.from_numpy(rotate_reference(kk, pos, 10000.0)).to(dt).double().numpy()
+                vv = history[b][:, (Hq + Hkv) * hd:].reshape(n, Hkv, hd)
+                qq = torch.from_numpy(rotate_reference(history[b][:, :Hq * hd].reshape(n, Hq, hd), pos, 10000.0)).to(dt).double().numpy()[n - f:]
+                # (a rounding of a rotated value that falls the other way moves a score by a step of the type at most)
+                want, tol = ou.attention_reference(qq, kk[None].transpose(0, 2, 1, 3), vv[None].transpose(0, 2, 1, 3), np.zeros((1, 1), int), [0, f], [n],
+                                                   1 / np.sqrt(hd), 4 * half)
+                ou.check_close(got[at:at + f], want, tol, (it, b))
+            at += f
+        assert (got[total:] == 3.0).all()
+        toks = token.cpu().numpy()
+        logits = out.double().cpu().numpy()
+        for t in range(total):
+            assert toks[t] == ou.sample_reference(logits[t, :V], uni[t])[0]
+        for b in range(B):                                                # roll back: some of the k drafts were not kept
+            keep = int(rng.integers(0, k + 1))
+            if want_fresh[b] == k + 1:
+                history[b] = history[b][:len(history[b]) - keep]
+    free_now = sorted(free.cpu().numpy()[:int(n_free)].tolist() + [int(p) for b in range(B) for p in table[b, :int(held[b])].tolist()])
+    assert free_now == list(range(n_pages))                               # no page lost, none twice
+
+
+def test_calls_on_a_stream_of_the_callers():
+    import torch
+    a = ou.Attend("fp16", [700, 20], [3, 20], 8, 2, 64, 32)
+    first = a.call()
+    side = torch.cuda.Stream()
+    assert np.array_equal(a.call(stream=side.cuda_stream), first)

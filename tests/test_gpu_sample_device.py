@@ -1,0 +1,204 @@
+"""GPU: drawing tokens from given uniform numbers against a plain implementation in 64 bits (operators_util.py), and the same
+rules in the sampled generation calls."""
+import numpy as np
+import pytest
+
+import paper_2407_19947_amd as pkg
+import operators_util as ou
+import synth_inputs as si
+
+pytestmark = pytest.mark.gpu
+
+
+def logits_like_a_model(n, V, seed, spread=2.0):
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(n, V, generator=g) * spread
+    at = torch.randint(0, V, (n, min(V, 12)), generator=g)
+    return x.scatter_add(1, at, torch.rand(at.shape, generator=g) * 9)
+
+
+def check(logits, dtype, u, ld=None, **rules):
+    n = logits.shape[0]
+    token, lp, kept, x = ou.sample_call(logits, dtype, u, ld=ld, **rules)
+    of = lambda name, r, off: off if rules.get(name) is None else np.broadcast_to(rules[name], (n,))[r].item()  # noqa: E731
+    u = np.broadcast_to(np.asarray(u, np.float32), (n,))
+    for r in range(n):
+        want = ou.sample_reference(x[r], u[r], float(np.float32(of("temperature", r, 1.0))), of("top_k", r, 0), of("top_p", r, 1.0), of("min_p", r, 0.0))
+        assert (int(token[r]), int(kept[r])) == (want[0], want[2]), (r, token[r], kept[r], want)
+        # half a step of float, and sums in 64 bits (weights to 2^-45 of the largest, 2^19 of them at most)
+        assert lp[r] == want[1] or abs(lp[r] - want[1]) <= 2.0 ** -24 * abs(want[1]) + 2.0 ** -25, (r, lp[r], want)
+
+
+RULES = [dict(), dict(temperature=0.7), dict(top_k=1), dict(top_k=40), dict(top_p=0.9), dict(top_p=0.2), dict(min_p=0.05), dict(min_p=1.0),
+         dict(temperature=1.3, top_k=100, top_p=0.95, min_p=0.02), dict(temperature=0.05, top_p=0.999), dict(temperature=30.0, top_k=7, top_p=0.5)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("V", [1, 2, 63, 64, 65, 1000, 1024, 1025, 4097, 32000])
+def test_every_rule(dtype, V):
+    rng = np.random.default_rng(V)
+    n = 6
+    x = logits_like_a_model(n, V, V)
+    for rules in RULES:
+        check(x, dtype, rng.random(n).astype(np.float32), **rules)
+
+
+@pytest.mark.parametrize("V", [65537, 131072, 200001, 524288])
+def test_large_vocabularies(V):
+    rng = np.random.default_rng(V)
+    x = logits_like_a_model(3, V, V)
+    for dtype in ("fp32", "bf16"):
+        for rules in (dict(), dict(top_k=50), dict(top_p=0.97), dict(temperature=1.5, top_k=5000, top_p=0.9, min_p=1e-4)):
+            check(x, dtype, rng.random(3).astype(np.float32), **rules)
+
+
+def test_rows_with_rules_of_their_own():
+    rng = np.random.default_rng(1)
+    n, V = 200, 5000
+    check(logits_like_a_model(n, V, 9), "fp32", rng.random(n).astype(np.float32), temperature=rng.choice([0.0, 0.4, 1.0, 2.0, -1.0], n).astype(np.float32),
+          top_k=rng.choice([0, 1, 5, 300, 5000, 6000, -3], n).astype(np.int32), top_p=rng.choice([0.1, 0.8, 0.99, 1.0, 2.0], n).astype(np.float32),
+          min_p=rng.choice([0.0, 0.01, 0.5, 1.0, 3.0, -1.0], n).astype(np.float32), ld=5003)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_equal_logits_are_cut_by_index(dtype):
+    import torch
+    rng = np.random.default_rng(4)
+    V = 3000
+    few = torch.from_numpy(rng.choice([-2.0, -1.0, 0.0, 0.5, 3.0], (8, V), p=[.3, .3, .2, .19, .01]).astype(np.float32))
+    for x in (few, torch.zeros(8, V), torch.full((8, V), -3.0)):
+        for rules in (dict(), dict(top_k=1), dict(top_k=17), dict(top_k=500), dict(top_p=0.3), dict(top_p=0.7, top_k=1000), dict(min_p=0.9)):
+            check(x, dtype, rng.random(8).astype(np.float32), **rules)
+    both = torch.zeros(2, 100)
+    both[:, ::2] = -0.0                                     # the two zeros are one logit
+    check(both, dtype, np.float32([0.3, 0.99]), top_k=30)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_masked_infinite_and_missing_logits(dtype):
+    import torch
+    t = ou.torch_type(dtype)
+    low = torch.finfo(t).min
+    V = 700
+    x = logits_like_a_model(9, V, 2)
+    x[0, :] = -float("inf")
+    x[1, :] = float("nan")
+    x[2, :] = low
+    x[3, 10:] = -float("inf")
+    x[4, 10:] = low
+    x[5, 5::7] = float("nan")
+    x[6, 100] = x[6, 300] = x[6, 301] = float("inf")
+    x[7, :] = -float("inf")
+    x[7, 699] = -5.0
+    x[8, ::2] = float("nan")
+    x[8, 1::2] = -float("inf")
+    for rules in (dict(), dict(top_k=2), dict(top_p=0.5), dict(min_p=0.3), dict(temperature=0.0), dict(top_k=600, top_p=0.999), dict(temperature=1e30)):
+        check(x, dtype, np.float32(0.77), **rules)
+
+
+def test_uniform_numbers_at_the_ends():
+    x = logits_like_a_model(4, 300, 1)
+    top = float(np.nextafter(np.float32(1), np.float32(0)))
+    check(x, "fp32", np.float32(0.0))
+    check(x, "fp32", np.float32(top))
+    check(x, "fp32", np.float32(top), top_k=3)
+    one, _, _, _ = ou.sample_call(x, "fp32", np.float32(1.0))
+    last, _, _, _ = ou.sample_call(x, "fp32", np.float32(top))
+    assert ((one >= 0) & (one < 300)).all() and (one >= last).all()
+    for u in (-1.0, float("nan")):                          # brought inside
+        assert np.array_equal(ou.sample_call(x, "fp32", np.float32(u))[0], ou.sample_call(x, "fp32", np.float32(0.0))[0])
+    assert np.array_equal(ou.sample_call(x, "fp32", None)[0], ou.sample_call(x, "fp32", np.float32(0.0))[0])
+
+
+def test_a_row_does_not_depend_on_the_others_and_outputs_are_optional():
+    x = logits_like_a_model(40, 3001, 8)
+    rng = np.random.default_rng(0)
+    u = rng.random(40).astype(np.float32)
+    token, lp, kept, _ = ou.sample_call(x, "bf16", u, top_p=0.9, ld=3005)
+    for r in (0, 17, 39):
+        t1, l1, k1, _ = ou.sample_call(x[r:r + 1], "bf16", u[r:r + 1], top_p=0.9)
+        assert (t1[0], l1[0], k1[0]) == (token[r], lp[r], kept[r])
+    only, none, nothing, _ = ou.sample_call(x, "bf16", u, top_p=0.9, want=())
+    assert np.array_equal(only, token) and none is None and nothing is None
+
+
+def test_drawn_tokens_follow_the_probabilities():
+    """Evenly spaced numbers: each token's count is its share to within one, by the definition."""
+    import torch
+    n, V = 4096, 50
+    x = logits_like_a_model(1, V, 3).expand(n, V).contiguous()
+    u = ((np.arange(n) + 0.5) / n).astype(np.float32)
+    token, _, _, _ = ou.sample_call(x, "fp32", u, top_k=20, temperature=0.8)
+    keep, w = ou.keep_reference(x[0].double().numpy(), float(np.float32(0.8)), 20)
+    share = np.where(keep, w, 0) / np.where(keep, w, 0).sum()
+    assert (np.abs(np.bincount(token, minlength=V) - n * share) <= 1.0 + 1e-6).all()
+
+
+# ---- the rules in the sampled generation calls ------------------------------------------------------------------------
+def _pair():
+    w = si.scaled_workload("cfg1_tiny_fp32", G=24)
+    return (*si.make_pair(w), si.make_prompt(w), w)
+
+
+RULE_SETS = [dict(top_k=5), dict(top_p=0.5), dict(min_p=0.3), dict(top_k=50, top_p=0.9, min_p=0.05)]
+
+
+@pytest.mark.parametrize("rules", RULE_SETS, ids=str)
+def test_proposals_and_verifications_keep_what_the_rules_keep(rules):
+    target, draft, prompt, w = _pair()
+    T, k = 0.9, 4
+    with pkg.Stairs(target, draft, k_max=k, max_seq=w["P"] + 80) as s:
+        s.prefill(prompt)
+        s.propose_sampled(k, T, 11)
+        free_target = s.verify_sampled(k, T, 11)[2]                      # the same position without rules
+        s.prefill(prompt)
+        s.set_truncation(**rules)
+        d, dl = s.propose_sampled(k, T, 11)
+        emitted, n, tl = s.verify_sampled(k, T, 11)
+        first = ou.keep_reference(free_target[0].astype(np.float64), 1 / float(np.float32(1) / np.float32(T)), rules.get("top_k", 0), rules.get("top_p", 1.0),
+                                  rules.get("min_p", 0.0))[0]
+        assert np.array_equal(tl[0] > -np.inf, first) and np.array_equal(tl[0][first], free_target[0][first])
+        for rows, tokens in ((dl, d), (tl[:n + 1], emitted)):
+            for r, t in enumerate(tokens):
+                assert rows[r, t] > -np.inf
+                assert rows[r].max() > -np.inf and (rows[r] > -np.inf).sum() >= 1
+                if rules.get("top_k"):
+                    assert (rows[r] > -np.inf).sum() <= rules["top_k"]
+        assert np.all(emitted[:n] == d[:n])
+
+
+@pytest.mark.parametrize("k", [0, 3])
+def test_generation_with_rules(k):
+    """Graphs and single launches give the same tokens, a repeated call too; one token is greedy decoding; rules turned off
+    again give what they gave before they were on."""
+    target, draft, prompt, w = _pair()
+    G = 24
+    with pkg.Stairs(target, draft, k_max=4, max_seq=w["P"] + G + 8) as s:
+        plain, _ = s.generate_sampled(prompt, G, k, 0.8, 5)
+        s.set_truncation(top_k=20, top_p=0.9)
+        one, _ = s.generate_sampled(prompt, G, k, 0.8, 5)
+        two, _ = s.generate_sampled(prompt, G, k, 0.8, 5)
+        assert np.array_equal(one, two)
+        s.set_truncation(top_k=1)
+        greedy, _ = s.generate(prompt, G, 0)
+        only, _ = s.generate_sampled(prompt, G, k, 0.8, 5)
+        assert np.array_equal(only, greedy)
+        s.set_truncation()
+        assert np.array_equal(s.generate_sampled(prompt, G, k, 0.8, 5)[0], plain)
+
+
+def test_rules_that_are_refused():
+    target, draft, prompt, w = _pair()
+    with pkg.Stairs(target, draft, k_max=4, max_seq=w["P"] + 40) as s:
+        for bad in (dict(top_k=-1), dict(top_p=0.0), dict(top_p=1.5), dict(top_p=float("nan")), dict(min_p=-0.1), dict(min_p=1.1), dict(min_p=float("nan"))):
+            with pytest.raises(pkg.StairsError) as e:
+                s.set_truncation(**bad)
+            assert e.value.code == -1
+        s.prefill(prompt)
+        s.propose_sampled(2, 1.0, 1)
+        with pytest.raises(pkg.StairsError) as e:
+            s.set_truncation(top_k=3)
+        assert e.value.code == -3
+        s.verify_sampled(2, 1.0, 1)
+        s.set_truncation(top_k=3)
