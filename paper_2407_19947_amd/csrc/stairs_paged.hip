@@ -4,7 +4,10 @@
 #include "../../include/stairs.h"
 #include "stairs_device.h"
 
+#include <algorithm>
 #include <cmath>
+#include <cstdint>
+#include <type_traits>
 
 namespace stairs {
 namespace {
@@ -192,52 +195,412 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
 // ---------------------------------------------------------------------------------------
 // attention
 // ---------------------------------------------------------------------------------------
-// a wave per row and head: 64 keys at a time, a lane a key; then a lane HD / 64 dims of the values
-template <typename T, int HD>
-__global__ __launch_bounds__(64) void k_paged_attend(stairs_paged_cache c, stairs_paged_attn a, float scale) {
-  __shared__ float s_q[HD];
-  __shared__ float s_p[64];
-  const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
-  if (t < a.row_start[0] || t >= a.row_start[a.n_seqs]) return;
-  const int b = find_seq(a.row_start, a.n_seqs, t);
-  const int last = min(a.seq_len[b] - (a.row_start[b + 1] - t), a.max_blocks * c.page_size - 1);   // last position the row may see
-  const int kvh = h / (a.n_heads / c.n_kv_heads);
-  for (int e = lane; e < HD; e += 64) s_q[e] = scale * Elem<T>::up(static_cast<const T*>(a.q)[(size_t)t * a.q_stride + h * HD + e]);
-  __syncthreads();
-  const size_t head_elems = (size_t)c.page_size * HD, page_elems = head_elems * c.n_kv_heads;
-  const T* K = static_cast<const T*>(c.k) + kvh * head_elems;
-  const T* V = static_cast<const T*>(c.v) + kvh * head_elems;
-  const int* table = a.block_table + (size_t)b * a.max_blocks;
-  float m = -INFINITY, l = 0.f, o[HD / 64] = {};
-  for (int k0 = 0; k0 <= last; k0 += 64) {
-    const int key = k0 + lane, blk = key / c.page_size;
-    const int page = key <= last && blk < a.max_blocks ? table[blk] : -1;
-    float x = -INFINITY;
-    if ((unsigned)page < (unsigned)c.n_pages) {
-      const T* kp = K + page * page_elems;
-      x = 0.f;
-      for (int e = 0; e < HD; ++e) x += s_q[e] * Elem<T>::up(kp[k_cache_off(key % c.page_size, e, HD)]);
-    }
-    const float mn = fmaxf(m, wave_max(x));
-    const float keep = mn == -INFINITY ? 0.f : expf(m - mn), pr = mn == -INFINITY ? 0.f : expf(x - mn);
-    m = mn;
-    l = l * keep + wave_sum(pr);
-    __syncthreads();
-    s_p[lane] = x == -INFINITY ? -1.f : Elem<T>::up(Elem<T>::down(pr));
-    __syncthreads();
+// A tile is up to 16 CT columns of one key head of one sequence; a column is (row, query head of the group), so that heads that
+// share keys share the loads.  Scores are computed transposed, S^T = K Q^T: a lane then holds the scores of ONE column for 8 of 32
+// keys, which are already the operand O^T = V^T P^T wants from it (the value tiles are laid out for that order of keys), so the
+// probabilities never leave their registers, and maximum and sum are per lane but for two exchanges between lane groups.
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kMaxSlack = 8.f;      // the running maximum follows once a score exceeds it by 2^8: sums and rounded
+                                      // probabilities keep their relative precision whatever the reference point is
+
+// (a lane's value, those of the lanes 16, 32 and 48 further) -> the largest / the sum, in all four
+__device__ __forceinline__ float groups_max(float v) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float groups_sum(float v) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Whether any of the eight halves of v is an infinity or not a number: exponent bits all ones, found by one carry
+template <typename T>
+__device__ __forceinline__ uint32_t odd_bits(uint32_t u) {
+  constexpr uint32_t m = sizeof(T) == 2 && __is_same(T, __bf16) ? 0x7F807F80u : 0x7C007C00u, one = __is_same(T, __bf16) ? 0x00800080u : 0x04000400u;
+  return ((u & m) + one) & 0x80008000u;
+}
+
+// Takes the infinities and NaNs out of a pair of values and says what they were: 1 for +infinity, 64 for -infinity, 4096 for NaN.
+// Summed over the keys that a column sees (32 at most, so the three counts stay apart) they say what belongs in its sum.
+template <typename T>
+__device__ __forceinline__ uint32_t take_odd(uint32_t& v) {
+  constexpr bool b = __is_same(T, __bf16);
+  constexpr uint32_t inf = b ? 0x7F80u : 0x7C00u, one = b ? 0x3F80u : 0x3C00u, k64 = b ? 0x4280u : 0x5400u, k4096 = b ? 0x4580u : 0x6C00u;
+  uint32_t kinds = 0, left = 0;
 #pragma unroll
-    for (int i = 0; i < HD / 64; ++i) o[i] *= keep;
-    for (int j = 0; j < 64; ++j) {
-      const float pj = s_p[j];
-      if (pj < 0.f) continue;                      // not seen: its values may be anything
-      const int k = k0 + j;
-      const T* vp = V + table[k / c.page_size] * page_elems;
-#pragma unroll
-      for (int i = 0; i < HD / 64; ++i) o[i] += pj * Elem<T>::up(vp[v_cache_off(k % c.page_size, i * 64 + lane, HD)]);
+  for (int h = 0; h < 32; h += 16) {
+    const uint32_t x = (v >> h) & 0xFFFFu, m = x & 0x7FFFu;
+    kinds |= (m < inf ? 0u : m > inf ? k4096 : x > m ? k64 : one) << h;
+    left |= (m < inf ? x : 0u) << h;
+  }
+  v = left;
+  return kinds;
+}
+__device__ __forceinline__ float odd_value(float n) {
+  const int c = (int)n;
+  return (c & 63 ? INFINITY : 0.f) + (c & (63 << 6) ? -INFINITY : 0.f) + (c >> 12 ? __uint_as_float(0x7FC00000u) : 0.f);
+}
+
+// ---- which piece of the work a work-group takes -------------------------------------------------------------------
+// The lengths are on the device, so the split is made there, by every wave for itself (64 sequences at a time, a lane each; no
+// memory but the counts): a tile's keys are cut into pieces of `per` units so that all pieces together are about `slots`, the
+// work-groups that run at once.  Then one long sequence among short ones is spread over the chip, and a batch that fills it is not
+// split at all.  Work-group i takes key head i % n_kv_heads (neighbouring work-groups go to different XCDs: with 8 key heads and
+// more a head's work-groups share an L2).
+struct Span {
+  int min_cols, max_cols;     // sequences with so many columns (rows times heads a key head has)
+  int tile_cols, unit;        // columns of a tile, keys of a unit
+  int slots;
+};
+constexpr int kMaxPieces = 64;        // of a tile: whoever joins them reads them all
+struct Piece {
+  int seq, row0, rows, len;   // rows of the sequence, its length (not cut to the table)
+  int group, piece, pieces;   // tile of the sequence, piece of the tile
+  int u0, u1;                 // its units
+  int first;                  // number of the tile's first piece among the pieces of split tiles
+  int kvh;
+};
+struct SeqWork { int row0, rows, len, groups, units; };
+__device__ __forceinline__ SeqWork seq_work(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, int b) {
+  SeqWork w{0, 0, 0, 0, 0};
+  if (b < a.n_seqs) {
+    w.row0 = a.row_start[b];
+    w.rows = a.row_start[b + 1] - w.row0;
+    w.len = a.seq_len[b];
+    const long long cols = (long long)w.rows * (a.n_heads / c.n_kv_heads);
+    if (w.row0 >= 0 && w.rows > 0 && w.rows <= a.rows - w.row0 && cols >= sp.min_cols && cols <= sp.max_cols) {
+      w.groups = (int)((cols + sp.tile_cols - 1) / sp.tile_cols);
+      w.units = (min(max(w.len, 0), a.max_blocks * c.page_size) + sp.unit - 1) / sp.unit;
     }
   }
-  for (int i = 0; i < HD / 64; ++i)
-    static_cast<T*>(a.out)[(size_t)t * a.out_stride + h * HD + i * 64 + lane] = Elem<T>::down(l == 0.f ? 0.f : o[i] / l);
+  return w;
+}
+template <typename T>
+__device__ __forceinline__ T wave_scan(T v) {                  // inclusive
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const T o = __shfl_up(v, off);
+    if (lane >= off) v += o;
+  }
+  return v;
+}
+__device__ __forceinline__ bool find_piece(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, Piece& out) {
+  const int lane = threadIdx.x & 63;
+  const int kvh = blockIdx.x % c.n_kv_heads, item = blockIdx.x / c.n_kv_heads;
+  long long units = 0;
+  SeqWork w;
+  for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
+    w = seq_work(c, a, sp, b0 + lane);
+    units += (long long)w.groups * w.units;
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) units += __shfl_xor(units, off);
+  const int per = __builtin_amdgcn_readfirstlane(max(2, (int)((units * c.n_kv_heads + sp.slots - 1) / sp.slots)));
+  int before = 0, split_before = 0;
+  for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
+    if (b0 > 0 || a.n_seqs > 64) w = seq_work(c, a, sp, b0 + lane);
+    const int pieces = min(kMaxPieces, max(1, (w.units + per - 1) / per));
+    const int mine = w.groups * pieces, split = pieces > 1 ? mine : 0;
+    const int to = before + wave_scan(mine), split_to = split_before + wave_scan(split);
+    const unsigned long long there = __ballot(to > item);
+    if (there) {
+      const int l = __builtin_ctzll(there);
+      const int at = item - (__builtin_amdgcn_readlane(to, l) - __builtin_amdgcn_readlane(mine, l));
+      out.seq = b0 + l;
+      out.row0 = __builtin_amdgcn_readlane(w.row0, l);
+      out.rows = __builtin_amdgcn_readlane(w.rows, l);
+      out.len = __builtin_amdgcn_readlane(w.len, l);
+      out.pieces = __builtin_amdgcn_readlane(pieces, l);
+      out.group = at / out.pieces;
+      out.piece = at - out.group * out.pieces;
+      const int u = __builtin_amdgcn_readlane(w.units, l);
+      out.u0 = (int)((long long)u * out.piece / out.pieces);
+      out.u1 = (int)((long long)u * (out.piece + 1) / out.pieces);
+      out.first = (__builtin_amdgcn_readlane(split_to, l) - __builtin_amdgcn_readlane(split, l) + out.group * out.pieces) * c.n_kv_heads + kvh;
+      out.kvh = kvh;
+      return true;
+    }
+    before = __builtin_amdgcn_readlane(to, 63);
+    split_before = __builtin_amdgcn_readlane(split_to, 63);
+  }
+  return false;
+}
+// a split tile's pieces are numbered first + piece * n_kv_heads; all of them together are at most this many: a split
+// sequence has more units than `per`, so fewer than 2 units / per pieces
+__host__ __device__ constexpr int most_pieces(int slots) { return 2 * slots; }
+
+// ---- joining ------------------------------------------------------------------------------------------------------------
+// Partial results of a piece: [tile_cols][HD] outputs relative to the column's maximum, then [tile_cols] (maximum, sum) pairs.
+template <int HD>
+__host__ __device__ constexpr size_t piece_floats(int tile_cols) { return (size_t)tile_cols * (HD + 2); }
+
+template <typename T, int HD>
+__device__ __forceinline__ void store_out(const stairs_paged_cache& c, const stairs_paged_attn& a, const Piece& w, int col, int e, float4 v, float l) {
+  const int G = a.n_heads / c.n_kv_heads, r = col / G;
+  const float f = l == 0.f ? 0.f : 1.f / l;                      // (0: the row has seen nothing)
+  T out[4] = {Elem<T>::down(v.x * f), Elem<T>::down(v.y * f), Elem<T>::down(v.z * f), Elem<T>::down(v.w * f)};
+  *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + (size_t)(w.row0 + r) * a.out_stride + (w.kvh * G + col - r * G) * HD + e) =
+      *reinterpret_cast<const uint2*>(out);
+}
+__device__ __forceinline__ float weight_of(float m, float all) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - all); }
+
+// the last of a split tile's work-groups joins its pieces, in their order whoever it is
+template <typename T, int HD>
+__device__ __forceinline__ void join_pieces(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, const Piece& w, int* s_last) {
+  int* counter = static_cast<int*>(a.workspace) + w.first;
+  if (!last_arrival(counter, w.pieces, s_last)) return;
+  const size_t step = piece_floats<HD>(sp.tile_cols) * c.n_kv_heads;
+  const float* base = reinterpret_cast<const float*>(static_cast<int*>(a.workspace) + most_pieces(sp.slots)) + (size_t)w.first * piece_floats<HD>(sp.tile_cols);
+  const int G = a.n_heads / c.n_kv_heads, col0 = w.group * sp.tile_cols, cols = min(sp.tile_cols, w.rows * G - col0);
+  for (int i = threadIdx.x; i < cols * (HD / 4); i += blockDim.x) {
+    const int col = i / (HD / 4), e = i % (HD / 4) * 4;
+    const float* ml = base + sp.tile_cols * HD + col * 2;
+    float m = -INFINITY;
+    for (int p = 0; p < w.pieces; ++p) m = fmaxf(m, ld_dev(ml + p * step));
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+#pragma unroll 4
+    for (int p = 0; p < w.pieces; ++p) {
+      const float2 pm = ld_dev2(ml + p * step), x = ld_dev2(base + p * step + col * HD + e), y = ld_dev2(base + p * step + col * HD + e + 2);
+      const float f = weight_of(pm.x, m);
+      l += f * pm.y;
+      v.x += f * x.x;
+      v.y += f * x.y;
+      v.z += f * y.x;
+      v.w += f * y.y;
+    }
+    store_out<T, HD>(c, a, w, col0 + col, e, v, l);
+  }
+  if (threadIdx.x == 0) *counter = 0;
+}
+
+// the four waves' results of a piece -> the output, or a partial result
+template <typename T, int HD, int COLS>
+__device__ __forceinline__ void join_waves(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, const Piece& w,
+                                           float (*s_o)[COLS][HD + 4], float (*s_m)[COLS], float (*s_l)[COLS], int* s_last) {
+  const int G = a.n_heads / c.n_kv_heads, col0 = w.group * COLS, cols = min(COLS, w.rows * G - col0);
+  float* part = reinterpret_cast<float*>(static_cast<int*>(a.workspace) + most_pieces(sp.slots)) +
+                (size_t)(w.first + w.piece * c.n_kv_heads) * piece_floats<HD>(COLS);
+  for (int i = threadIdx.x; i < cols * (HD / 4); i += 256) {
+    const int col = i / (HD / 4), e = i % (HD / 4) * 4;
+    const float m = fmaxf(fmaxf(s_m[0][col], s_m[1][col]), fmaxf(s_m[2][col], s_m[3][col]));
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float f = weight_of(s_m[k][col], m);
+      const float4 x = *reinterpret_cast<const float4*>(&s_o[k][col][e]);
+      l += f * s_l[k][col];
+      v.x += f * x.x;
+      v.y += f * x.y;
+      v.z += f * x.z;
+      v.w += f * x.w;
+    }
+    if (w.pieces == 1) {
+      store_out<T, HD>(c, a, w, col0 + col, e, v, l);
+    } else {
+      st_dev2(part + col * HD + e, v.x, v.y);
+      st_dev2(part + col * HD + e + 2, v.z, v.w);
+      if (e == 0) st_dev2(part + COLS * HD + col * 2, m, l);
+    }
+  }
+  if (w.pieces > 1) join_pieces<T, HD>(c, a, sp, w, s_last);
+}
+
+// ---- few columns: a wave per 32 keys ----------------------------------------------------------------------------------
+// Bound by the bytes of the cache.  A work-group takes a piece of a tile of 16 CT columns; its four waves take 32-key blocks in
+// turn, straight from memory into the matrix operands (a block of a head is 2 x 64 HD contiguous bytes, every load 1 KiB of a
+// wave), no LDS, and are joined at the end.  Values are requested before the scores they wait for, the next block's keys as
+// soon as this block's are used.
+constexpr int kRowUnit = 128;
+template <typename T, int HD, int CT>
+__global__ __launch_bounds__(256, CT == 1 ? 3 : 2) void k_paged_rows(stairs_paged_cache c, stairs_paged_attn a, Span sp, float scale2) {
+  typedef typename Elem<T>::x8 x8;
+  constexpr int KK = HD / 32, ET = HD / 16, LD = HD + 4;
+  __shared__ float s_o[4][16 * CT][LD];
+  __shared__ float s_m[4][16 * CT], s_l[4][16 * CT];
+  __shared__ int s_last;
+  Piece w;
+  if (!find_piece(c, a, sp, w)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, g = lane >> 4;
+  const int G = a.n_heads / c.n_kv_heads, cols = w.rows * G, col0 = w.group * 16 * CT;
+  const int limit = a.max_blocks * c.page_size;
+  const int pos0 = w.len - w.rows;                              // position of the sequence's first row
+  const int first_last = min(pos0 + col0 / G, limit - 1);        // last position the tile's first and last column see
+  const int last_last = min(pos0 + (min(cols, col0 + 16 * CT) - 1) / G, limit - 1);
+  int last[CT];
+  x8 q[CT][KK];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int col = col0 + ct * 16 + j;
+    last[ct] = -1;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) q[ct][kk] = x8{};
+    if (col < cols) {
+      const int r = col / G;
+      last[ct] = min(pos0 + r, limit - 1);
+      const T* qp = static_cast<const T*>(a.q) + (size_t)(w.row0 + r) * a.q_stride + (w.kvh * G + col - r * G) * HD + g * 8;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) q[ct][kk] = *reinterpret_cast<const x8*>(qp + kk * 32);
+    }
+  }
+  f32x4 o[CT][ET];
+  float m[CT], l[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    m[ct] = -INFINITY;
+    l[ct] = 0.f;
+#pragma unroll
+    for (int et = 0; et < ET; ++et) o[ct][et] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const size_t head_elems = (size_t)c.page_size * HD, page_elems = head_elems * c.n_kv_heads;
+  const T* K = static_cast<const T*>(c.k) + w.kvh * head_elems;
+  const T* V = static_cast<const T*>(c.v) + w.kvh * head_elems;
+  const int* table = a.block_table + (size_t)w.seq * a.max_blocks;
+  const int ps_shift = __builtin_ctz(c.page_size);
+
+  // the wave's blocks: unit u's block is keys 128 u + 32 wave ..; page numbers 64 units at a time, a lane each
+  int pages = -1, pages_at = w.u0;
+  const int u1 = min(w.u1, last_last < 0 ? 0 : (last_last - 32 * wave) / kRowUnit + (last_last >= 32 * wave));
+  auto fetch_pages = [&](int u) {
+    pages_at = u;
+    const int key = (u + lane) * kRowUnit + wave * 32;
+    pages = u + lane < u1 ? table[key >> ps_shift] : -1;
+    if ((unsigned)pages >= (unsigned)c.n_pages) pages = -1;
+  };
+  auto next_block = [&](int u) {                                // the first unit from u on that has a page
+    for (;;) {
+      if (u >= u1) return u1;
+      if (u >= pages_at + 64) fetch_pages(u);
+      const unsigned long long there = __ballot(pages >= 0) & (~0ull << (u - pages_at));
+      if (there) return pages_at + (int)__builtin_ctzll(there);
+      u = pages_at + 64;
+    }
+  };
+  uint4 kf[2 * KK], vf[ET];
+  auto block_at = [&](int u) -> size_t {                        // elements in front of the block in its pool
+    const int key = u * kRowUnit + wave * 32;
+    return (size_t)__builtin_amdgcn_readlane(pages, u - pages_at) * page_elems + (size_t)(key & (c.page_size - 1)) * HD;
+  };
+  auto load_keys = [&](size_t at) {
+#pragma unroll
+    for (int i = 0; i < 2 * KK; ++i) kf[i] = *reinterpret_cast<const uint4*>(K + at + (i * 64 + lane) * 8);
+  };
+  if (w.u0 < u1) fetch_pages(w.u0);
+  int u = next_block(w.u0);
+  size_t at = 0;
+  if (u < u1) {
+    at = block_at(u);
+    load_keys(at);
+  }
+  while (u < u1) {
+#pragma unroll
+    for (int i = 0; i < ET; ++i) vf[i] = *reinterpret_cast<const uint4*>(V + at + (i * 64 + lane) * 8);
+    f32x4 s[CT][2];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        s[ct][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) s[ct][t] = mma(__builtin_bit_cast(x8, kf[t * KK + kk]), q[ct][kk], s[ct][t]);
+      }
+    const int key0 = u * kRowUnit + wave * 32;
+    const int un = next_block(u + 1);
+    if (un < u1) {
+      at = block_at(un);
+      load_keys(at);
+    }
+    const bool full = key0 + 31 <= first_last;
+    x8 p[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = s[ct][i >> 2][i & 3] * scale2;
+      if (!full) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = key0 + (i >> 2) * 16 + g * 4 + (i & 3) <= last[ct] ? x[i] : -INFINITY;
+      }
+      float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      if (__any(mx > m[ct] + kMaxSlack)) {
+        const float mn = fmaxf(m[ct], groups_max(mx));
+        const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[ct] - mn);
+        m[ct] = mn;
+        l[ct] *= f;
+#pragma unroll
+        for (int et = 0; et < ET; ++et) o[ct][et] *= f;
+      }
+      const float mr = m[ct] == -INFINITY ? 0.f : m[ct];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] = __builtin_amdgcn_exp2f(x[i] - mr);
+        l[ct] += x[i];
+        p[ct][i] = Elem<T>::down(x[i]);
+      }
+    }
+    if (!full) {
+      // Some keys of the block are not seen by all columns.  Their probability is 0, and 0 times what is there must be 0: what
+      // no column sees is cleared, an infinity or NaN that some columns see is taken out and given to those that do.
+      uint32_t keep[4], odd = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = key0 + (i >> 1) * 16 + g * 4 + (i & 1) * 2;
+        keep[i] = (key <= last_last ? 0xFFFFu : 0u) | (key + 1 <= last_last ? 0xFFFF0000u : 0u);
+      }
+#pragma unroll
+      for (int et = 0; et < ET; ++et) {
+        uint4& v = vf[et];
+        v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
+        odd |= odd_bits<T>(v.x) | odd_bits<T>(v.y) | odd_bits<T>(v.z) | odd_bits<T>(v.w);
+      }
+      if (__any(odd != 0)) {
+        x8 seen[CT];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) seen[ct][i] = key0 + (i >> 2) * 16 + g * 4 + (i & 3) <= last[ct] ? (T)1.f : (T)0.f;
+#pragma unroll
+        for (int et = 0; et < ET; ++et) {
+          __builtin_amdgcn_sched_barrier(0);                    // (one tile after the other: the path is rare, registers are not)
+          const uint4 kinds = make_uint4(take_odd<T>(vf[et].x), take_odd<T>(vf[et].y), take_odd<T>(vf[et].z), take_odd<T>(vf[et].w));
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            const f32x4 n = mma(__builtin_bit_cast(x8, kinds), seen[ct], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[ct][et][i] += odd_value(n[i]);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int et = 0; et < ET; ++et)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) o[ct][et] = mma(__builtin_bit_cast(x8, vf[et]), p[ct], o[ct][et]);
+    u = un;
+  }
+
+  // the four waves: maximum, sum and outputs as they are; whoever adds them scales them
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const float sum = groups_sum(l[ct]);
+    if (g == 0) {
+      s_m[wave][ct * 16 + j] = m[ct];
+      s_l[wave][ct * 16 + j] = sum;
+    }
+#pragma unroll
+    for (int et = 0; et < ET; ++et)
+      *reinterpret_cast<float4*>(&s_o[wave][ct * 16 + j][et * 16 + g * 4]) = make_float4(o[ct][et][0], o[ct][et][1], o[ct][et][2], o[ct][et][3]);
+  }
+  __syncthreads();
+  join_waves<T, HD, 16 * CT>(c, a, sp, w, s_o, s_m, s_l, &s_last);
 }
 
 }  // namespace
@@ -324,9 +687,33 @@ extern "C" int stairs_paged_append(const stairs_paged_cache* c, const stairs_pag
   return launched();
 }
 
+namespace {
+
+// ---- how a call is spread: by its sizes on the host, by the lengths on the device (find_piece) ------------------------
+constexpr int kCus = 256;
+struct Launch {
+  Span span;
+  int ct;
+  size_t work_bytes;
+  unsigned grid;
+};
+Launch plan_rows(const stairs_paged_cache* c, const stairs_paged_attn* a) {
+  const int G = a->n_heads / c->n_kv_heads;
+  Launch l{};
+  l.ct = (int64_t)a->max_fresh * G <= 16 ? 1 : 2;
+  l.span = Span{1, INT32_MAX, 16 * l.ct, kRowUnit, (l.ct == 1 ? 3 : 2) * kCus};
+  l.work_bytes = (size_t)most_pieces(l.span.slots) * (sizeof(int) + (size_t)l.span.tile_cols * (c->head_dim + 2) * sizeof(float));
+  // at most `slots` pieces and one a tile
+  const int64_t tiles = a->n_seqs + (int64_t)a->rows * G / l.span.tile_cols;
+  l.grid = (unsigned)std::min<int64_t>(l.span.slots + tiles * c->n_kv_heads, INT32_MAX);
+  return l;
+}
+
+}  // namespace
+
 extern "C" int64_t stairs_paged_attention_workspace(const stairs_paged_cache* c, const stairs_paged_attn* a) {
   if (!attn_sizes_ok(c, a)) return STAIRS_EINVAL;
-  return 0;
+  return (int64_t)plan_rows(c, a).work_bytes;
 }
 
 extern "C" int stairs_paged_attention(const stairs_paged_cache* c, const stairs_paged_attn* a, void* hip_stream) {
@@ -335,11 +722,19 @@ extern "C" int stairs_paged_attention(const stairs_paged_cache* c, const stairs_
   if (!a->q || !a->out || a->q == a->out || !a->block_table || !a->row_start || !a->seq_len) return STAIRS_EINVAL;
   if (!aligned16(a->q) || !aligned16(a->out) || !stride_ok(a->q_stride, a->n_heads, c->head_dim) || !stride_ok(a->out_stride, a->n_heads, c->head_dim))
     return STAIRS_EINVAL;
+  if (!a->workspace || !aligned16(a->workspace)) return STAIRS_EINVAL;
+  const Launch rows = plan_rows(c, a);
+  if (a->workspace_bytes < (int64_t)rows.work_bytes) return STAIRS_ECAPACITY;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (const int rc = check_stream(st)) return rc;
-  const float scale = a->scale > 0.f ? a->scale : 1.0f / sqrtf((float)c->head_dim);
+  const float scale2 = (a->scale > 0.f ? a->scale : 1.0f / sqrtf((float)c->head_dim)) * kLog2e;
   by_type(c, [&](auto type, auto hd) {
-    hipLaunchKernelGGL((k_paged_attend<decltype(type), decltype(hd)::value>), dim3(a->rows, a->n_heads), dim3(64), 0, st, *c, *a, scale);
+    typedef decltype(type) T;
+    constexpr int HD = decltype(hd)::value;
+    if (rows.ct == 1)
+      hipLaunchKernelGGL((k_paged_rows<T, HD, 1>), dim3(rows.grid), dim3(256), 0, st, *c, *a, rows.span, scale2);
+    else
+      hipLaunchKernelGGL((k_paged_rows<T, HD, 2>), dim3(rows.grid), dim3(256), 0, st, *c, *a, rows.span, scale2);
   });
   return launched();
 }
