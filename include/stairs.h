@@ -376,7 +376,8 @@ int stairs_paged_append(const stairs_paged_cache *cache, const stairs_paged_rows
  * sequences share a call only up to the last bits: the split of a long sequence follows the whole batch.
  * workspace: stairs_paged_attention_workspace bytes (0 <= result; depends on n_heads, head_dim, n_kv_heads and max_fresh alone),
  * 16-byte aligned, all zeros before its first use, left fit for the next call; calls that may overlap need one each.
- * 0 <= n_seqs <= STAIRS_PAGED_MAX_SEQS; n_heads a multiple of n_kv_heads; pointers 16-byte aligned, strides multiples of 8. */
+ * 0 <= n_seqs <= STAIRS_PAGED_MAX_SEQS; row_start ascending; n_heads a multiple of n_kv_heads; rows * n_heads / n_kv_heads at most
+ * 2^24; pointers 16-byte aligned, strides multiples of 8. */
 typedef struct {
   int32_t n_seqs, max_blocks, rows, n_heads, max_fresh;
   const void *q;                   /* [rows][n_heads][head_dim] */

@@ -11,7 +11,6 @@
 
 namespace stairs {
 namespace {
-
 // ---------------------------------------------------------------------------------------
 // pages and slots
 // ---------------------------------------------------------------------------------------
@@ -258,7 +257,9 @@ struct Span {
   int tile_cols, unit;        // columns of a tile, keys of a unit
   int slots;
 };
-constexpr int kMaxPieces = 64;        // of a tile: whoever joins them reads them all
+constexpr int kMinUnits = 4;          // of a piece: fewer cost more to join than they save (8000 keys of 8 heads alone: 25 us with 2, 19 with 4)
+constexpr int kWhole = 200;            // tiles that make nearly every CU busy
+constexpr int kMaxPieces = 32;        // of a tile: whoever joins them reads them all
 struct Piece {
   int seq, row0, rows, len;   // rows of the sequence, its length (not cut to the table)
   int group, piece, pieces;   // tile of the sequence, piece of the tile
@@ -291,38 +292,73 @@ __device__ __forceinline__ T wave_scan(T v) {                  // inclusive
   }
   return v;
 }
+__device__ __forceinline__ int quotient(long long a, int b) {    // a >= 0, b > 0 (a division of 64 bits is over a hundred instructions)
+  return (a >> 32) == 0 ? (int)((unsigned)a / (unsigned)b) : (int)min(a / b, (long long)INT32_MAX);
+}
 __device__ __forceinline__ bool find_piece(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, Piece& out) {
   const int lane = threadIdx.x & 63;
   const int kvh = blockIdx.x % c.n_kv_heads, item = blockIdx.x / c.n_kv_heads;
   long long units = 0;
+  int tiles = 0, most = 0;
   SeqWork w;
   for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
     w = seq_work(c, a, sp, b0 + lane);
     units += (long long)w.groups * w.units;
+    tiles += w.groups;
+    most = max(most, w.units);
   }
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) units += __shfl_xor(units, off);
-  const int per = __builtin_amdgcn_readfirstlane(max(2, (int)((units * c.n_kv_heads + sp.slots - 1) / sp.slots)));
+  for (int off = 32; off >= 1; off >>= 1) {
+    units += __shfl_xor(units, off);
+    tiles += __shfl_xor(tiles, off);
+    most = max(most, __shfl_xor(most, off));
+  }
+  units *= c.n_kv_heads;
+  const long long all_tiles = (long long)tiles * c.n_kv_heads;
+  int per;
+  if (all_tiles >= kWhole && units * 4 >= all_tiles * most * 3) {
+    // Tiles of about one length for nearly every CU stay whole: half as many streams, and nothing to join (32 sequences of 2048
+    // keys, 8 heads: 46 us whole, 58 in halves; of 8192 keys 162 and 189).
+    per = max(1, most);
+  } else {
+    // Pieces of one size, for which they all run at once: a second round, however short, costs a whole piece's latencies (32
+    // verifications of 200 .. 8000 keys: 79 us with 612 pieces, 66 with 490).  With more tiles than run at once anyway, or more
+    // sequences than lanes, the even share.
+    per = max(kMinUnits, quotient(units + sp.slots - 1, sp.slots));
+    if (a.n_seqs <= 64 && per > kMinUnits && per < most) {
+      const float fit = (float)(sp.slots / c.n_kv_heads);
+      int lo = per, hi = 4 * per;                               // (up to 4 shares: beyond that one round is no aim any more)
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        const float pieces = fmaxf(1.f, floorf(((float)(w.units + mid) - 0.5f) * __builtin_amdgcn_rcpf((float)mid)));
+        if (__builtin_amdgcn_readfirstlane(__float_as_int(wave_sum((float)w.groups * pieces) - fit)) <= 0) hi = mid;
+        else lo = mid + 1;
+      }
+      if (lo < 4 * per) per = lo;
+    }
+  }
+  per = __builtin_amdgcn_readfirstlane(per);
   int before = 0, split_before = 0;
   for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
-    if (b0 > 0 || a.n_seqs > 64) w = seq_work(c, a, sp, b0 + lane);
-    const int pieces = min(kMaxPieces, max(1, (w.units + per - 1) / per));
+    if (a.n_seqs > 64) w = seq_work(c, a, sp, b0 + lane);
+    const int pieces = min(kMaxPieces, max(1, (int)((unsigned)(w.units + per - 1) / (unsigned)per)));
     const int mine = w.groups * pieces, split = pieces > 1 ? mine : 0;
     const int to = before + wave_scan(mine), split_to = split_before + wave_scan(split);
     const unsigned long long there = __ballot(to > item);
     if (there) {
       const int l = __builtin_ctzll(there);
-      const int at = item - (__builtin_amdgcn_readlane(to, l) - __builtin_amdgcn_readlane(mine, l));
+      const unsigned at = item - (__builtin_amdgcn_readlane(to, l) - __builtin_amdgcn_readlane(mine, l));
+      const unsigned n = __builtin_amdgcn_readlane(pieces, l), group = at / n;
+      const int u = __builtin_amdgcn_readlane(w.units, l);
       out.seq = b0 + l;
       out.row0 = __builtin_amdgcn_readlane(w.row0, l);
       out.rows = __builtin_amdgcn_readlane(w.rows, l);
       out.len = __builtin_amdgcn_readlane(w.len, l);
-      out.pieces = __builtin_amdgcn_readlane(pieces, l);
-      out.group = at / out.pieces;
-      out.piece = at - out.group * out.pieces;
-      const int u = __builtin_amdgcn_readlane(w.units, l);
-      out.u0 = (int)((long long)u * out.piece / out.pieces);
-      out.u1 = (int)((long long)u * (out.piece + 1) / out.pieces);
+      out.pieces = n;
+      out.group = __builtin_amdgcn_readfirstlane(group);
+      out.piece = __builtin_amdgcn_readfirstlane(at - group * n);
+      out.u0 = __builtin_amdgcn_readfirstlane((unsigned)u * out.piece / n);        // (26 bits of units, 5 of pieces)
+      out.u1 = __builtin_amdgcn_readfirstlane((unsigned)u * (out.piece + 1) / n);
       out.first = (__builtin_amdgcn_readlane(split_to, l) - __builtin_amdgcn_readlane(split, l) + out.group * out.pieces) * c.n_kv_heads + kvh;
       out.kvh = kvh;
       return true;
@@ -351,32 +387,61 @@ __device__ __forceinline__ void store_out(const stairs_paged_cache& c, const sta
 }
 __device__ __forceinline__ float weight_of(float m, float all) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - all); }
 
-// the last of a split tile's work-groups joins its pieces, in their order whoever it is
-template <typename T, int HD>
-__device__ __forceinline__ void join_pieces(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, const Piece& w, int* s_last) {
+// The last of a split tile's work-groups joins its pieces, in their order whoever it is.  Everything is requested before anything
+// is waited for: all pieces' maxima and sums, and eight outputs a thread (one after the other, each a round trip past the
+// caches, the maxima and sums alone of 32 pieces were 30 us).
+template <typename T, int HD, int COLS>
+__device__ __forceinline__ void join_pieces(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, const Piece& w, float2* s_ml, int* s_last) {
   int* counter = static_cast<int*>(a.workspace) + w.first;
   if (!last_arrival(counter, w.pieces, s_last)) return;
-  const size_t step = piece_floats<HD>(sp.tile_cols) * c.n_kv_heads;
-  const float* base = reinterpret_cast<const float*>(static_cast<int*>(a.workspace) + most_pieces(sp.slots)) + (size_t)w.first * piece_floats<HD>(sp.tile_cols);
-  const int G = a.n_heads / c.n_kv_heads, col0 = w.group * sp.tile_cols, cols = min(sp.tile_cols, w.rows * G - col0);
-  for (int i = threadIdx.x; i < cols * (HD / 4); i += blockDim.x) {
-    const int col = i / (HD / 4), e = i % (HD / 4) * 4;
-    const float* ml = base + sp.tile_cols * HD + col * 2;
-    float m = -INFINITY;
-    for (int p = 0; p < w.pieces; ++p) m = fmaxf(m, ld_dev(ml + p * step));
+  constexpr int NT = 256;
+  const int step = (int)(piece_floats<HD>(COLS) * c.n_kv_heads);
+  const float* base = reinterpret_cast<const float*>(static_cast<int*>(a.workspace) + most_pieces(sp.slots)) + (size_t)w.first * piece_floats<HD>(COLS);
+  const int G = a.n_heads / c.n_kv_heads, col0 = w.group * COLS, cols = min(COLS, w.rows * G - col0);
+  constexpr int MLS = (kMaxPieces * COLS + NT - 1) / NT;
+  float2 ml[MLS];
+#pragma unroll
+  for (int k = 0; k < MLS; ++k) ml[k] = ld_dev2(base + min((int)(threadIdx.x + k * NT) / COLS, w.pieces - 1) * step + COLS * HD + threadIdx.x % COLS * 2);
+  float mine = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < MLS; ++k) mine = fmaxf(mine, ml[k].x);
+  float* s_max = reinterpret_cast<float*>(s_ml + kMaxPieces * COLS);
+  s_max[threadIdx.x] = mine;
+  __syncthreads();
+  float all = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < NT / COLS; ++k) all = fmaxf(all, s_max[threadIdx.x % COLS + k * COLS]);
+#pragma unroll
+  for (int k = 0; k < MLS; ++k) {
+    const float f = (int)(threadIdx.x + k * NT) / COLS < w.pieces ? weight_of(ml[k].x, all) : 0.f;
+    s_ml[threadIdx.x + k * NT] = make_float2(f, f * ml[k].y);
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int i = threadIdx.x; i < cols * (HD / 4); i += NT) {
+    const int col = i / (HD / 4);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     float l = 0.f;
-#pragma unroll 4
-    for (int p = 0; p < w.pieces; ++p) {
-      const float2 pm = ld_dev2(ml + p * step), x = ld_dev2(base + p * step + col * HD + e), y = ld_dev2(base + p * step + col * HD + e + 2);
-      const float f = weight_of(pm.x, m);
-      l += f * pm.y;
-      v.x += f * x.x;
-      v.y += f * x.y;
-      v.z += f * y.x;
-      v.w += f * y.y;
+#pragma unroll 1
+    for (int p0 = 0; p0 < w.pieces; p0 += 8) {
+      float2 x[8], y[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float* at = base + min(p0 + k, w.pieces - 1) * step + i * 4;
+        x[k] = ld_dev2(at);
+        y[k] = ld_dev2(at + 2);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float2 f = s_ml[(p0 + k) * COLS + col];
+        l += f.y;
+        v.x += f.x * x[k].x;
+        v.y += f.x * x[k].y;
+        v.z += f.x * y[k].x;
+        v.w += f.x * y[k].y;
+      }
     }
-    store_out<T, HD>(c, a, w, col0 + col, e, v, l);
+    store_out<T, HD>(c, a, w, col0 + col, i % (HD / 4) * 4, v, l);
   }
   if (threadIdx.x == 0) *counter = 0;
 }
@@ -385,12 +450,15 @@ __device__ __forceinline__ void join_pieces(const stairs_paged_cache& c, const s
 template <typename T, int HD, int COLS>
 __device__ __forceinline__ void join_waves(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, const Piece& w,
                                            float (*s_o)[COLS][HD + 4], float (*s_m)[COLS], float (*s_l)[COLS], int* s_last) {
+  static_assert(4 * COLS * (HD + 4) >= 2 * kMaxPieces * COLS + 256, "the pieces' maxima and sums fit where the waves' outputs were");
   const int G = a.n_heads / c.n_kv_heads, col0 = w.group * COLS, cols = min(COLS, w.rows * G - col0);
   float* part = reinterpret_cast<float*>(static_cast<int*>(a.workspace) + most_pieces(sp.slots)) +
                 (size_t)(w.first + w.piece * c.n_kv_heads) * piece_floats<HD>(COLS);
   for (int i = threadIdx.x; i < cols * (HD / 4); i += 256) {
     const int col = i / (HD / 4), e = i % (HD / 4) * 4;
-    const float m = fmaxf(fmaxf(s_m[0][col], s_m[1][col]), fmaxf(s_m[2][col], s_m[3][col]));
+    float m = s_m[0][col];
+#pragma unroll
+    for (int k = 1; k < 4; ++k) m = fmaxf(m, s_m[k][col]);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     float l = 0.f;
 #pragma unroll
@@ -411,7 +479,7 @@ __device__ __forceinline__ void join_waves(const stairs_paged_cache& c, const st
       if (e == 0) st_dev2(part + COLS * HD + col * 2, m, l);
     }
   }
-  if (w.pieces > 1) join_pieces<T, HD>(c, a, sp, w, s_last);
+  if (w.pieces > 1) join_pieces<T, HD, COLS>(c, a, sp, w, reinterpret_cast<float2*>(s_o), s_last);
 }
 
 // ---- few columns: a wave per 32 keys ----------------------------------------------------------------------------------
@@ -419,9 +487,14 @@ __device__ __forceinline__ void join_waves(const stairs_paged_cache& c, const st
 // turn, straight from memory into the matrix operands (a block of a head is 2 x 64 HD contiguous bytes, every load 1 KiB of a
 // wave), no LDS, and are joined at the end.  Values are requested before the scores they wait for, the next block's keys as
 // soon as this block's are used.
-constexpr int kRowUnit = 128;
+constexpr int kRowUnit = 32 * 4;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 ld_once(const void* p) {        // (streaming hint: 3 x 32 heads of up to 59999 keys 384 -> 366 us)
+  const u32x4 v = __builtin_nontemporal_load(static_cast<const u32x4*>(p));
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
 template <typename T, int HD, int CT>
-__global__ __launch_bounds__(256, CT == 1 ? 3 : 2) void k_paged_rows(stairs_paged_cache c, stairs_paged_attn a, Span sp, float scale2) {
+__global__ __launch_bounds__(256, 2) void k_paged_rows(stairs_paged_cache c, stairs_paged_attn a, Span sp, float scale2) {
   typedef typename Elem<T>::x8 x8;
   constexpr int KK = HD / 32, ET = HD / 16, LD = HD + 4;
   __shared__ float s_o[4][16 * CT][LD];
@@ -491,7 +564,7 @@ __global__ __launch_bounds__(256, CT == 1 ? 3 : 2) void k_paged_rows(stairs_page
   };
   auto load_keys = [&](size_t at) {
 #pragma unroll
-    for (int i = 0; i < 2 * KK; ++i) kf[i] = *reinterpret_cast<const uint4*>(K + at + (i * 64 + lane) * 8);
+    for (int i = 0; i < 2 * KK; ++i) kf[i] = ld_once(K + at + (i * 64 + lane) * 8);
   };
   if (w.u0 < u1) fetch_pages(w.u0);
   int u = next_block(w.u0);
@@ -502,7 +575,7 @@ __global__ __launch_bounds__(256, CT == 1 ? 3 : 2) void k_paged_rows(stairs_page
   }
   while (u < u1) {
 #pragma unroll
-    for (int i = 0; i < ET; ++i) vf[i] = *reinterpret_cast<const uint4*>(V + at + (i * 64 + lane) * 8);
+    for (int i = 0; i < ET; ++i) vf[i] = ld_once(V + at + (i * 64 + lane) * 8);
     f32x4 s[CT][2];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
@@ -647,6 +720,7 @@ bool attn_sizes_ok(const stairs_paged_cache* c, const stairs_paged_attn* a) {
   if (!cache_ok(c) || !a) return false;
   if (a->n_seqs < 0 || a->n_seqs > STAIRS_PAGED_MAX_SEQS || a->max_blocks < 1 || a->rows < 0 || a->max_fresh < 0) return false;
   if ((int64_t)a->max_blocks * c->page_size > INT32_MAX) return false;
+  if (a->n_heads < 1 || (int64_t)a->rows * a->n_heads / c->n_kv_heads > 1 << 24) return false;   // (counts of tiles stay ints)
   return a->n_heads >= 1 && a->n_heads <= 4096 && a->n_heads % c->n_kv_heads == 0;
 }
 
@@ -701,7 +775,7 @@ Launch plan_rows(const stairs_paged_cache* c, const stairs_paged_attn* a) {
   const int G = a->n_heads / c->n_kv_heads;
   Launch l{};
   l.ct = (int64_t)a->max_fresh * G <= 16 ? 1 : 2;
-  l.span = Span{1, INT32_MAX, 16 * l.ct, kRowUnit, (l.ct == 1 ? 3 : 2) * kCus};
+  l.span = Span{1, INT32_MAX, 16 * l.ct, kRowUnit, 2 * kCus};
   l.work_bytes = (size_t)most_pieces(l.span.slots) * (sizeof(int) + (size_t)l.span.tile_cols * (c->head_dim + 2) * sizeof(float));
   // at most `slots` pieces and one a tile
   const int64_t tiles = a->n_seqs + (int64_t)a->rows * G / l.span.tile_cols;

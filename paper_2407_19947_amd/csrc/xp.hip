@@ -1,0 +1,814 @@
+// Operators over paged key/value caches: pages and slots for the requests of a step, storing the new rows, attention of the
+// new rows over the pages.  The page layout is the tiled layout of the framework's own half caches (k_cache_off, v_cache_off),
+// page by page.
+#include "../../include/stairs.h"
+#include "stairs_device.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+namespace stairs {
+namespace {
+// ---------------------------------------------------------------------------------------
+// pages and slots
+// ---------------------------------------------------------------------------------------
+constexpr int kPlanThreads = 1024;
+static_assert(kPlanThreads >= STAIRS_PAGED_MAX_SEQS, "a thread per sequence");
+
+// exclusive sum over the threads of the block
+__device__ __forceinline__ long long block_scan(long long v, long long* s_part, long long* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  long long x = v;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const long long o = __shfl_up(x, off);
+    if (lane >= off) x += o;
+  }
+  __syncthreads();
+  if (lane == 63) s_part[wave] = x;
+  __syncthreads();
+  long long before = 0, all = 0;
+  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) {
+    if (w < wave) before += s_part[w];
+    all += s_part[w];
+  }
+  *total = all;
+  return before + x - v;
+}
+
+// the last index b < n with first[b] <= i, first ascending, first[0] <= i
+__device__ __forceinline__ int find_seq(const int* first, int n, int i) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first[mid] <= i) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// position and slot of row t, from what the plan has left
+__device__ __forceinline__ void row_slot(const stairs_page_plan& p, const int* row_start, int t, int total) {
+  int pos = -1, slot = -1;
+  if (t < total) {
+    const int b = find_seq(row_start, p.n_seqs, t);
+    const int len = p.seq_len[b];
+    if (len > 0) {
+      pos = len - (row_start[b + 1] - t);
+      if (pos < 0 || pos >= len) pos = -1;          // (counts whose sum is no int)
+      const int page = pos < 0 ? -1 : p.block_table[(size_t)b * p.max_blocks + pos / p.page_size];
+      if ((unsigned)page < (unsigned)p.n_pages) slot = page * p.page_size + pos % p.page_size;
+    }
+  }
+  p.position[t] = pos;
+  p.slot[t] = slot;
+}
+
+// One block: a thread per sequence counts, three sums over the sequences say where everything goes, then the pages that change
+// hands and the rows are spread over all threads (a sequence that ends with a thousand pages is not one thread's work).
+__global__ __launch_bounds__(kPlanThreads) void k_paged_plan(stairs_page_plan p, int rows_here) {
+  __shared__ long long s_part[kPlanThreads / 64];
+  __shared__ int s_rows[STAIRS_PAGED_MAX_SEQS + 1], s_drop[STAIRS_PAGED_MAX_SEQS + 1], s_ask[STAIRS_PAGED_MAX_SEQS + 1];
+  __shared__ int s_need[STAIRS_PAGED_MAX_SEQS], s_held[STAIRS_PAGED_MAX_SEQS];
+  const int b = threadIdx.x;
+  const bool here = b < p.n_seqs;
+  const int cached = here ? max(p.cached[b], 0) : 0, fresh = here ? max(p.fresh[b], 0) : 0;
+  const int held = here ? min(max(p.held[b], 0), p.max_blocks) : 0;
+  const int n_free = min(max(p.n_free[0], 0), p.n_pages);
+  const long long wants = ((long long)cached + fresh + p.page_size - 1) / p.page_size;
+  const bool fits = wants <= p.max_blocks;
+  const int need = fits ? (int)wants : held;
+  const int ask = max(need - held, 0), drop = held - min(need, held);
+  long long rows_l, asked, dropped_l, granted_l;
+  const int row0 = (int)block_scan(fresh, s_part, &rows_l);
+  const long long ask0 = block_scan(ask, s_part, &asked);
+  const int drop0 = (int)min(block_scan(drop, s_part, &dropped_l), (long long)INT32_MAX);
+  const int dropped = (int)min(dropped_l, (long long)(p.n_pages - n_free)), avail = n_free + dropped;
+  const bool ok = fits && (ask == 0 || ask0 + ask <= avail);
+  const int grant0 = (int)block_scan(ok ? ask : 0, s_part, &granted_l);     // (at most avail)
+  const int rows = (int)rows_l, granted = (int)granted_l;
+  if (here) {
+    s_rows[b] = row0;
+    s_drop[b] = drop0;
+    s_ask[b] = grant0;
+    s_need[b] = need;
+    s_held[b] = held;
+  }
+  if (b == 0) s_rows[p.n_seqs] = rows;
+  __syncthreads();
+  // pages given back, behind the free ones
+  for (int i = threadIdx.x; i < dropped; i += kPlanThreads) {
+    const int q = find_seq(s_drop, p.n_seqs, i);
+    p.free_pages[n_free + i] = p.block_table[(size_t)q * p.max_blocks + s_need[q] + (i - s_drop[q])];
+  }
+  __syncthreads();
+  // pages taken, from the end of the stack
+  for (int i = threadIdx.x; i < granted; i += kPlanThreads) {
+    const int q = find_seq(s_ask, p.n_seqs, i);
+    p.block_table[(size_t)q * p.max_blocks + s_held[q] + (i - s_ask[q])] = p.free_pages[avail - 1 - i];
+  }
+  if (here) {
+    p.held_out[b] = ok ? need : held;
+    p.row_start[b] = row0;
+    p.seq_len[b] = ok ? cached + fresh : 0;
+  }
+  if (b == 0) {
+    p.n_free_out[0] = avail - granted;
+    p.row_start[p.n_seqs] = rows;
+  }
+  __syncthreads();
+  for (int t = threadIdx.x; t < rows_here; t += kPlanThreads) row_slot(p, s_rows, t, rows);
+}
+
+__global__ __launch_bounds__(256) void k_paged_slots(stairs_page_plan p) {
+  const int t = blockIdx.x * 256 + threadIdx.x;
+  if (t < p.max_rows) row_slot(p, p.row_start, t, p.row_start[p.n_seqs]);
+}
+
+// ---------------------------------------------------------------------------------------
+// storing rows
+// ---------------------------------------------------------------------------------------
+template <typename T> struct Elem;
+template <> struct Elem<__bf16> {
+  typedef bf16x8 x8;
+  static __device__ __forceinline__ float up(__bf16 v) { return (float)v; }
+  static __device__ __forceinline__ __bf16 down(float v) { return (__bf16)v; }
+};
+template <> struct Elem<_Float16> {
+  typedef f16x8 x8;
+  static __device__ __forceinline__ float up(_Float16 v) { return (float)v; }
+  static __device__ __forceinline__ _Float16 down(float v) { return (_Float16)v; }
+};
+
+// a block per row: q and k rotated, k and v stored
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stairs_paged_rows a) {
+  __shared__ float2 s_cs[HD / 2];
+  const int t = blockIdx.x;
+  const int slot = a.slot[t];
+  const bool rotate = a.rope_theta > 0.f;
+  const int pos = rotate ? a.position[t] : 0;
+  if (rotate && threadIdx.x < HD / 2) {
+    const double angle = (double)pos * exp2(-(2.0 * threadIdx.x / HD) * log2((double)a.rope_theta));
+    double s, co;
+    sincos(angle, &s, &co);
+    s_cs[threadIdx.x] = make_float2((float)co, (float)s);
+  }
+  __syncthreads();
+  const bool store = (unsigned)slot < (unsigned)c.n_pages * (unsigned)c.page_size;
+  const int page = store ? slot / c.page_size : 0, p = store ? slot % c.page_size : 0;
+  const size_t head_elems = (size_t)c.page_size * HD;
+  const int nq = a.n_heads, nk = c.n_kv_heads;
+  for (int i = threadIdx.x; i < (nq + nk) * (HD / 2); i += 256) {
+    const int h = i / (HD / 2), e = i % (HD / 2);
+    const bool is_q = h < nq;
+    if (is_q ? pos < 0 : !store) continue;
+    const T* src = is_q ? static_cast<const T*>(a.q) + (size_t)t * a.q_stride + h * HD
+                        : static_cast<const T*>(a.k) + (size_t)t * a.k_stride + (h - nq) * HD;
+    T lo = src[e], hi = src[e + HD / 2];
+    if (rotate) {
+      const float2 r = rope_rotate(Elem<T>::up(lo), Elem<T>::up(hi), s_cs[e]);
+      lo = Elem<T>::down(r.x);
+      hi = Elem<T>::down(r.y);
+    }
+    if (is_q) {
+      T* dst = static_cast<T*>(a.q_out) + (size_t)t * a.q_out_stride + h * HD;
+      dst[e] = lo;
+      dst[e + HD / 2] = hi;
+    } else {
+      T* dst = static_cast<T*>(c.k) + ((size_t)page * nk + (h - nq)) * head_elems;
+      dst[k_cache_off(p, e, HD)] = lo;
+      dst[k_cache_off(p, e + HD / 2, HD)] = hi;
+    }
+  }
+  if (store)
+    for (int i = threadIdx.x; i < nk * HD; i += 256) {
+      const int h = i / HD, e = i % HD;
+      T* dst = static_cast<T*>(c.v) + ((size_t)page * nk + h) * head_elems;
+      dst[v_cache_off(p, e, HD)] = static_cast<const T*>(a.v)[(size_t)t * a.v_stride + i];
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// attention
+// ---------------------------------------------------------------------------------------
+// A tile is up to 16 CT columns of one key head of one sequence; a column is (row, query head of the group), so that heads that
+// share keys share the loads.  Scores are computed transposed, S^T = K Q^T: a lane then holds the scores of ONE column for 8 of 32
+// keys, which are already the operand O^T = V^T P^T wants from it (the value tiles are laid out for that order of keys), so the
+// probabilities never leave their registers, and maximum and sum are per lane but for two exchanges between lane groups.
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kMaxSlack = 8.f;      // the running maximum follows once a score exceeds it by 2^8: sums and rounded
+                                      // probabilities keep their relative precision whatever the reference point is
+
+// (a lane's value, those of the lanes 16, 32 and 48 further) -> the largest / the sum, in all four
+__device__ __forceinline__ float groups_max(float v) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float groups_sum(float v) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Whether any of the eight halves of v is an infinity or not a number: exponent bits all ones, found by one carry
+template <typename T>
+__device__ __forceinline__ uint32_t odd_bits(uint32_t u) {
+  constexpr uint32_t m = sizeof(T) == 2 && __is_same(T, __bf16) ? 0x7F807F80u : 0x7C007C00u, one = __is_same(T, __bf16) ? 0x00800080u : 0x04000400u;
+  return ((u & m) + one) & 0x80008000u;
+}
+
+// Takes the infinities and NaNs out of a pair of values and says what they were: 1 for +infinity, 64 for -infinity, 4096 for NaN.
+// Summed over the keys that a column sees (32 at most, so the three counts stay apart) they say what belongs in its sum.
+template <typename T>
+__device__ __forceinline__ uint32_t take_odd(uint32_t& v) {
+  constexpr bool b = __is_same(T, __bf16);
+  constexpr uint32_t inf = b ? 0x7F80u : 0x7C00u, one = b ? 0x3F80u : 0x3C00u, k64 = b ? 0x4280u : 0x5400u, k4096 = b ? 0x4580u : 0x6C00u;
+  uint32_t kinds = 0, left = 0;
+#pragma unroll
+  for (int h = 0; h < 32; h += 16) {
+    const uint32_t x = (v >> h) & 0xFFFFu, m = x & 0x7FFFu;
+    kinds |= (m < inf ? 0u : m > inf ? k4096 : x > m ? k64 : one) << h;
+    left |= (m < inf ? x : 0u) << h;
+  }
+  v = left;
+  return kinds;
+}
+__device__ __forceinline__ float odd_value(float n) {
+  const int c = (int)n;
+  return (c & 63 ? INFINITY : 0.f) + (c & (63 << 6) ? -INFINITY : 0.f) + (c >> 12 ? __uint_as_float(0x7FC00000u) : 0.f);
+}
+
+// ---- which piece of the work a work-group takes -------------------------------------------------------------------
+// The lengths are on the device, so the split is made there, by every wave for itself (64 sequences at a time, a lane each; no
+// memory but the counts): a tile's keys are cut into pieces of `per` units so that all pieces together are about `slots`, the
+// work-groups that run at once.  Then one long sequence among short ones is spread over the chip, and a batch that fills it is not
+// split at all.  Work-group i takes key head i % n_kv_heads (neighbouring work-groups go to different XCDs: with 8 key heads and
+// more a head's work-groups share an L2).
+struct Span {
+  int min_cols, max_cols;     // sequences with so many columns (rows times heads a key head has)
+  int tile_cols, unit;        // columns of a tile, keys of a unit
+  int slots;
+};
+constexpr int kMinUnits = 4;          // of a piece: fewer cost more to join than they save (8000 keys of 8 heads alone: 25 us with 2, 19 with 4)
+constexpr int kWhole = 200;            // tiles that make nearly every CU busy
+constexpr int kMaxPieces = 32;        // of a tile: whoever joins them reads them all
+struct Piece {
+  int seq, row0, rows, len;   // rows of the sequence, its length (not cut to the table)
+  int group, piece, pieces;   // tile of the sequence, piece of the tile
+  int u0, u1;                 // its units
+  int first;                  // number of the tile's first piece among the pieces of split tiles
+  int kvh;
+};
+struct SeqWork { int row0, rows, len, groups, units; };
+__device__ __forceinline__ SeqWork seq_work(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, int b) {
+  SeqWork w{0, 0, 0, 0, 0};
+  if (b < a.n_seqs) {
+    w.row0 = a.row_start[b];
+    w.rows = a.row_start[b + 1] - w.row0;
+    w.len = a.seq_len[b];
+    const long long cols = (long long)w.rows * (a.n_heads / c.n_kv_heads);
+    if (w.row0 >= 0 && w.rows > 0 && w.rows <= a.rows - w.row0 && cols >= sp.min_cols && cols <= sp.max_cols) {
+      w.groups = (int)((cols + sp.tile_cols - 1) / sp.tile_cols);
+      w.units = (min(max(w.len, 0), a.max_blocks * c.page_size) + sp.unit - 1) / sp.unit;
+    }
+  }
+  return w;
+}
+template <typename T>
+__device__ __forceinline__ T wave_scan(T v) {                  // inclusive
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const T o = __shfl_up(v, off);
+    if (lane >= off) v += o;
+  }
+  return v;
+}
+__device__ __forceinline__ int quotient(long long a, int b) {    // a >= 0, b > 0 (a division of 64 bits is over a hundred instructions)
+  return (a >> 32) == 0 ? (int)((unsigned)a / (unsigned)b) : (int)min(a / b, (long long)INT32_MAX);
+}
+__device__ __forceinline__ bool find_piece(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, Piece& out) {
+  const int lane = threadIdx.x & 63;
+  const int kvh = blockIdx.x % c.n_kv_heads, item = blockIdx.x / c.n_kv_heads;
+  long long units = 0;
+  int tiles = 0, most = 0;
+  SeqWork w;
+  for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
+    w = seq_work(c, a, sp, b0 + lane);
+    units += (long long)w.groups * w.units;
+    tiles += w.groups;
+    most = max(most, w.units);
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) {
+    units += __shfl_xor(units, off);
+    tiles += __shfl_xor(tiles, off);
+    most = max(most, __shfl_xor(most, off));
+  }
+  units *= c.n_kv_heads;
+  const long long all_tiles = (long long)tiles * c.n_kv_heads;
+  int per;
+  if (all_tiles >= kWhole && units * 4 >= all_tiles * most * 3) {
+    // Tiles of about one length for nearly every CU stay whole: half as many streams, and nothing to join (32 sequences of 2048
+    // keys, 8 heads: 46 us whole, 58 in halves; of 8192 keys 162 and 189).
+    per = max(1, most);
+  } else {
+    // Pieces of one size, for which they all run at once: a second round, however short, costs a whole piece's latencies (32
+    // verifications of 200 .. 8000 keys: 79 us with 612 pieces, 66 with 490).  With more tiles than run at once anyway, or more
+    // sequences than lanes, the even share.
+    per = max(kMinUnits, quotient(units + sp.slots - 1, sp.slots));
+    if (a.n_seqs <= 64 && per > kMinUnits && per < most) {
+      const float fit = (float)(sp.slots / c.n_kv_heads);
+      int lo = per, hi = 4 * per;                               // (up to 4 shares: beyond that one round is no aim any more)
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        const float pieces = fmaxf(1.f, floorf(((float)(w.units + mid) - 0.5f) * __builtin_amdgcn_rcpf((float)mid)));
+        if (__builtin_amdgcn_readfirstlane(__float_as_int(wave_sum((float)w.groups * pieces) - fit)) <= 0) hi = mid;
+        else lo = mid + 1;
+      }
+      if (lo < 4 * per) per = lo;
+    }
+  }
+  per = __builtin_amdgcn_readfirstlane(per);
+  int before = 0, split_before = 0;
+  for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
+    if (a.n_seqs > 64) w = seq_work(c, a, sp, b0 + lane);
+    const int pieces = min(kMaxPieces, max(1, (int)((unsigned)(w.units + per - 1) / (unsigned)per)));
+    const int mine = w.groups * pieces, split = pieces > 1 ? mine : 0;
+    const int to = before + wave_scan(mine), split_to = split_before + wave_scan(split);
+    const unsigned long long there = __ballot(to > item);
+    if (there) {
+      const int l = __builtin_ctzll(there);
+      const unsigned at = item - (__builtin_amdgcn_readlane(to, l) - __builtin_amdgcn_readlane(mine, l));
+      const unsigned n = __builtin_amdgcn_readlane(pieces, l), group = at / n;
+      const int u = __builtin_amdgcn_readlane(w.units, l);
+      out.seq = b0 + l;
+      out.row0 = __builtin_amdgcn_readlane(w.row0, l);
+      out.rows = __builtin_amdgcn_readlane(w.rows, l);
+      out.len = __builtin_amdgcn_readlane(w.len, l);
+      out.pieces = n;
+      out.group = __builtin_amdgcn_readfirstlane(group);
+      out.piece = __builtin_amdgcn_readfirstlane(at - group * n);
+      out.u0 = __builtin_amdgcn_readfirstlane((unsigned)u * out.piece / n);        // (26 bits of units, 5 of pieces)
+      out.u1 = __builtin_amdgcn_readfirstlane((unsigned)u * (out.piece + 1) / n);
+      out.first = (__builtin_amdgcn_readlane(split_to, l) - __builtin_amdgcn_readlane(split, l) + out.group * out.pieces) * c.n_kv_heads + kvh;
+      out.kvh = kvh;
+      return true;
+    }
+    before = __builtin_amdgcn_readlane(to, 63);
+    split_before = __builtin_amdgcn_readlane(split_to, 63);
+  }
+  return false;
+}
+// a split tile's pieces are numbered first + piece * n_kv_heads; all of them together are at most this many: a split
+// sequence has more units than `per`, so fewer than 2 units / per pieces
+__host__ __device__ constexpr int most_pieces(int slots) { return 2 * slots; }
+
+// ---- joining ------------------------------------------------------------------------------------------------------------
+// Partial results of a piece: [tile_cols][HD] outputs relative to the column's maximum, then [tile_cols] (maximum, sum) pairs.
+template <int HD>
+__host__ __device__ constexpr size_t piece_floats(int tile_cols) { return (size_t)tile_cols * (HD + 2); }
+
+template <typename T, int HD>
+__device__ __forceinline__ void store_out(const stairs_paged_cache& c, const stairs_paged_attn& a, const Piece& w, int col, int e, float4 v, float l) {
+  const int G = a.n_heads / c.n_kv_heads, r = col / G;
+  const float f = l == 0.f ? 0.f : 1.f / l;                      // (0: the row has seen nothing)
+  T out[4] = {Elem<T>::down(v.x * f), Elem<T>::down(v.y * f), Elem<T>::down(v.z * f), Elem<T>::down(v.w * f)};
+  *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + (size_t)(w.row0 + r) * a.out_stride + (w.kvh * G + col - r * G) * HD + e) =
+      *reinterpret_cast<const uint2*>(out);
+}
+__device__ __forceinline__ float weight_of(float m, float all) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - all); }
+
+// The last of a split tile's work-groups joins its pieces, in their order whoever it is.  Everything is requested before anything
+// is waited for: all pieces' maxima and sums, and eight outputs a thread (one after the other, each a round trip past the
+// caches, the maxima and sums alone of 32 pieces were 30 us).
+template <typename T, int HD, int COLS>
+__device__ __forceinline__ void join_pieces(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, const Piece& w, float2* s_ml, int* s_last) {
+  int* counter = static_cast<int*>(a.workspace) + w.first;
+  if (!last_arrival(counter, w.pieces, s_last)) return;
+  constexpr int NT = 256;
+  const int step = (int)(piece_floats<HD>(COLS) * c.n_kv_heads);
+  const float* base = reinterpret_cast<const float*>(static_cast<int*>(a.workspace) + most_pieces(sp.slots)) + (size_t)w.first * piece_floats<HD>(COLS);
+  const int G = a.n_heads / c.n_kv_heads, col0 = w.group * COLS, cols = min(COLS, w.rows * G - col0);
+  constexpr int MLS = (kMaxPieces * COLS + NT - 1) / NT;
+  float2 ml[MLS];
+#pragma unroll
+  for (int k = 0; k < MLS; ++k) ml[k] = ld_dev2(base + min((int)(threadIdx.x + k * NT) / COLS, w.pieces - 1) * step + COLS * HD + threadIdx.x % COLS * 2);
+  float mine = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < MLS; ++k) mine = fmaxf(mine, ml[k].x);
+  float* s_max = reinterpret_cast<float*>(s_ml + kMaxPieces * COLS);
+  s_max[threadIdx.x] = mine;
+  __syncthreads();
+  float all = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < NT / COLS; ++k) all = fmaxf(all, s_max[threadIdx.x % COLS + k * COLS]);
+#pragma unroll
+  for (int k = 0; k < MLS; ++k) {
+    const float f = (int)(threadIdx.x + k * NT) / COLS < w.pieces ? weight_of(ml[k].x, all) : 0.f;
+    s_ml[threadIdx.x + k * NT] = make_float2(f, f * ml[k].y);
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int i = threadIdx.x; i < cols * (HD / 4); i += NT) {
+    const int col = i / (HD / 4);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+#pragma unroll 1
+    for (int p0 = 0; p0 < w.pieces; p0 += 8) {
+      float2 x[8], y[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float* at = base + min(p0 + k, w.pieces - 1) * step + i * 4;
+        x[k] = ld_dev2(at);
+        y[k] = ld_dev2(at + 2);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float2 f = s_ml[(p0 + k) * COLS + col];
+        l += f.y;
+        v.x += f.x * x[k].x;
+        v.y += f.x * x[k].y;
+        v.z += f.x * y[k].x;
+        v.w += f.x * y[k].y;
+      }
+    }
+    store_out<T, HD>(c, a, w, col0 + col, i % (HD / 4) * 4, v, l);
+  }
+  if (threadIdx.x == 0) *counter = 0;
+}
+
+// the four waves' results of a piece -> the output, or a partial result
+template <typename T, int HD, int COLS>
+__device__ __forceinline__ void join_waves(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, const Piece& w,
+                                           float (*s_o)[COLS][HD + 4], float (*s_m)[COLS], float (*s_l)[COLS], int* s_last) {
+  static_assert(4 * COLS * (HD + 4) >= 2 * kMaxPieces * COLS + 256, "the pieces' maxima and sums fit where the waves' outputs were");
+  const int G = a.n_heads / c.n_kv_heads, col0 = w.group * COLS, cols = min(COLS, w.rows * G - col0);
+  float* part = reinterpret_cast<float*>(static_cast<int*>(a.workspace) + most_pieces(sp.slots)) +
+                (size_t)(w.first + w.piece * c.n_kv_heads) * piece_floats<HD>(COLS);
+  for (int i = threadIdx.x; i < cols * (HD / 4); i += 256) {
+    const int col = i / (HD / 4), e = i % (HD / 4) * 4;
+    float m = s_m[0][col];
+#pragma unroll
+    for (int k = 1; k < 4; ++k) m = fmaxf(m, s_m[k][col]);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float f = weight_of(s_m[k][col], m);
+      const float4 x = *reinterpret_cast<const float4*>(&s_o[k][col][e]);
+      l += f * s_l[k][col];
+      v.x += f * x.x;
+      v.y += f * x.y;
+      v.z += f * x.z;
+      v.w += f * x.w;
+    }
+    if (w.pieces == 1) {
+      store_out<T, HD>(c, a, w, col0 + col, e, v, l);
+    } else {
+      st_dev2(part + col * HD + e, v.x, v.y);
+      st_dev2(part + col * HD + e + 2, v.z, v.w);
+      if (e == 0) st_dev2(part + COLS * HD + col * 2, m, l);
+    }
+  }
+  if (w.pieces > 1) join_pieces<T, HD, COLS>(c, a, sp, w, reinterpret_cast<float2*>(s_o), s_last);
+}
+
+// ---- few columns: a wave per 32 keys ----------------------------------------------------------------------------------
+// Bound by the bytes of the cache.  A work-group takes a piece of a tile of 16 CT columns; its four waves take 32-key blocks in
+// turn, straight from memory into the matrix operands (a block of a head is 2 x 64 HD contiguous bytes, every load 1 KiB of a
+// wave), no LDS, and are joined at the end.  Values are requested before the scores they wait for, the next block's keys as
+// soon as this block's are used.
+constexpr int kRowUnit = 32 * 4;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 ld_once(const void* p) {        // (streaming hint: 3 x 32 heads of up to 59999 keys 384 -> 366 us)
+  const u32x4 v = __builtin_nontemporal_load(static_cast<const u32x4*>(p));
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+template <typename T, int HD, int CT>
+__global__ __launch_bounds__(256, 2) void k_paged_rows(stairs_paged_cache c, stairs_paged_attn a, Span sp, float scale2) {
+  typedef typename Elem<T>::x8 x8;
+  constexpr int KK = HD / 32, ET = HD / 16, LD = HD + 4;
+  __shared__ float s_o[4][16 * CT][LD];
+  __shared__ float s_m[4][16 * CT], s_l[4][16 * CT];
+  __shared__ int s_last;
+  Piece w;
+  if (!find_piece(c, a, sp, w)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, g = lane >> 4;
+  const int G = a.n_heads / c.n_kv_heads, cols = w.rows * G, col0 = w.group * 16 * CT;
+  const int limit = a.max_blocks * c.page_size;
+  const int pos0 = w.len - w.rows;                              // position of the sequence's first row
+  const int first_last = min(pos0 + col0 / G, limit - 1);        // last position the tile's first and last column see
+  const int last_last = min(pos0 + (min(cols, col0 + 16 * CT) - 1) / G, limit - 1);
+  int last[CT];
+  x8 q[CT][KK];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int col = col0 + ct * 16 + j;
+    last[ct] = -1;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) q[ct][kk] = x8{};
+    if (col < cols) {
+      const int r = col / G;
+      last[ct] = min(pos0 + r, limit - 1);
+      const T* qp = static_cast<const T*>(a.q) + (size_t)(w.row0 + r) * a.q_stride + (w.kvh * G + col - r * G) * HD + g * 8;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) q[ct][kk] = *reinterpret_cast<const x8*>(qp + kk * 32);
+    }
+  }
+  f32x4 o[CT][ET];
+  float m[CT], l[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    m[ct] = -INFINITY;
+    l[ct] = 0.f;
+#pragma unroll
+    for (int et = 0; et < ET; ++et) o[ct][et] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const size_t head_elems = (size_t)c.page_size * HD, page_elems = head_elems * c.n_kv_heads;
+  const T* K = static_cast<const T*>(c.k) + w.kvh * head_elems;
+  const T* V = static_cast<const T*>(c.v) + w.kvh * head_elems;
+  const int* table = a.block_table + (size_t)w.seq * a.max_blocks;
+  const int ps_shift = __builtin_ctz(c.page_size);
+
+  // the wave's blocks: unit u's block is keys 128 u + 32 wave ..; page numbers 64 units at a time, a lane each
+  int pages = -1, pages_at = w.u0;
+  const int u1 = min(w.u1, last_last < 0 ? 0 : (last_last - 32 * wave) / kRowUnit + (last_last >= 32 * wave));
+  auto fetch_pages = [&](int u) {
+    pages_at = u;
+    const int key = (u + lane) * kRowUnit + wave * 32;
+    pages = u + lane < u1 ? table[key >> ps_shift] : -1;
+    if ((unsigned)pages >= (unsigned)c.n_pages) pages = -1;
+  };
+  auto next_block = [&](int u) {                                // the first unit from u on that has a page
+    for (;;) {
+      if (u >= u1) return u1;
+      if (u >= pages_at + 64) fetch_pages(u);
+      const unsigned long long there = __ballot(pages >= 0) & (~0ull << (u - pages_at));
+      if (there) return pages_at + (int)__builtin_ctzll(there);
+      u = pages_at + 64;
+    }
+  };
+  uint4 kf[2 * KK], vf[ET];
+  auto block_at = [&](int u) -> size_t {                        // elements in front of the block in its pool
+    const int key = u * kRowUnit + wave * 32;
+    return (size_t)__builtin_amdgcn_readlane(pages, u - pages_at) * page_elems + (size_t)(key & (c.page_size - 1)) * HD;
+  };
+  auto load_keys = [&](size_t at) {
+#pragma unroll
+    for (int i = 0; i < 2 * KK; ++i) kf[i] = ld_once(K + at + (i * 64 + lane) * 8);
+  };
+  if (w.u0 < u1) fetch_pages(w.u0);
+  int u = next_block(w.u0);
+  size_t at = 0;
+  if (u < u1) {
+    at = block_at(u);
+    load_keys(at);
+  }
+  while (u < u1) {
+#pragma unroll
+    for (int i = 0; i < ET; ++i) vf[i] = ld_once(V + at + (i * 64 + lane) * 8);
+    f32x4 s[CT][2];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        s[ct][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) s[ct][t] = mma(__builtin_bit_cast(x8, kf[t * KK + kk]), q[ct][kk], s[ct][t]);
+      }
+    const int key0 = u * kRowUnit + wave * 32;
+    const int un = next_block(u + 1);
+    if (un < u1) {
+      at = block_at(un);
+      load_keys(at);
+    }
+    const bool full = key0 + 31 <= first_last;
+    x8 p[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = s[ct][i >> 2][i & 3] * scale2;
+      if (!full) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = key0 + (i >> 2) * 16 + g * 4 + (i & 3) <= last[ct] ? x[i] : -INFINITY;
+      }
+      float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      if (__any(mx > m[ct] + kMaxSlack)) {
+        const float mn = fmaxf(m[ct], groups_max(mx));
+        const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[ct] - mn);
+        m[ct] = mn;
+        l[ct] *= f;
+#pragma unroll
+        for (int et = 0; et < ET; ++et) o[ct][et] *= f;
+      }
+      const float mr = m[ct] == -INFINITY ? 0.f : m[ct];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] = __builtin_amdgcn_exp2f(x[i] - mr);
+        l[ct] += x[i];
+        p[ct][i] = Elem<T>::down(x[i]);
+      }
+    }
+    if (!full) {
+      // Some keys of the block are not seen by all columns.  Their probability is 0, and 0 times what is there must be 0: what
+      // no column sees is cleared, an infinity or NaN that some columns see is taken out and given to those that do.
+      uint32_t keep[4], odd = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = key0 + (i >> 1) * 16 + g * 4 + (i & 1) * 2;
+        keep[i] = (key <= last_last ? 0xFFFFu : 0u) | (key + 1 <= last_last ? 0xFFFF0000u : 0u);
+      }
+#pragma unroll
+      for (int et = 0; et < ET; ++et) {
+        uint4& v = vf[et];
+        v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
+        odd |= odd_bits<T>(v.x) | odd_bits<T>(v.y) | odd_bits<T>(v.z) | odd_bits<T>(v.w);
+      }
+      if (__any(odd != 0)) {
+        x8 seen[CT];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) seen[ct][i] = key0 + (i >> 2) * 16 + g * 4 + (i & 3) <= last[ct] ? (T)1.f : (T)0.f;
+#pragma unroll
+        for (int et = 0; et < ET; ++et) {
+          __builtin_amdgcn_sched_barrier(0);                    // (one tile after the other: the path is rare, registers are not)
+          const uint4 kinds = make_uint4(take_odd<T>(vf[et].x), take_odd<T>(vf[et].y), take_odd<T>(vf[et].z), take_odd<T>(vf[et].w));
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            const f32x4 n = mma(__builtin_bit_cast(x8, kinds), seen[ct], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[ct][et][i] += odd_value(n[i]);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int et = 0; et < ET; ++et)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) o[ct][et] = mma(__builtin_bit_cast(x8, vf[et]), p[ct], o[ct][et]);
+    u = un;
+  }
+
+  // the four waves: maximum, sum and outputs as they are; whoever adds them scales them
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const float sum = groups_sum(l[ct]);
+    if (g == 0) {
+      s_m[wave][ct * 16 + j] = m[ct];
+      s_l[wave][ct * 16 + j] = sum;
+    }
+#pragma unroll
+    for (int et = 0; et < ET; ++et)
+      *reinterpret_cast<float4*>(&s_o[wave][ct * 16 + j][et * 16 + g * 4]) = make_float4(o[ct][et][0], o[ct][et][1], o[ct][et][2], o[ct][et][3]);
+  }
+  __syncthreads();
+  join_waves<T, HD, 16 * CT>(c, a, sp, w, s_o, s_m, s_l, &s_last);
+}
+
+}  // namespace
+
+int check_stream(hipStream_t st) {
+  int here = -1;
+  if (hipGetDevice(&here) != hipSuccess) return STAIRS_EHIP;
+  if (!st) return STAIRS_OK;
+  hipDevice_t its = -1;
+  if (hipStreamGetDevice(st, &its) != hipSuccess) return STAIRS_EHIP;
+  return its == here ? STAIRS_OK : STAIRS_EINVAL;
+}
+
+}  // namespace stairs
+
+using namespace stairs;
+
+namespace {
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+bool cache_ok(const stairs_paged_cache* c) {
+  if (!c || (c->dtype != STAIRS_DTYPE_BF16 && c->dtype != STAIRS_DTYPE_FP16)) return false;
+  if (c->page_size != 32 && c->page_size != 64 && c->page_size != 128 && c->page_size != 256) return false;
+  if (c->head_dim != 64 && c->head_dim != 128) return false;
+  if (c->n_kv_heads < 1 || c->n_kv_heads > 4096 || c->n_pages < 1 || (int64_t)c->n_pages * c->page_size > INT32_MAX) return false;
+  return c->k && c->v && aligned16(c->k) && aligned16(c->v);
+}
+
+// every stride holds a row and keeps its 16-byte alignment
+bool stride_ok(int64_t stride, int heads, int hd) { return stride >= (int64_t)heads * hd && stride % 8 == 0; }
+
+int launched() { return hipGetLastError() == hipSuccess ? STAIRS_OK : STAIRS_EHIP; }
+
+// f(type, head_dim) for the cache's
+template <typename F>
+void by_type(const stairs_paged_cache* c, F f) {
+  const bool b = c->dtype == STAIRS_DTYPE_BF16;
+  if (c->head_dim == 64) b ? f(__bf16{}, std::integral_constant<int, 64>{}) : f(_Float16{}, std::integral_constant<int, 64>{});
+  else b ? f(__bf16{}, std::integral_constant<int, 128>{}) : f(_Float16{}, std::integral_constant<int, 128>{});
+}
+
+bool attn_sizes_ok(const stairs_paged_cache* c, const stairs_paged_attn* a) {
+  if (!cache_ok(c) || !a) return false;
+  if (a->n_seqs < 0 || a->n_seqs > STAIRS_PAGED_MAX_SEQS || a->max_blocks < 1 || a->rows < 0 || a->max_fresh < 0) return false;
+  if ((int64_t)a->max_blocks * c->page_size > INT32_MAX) return false;
+  if (a->n_heads < 1 || (int64_t)a->rows * a->n_heads / c->n_kv_heads > 1 << 24) return false;   // (counts of tiles stay ints)
+  return a->n_heads >= 1 && a->n_heads <= 4096 && a->n_heads % c->n_kv_heads == 0;
+}
+
+}  // namespace
+
+extern "C" int stairs_paged_plan(const stairs_page_plan* p, void* hip_stream) {
+  if (!p || p->n_seqs < 0 || p->n_seqs > STAIRS_PAGED_MAX_SEQS || p->max_blocks < 1 || p->max_rows < 0 || p->n_pages < 1) return STAIRS_EINVAL;
+  if (p->page_size != 32 && p->page_size != 64 && p->page_size != 128 && p->page_size != 256) return STAIRS_EINVAL;
+  if ((int64_t)p->n_pages * p->page_size > INT32_MAX || (int64_t)p->max_blocks * p->page_size > INT32_MAX) return STAIRS_EINVAL;
+  if (!p->n_free || !p->n_free_out || !p->free_pages || !p->row_start) return STAIRS_EINVAL;
+  if (p->n_seqs > 0 && (!p->cached || !p->fresh || !p->held || !p->held_out || !p->block_table || !p->seq_len)) return STAIRS_EINVAL;
+  if (p->max_rows > 0 && (!p->position || !p->slot)) return STAIRS_EINVAL;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (const int rc = check_stream(st)) return rc;
+  const bool one = p->max_rows <= 4 * kPlanThreads;
+  hipLaunchKernelGGL(k_paged_plan, dim3(1), dim3(kPlanThreads), 0, st, *p, one ? p->max_rows : 0);
+  if (!one) hipLaunchKernelGGL(k_paged_slots, dim3((p->max_rows + 255) / 256), dim3(256), 0, st, *p);
+  return launched();
+}
+
+extern "C" int stairs_paged_append(const stairs_paged_cache* c, const stairs_paged_rows* a, void* hip_stream) {
+  if (!cache_ok(c) || !a || a->rows < 0 || a->n_heads < 0 || a->n_heads > 4096) return STAIRS_EINVAL;
+  if (!(a->rope_theta >= 0.f) || std::isinf(a->rope_theta)) return STAIRS_EINVAL;
+  if (a->rows == 0) return STAIRS_OK;
+  if (!a->k || !a->v || !a->slot || (a->rope_theta > 0.f && !a->position)) return STAIRS_EINVAL;
+  if (!aligned16(a->k) || !aligned16(a->v) || !stride_ok(a->k_stride, c->n_kv_heads, c->head_dim) || !stride_ok(a->v_stride, c->n_kv_heads, c->head_dim))
+    return STAIRS_EINVAL;
+  if (a->n_heads > 0 && (!a->q || !a->q_out || !aligned16(a->q) || !aligned16(a->q_out) || !stride_ok(a->q_stride, a->n_heads, c->head_dim) ||
+                         !stride_ok(a->q_out_stride, a->n_heads, c->head_dim) || (a->q == a->q_out && a->q_stride != a->q_out_stride)))
+    return STAIRS_EINVAL;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (const int rc = check_stream(st)) return rc;
+  stairs_paged_rows r = *a;
+  if (r.rope_theta == 0.f && r.q == r.q_out) r.n_heads = 0;       // nothing happens to q
+  by_type(c, [&](auto type, auto hd) {
+    hipLaunchKernelGGL((k_paged_append<decltype(type), decltype(hd)::value>), dim3(r.rows), dim3(256), 0, st, *c, r);
+  });
+  return launched();
+}
+
+namespace {
+
+// ---- how a call is spread: by its sizes on the host, by the lengths on the device (find_piece) ------------------------
+constexpr int kCus = 256;
+struct Launch {
+  Span span;
+  int ct;
+  size_t work_bytes;
+  unsigned grid;
+};
+Launch plan_rows(const stairs_paged_cache* c, const stairs_paged_attn* a) {
+  const int G = a->n_heads / c->n_kv_heads;
+  Launch l{};
+  l.ct = (int64_t)a->max_fresh * G <= 16 ? 1 : 2;
+  l.span = Span{1, INT32_MAX, 16 * l.ct, kRowUnit, 2 * kCus};
+  l.work_bytes = (size_t)most_pieces(l.span.slots) * (sizeof(int) + (size_t)l.span.tile_cols * (c->head_dim + 2) * sizeof(float));
+  // at most `slots` pieces and one a tile
+  const int64_t tiles = a->n_seqs + (int64_t)a->rows * G / l.span.tile_cols;
+  l.grid = (unsigned)std::min<int64_t>(l.span.slots + tiles * c->n_kv_heads, INT32_MAX);
+  return l;
+}
+
+}  // namespace
+
+extern "C" int64_t stairs_paged_attention_workspace(const stairs_paged_cache* c, const stairs_paged_attn* a) {
+  if (!attn_sizes_ok(c, a)) return STAIRS_EINVAL;
+  return (int64_t)plan_rows(c, a).work_bytes;
+}
+
+extern "C" int stairs_paged_attention(const stairs_paged_cache* c, const stairs_paged_attn* a, void* hip_stream) {
+  if (!attn_sizes_ok(c, a) || std::isnan(a->scale) || std::isinf(a->scale)) return STAIRS_EINVAL;
+  if (a->n_seqs == 0 || a->rows == 0) return STAIRS_OK;
+  if (!a->q || !a->out || a->q == a->out || !a->block_table || !a->row_start || !a->seq_len) return STAIRS_EINVAL;
+  if (!aligned16(a->q) || !aligned16(a->out) || !stride_ok(a->q_stride, a->n_heads, c->head_dim) || !stride_ok(a->out_stride, a->n_heads, c->head_dim))
+    return STAIRS_EINVAL;
+  if (!a->workspace || !aligned16(a->workspace)) return STAIRS_EINVAL;
+  const Launch rows = plan_rows(c, a);
+  if (a->workspace_bytes < (int64_t)rows.work_bytes) return STAIRS_ECAPACITY;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (const int rc = check_stream(st)) return rc;
+  const float scale2 = (a->scale > 0.f ? a->scale : 1.0f / sqrtf((float)c->head_dim)) * kLog2e;
+  by_type(c, [&](auto type, auto hd) {
+    typedef decltype(type) T;
+    constexpr int HD = decltype(hd)::value;
+    if (rows.ct == 1)
+      hipLaunchKernelGGL((k_paged_rows<T, HD, 1>), dim3(rows.grid), dim3(256), 0, st, *c, *a, rows.span, scale2);
+    else
+      hipLaunchKernelGGL((k_paged_rows<T, HD, 2>), dim3(rows.grid), dim3(256), 0, st, *c, *a, rows.span, scale2);
+  });
+  return launched();
+}
