@@ -225,20 +225,26 @@ __device__ __forceinline__ uint32_t odd_bits(uint32_t u) {
   return ((u & m) + one) & 0x80008000u;
 }
 
-// Takes the infinities and NaNs out of a pair of values and says what they were: 1 for +infinity, 64 for -infinity, 4096 for NaN.
-// Summed over the keys that a column sees (32 at most, so the three counts stay apart) they say what belongs in its sum.
+// Keeps of a pair of values what `keep` says but infinities and NaNs; not 0: there was one
 template <typename T>
-__device__ __forceinline__ uint32_t take_odd(uint32_t& v) {
+__device__ __forceinline__ uint32_t clear_odd(uint32_t& v, uint32_t keep) {
+  v &= keep;
+  const uint32_t e = odd_bits<T>(v);
+  v &= ~((e >> 15) * 0xFFFFu);
+  return e;
+}
+// What a pair of values is: 1 for +infinity, 64 for -infinity, 4096 for NaN, as numbers of the type.  Summed over the keys that a
+// column sees (32 at most, so the three counts stay apart) they say what belongs in its sum.
+template <typename T>
+__device__ __forceinline__ uint32_t odd_kinds(uint32_t v) {
   constexpr bool b = __is_same(T, __bf16);
   constexpr uint32_t inf = b ? 0x7F80u : 0x7C00u, one = b ? 0x3F80u : 0x3C00u, k64 = b ? 0x4280u : 0x5400u, k4096 = b ? 0x4580u : 0x6C00u;
-  uint32_t kinds = 0, left = 0;
+  uint32_t kinds = 0;
 #pragma unroll
   for (int h = 0; h < 32; h += 16) {
     const uint32_t x = (v >> h) & 0xFFFFu, m = x & 0x7FFFu;
     kinds |= (m < inf ? 0u : m > inf ? k4096 : x > m ? k64 : one) << h;
-    left |= (m < inf ? x : 0u) << h;
   }
-  v = left;
   return kinds;
 }
 __device__ __forceinline__ float odd_value(float n) {
@@ -390,16 +396,26 @@ __device__ __forceinline__ void store_out(const stairs_paged_cache& c, const sta
 }
 __device__ __forceinline__ float weight_of(float m, float all) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - all); }
 
-// The last of a split tile's work-groups joins its pieces, in their order whoever it is.  Everything is requested before anything
-// is waited for: all pieces' maxima and sums, and eight outputs a thread (one after the other, each a round trip past the
-// caches, the maxima and sums alone of 32 pieces were 30 us).
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// 16 bytes past the caches that XCDs do not share (what ld_dev and st_dev do for 4 and 8)
+__device__ __forceinline__ float4 ld_dev4(const float* base, int offset) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0, 0xFFFFFFFFu, 0x00027000);
+  return __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(r, offset * 4, 0, 16));
+}
+__device__ __forceinline__ void st_dev4(float* base, int offset, float4 v) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(base, 0, 0xFFFFFFFFu, 0x00027000);
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, offset * 4, 0, 16);
+}
+// The last of a split tile's work-groups joins its pieces, in their order whoever it is.  All maxima and sums are requested at once,
+// then sixteen outputs a thread (one after the other, each a round trip past the caches, the maxima and sums alone of 32
+// pieces were 30 us); the code is kept short, it runs once and comes from memory (unrolled over everything: 5 us more).
 template <typename T, int HD, int COLS>
 __device__ __forceinline__ void join_pieces(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, const Piece& w, float2* s_ml, int* s_last) {
   int* counter = tickets(a, sp) + w.first;
   if (!last_arrival(counter, w.pieces, s_last)) return;
-  constexpr int NT = 256;
-  const int step = (int)(piece_floats<HD>(COLS) * c.n_kv_heads);
-  const float* base = partials(a, sp) + (size_t)w.first * piece_floats<HD>(COLS);
+  constexpr int NT = 256, TB = COLS <= 32 ? 1 : 4, PB = 16 / TB;
+  const size_t step = piece_floats<HD>(COLS) * c.n_kv_heads;
+  float* base = partials(a, sp) + (size_t)w.first * piece_floats<HD>(COLS);
   const int G = a.n_heads / c.n_kv_heads, col0 = w.group * COLS, cols = min(COLS, w.rows * G - col0);
   constexpr int MLS = (kMaxPieces * COLS + NT - 1) / NT;
   float2 ml[MLS];
@@ -421,30 +437,41 @@ __device__ __forceinline__ void join_pieces(const stairs_paged_cache& c, const s
   }
   __syncthreads();
 #pragma unroll 1
-  for (int i = threadIdx.x; i < cols * (HD / 4); i += NT) {
-    const int col = i / (HD / 4);
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
+  for (int t0 = 0; t0 * NT < cols * (HD / 4); t0 += TB) {
+    float4 v[TB];
+    float l[TB];
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+      v[t] = make_float4(0.f, 0.f, 0.f, 0.f);
+      l[t] = 0.f;
+    }
 #pragma unroll 1
-    for (int p0 = 0; p0 < w.pieces; p0 += 8) {
-      float2 x[8], y[8];
+    for (int p0 = 0; p0 < w.pieces; p0 += PB) {
+      float4 x[PB][TB];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float* at = base + min(p0 + k, w.pieces - 1) * step + i * 4;
-        x[k] = ld_dev2(at);
-        y[k] = ld_dev2(at + 2);
-      }
+      for (int k = 0; k < PB; ++k)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float2 f = s_ml[(p0 + k) * COLS + col];
-        l += f.y;
-        v.x += f.x * x[k].x;
-        v.y += f.x * x[k].y;
-        v.z += f.x * y[k].x;
-        v.w += f.x * y[k].y;
+        for (int t = 0; t < TB; ++t) x[k][t] = ld_dev4(base + min(p0 + k, w.pieces - 1) * step, (threadIdx.x + (t0 + t) * NT) * 4);
+      __builtin_amdgcn_sched_barrier(0);                        // (all of them on their way before the first is waited for)
+#pragma unroll
+      for (int k = 0; k < PB; ++k) {
+        const bool there = p0 + k < w.pieces;                   // (behind the last piece: the last one again, for nothing)
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+          const float2 f = s_ml[(p0 + k) * COLS + (threadIdx.x + (t0 + t) * NT) / (HD / 4)];
+          l[t] += f.y;
+          v[t].x += there ? f.x * x[k][t].x : 0.f;
+          v[t].y += there ? f.x * x[k][t].y : 0.f;
+          v[t].z += there ? f.x * x[k][t].z : 0.f;
+          v[t].w += there ? f.x * x[k][t].w : 0.f;
+        }
       }
     }
-    store_out<T, HD>(c, a, w, col0 + col, i % (HD / 4) * 4, v, l);
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+      const int i = threadIdx.x + (t0 + t) * NT;
+      if (i < cols * (HD / 4)) store_out<T, HD>(c, a, w, col0 + i / (HD / 4), i % (HD / 4) * 4, v[t], l[t]);
+    }
   }
   if (threadIdx.x == 0) *counter = 0;
 }
@@ -477,8 +504,7 @@ __device__ __forceinline__ void join_waves(const stairs_paged_cache& c, const st
     if (w.pieces == 1) {
       store_out<T, HD>(c, a, w, col0 + col, e, v, l);
     } else {
-      st_dev2(part + col * HD + e, v.x, v.y);
-      st_dev2(part + col * HD + e + 2, v.z, v.w);
+      st_dev4(part, col * HD + e, v);
       if (e == 0) st_dev2(part + COLS * HD + col * 2, m, l);
     }
   }
@@ -491,7 +517,6 @@ __device__ __forceinline__ void join_waves(const stairs_paged_cache& c, const st
 // wave), no LDS, and are joined at the end.  Values are requested before the scores they wait for, the next block's keys as
 // soon as this block's are used.
 constexpr int kRowUnit = 32 * 4;
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint4 ld_once(const void* p) {        // (streaming hint: 3 x 32 heads of up to 59999 keys 384 -> 366 us)
   const u32x4 v = __builtin_nontemporal_load(static_cast<const u32x4*>(p));
   return make_uint4(v[0], v[1], v[2], v[3]);
@@ -515,6 +540,7 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
   const int last_last = min(pos0 + (min(cols, col0 + 16 * CT) - 1) / G, limit - 1);
   int last[CT];
   x8 q[CT][KK];
+  bool had_odd = false;                                         // the wave has left infinities or NaNs in its part of lds.o
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
     const int col = col0 + ct * 16 + j;
@@ -592,6 +618,7 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
       }
     const int key0 = u * kRowUnit + wave * 32;
     const int un = next_block(u + 1);
+    const size_t at_here = at;
     if (un < u1) {
       at = block_at(un);
       load_keys(at);
@@ -626,7 +653,7 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
     }
     if (!full) {
       // Some keys of the block are not seen by all columns.  Their probability is 0, and 0 times what is there must be 0: what
-      // no column sees is cleared, an infinity or NaN that some columns see is taken out and given to those that do.
+      // no column sees is cleared, and so are infinities and NaNs; those that some columns see are looked at again (odd_values).
       uint32_t keep[4], odd = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -635,25 +662,31 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
       }
 #pragma unroll
       for (int et = 0; et < ET; ++et) {
-        uint4& v = vf[et];
-        v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
-        odd |= odd_bits<T>(v.x) | odd_bits<T>(v.y) | odd_bits<T>(v.z) | odd_bits<T>(v.w);
+        odd |= clear_odd<T>(vf[et].x, keep[0]);
+        odd |= clear_odd<T>(vf[et].y, keep[1]);
+        odd |= clear_odd<T>(vf[et].z, keep[2]);
+        odd |= clear_odd<T>(vf[et].w, keep[3]);
+        __builtin_amdgcn_sched_barrier(0);                      // (one tile after the other: their temporaries share registers)
       }
       if (__any(odd != 0)) {
+        if (!had_odd)
+          for (int i = lane; i < 16 * CT * (HD + 4); i += 64) (&lds.o[wave][0][0])[i] = 0.f;
+        had_odd = true;
         x8 seen[CT];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
           for (int i = 0; i < 8; ++i) seen[ct][i] = key0 + (i >> 2) * 16 + g * 4 + (i & 3) <= last[ct] ? (T)1.f : (T)0.f;
-#pragma unroll
+#pragma unroll 1
         for (int et = 0; et < ET; ++et) {
-          __builtin_amdgcn_sched_barrier(0);                    // (one tile after the other: the path is rare, registers are not)
-          const uint4 kinds = make_uint4(take_odd<T>(vf[et].x), take_odd<T>(vf[et].y), take_odd<T>(vf[et].z), take_odd<T>(vf[et].w));
+          uint4 v = *reinterpret_cast<const uint4*>(V + at_here + (et * 64 + lane) * 8);
+          v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
+          const uint4 kinds = make_uint4(odd_kinds<T>(v.x), odd_kinds<T>(v.y), odd_kinds<T>(v.z), odd_kinds<T>(v.w));
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
-            const f32x4 n = mma(__builtin_bit_cast(x8, kinds), seen[ct], f32x4{0.f, 0.f, 0.f, 0.f});
+            const f32x4 count = mma(__builtin_bit_cast(x8, kinds), seen[ct], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[ct][et][i] += odd_value(n[i]);
+            for (int i = 0; i < 4; ++i) lds.o[wave][ct * 16 + j][et * 16 + g * 4 + i] += odd_value(count[i]);
           }
         }
       }
@@ -674,8 +707,15 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
       lds.l[wave][ct * 16 + j] = sum;
     }
 #pragma unroll
-    for (int et = 0; et < ET; ++et)
-      *reinterpret_cast<float4*>(&lds.o[wave][ct * 16 + j][et * 16 + g * 4]) = make_float4(o[ct][et][0], o[ct][et][1], o[ct][et][2], o[ct][et][3]);
+    for (int et = 0; et < ET; ++et) {
+      float4* dst = reinterpret_cast<float4*>(&lds.o[wave][ct * 16 + j][et * 16 + g * 4]);
+      float4 v = make_float4(o[ct][et][0], o[ct][et][1], o[ct][et][2], o[ct][et][3]);
+      if (had_odd) {
+        const float4 x = *dst;
+        v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+      }
+      *dst = v;
+    }
   }
   __syncthreads();
   join_waves<T, HD, 16 * CT>(c, a, sp, w, lds.o, lds.m, lds.l, &lds.last);
@@ -769,98 +809,119 @@ __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const 
     fetch_pages(w.u0);
     request(w.u0, w.u0 & 1);
   }
-  for (int u = w.u0; u < u1; ++u) {
-    const int buf = u & 1;
-    const int page0 = page_of(u, 0), page1 = page_of(u, 1);
+  // Two loops of one body: units that all of the wave's columns see, then those with masks (with both in one loop the 64 output
+  // registers were copied twice a unit).  A wave goes from one to the other when it has to; barriers are one a unit in both.
+  int u = w.u0;
+  int page0 = -1, page1 = -1;
+  auto next_unit = [&]() {                                      // unit u is in LDS, the next one on its way
+    page0 = page_of(u, 0);
+    page1 = page_of(u, 1);
     if (u + 1 - pages_at >= 32) fetch_pages(u + 1);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // this unit is there, the other buffer has been read
-    if (u + 1 < u1) request(u + 1, buf ^ 1);
-    const int key0 = u * kChunkUnit;
-    if (key0 > last_wave) continue;                             // (nothing for this wave any more)
-    f32x16 s[2];
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // unit u is there, the other buffer has been read
+    if (u + 1 < u1) request(u + 1, (u + 1) & 1);
+  };
+  auto scores = [&](f32x16 (&s)[2]) {
+    s[0] = s[1] = f32x16{};
+    const uint4* kt = lds.tile[u & 1][0][0] + (n >> 4) * (HD / 32) * 64 + (n & 15) + 16 * h;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      s[b] = f32x16{};
-      const uint4* kt = lds.tile[buf][b][0] + (n >> 4) * (HD / 32) * 64 + (n & 15) + 16 * h;
+    for (int k = 0; k < KS; ++k)
 #pragma unroll
-      for (int k = 0; k < KS; ++k) s[b] = mma(__builtin_bit_cast(x8, kt[(k >> 1) * 64 + 32 * (k & 1)]), q[k], s[b]);
-    }
-    const bool full = key0 + kChunkUnit - 1 <= first_wave && page0 >= 0 && page1 >= 0;
-    float x[32];
+      for (int b = 0; b < 2; ++b) s[b] = mma(__builtin_bit_cast(x8, kt[b * 8 * HD + (k >> 1) * 64 + 32 * (k & 1)]), q[k], s[b]);
+  };
+  // (m: the reference point in units of the raw score)
+  auto probabilities = [&](const f32x16 (&s)[2], x8 (&p)[2][2]) {
+    // (the maximum that passes NaN on, one instruction for three values; a NaN makes the column's sum NaN whatever m is)
+    float mx = __builtin_elementwise_maximum(s[0][0], s[1][0]);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) x[i] = s[i >> 4][i & 15] * scale2;
-    if (!full) {
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const int key = key0 + (i >> 4) * 32 + (i >> 2 & 3) * 8 + h * 4 + (i & 3);
-        x[i] = key <= last && (i < 16 ? page0 : page1) >= 0 ? x[i] : -INFINITY;
-      }
-    }
-    float mx = x[0];
-#pragma unroll
-    for (int i = 1; i < 32; ++i) mx = fmaxf(mx, x[i]);
-    if (__any(mx > m + kMaxSlack)) {
+    for (int i = 1; i < 16; ++i) mx = __builtin_elementwise_maximum(mx, __builtin_elementwise_maximum(s[0][i], s[1][i]));
+    if (__any(mx * scale2 > m * scale2 + kMaxSlack)) {
       const float mn = fmaxf(m, halves_max(mx));
-      const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * scale2);
       m = mn;
       l *= f;
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] *= f;
     }
-    const float mr = m == -INFINITY ? 0.f : m;
-    x8 p[2][2];
+    const float mr = m == -INFINITY ? 0.f : -m * scale2;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-      x[i] = __builtin_amdgcn_exp2f(x[i] - mr);
-      sum[i & 3] += x[i];
-      p[i >> 4][i >> 2 & 1][(i & 3) + 4 * (i >> 3 & 1)] = Elem<T>::down(x[i]);
+      const float x = __builtin_amdgcn_exp2f(fmaf(s[i >> 4][i & 15], scale2, mr));
+      sum[i & 3] += x;
+      p[i >> 4][i >> 2 & 1][(i & 3) + 4 * (i >> 3 & 1)] = Elem<T>::down(x);
     }
     l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    if (full) {
+  };
+  for (; u < u1; ++u) {
+    const int key0 = u * kChunkUnit;
+    if (key0 + kChunkUnit - 1 > first_wave || page_of(u, 0) < 0 || page_of(u, 1) < 0) break;
+    next_unit();
+    f32x16 s[2];
+    x8 p[2][2];
+    scores(s);
+    probabilities(s, p);
+    const uint4* vt = lds.tile[u & 1][0][1] + (n >> 4) * 64 + (n & 15) + 16 * h;
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const uint4* vt = lds.tile[buf][b][1] + (2 * d + (n >> 4)) * 64 + (n & 15) + 16 * h;
-          o[d] = mma(__builtin_bit_cast(x8, vt[0]), p[b][0], o[d]);
-          o[d] = mma(__builtin_bit_cast(x8, vt[32]), p[b][1], o[d]);
-        }
-    } else {
-      // as in attend_rows: what no column of the wave sees is cleared, infinities and NaNs go to the columns that see them
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] = mma(__builtin_bit_cast(x8, vt[b * 8 * HD + d * 128 + r * 32]), p[b][r], o[d]);
+  }
 #pragma unroll 1
-      for (int b = 0; b < 2; ++b) {
-        const int end = (b ? page1 : page0) < 0 ? -1 : last_wave, mine = (b ? page1 : page0) < 0 ? -1 : last;
+  for (; u < u1; ++u) {
+    const int key0 = u * kChunkUnit;
+    next_unit();
+    if (key0 > last_wave) continue;                             // (nothing for this wave any more)
+    f32x16 s[2];
+    x8 p[2][2];
+    scores(s);
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const int key = key0 + b * 32 + r * 8 + h * 4;
-          uint32_t keep[4];
+    for (int i = 0; i < 32; ++i) {
+      const int key = key0 + (i >> 4) * 32 + (i >> 2 & 3) * 8 + h * 4 + (i & 3);
+      float& x = reinterpret_cast<float*>(&s[i >> 4])[i & 15];
+      x = key <= last && (i < 16 ? page0 : page1) >= 0 ? x : -INFINITY;
+    }
+    probabilities(s, p);
+    // as in attend_rows: what no column of the wave sees is cleared, infinities and NaNs go to the columns that see them
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int end = (b ? page1 : page0) < 0 ? -1 : last_wave, mine = (b ? page1 : page0) < 0 ? -1 : last;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int key = key0 + b * 32 + r * 8 + h * 4;
+        uint32_t keep[4], odd = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int k = key + (i >> 1) * 16 + (i & 1) * 2;
+          keep[i] = (k <= end ? 0xFFFFu : 0u) | (k + 1 <= end ? 0xFFFF0000u : 0u);
+        }
+        const uint4* vt = lds.tile[u & 1][b][1] + (n >> 4) * 64 + (n & 15) + 16 * h + r * 32;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          uint4 v = vt[d * 128];
+          odd |= clear_odd<T>(v.x, keep[0]) | clear_odd<T>(v.y, keep[1]) | clear_odd<T>(v.z, keep[2]) | clear_odd<T>(v.w, keep[3]);
+          o[d] = mma(__builtin_bit_cast(x8, v), p[b][r], o[d]);
+        }
+        if (__any(odd != 0)) {
           x8 seen;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int k = key + (i >> 1) * 16 + (i & 1) * 2;
-            keep[i] = (k <= end ? 0xFFFFu : 0u) | (k + 1 <= end ? 0xFFFF0000u : 0u);
-            seen[2 * i] = k <= mine ? (T)1.f : (T)0.f;
-            seen[2 * i + 1] = k + 1 <= mine ? (T)1.f : (T)0.f;
-          }
-          const x8 pr = b ? p[1][r] : p[0][r];
+          for (int i = 0; i < 8; ++i) seen[i] = key + (i >> 2) * 16 + (i & 3) <= mine ? (T)1.f : (T)0.f;
 #pragma unroll
           for (int d = 0; d < DT; ++d) {
-            uint4 v = lds.tile[buf][b][1][(2 * d + (n >> 4)) * 64 + (n & 15) + 16 * h + 32 * r];
+            uint4 v = vt[d * 128];
             v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
-            if (__any((odd_bits<T>(v.x) | odd_bits<T>(v.y) | odd_bits<T>(v.z) | odd_bits<T>(v.w)) != 0)) {
-              const uint4 kinds = make_uint4(take_odd<T>(v.x), take_odd<T>(v.y), take_odd<T>(v.z), take_odd<T>(v.w));
-              const f32x16 count = mma(__builtin_bit_cast(x8, kinds), seen, f32x16{});
+            const uint4 kinds = make_uint4(odd_kinds<T>(v.x), odd_kinds<T>(v.y), odd_kinds<T>(v.z), odd_kinds<T>(v.w));
+            const f32x16 count = mma(__builtin_bit_cast(x8, kinds), seen, f32x16{});
 #pragma unroll
-              for (int i = 0; i < 16; ++i) o[d][i] += odd_value(count[i]);
-            }
-            o[d] = mma(__builtin_bit_cast(x8, v), pr, o[d]);
+            for (int i = 0; i < 16; ++i) o[d][i] += odd_value(count[i]);
           }
         }
       }
     }
   }
   l = halves_sum(l);
+  m = m == -INFINITY ? m : m * scale2;                          // (what the join works with)
   if (w.pieces == 1) {
     if (col < cols) {
       const float f = l == 0.f ? 0.f : 1.f / l;
@@ -879,13 +940,12 @@ __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const 
   }
   float* part = partials(a, sp) + (size_t)(w.first + w.piece * c.n_kv_heads) * piece_floats<HD>(kChunkCols);
   if (col < cols) {
-    float* dst = part + (col - col0) * HD + h * 4;
+    const int dst = (col - col0) * HD + h * 4;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        st_dev2(dst + d * 32 + b * 8, o[d][b * 4], o[d][b * 4 + 1]);
-        st_dev2(dst + d * 32 + b * 8 + 2, o[d][b * 4 + 2], o[d][b * 4 + 3]);
+        st_dev4(part, dst + d * 32 + b * 8, make_float4(o[d][b * 4], o[d][b * 4 + 1], o[d][b * 4 + 2], o[d][b * 4 + 3]));
       }
     if (h == 0) st_dev2(part + kChunkCols * HD + (col - col0) * 2, m, l);
   }

@@ -225,20 +225,26 @@ __device__ __forceinline__ uint32_t odd_bits(uint32_t u) {
   return ((u & m) + one) & 0x80008000u;
 }
 
-// Takes the infinities and NaNs out of a pair of values and says what they were: 1 for +infinity, 64 for -infinity, 4096 for NaN.
-// Summed over the keys that a column sees (32 at most, so the three counts stay apart) they say what belongs in its sum.
+// Keeps of a pair of values what `keep` says but infinities and NaNs; not 0: there was one
 template <typename T>
-__device__ __forceinline__ uint32_t take_odd(uint32_t& v) {
+__device__ __forceinline__ uint32_t clear_odd(uint32_t& v, uint32_t keep) {
+  v &= keep;
+  const uint32_t e = odd_bits<T>(v);
+  v &= ~((e >> 15) * 0xFFFFu);
+  return e;
+}
+// What a pair of values is: 1 for +infinity, 64 for -infinity, 4096 for NaN, as numbers of the type.  Summed over the keys that a
+// column sees (32 at most, so the three counts stay apart) they say what belongs in its sum.
+template <typename T>
+__device__ __forceinline__ uint32_t odd_kinds(uint32_t v) {
   constexpr bool b = __is_same(T, __bf16);
   constexpr uint32_t inf = b ? 0x7F80u : 0x7C00u, one = b ? 0x3F80u : 0x3C00u, k64 = b ? 0x4280u : 0x5400u, k4096 = b ? 0x4580u : 0x6C00u;
-  uint32_t kinds = 0, left = 0;
+  uint32_t kinds = 0;
 #pragma unroll
   for (int h = 0; h < 32; h += 16) {
     const uint32_t x = (v >> h) & 0xFFFFu, m = x & 0x7FFFu;
     kinds |= (m < inf ? 0u : m > inf ? k4096 : x > m ? k64 : one) << h;
-    left |= (m < inf ? x : 0u) << h;
   }
-  v = left;
   return kinds;
 }
 __device__ __forceinline__ float odd_value(float n) {
@@ -256,9 +262,10 @@ struct Span {
   int min_cols, max_cols;     // sequences with so many columns (rows times heads a key head has)
   int tile_cols, unit;        // columns of a tile, keys of a unit
   int slots;
+  int min_units, whole;       // of a piece; tiles that are not cut (find_piece)
+  int first_block;            // the launch's work-groups from here on
+  int64_t work;               // bytes in front of its part of the workspace
 };
-constexpr int kMinUnits = 4;          // of a piece: fewer cost more to join than they save (8000 keys of 8 heads alone: 25 us with 2, 19 with 4)
-constexpr int kWhole = 200;            // tiles that make nearly every CU busy
 constexpr int kMaxPieces = 32;        // of a tile: whoever joins them reads them all
 struct Piece {
   int seq, row0, rows, len;   // rows of the sequence, its length (not cut to the table)
@@ -297,7 +304,7 @@ __device__ __forceinline__ int quotient(long long a, int b) {    // a >= 0, b > 
 }
 __device__ __forceinline__ bool find_piece(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, Piece& out) {
   const int lane = threadIdx.x & 63;
-  const int kvh = blockIdx.x % c.n_kv_heads, item = blockIdx.x / c.n_kv_heads;
+  const int block = blockIdx.x - sp.first_block, kvh = block % c.n_kv_heads, item = block / c.n_kv_heads;
   long long units = 0;
   int tiles = 0, most = 0;
   SeqWork w;
@@ -316,7 +323,7 @@ __device__ __forceinline__ bool find_piece(const stairs_paged_cache& c, const st
   units *= c.n_kv_heads;
   const long long all_tiles = (long long)tiles * c.n_kv_heads;
   int per;
-  if (all_tiles >= kWhole && units * 4 >= all_tiles * most * 3) {
+  if (all_tiles >= sp.whole && units * 4 >= all_tiles * most * 3) {
     // Tiles of about one length for nearly every CU stay whole: half as many streams, and nothing to join (32 sequences of 2048
     // keys, 8 heads: 46 us whole, 58 in halves; of 8192 keys 162 and 189).
     per = max(1, most);
@@ -324,8 +331,8 @@ __device__ __forceinline__ bool find_piece(const stairs_paged_cache& c, const st
     // Pieces of one size, for which they all run at once: a second round, however short, costs a whole piece's latencies (32
     // verifications of 200 .. 8000 keys: 79 us with 612 pieces, 66 with 490).  With more tiles than run at once anyway, or more
     // sequences than lanes, the even share.
-    per = max(kMinUnits, quotient(units + sp.slots - 1, sp.slots));
-    if (a.n_seqs <= 64 && per > kMinUnits && per < most) {
+    per = max(sp.min_units, quotient(units + sp.slots - 1, sp.slots));
+    if (a.n_seqs <= 64 && per > sp.min_units && per < most) {
       const float fit = (float)(sp.slots / c.n_kv_heads);
       int lo = per, hi = 4 * per;                               // (up to 4 shares: beyond that one round is no aim any more)
       while (lo < hi) {
@@ -355,11 +362,11 @@ __device__ __forceinline__ bool find_piece(const stairs_paged_cache& c, const st
       out.rows = __builtin_amdgcn_readlane(w.rows, l);
       out.len = __builtin_amdgcn_readlane(w.len, l);
       out.pieces = n;
-      out.group = __builtin_amdgcn_readfirstlane(group);
+      out.group = __builtin_amdgcn_readlane(w.groups, l) - 1 - __builtin_amdgcn_readfirstlane(group);   // (the last rows see most: first)
       out.piece = __builtin_amdgcn_readfirstlane(at - group * n);
       out.u0 = __builtin_amdgcn_readfirstlane((unsigned)u * out.piece / n);        // (26 bits of units, 5 of pieces)
       out.u1 = __builtin_amdgcn_readfirstlane((unsigned)u * (out.piece + 1) / n);
-      out.first = (__builtin_amdgcn_readlane(split_to, l) - __builtin_amdgcn_readlane(split, l) + out.group * out.pieces) * c.n_kv_heads + kvh;
+      out.first = (__builtin_amdgcn_readlane(split_to, l) - __builtin_amdgcn_readlane(split, l) + (int)at - out.piece) * c.n_kv_heads + kvh;
       out.kvh = kvh;
       return true;
     }
@@ -374,6 +381,8 @@ __host__ __device__ constexpr int most_pieces(int slots) { return 2 * slots; }
 
 // ---- joining ------------------------------------------------------------------------------------------------------------
 // Partial results of a piece: [tile_cols][HD] outputs relative to the column's maximum, then [tile_cols] (maximum, sum) pairs.
+__device__ __forceinline__ int* tickets(const stairs_paged_attn& a, const Span& sp) { return reinterpret_cast<int*>(static_cast<char*>(a.workspace) + sp.work); }
+__device__ __forceinline__ float* partials(const stairs_paged_attn& a, const Span& sp) { return reinterpret_cast<float*>(tickets(a, sp) + most_pieces(sp.slots)); }
 template <int HD>
 __host__ __device__ constexpr size_t piece_floats(int tile_cols) { return (size_t)tile_cols * (HD + 2); }
 
@@ -387,16 +396,26 @@ __device__ __forceinline__ void store_out(const stairs_paged_cache& c, const sta
 }
 __device__ __forceinline__ float weight_of(float m, float all) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - all); }
 
-// The last of a split tile's work-groups joins its pieces, in their order whoever it is.  Everything is requested before anything
-// is waited for: all pieces' maxima and sums, and eight outputs a thread (one after the other, each a round trip past the
-// caches, the maxima and sums alone of 32 pieces were 30 us).
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// 16 bytes past the caches that XCDs do not share (what ld_dev and st_dev do for 4 and 8)
+__device__ __forceinline__ float4 ld_dev4(const float* base, int offset) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0, 0xFFFFFFFFu, 0x00027000);
+  return __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(r, offset * 4, 0, 16));
+}
+__device__ __forceinline__ void st_dev4(float* base, int offset, float4 v) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(base, 0, 0xFFFFFFFFu, 0x00027000);
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, offset * 4, 0, 16);
+}
+// The last of a split tile's work-groups joins its pieces, in their order whoever it is.  All maxima and sums are requested at once,
+// then sixteen outputs a thread (one after the other, each a round trip past the caches, the maxima and sums alone of 32
+// pieces were 30 us); the code is kept short, it runs once and comes from memory (unrolled over everything: 5 us more).
 template <typename T, int HD, int COLS>
 __device__ __forceinline__ void join_pieces(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, const Piece& w, float2* s_ml, int* s_last) {
-  int* counter = static_cast<int*>(a.workspace) + w.first;
+  int* counter = tickets(a, sp) + w.first;
   if (!last_arrival(counter, w.pieces, s_last)) return;
-  constexpr int NT = 256;
-  const int step = (int)(piece_floats<HD>(COLS) * c.n_kv_heads);
-  const float* base = reinterpret_cast<const float*>(static_cast<int*>(a.workspace) + most_pieces(sp.slots)) + (size_t)w.first * piece_floats<HD>(COLS);
+  constexpr int NT = 256, TB = COLS <= 32 ? 1 : 4, PB = X_PB / TB;
+  const size_t step = piece_floats<HD>(COLS) * c.n_kv_heads;
+  float* base = partials(a, sp) + (size_t)w.first * piece_floats<HD>(COLS);
   const int G = a.n_heads / c.n_kv_heads, col0 = w.group * COLS, cols = min(COLS, w.rows * G - col0);
   constexpr int MLS = (kMaxPieces * COLS + NT - 1) / NT;
   float2 ml[MLS];
@@ -418,30 +437,41 @@ __device__ __forceinline__ void join_pieces(const stairs_paged_cache& c, const s
   }
   __syncthreads();
 #pragma unroll 1
-  for (int i = threadIdx.x; i < cols * (HD / 4); i += NT) {
-    const int col = i / (HD / 4);
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
+  for (int t0 = 0; t0 * NT < cols * (HD / 4); t0 += TB) {
+    float4 v[TB];
+    float l[TB];
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+      v[t] = make_float4(0.f, 0.f, 0.f, 0.f);
+      l[t] = 0.f;
+    }
 #pragma unroll 1
-    for (int p0 = 0; p0 < w.pieces; p0 += 8) {
-      float2 x[8], y[8];
+    for (int p0 = 0; p0 < w.pieces; p0 += PB) {
+      float4 x[PB][TB];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float* at = base + min(p0 + k, w.pieces - 1) * step + i * 4;
-        x[k] = ld_dev2(at);
-        y[k] = ld_dev2(at + 2);
-      }
+      for (int k = 0; k < PB; ++k)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float2 f = s_ml[(p0 + k) * COLS + col];
-        l += f.y;
-        v.x += f.x * x[k].x;
-        v.y += f.x * x[k].y;
-        v.z += f.x * y[k].x;
-        v.w += f.x * y[k].y;
+        for (int t = 0; t < TB; ++t) x[k][t] = ld_dev4(base + min(p0 + k, w.pieces - 1) * step, (threadIdx.x + (t0 + t) * NT) * 4);
+      __builtin_amdgcn_sched_barrier(0);                        // (all of them on their way before the first is waited for)
+#pragma unroll
+      for (int k = 0; k < PB; ++k) {
+        const bool there = p0 + k < w.pieces;                   // (behind the last piece: the last one again, for nothing)
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+          const float2 f = s_ml[(p0 + k) * COLS + (threadIdx.x + (t0 + t) * NT) / (HD / 4)];
+          l[t] += f.y;
+          v[t].x += there ? f.x * x[k][t].x : 0.f;
+          v[t].y += there ? f.x * x[k][t].y : 0.f;
+          v[t].z += there ? f.x * x[k][t].z : 0.f;
+          v[t].w += there ? f.x * x[k][t].w : 0.f;
+        }
       }
     }
-    store_out<T, HD>(c, a, w, col0 + col, i % (HD / 4) * 4, v, l);
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+      const int i = threadIdx.x + (t0 + t) * NT;
+      if (i < cols * (HD / 4)) store_out<T, HD>(c, a, w, col0 + i / (HD / 4), i % (HD / 4) * 4, v[t], l[t]);
+    }
   }
   if (threadIdx.x == 0) *counter = 0;
 }
@@ -452,7 +482,7 @@ __device__ __forceinline__ void join_waves(const stairs_paged_cache& c, const st
                                            float (*s_o)[COLS][HD + 4], float (*s_m)[COLS], float (*s_l)[COLS], int* s_last) {
   static_assert(4 * COLS * (HD + 4) >= 2 * kMaxPieces * COLS + 256, "the pieces' maxima and sums fit where the waves' outputs were");
   const int G = a.n_heads / c.n_kv_heads, col0 = w.group * COLS, cols = min(COLS, w.rows * G - col0);
-  float* part = reinterpret_cast<float*>(static_cast<int*>(a.workspace) + most_pieces(sp.slots)) +
+  float* part = partials(a, sp) +
                 (size_t)(w.first + w.piece * c.n_kv_heads) * piece_floats<HD>(COLS);
   for (int i = threadIdx.x; i < cols * (HD / 4); i += 256) {
     const int col = i / (HD / 4), e = i % (HD / 4) * 4;
@@ -474,8 +504,7 @@ __device__ __forceinline__ void join_waves(const stairs_paged_cache& c, const st
     if (w.pieces == 1) {
       store_out<T, HD>(c, a, w, col0 + col, e, v, l);
     } else {
-      st_dev2(part + col * HD + e, v.x, v.y);
-      st_dev2(part + col * HD + e + 2, v.z, v.w);
+      st_dev4(part, col * HD + e, v);
       if (e == 0) st_dev2(part + COLS * HD + col * 2, m, l);
     }
   }
@@ -488,18 +517,19 @@ __device__ __forceinline__ void join_waves(const stairs_paged_cache& c, const st
 // wave), no LDS, and are joined at the end.  Values are requested before the scores they wait for, the next block's keys as
 // soon as this block's are used.
 constexpr int kRowUnit = 32 * 4;
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint4 ld_once(const void* p) {        // (streaming hint: 3 x 32 heads of up to 59999 keys 384 -> 366 us)
   const u32x4 v = __builtin_nontemporal_load(static_cast<const u32x4*>(p));
   return make_uint4(v[0], v[1], v[2], v[3]);
 }
+template <int HD, int CT>
+struct RowsLds {
+  float o[4][16 * CT][HD + 4], m[4][16 * CT], l[4][16 * CT];
+  int last;
+};
 template <typename T, int HD, int CT>
-__global__ __launch_bounds__(256, 2) void k_paged_rows(stairs_paged_cache c, stairs_paged_attn a, Span sp, float scale2) {
+__device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, float scale2, RowsLds<HD, CT>& lds) {
   typedef typename Elem<T>::x8 x8;
-  constexpr int KK = HD / 32, ET = HD / 16, LD = HD + 4;
-  __shared__ float s_o[4][16 * CT][LD];
-  __shared__ float s_m[4][16 * CT], s_l[4][16 * CT];
-  __shared__ int s_last;
+  constexpr int KK = HD / 32, ET = HD / 16;
   Piece w;
   if (!find_piece(c, a, sp, w)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, g = lane >> 4;
@@ -510,6 +540,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_rows(stairs_paged_cache c, sta
   const int last_last = min(pos0 + (min(cols, col0 + 16 * CT) - 1) / G, limit - 1);
   int last[CT];
   x8 q[CT][KK];
+  bool had_odd = false;                                         // the wave has left infinities or NaNs in its part of lds.o
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
     const int col = col0 + ct * 16 + j;
@@ -587,6 +618,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_rows(stairs_paged_cache c, sta
       }
     const int key0 = u * kRowUnit + wave * 32;
     const int un = next_block(u + 1);
+    const size_t at_here = at;
     if (un < u1) {
       at = block_at(un);
       load_keys(at);
@@ -621,7 +653,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_rows(stairs_paged_cache c, sta
     }
     if (!full) {
       // Some keys of the block are not seen by all columns.  Their probability is 0, and 0 times what is there must be 0: what
-      // no column sees is cleared, an infinity or NaN that some columns see is taken out and given to those that do.
+      // no column sees is cleared, and so are infinities and NaNs; those that some columns see are looked at again (odd_values).
       uint32_t keep[4], odd = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -630,25 +662,31 @@ __global__ __launch_bounds__(256, 2) void k_paged_rows(stairs_paged_cache c, sta
       }
 #pragma unroll
       for (int et = 0; et < ET; ++et) {
-        uint4& v = vf[et];
-        v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
-        odd |= odd_bits<T>(v.x) | odd_bits<T>(v.y) | odd_bits<T>(v.z) | odd_bits<T>(v.w);
+        odd |= clear_odd<T>(vf[et].x, keep[0]);
+        odd |= clear_odd<T>(vf[et].y, keep[1]);
+        odd |= clear_odd<T>(vf[et].z, keep[2]);
+        odd |= clear_odd<T>(vf[et].w, keep[3]);
+        __builtin_amdgcn_sched_barrier(0);                      // (one tile after the other: their temporaries share registers)
       }
       if (__any(odd != 0)) {
+        if (!had_odd)
+          for (int i = lane; i < 16 * CT * (HD + 4); i += 64) (&lds.o[wave][0][0])[i] = 0.f;
+        had_odd = true;
         x8 seen[CT];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
           for (int i = 0; i < 8; ++i) seen[ct][i] = key0 + (i >> 2) * 16 + g * 4 + (i & 3) <= last[ct] ? (T)1.f : (T)0.f;
-#pragma unroll
+#pragma unroll 1
         for (int et = 0; et < ET; ++et) {
-          __builtin_amdgcn_sched_barrier(0);                    // (one tile after the other: the path is rare, registers are not)
-          const uint4 kinds = make_uint4(take_odd<T>(vf[et].x), take_odd<T>(vf[et].y), take_odd<T>(vf[et].z), take_odd<T>(vf[et].w));
+          uint4 v = *reinterpret_cast<const uint4*>(V + at_here + (et * 64 + lane) * 8);
+          v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
+          const uint4 kinds = make_uint4(odd_kinds<T>(v.x), odd_kinds<T>(v.y), odd_kinds<T>(v.z), odd_kinds<T>(v.w));
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
-            const f32x4 n = mma(__builtin_bit_cast(x8, kinds), seen[ct], f32x4{0.f, 0.f, 0.f, 0.f});
+            const f32x4 count = mma(__builtin_bit_cast(x8, kinds), seen[ct], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[ct][et][i] += odd_value(n[i]);
+            for (int i = 0; i < 4; ++i) lds.o[wave][ct * 16 + j][et * 16 + g * 4 + i] += odd_value(count[i]);
           }
         }
       }
@@ -665,15 +703,266 @@ __global__ __launch_bounds__(256, 2) void k_paged_rows(stairs_paged_cache c, sta
   for (int ct = 0; ct < CT; ++ct) {
     const float sum = groups_sum(l[ct]);
     if (g == 0) {
-      s_m[wave][ct * 16 + j] = m[ct];
-      s_l[wave][ct * 16 + j] = sum;
+      lds.m[wave][ct * 16 + j] = m[ct];
+      lds.l[wave][ct * 16 + j] = sum;
     }
 #pragma unroll
-    for (int et = 0; et < ET; ++et)
-      *reinterpret_cast<float4*>(&s_o[wave][ct * 16 + j][et * 16 + g * 4]) = make_float4(o[ct][et][0], o[ct][et][1], o[ct][et][2], o[ct][et][3]);
+    for (int et = 0; et < ET; ++et) {
+      float4* dst = reinterpret_cast<float4*>(&lds.o[wave][ct * 16 + j][et * 16 + g * 4]);
+      float4 v = make_float4(o[ct][et][0], o[ct][et][1], o[ct][et][2], o[ct][et][3]);
+      if (had_odd) {
+        const float4 x = *dst;
+        v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+      }
+      *dst = v;
+    }
   }
   __syncthreads();
-  join_waves<T, HD, 16 * CT>(c, a, sp, w, s_o, s_m, s_l, &s_last);
+  join_waves<T, HD, 16 * CT>(c, a, sp, w, lds.o, lds.m, lds.l, &lds.last);
+}
+template <typename T, int HD, int CT>
+__global__ __launch_bounds__(256, 2) void k_paged_rows(stairs_paged_cache c, stairs_paged_attn a, Span sp, float scale2) {
+  __shared__ RowsLds<HD, CT> lds;
+  attend_rows<T, HD, CT>(c, a, sp, scale2, lds);
+}
+
+// ---- many columns: tiles of 128 columns, keys and values shared through LDS ------------------------------------------
+// Bound by the matrix units and by the exponentials beside them.  A wave has 32 columns, the work-group's four waves read 64
+// keys at a time, copied to LDS while the 64 before are used.  On the 32 x 32 instruction the tiled page layout fits as it is: a
+// lane's 16 scores of 32 keys are two operands of the value product (keys 4 h + i and 16 + 4 h + i, and 8 further, of lane
+// half h), whose other operand is one 16-byte read of a value tile.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ float halves_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float halves_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// lane l: lds[l] = base[offset / 16 + l]
+__device__ __forceinline__ void copy_tile(const void* base, uint32_t offset, uint4* lds, uint32_t lane_bytes) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, 0xFFFFFFFFu, 0x00027000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds))), 16,
+                                           lane_bytes, offset, 0, 0);
+}
+constexpr int kChunkCols = 128, kChunkUnit = 64;
+template <int HD>
+struct ChunkLds {
+  union {
+    uint4 tile[2][2][2][4 * HD];   // [buffer][32-key block][keys, values][64 HD bytes]
+    float join[2 * kMaxPieces * kChunkCols + 256];
+  };
+  int last;
+};
+template <typename T, int HD>
+__device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, float scale2, ChunkLds<HD>& lds) {
+  typedef typename Elem<T>::x8 x8;
+  constexpr int KS = HD / 16, DT = HD / 32;                     // steps of 16 dims, tiles of 32 dims
+  Piece w;
+  if (!find_piece(c, a, sp, w)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
+  const int G = a.n_heads / c.n_kv_heads, cols = w.rows * G, col0 = w.group * kChunkCols, wcol = col0 + wave * 32;
+  const int limit = a.max_blocks * c.page_size, pos0 = w.len - w.rows;
+  // last positions that the work-group's, the wave's and the lane's columns see
+  const int last_group = min(pos0 + (min(cols, col0 + kChunkCols) - 1) / G, limit - 1);
+  const int first_wave = wcol < cols ? min(pos0 + wcol / G, limit - 1) : -1;
+  const int last_wave = wcol < cols ? min(pos0 + (min(cols, wcol + 32) - 1) / G, limit - 1) : -1;
+  const int col = wcol + n, row = col < cols ? col / G : 0;
+  const int last = col < cols ? min(pos0 + row, limit - 1) : -1;
+  const size_t at_row = (size_t)(w.row0 + row), at_head = (size_t)(w.kvh * G + (col < cols ? col - row * G : 0)) * HD;
+  x8 q[KS];
+  {
+    const T* qp = static_cast<const T*>(a.q) + at_row * a.q_stride + at_head + h * 8;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) q[k] = *reinterpret_cast<const x8*>(qp + k * 16);
+  }
+  f32x16 o[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d) o[d] = f32x16{};
+  float m = -INFINITY, l = 0.f;
+
+  const size_t head_elems = (size_t)c.page_size * HD, page_elems = head_elems * c.n_kv_heads;
+  // the wave copies block wave / 2 of a unit, its keys or its values
+  const T* pool = static_cast<const T*>(wave & 1 ? c.v : c.k) + w.kvh * head_elems;
+  const int* table = a.block_table + (size_t)w.seq * a.max_blocks;
+  const int ps_shift = __builtin_ctz(c.page_size);
+  const int u1 = min(w.u1, last_group < 0 ? 0 : last_group / kChunkUnit + 1);
+  int pages = -1, pages_at = w.u0;                              // of the blocks 2 pages_at .., a lane each
+  auto fetch_pages = [&](int u) {
+    pages_at = u;
+    const int key = u * kChunkUnit + lane * 32;
+    pages = key <= last_group ? table[key >> ps_shift] : -1;
+    if ((unsigned)pages >= (unsigned)c.n_pages) pages = -1;
+  };
+  auto page_of = [&](int u, int block) { return __builtin_amdgcn_readlane(pages, (u - pages_at) * 2 + block); };
+  auto request = [&](int u, int buf) {                          // (a block without a page: another's bytes, masked below)
+    const int b = wave >> 1, key = u * kChunkUnit + b * 32;
+    const T* src = pool + (size_t)max(page_of(u, b), 0) * page_elems + (size_t)(key & (c.page_size - 1)) * HD;
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) copy_tile(src, i * 1024, &lds.tile[buf][b][wave & 1][i * 64], lane * 16);
+  };
+  __syncthreads();
+  if (w.u0 < u1) {
+    fetch_pages(w.u0);
+    request(w.u0, w.u0 & 1);
+  }
+  // Two loops of one body: units that all of the wave's columns see, then those with masks (with both in one loop the 64 output
+  // registers were copied twice a unit).  A wave goes from one to the other when it has to; barriers are one a unit in both.
+  int u = w.u0;
+  int page0 = -1, page1 = -1;
+  auto next_unit = [&]() {                                      // unit u is in LDS, the next one on its way
+    page0 = page_of(u, 0);
+    page1 = page_of(u, 1);
+    if (u + 1 - pages_at >= 32) fetch_pages(u + 1);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // unit u is there, the other buffer has been read
+    if (u + 1 < u1) request(u + 1, (u + 1) & 1);
+  };
+  auto scores = [&](f32x16 (&s)[2]) {
+    s[0] = s[1] = f32x16{};
+    const uint4* kt = lds.tile[u & 1][0][0] + (n >> 4) * (HD / 32) * 64 + (n & 15) + 16 * h;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) s[b] = mma(__builtin_bit_cast(x8, kt[b * 8 * HD + (k >> 1) * 64 + 32 * (k & 1)]), q[k], s[b]);
+  };
+  // (m: the reference point in units of the raw score)
+  auto probabilities = [&](const f32x16 (&s)[2], x8 (&p)[2][2]) {
+    // (the maximum that passes NaN on, one instruction for three values; a NaN makes the column's sum NaN whatever m is)
+    float mx = __builtin_elementwise_maximum(s[0][0], s[1][0]);
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = __builtin_elementwise_maximum(mx, __builtin_elementwise_maximum(s[0][i], s[1][i]));
+    if (__any(mx * scale2 > m * scale2 + kMaxSlack)) {
+      const float mn = fmaxf(m, halves_max(mx));
+      const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * scale2);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= f;
+    }
+    const float mr = m == -INFINITY ? 0.f : -m * scale2;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float x = __builtin_amdgcn_exp2f(fmaf(s[i >> 4][i & 15], scale2, mr));
+      sum[i & 3] += x;
+      p[i >> 4][i >> 2 & 1][(i & 3) + 4 * (i >> 3 & 1)] = Elem<T>::down(x);
+    }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  };
+  for (; u < u1; ++u) {
+    const int key0 = u * kChunkUnit;
+    if (key0 + kChunkUnit - 1 > first_wave || page_of(u, 0) < 0 || page_of(u, 1) < 0) break;
+    next_unit();
+    f32x16 s[2];
+    x8 p[2][2];
+    scores(s);
+    probabilities(s, p);
+    const uint4* vt = lds.tile[u & 1][0][1] + (n >> 4) * 64 + (n & 15) + 16 * h;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] = mma(__builtin_bit_cast(x8, vt[b * 8 * HD + d * 128 + r * 32]), p[b][r], o[d]);
+  }
+#pragma unroll 1
+  for (; u < u1; ++u) {
+    const int key0 = u * kChunkUnit;
+    next_unit();
+    if (key0 > last_wave) continue;                             // (nothing for this wave any more)
+    f32x16 s[2];
+    x8 p[2][2];
+    scores(s);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const int key = key0 + (i >> 4) * 32 + (i >> 2 & 3) * 8 + h * 4 + (i & 3);
+      float& x = reinterpret_cast<float*>(&s[i >> 4])[i & 15];
+      x = key <= last && (i < 16 ? page0 : page1) >= 0 ? x : -INFINITY;
+    }
+    probabilities(s, p);
+    // as in attend_rows: what no column of the wave sees is cleared, infinities and NaNs go to the columns that see them
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int end = (b ? page1 : page0) < 0 ? -1 : last_wave, mine = (b ? page1 : page0) < 0 ? -1 : last;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int key = key0 + b * 32 + r * 8 + h * 4;
+        uint32_t keep[4], odd = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int k = key + (i >> 1) * 16 + (i & 1) * 2;
+          keep[i] = (k <= end ? 0xFFFFu : 0u) | (k + 1 <= end ? 0xFFFF0000u : 0u);
+        }
+        const uint4* vt = lds.tile[u & 1][b][1] + (n >> 4) * 64 + (n & 15) + 16 * h + r * 32;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          uint4 v = vt[d * 128];
+          odd |= clear_odd<T>(v.x, keep[0]) | clear_odd<T>(v.y, keep[1]) | clear_odd<T>(v.z, keep[2]) | clear_odd<T>(v.w, keep[3]);
+          o[d] = mma(__builtin_bit_cast(x8, v), p[b][r], o[d]);
+        }
+        if (__any(odd != 0)) {
+          x8 seen;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) seen[i] = key + (i >> 2) * 16 + (i & 3) <= mine ? (T)1.f : (T)0.f;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            uint4 v = vt[d * 128];
+            v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
+            const uint4 kinds = make_uint4(odd_kinds<T>(v.x), odd_kinds<T>(v.y), odd_kinds<T>(v.z), odd_kinds<T>(v.w));
+            const f32x16 count = mma(__builtin_bit_cast(x8, kinds), seen, f32x16{});
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] += odd_value(count[i]);
+          }
+        }
+      }
+    }
+  }
+  l = halves_sum(l);
+  m = m == -INFINITY ? m : m * scale2;                          // (what the join works with)
+  if (w.pieces == 1) {
+    if (col < cols) {
+      const float f = l == 0.f ? 0.f : 1.f / l;
+      T* dst = static_cast<T*>(a.out) + at_row * a.out_stride + at_head + h * 4;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          T v[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = Elem<T>::down(o[d][b * 4 + i] * f);
+          *reinterpret_cast<uint2*>(dst + d * 32 + b * 8) = *reinterpret_cast<const uint2*>(v);
+        }
+    }
+    return;
+  }
+  float* part = partials(a, sp) + (size_t)(w.first + w.piece * c.n_kv_heads) * piece_floats<HD>(kChunkCols);
+  if (col < cols) {
+    const int dst = (col - col0) * HD + h * 4;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        st_dev4(part, dst + d * 32 + b * 8, make_float4(o[d][b * 4], o[d][b * 4 + 1], o[d][b * 4 + 2], o[d][b * 4 + 3]));
+      }
+    if (h == 0) st_dev2(part + kChunkCols * HD + (col - col0) * 2, m, l);
+  }
+  __syncthreads();                                              // (the tiles have been read: their place serves the join)
+  join_pieces<T, HD, kChunkCols>(c, a, sp, w, reinterpret_cast<float2*>(lds.join), &lds.last);
+}
+template <typename T, int HD>
+__global__ __launch_bounds__(256, 2) void k_paged_chunk(stairs_paged_cache c, stairs_paged_attn a, Span sp, float scale2) {
+  __shared__ ChunkLds<HD> lds;
+  attend_chunk<T, HD>(c, a, sp, scale2, lds);
+}
+// both in one launch: the chunks' work-groups first, the few rows of the others where there is room
+template <typename T, int HD>
+__global__ __launch_bounds__(256, 2) void k_paged_mixed(stairs_paged_cache c, stairs_paged_attn a, Span chunk, Span rows, float scale2) {
+  __shared__ union { ChunkLds<HD> chunk; RowsLds<HD, 2> rows; } lds;
+  if ((int)blockIdx.x < rows.first_block) attend_chunk<T, HD>(c, a, chunk, scale2, lds.chunk);
+  else attend_rows<T, HD, 2>(c, a, rows, scale2, lds.rows);
 }
 
 }  // namespace
@@ -764,22 +1053,40 @@ extern "C" int stairs_paged_append(const stairs_paged_cache* c, const stairs_pag
 namespace {
 
 // ---- how a call is spread: by its sizes on the host, by the lengths on the device (find_piece) ------------------------
-constexpr int kCus = 256;
+// A sequence's columns are its rows times the query heads of a key head.  Up to 32 of them (16 in one tile) go to attend_rows, more to
+// attend_chunk; max_fresh says which of the two a call needs, and with one sequence, or none with more, one kernel
+// takes whatever it finds.
+constexpr int kCus = 256, kFewCols = 32;
 struct Launch {
-  Span span;
-  int ct;
-  size_t work_bytes;
+  int ct;                      // column tiles of the rows' part, 0: there is none
+  bool chunk;
+  Span rows, chunks;
+  int64_t work_bytes;
   unsigned grid;
 };
-Launch plan_rows(const stairs_paged_cache* c, const stairs_paged_attn* a) {
+Launch plan_attention(const stairs_paged_cache* c, const stairs_paged_attn* a) {
   const int G = a->n_heads / c->n_kv_heads;
+  const int64_t cols = (int64_t)a->max_fresh * G;
   Launch l{};
-  l.ct = (int64_t)a->max_fresh * G <= 16 ? 1 : 2;
-  l.span = Span{1, INT32_MAX, 16 * l.ct, kRowUnit, 2 * kCus};
-  l.work_bytes = (size_t)most_pieces(l.span.slots) * (sizeof(int) + (size_t)l.span.tile_cols * (c->head_dim + 2) * sizeof(float));
-  // at most `slots` pieces and one a tile
-  const int64_t tiles = a->n_seqs + (int64_t)a->rows * G / l.span.tile_cols;
-  l.grid = (unsigned)std::min<int64_t>(l.span.slots + tiles * c->n_kv_heads, INT32_MAX);
+  l.chunk = cols > kFewCols;
+  l.ct = cols <= 16 ? 1 : !l.chunk || a->n_seqs > 1 ? 2 : 0;
+  auto add = [&](Span& s) {
+    s.first_block = (int)l.grid;
+    s.work = l.work_bytes;
+    // at most `slots` pieces and one a tile
+    const int64_t tiles = a->n_seqs + (int64_t)a->rows * G / s.tile_cols;
+    l.grid += (unsigned)(s.slots + tiles * c->n_kv_heads);
+    l.work_bytes += most_pieces(s.slots) * (int64_t)(sizeof(int) + s.tile_cols * (c->head_dim + 2) * sizeof(float));
+  };
+  if (l.chunk) {
+    l.chunks = Span{l.ct ? kFewCols + 1 : 1, INT32_MAX, kChunkCols, kChunkUnit, X_C, X_CM, X_CW, 0, 0};
+    add(l.chunks);
+  }
+  if (l.ct) {
+    // pieces of 4 units and more: shorter ones cost more to join than they save (8000 keys of 8 heads alone: 25 us with 2, 19 with 4)
+    l.rows = Span{1, l.chunk ? kFewCols : INT32_MAX, 16 * l.ct, kRowUnit, l.chunk ? X_R : 2 * kCus, X_RM, 200, 0, 0};
+    add(l.rows);
+  }
   return l;
 }
 
@@ -787,7 +1094,7 @@ Launch plan_rows(const stairs_paged_cache* c, const stairs_paged_attn* a) {
 
 extern "C" int64_t stairs_paged_attention_workspace(const stairs_paged_cache* c, const stairs_paged_attn* a) {
   if (!attn_sizes_ok(c, a)) return STAIRS_EINVAL;
-  return (int64_t)plan_rows(c, a).work_bytes;
+  return plan_attention(c, a).work_bytes;
 }
 
 extern "C" int stairs_paged_attention(const stairs_paged_cache* c, const stairs_paged_attn* a, void* hip_stream) {
@@ -797,18 +1104,19 @@ extern "C" int stairs_paged_attention(const stairs_paged_cache* c, const stairs_
   if (!aligned16(a->q) || !aligned16(a->out) || !stride_ok(a->q_stride, a->n_heads, c->head_dim) || !stride_ok(a->out_stride, a->n_heads, c->head_dim))
     return STAIRS_EINVAL;
   if (!a->workspace || !aligned16(a->workspace)) return STAIRS_EINVAL;
-  const Launch rows = plan_rows(c, a);
-  if (a->workspace_bytes < (int64_t)rows.work_bytes) return STAIRS_ECAPACITY;
+  const Launch l = plan_attention(c, a);
+  if (a->workspace_bytes < l.work_bytes) return STAIRS_ECAPACITY;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (const int rc = check_stream(st)) return rc;
   const float scale2 = (a->scale > 0.f ? a->scale : 1.0f / sqrtf((float)c->head_dim)) * kLog2e;
   by_type(c, [&](auto type, auto hd) {
     typedef decltype(type) T;
     constexpr int HD = decltype(hd)::value;
-    if (rows.ct == 1)
-      hipLaunchKernelGGL((k_paged_rows<T, HD, 1>), dim3(rows.grid), dim3(256), 0, st, *c, *a, rows.span, scale2);
-    else
-      hipLaunchKernelGGL((k_paged_rows<T, HD, 2>), dim3(rows.grid), dim3(256), 0, st, *c, *a, rows.span, scale2);
+    const dim3 grid(l.grid), block(256);
+    if (l.chunk && l.ct) hipLaunchKernelGGL((k_paged_mixed<T, HD>), grid, block, 0, st, *c, *a, l.chunks, l.rows, scale2);
+    else if (l.chunk) hipLaunchKernelGGL((k_paged_chunk<T, HD>), grid, block, 0, st, *c, *a, l.chunks, scale2);
+    else if (l.ct == 1) hipLaunchKernelGGL((k_paged_rows<T, HD, 1>), grid, block, 0, st, *c, *a, l.rows, scale2);
+    else hipLaunchKernelGGL((k_paged_rows<T, HD, 2>), grid, block, 0, st, *c, *a, l.rows, scale2);
   });
   return launched();
 }
