@@ -1,0 +1,612 @@
+// Drawing tokens from rows of logits with temperature, top-k, top-p and min-p from given uniform numbers
+// (stairs_sample_device), and the same cut applied to the rows of the sampled generation path (launch_truncate).
+//
+// Tokens are ordered by (logit, index); what the rules keep is a prefix of that order, and its end a key (the logit's bits in an
+// order-preserving form) with, among equal logits, an index.  It is found by a histogram of the keys' leading bits, by count (top-k)
+// or by weight (top-p), which names the bin it is in, and by sorting that bin's tokens; a bin that is too full (equal logits by
+// the thousand) is cut by radix selection instead, bin by bin down to one key, and the equal ones by index.  Weights are
+// multiples of 2^-44 of the largest, held in 64-bit integers: their sums do not depend on the order of additions, so neither the
+// histograms' atomics nor the split of a row over threads change a result, and equal borders are equal.  (2^-44 against sums of 1
+// and more: a border moves by about 1e-11 of the whole against sums in double; a 24-bit random number falls between
+// the two never in practice.)
+//
+// A row is one work-group's, read from memory once: up to 125 KiB of it stay in LDS beside the histogram.  Bound by
+// latencies (a dozen steps that wait for each other), and with top-p alone by the exponentials in double, one a logit.
+#include "../../include/stairs.h"
+#include "stairs_device.h"
+
+namespace stairs {
+namespace {
+__device__ unsigned long long* g_lg;
+#define TICK(i) do { __syncthreads(); if (threadIdx.x == 0 && lgp) lgp[blockIdx.x * 16 + i] = __builtin_amdgcn_s_memrealtime(); } while (0)
+
+
+typedef unsigned long long u64;
+constexpr int kBinBits = 12, kBins = 1 << kBinBits;
+constexpr int kList = 2048;                        // tokens that are sorted
+constexpr double kOne = 17592186044416.0;          // 2^44: the weight of the largest logit
+
+// Order-preserving keys: larger logit, larger key; -0 and +0 alike; NaN and -infinity are key 0 (never kept, never counted).
+template <typename T> struct Logit;
+template <> struct Logit<float> {
+  static constexpr int kBits = 32;
+  static __device__ __forceinline__ float value(float x) { return x; }
+};
+template <> struct Logit<uint16_t> {               // bfloat16
+  static constexpr int kBits = 16;
+  static __device__ __forceinline__ float value(uint16_t x) { return bf16_bits_to_float(x); }
+};
+template <> struct Logit<_Float16> {
+  static constexpr int kBits = 32;                 // (as float: 19 bits of the key differ)
+  static __device__ __forceinline__ float value(_Float16 x) { return (float)x; }
+};
+template <typename T>
+__device__ __forceinline__ uint32_t key_of(float x) {
+  if (!(x > -INFINITY)) return 0;
+  const uint32_t b = __float_as_uint(x + 0.f);
+  const uint32_t k = b ^ ((b >> 31) ? 0xFFFFFFFFu : 0x80000000u);
+  return Logit<T>::kBits == 16 ? k >> 16 : k;
+}
+
+struct Row {
+  float max;
+  double inv_temp;
+};
+// logarithm of the weight: 0 for the largest logits (infinite ones too)
+__device__ __forceinline__ double exponent(float x, const Row& r) { return x == r.max ? 0.0 : ((double)x - (double)r.max) * r.inv_temp; }
+constexpr double kNoWeight = -745.13;              // below it a weight is 0 in double
+
+// exp(d) for d <= 0 in multiples of 2^-44.  d = n ln 2 + r with |r| <= ln 2 / 2; exp(r / 4) by its series up to the 8th power
+// (the next term is 8e-16), squared twice; the number and the place of its last bit come from one multiply-add.
+__device__ __forceinline__ u64 fixed_exp(double d) {
+  d = fmax(d, -64.0);                              // (weights below 2^-45 are 0 here)
+  const double big = 6755399441055744.0;           // 1.5 * 2^52: adding it rounds to a whole number
+  const double nb = fma(d, 1.4426950408889634074, big), n = nb - big;
+  const double x = fma(n, -0.17328679513998632735, 0.25 * d);   // ln 2 / 4
+  double p = 1.0 / 40320;
+  p = fma(p, x, 1.0 / 5040);
+  p = fma(p, x, 1.0 / 720);
+  p = fma(p, x, 1.0 / 120);
+  p = fma(p, x, 1.0 / 24);
+  p = fma(p, x, 1.0 / 6);
+  p = fma(p, x, 0.5);
+  p = fma(p, x, 1.0);
+  p = fma(p, x, 1.0);
+  p *= p;
+  p *= p;
+  const int e = (int)(uint32_t)__double_as_longlong(nb);        // n, in the low bits
+  const double scale = __longlong_as_double((long long)(1023 + 44 + e) << 52);
+  return (u64)__double_as_longlong(fma(p, scale, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;   // + 2^52
+}
+__device__ __forceinline__ u64 weight(float x, const Row& r) { return fixed_exp(exponent(x, r)); }
+
+__device__ __forceinline__ u64 wave_sum_u64(u64 v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
+  return v;
+}
+__device__ __forceinline__ u64 wave_scan_u64(u64 v) {              // inclusive, by lane
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const u64 o = __shfl_up(v, off);
+    if (lane >= off) v += o;
+  }
+  return v;
+}
+
+// A work-group of NT threads; CACHE bytes of the row in LDS.  Small vocabularies take small work-groups, several to a CU.
+template <int NT, int CACHE>
+struct Lds {
+  static constexpr int kThreads = NT, kWaves = NT / 64, kCache = CACHE;
+  alignas(16) unsigned char row[CACHE];
+  union {
+    u64 bin[kBins];                                // histogram
+    struct { u64 order[kList]; } list;             // tokens of a bin, (key, index from the end)
+  };
+  u64 part[kWaves], part2[kWaves];
+  u64 found[3];
+  float fpart[kWaves];
+  int count;
+};
+
+// the row's values: what is in LDS from there
+template <typename T, typename L>
+struct Values {
+  const T* x;
+  const L* lds;
+  bool cached;
+  __device__ __forceinline__ float operator[](int v) const {
+    return Logit<T>::value(cached ? reinterpret_cast<const T*>(lds->row)[v] : x[v]);
+  }
+};
+// f(v, value) for the thread's share of the row, in no order; four loads at a time
+template <typename T, typename L, typename F>
+__device__ __forceinline__ void each(const Values<T, L>& x, int V, F f) {
+  int v = threadIdx.x;
+  for (; v + 3 * L::kThreads < V; v += 4 * L::kThreads) {
+    float a[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = x[v + i * L::kThreads];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f(v + i * L::kThreads, a[i]);
+  }
+  for (; v < V; v += L::kThreads) f(v, x[v]);
+}
+
+template <typename L>
+__device__ u64 block_sum(u64 v, L& s) {
+  v = wave_sum_u64(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) s.part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  u64 t = 0;
+  for (int w = 0; w < L::kWaves; ++w) t += s.part[w];
+  return t;
+}
+// sum of the threads in front
+template <typename L>
+__device__ u64 block_before(u64 v, L& s) {
+  const u64 to = wave_scan_u64(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) s.part[threadIdx.x >> 6] = to;
+  __syncthreads();
+  u64 before = to - v;
+  for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) before += s.part[w];
+  return before;
+}
+
+// Of the histogram's n bins, from the top: the first at which `over` and the bins so far reach the target -> s.found[0], what is
+// in front of it -> s.found[1]; s.found[0] is n if none does
+template <typename L>
+__device__ void find_bin(int n, u64 over, u64 target, L& s) {
+  const int per = (n + L::kThreads - 1) / L::kThreads, first = threadIdx.x * per;
+  if (threadIdx.x == 0) s.found[0] = n;
+  u64 mine = 0;
+  for (int i = first; i < min(first + per, n); ++i) mine += s.bin[n - 1 - i];
+  u64 before = over + block_before(mine, s);
+  if (before < target && before + mine >= target) {
+    for (int i = first; i < min(first + per, n); ++i) {
+      const u64 b = s.bin[n - 1 - i];
+      if (before < target && before + b >= target) {
+        s.found[0] = (u64)(n - 1 - i);
+        s.found[1] = before;
+      }
+      before += b;
+    }
+  }
+  __syncthreads();
+}
+template <typename L>
+__device__ __forceinline__ void clear_bins(int n, L& s) {
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += L::kThreads) s.bin[i] = 0;
+  __syncthreads();
+}
+
+// Histogram of the keys' leading bits: all lanes of a wave in one bin (masked logits, say) are one addition
+template <typename L>
+__device__ __forceinline__ void add_to_bin(uint32_t bin, u64 m, L& s) {
+  const uint32_t first = __builtin_amdgcn_readfirstlane(bin);
+  const bool same = bin == first;
+  if (__all(same)) {
+    const unsigned long long lanes = __ballot(true);
+    u64 sum = 0;
+    if (__all(m == 1)) sum = (u64)__popcll(lanes);
+    else if (lanes == ~0ull) sum = wave_sum_u64(m);
+    else {
+      if (m) atomicAdd(&s.bin[bin], m);
+      return;
+    }
+    if ((threadIdx.x & 63) == (unsigned)__builtin_ctzll(lanes)) atomicAdd(&s.bin[bin], sum);
+  } else if (m) {
+    atomicAdd(&s.bin[bin], m);
+  }
+}
+
+// The lowest index v with (measure of the indices <= v) > target, or V; measure(v) of a token.  The row is cut into a piece a wave,
+// the piece found likewise, until a wave can walk it.  s.part: the waves' sums of the first cut, where the caller has them.
+template <typename L, typename Measure>
+__device__ int find_index(Measure measure, int V, u64 target, L& s, bool have_parts) {
+  int lo = 0, n = V;
+  u64 before = 0;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  while (n > 64) {
+    const int piece = (n + L::kWaves - 1) / L::kWaves;
+    if (!have_parts) {
+      u64 m = 0;
+      for (int i = lane; i < piece; i += 64) {
+        const int v = wave * piece + i;
+        if (v < n) m += measure(lo + v);
+      }
+      m = wave_sum_u64(m);
+      __syncthreads();
+      if (lane == 0) s.part[wave] = m;
+      __syncthreads();
+    }
+    have_parts = false;
+    int w = 0;
+    for (; w < L::kWaves && before + s.part[w] <= target; ++w) before += s.part[w];
+    if (w == L::kWaves) return V;
+    lo += w * piece;
+    n = min(piece, n - w * piece);
+  }
+  const u64 to = before + wave_scan_u64(lane < n ? measure(lo + lane) : 0);
+  const unsigned long long over = __ballot(lane < n && to > target);
+  return over ? lo + __builtin_ctzll(over) : V;
+}
+
+struct Cut {                       // kept: key > key, or key == key and index <= index; and exponent >= least
+  uint32_t key;
+  int index;
+  double least;
+};
+
+// The tokens with low <= key < high, sorted into s.list.order; how many, or -1: too many
+template <typename T, typename L>
+__device__ int sort_bin(const Values<T, L>& x, int V, uint32_t low, u64 high, L& s) {
+  __syncthreads();
+  if (threadIdx.x == 0) s.count = 0;
+  __syncthreads();
+  each(x, V, [&](int v, float a) {
+    const uint32_t k = key_of<T>(a);
+    if (k >= low && k < high && k) {
+      const int at = atomicAdd(&s.count, 1);
+      if (at < kList) s.list.order[at] = ((u64)k << 32) | (0xFFFFFFFFu - (uint32_t)v);
+    }
+  });
+  __syncthreads();
+  const int c = s.count;
+  if (c > kList) return -1;
+  int n = 64;                                      // a power of two
+  while (n < c) n *= 2;
+  for (int i = c + threadIdx.x; i < n; i += L::kThreads) s.list.order[i] = 0;
+  __syncthreads();
+  // bitonic, largest first; pairs up to 64 apart stay within the 128 entries of a wave
+  for (int size = 2; size <= n; size *= 2)
+    for (int gap = size / 2; gap > 0; gap /= 2) {
+      for (int i = threadIdx.x; i < n / 2; i += L::kThreads) {
+        const int lo = 2 * i - (i & (gap - 1)), hi = lo + gap;
+        const u64 a = s.list.order[lo], b = s.list.order[hi];
+        if ((a < b) == ((lo & size) == 0)) {
+          s.list.order[lo] = b;
+          s.list.order[hi] = a;
+        }
+      }
+      if (gap > 64 || (gap == 1 && size >= 128)) __syncthreads();
+      else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+  __syncthreads();
+  return c;
+}
+__device__ __forceinline__ float value_of_key(uint32_t k, int bits) {
+  if (bits == 16) k = (k << 16) | ((k >> 15) ? 0u : 0xFFFFu);
+  return __uint_as_float(k >> 31 ? k ^ 0x80000000u : ~k);
+}
+
+// The largest key K with (measure of the keys >= K) >= target, among those whose bits above `below` are prefix; over: the measure of
+// the keys above those; -> what is above K too.  each_key(f): f(key, measure) for every token of the row.
+template <int KEYBITS, typename L, typename Each>
+__device__ uint32_t select_key(Each each_key, uint32_t prefix, int below, u64 over, u64 target, u64* above, L& s) {
+  while (below > 0) {
+    const int bits = below > kBinBits ? (below + 1) / 2 : below, shift = below - bits, n = 1 << bits;
+    clear_bins(n, s);
+    each_key([&](uint32_t key, u64 m) {
+      if ((key >> below) == prefix) add_to_bin((key >> shift) & (n - 1), m, s);
+    });
+    __syncthreads();
+    find_bin(n, over, target, s);
+    prefix = prefix << bits | (uint32_t)s.found[0];
+    over = s.found[1];
+    below = shift;
+    __syncthreads();
+  }
+  *above = over;
+  return prefix;
+}
+
+// the cut of the rules
+template <typename T, typename L>
+__device__ Cut find_cut(const Values<T, L>& x, int V, const Row& r, int top_k, float top_p, float min_p, L& s, unsigned long long* lgp = nullptr) {
+  constexpr int B = Logit<T>::kBits, LOW = B - kBinBits;
+  Cut c{1u, 0x7fffffff, min_p > 0.f ? fmax(kNoWeight, log((double)fminf(min_p, 1.f))) : kNoWeight};
+  u64 ties = ~0ull;                                 // kept of the tokens with key c.key, where c.index does not say it
+  u64 z = 0;                                        // weight of the first top_k
+  bool cut_k = false;
+  auto keys = [&](auto f) {
+    each(x, V, [&](int, float a) {
+      const uint32_t k = key_of<T>(a);
+      if (k) f(k, a);
+    });
+  };
+  if (top_k > 0 && top_k < V) {
+    clear_bins(kBins, s);
+    keys([&](uint32_t k, float) { add_to_bin(k >> LOW, 1, s); });
+    __syncthreads();
+    TICK(2);
+    find_bin(kBins, 0, (u64)top_k, s);
+    TICK(3);
+    const uint32_t bin = (uint32_t)s.found[0];
+    const u64 before = s.found[1];
+    if (bin < kBins) {                              // (else there are fewer tokens)
+      cut_k = true;
+      // everything down to that bin, so that the weights of all of the first top_k are at hand
+      const int n = sort_bin(x, V, bin << LOW, 1ull << B, s);
+      TICK(4);
+      if (n >= 0) {
+        constexpr int PER = kList / L::kThreads;
+        u64 w[PER], mine = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int at = threadIdx.x * PER + i;
+          w[i] = at < top_k && at < n ? weight(value_of_key((uint32_t)(s.list.order[at] >> 32), B), r) : 0;
+          mine += w[i];
+        }
+        u64 to = block_before(mine, s);
+        z = 0;
+        for (int k = 0; k < L::kWaves; ++k) z += s.part[k];
+        int stay = top_k;
+        if (top_p < 1.f) {
+          const double t = ceil((double)top_p * (double)z);
+          const u64 target = t < 1.0 ? 1ull : (u64)t;
+          u64 here = 0;
+#pragma unroll
+          for (int i = 0; i < PER; ++i) {
+            here += threadIdx.x * PER + i < top_k && to < target;
+            to += w[i];
+          }
+          stay = (int)block_sum(here, s);           // (weights do not grow along the order: a prefix)
+        }
+        const u64 last = s.list.order[stay - 1];
+        c.key = (uint32_t)(last >> 32);
+        c.index = (int)(0xFFFFFFFFu - (uint32_t)last);
+        __syncthreads();
+        return c;
+      }
+      u64 above;
+      c.key = select_key<B>([&](auto f) { keys([&](uint32_t k, float) { f(k, 1); }); }, bin, LOW, before, (u64)top_k, &above, s);
+      ties = (u64)top_k - above;
+    }
+  }
+  if (top_p < 1.f) {                                // (not for NaN)
+    clear_bins(kBins, s);
+    u64 sum = 0, tie = 0;
+    keys([&](uint32_t k, float a) {
+      const u64 w = weight(a, r);
+      if (!cut_k || k > c.key) sum += w;
+      else if (k == c.key) tie = w;
+      add_to_bin(k >> LOW, w, s);
+    });
+    TICK(5);
+    z = block_sum(sum, s);
+    if (cut_k) {
+      if (threadIdx.x == 0) s.found[2] = 0;
+      __syncthreads();
+      if (tie) s.found[2] = tie;                    // (equal logits, equal weights: whoever writes)
+      __syncthreads();
+      z += ties * s.found[2];
+    }
+    const double t = ceil((double)top_p * (double)z);
+    const u64 target = t < 1.0 ? 1ull : (u64)t;
+    find_bin(kBins, 0, target, s);
+    TICK(6);
+    const uint32_t bin = (uint32_t)s.found[0];
+    const u64 before = s.found[1];
+    const int n = cut_k ? -1 : sort_bin(x, V, bin << LOW, ((u64)bin + 1) << LOW, s);
+    TICK(7);
+    if (n >= 0) {
+      constexpr int PER = kList / L::kThreads;
+      u64 w[PER], mine = 0, here = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int at = threadIdx.x * PER + i;
+        w[i] = at < n ? weight(value_of_key((uint32_t)(s.list.order[at] >> 32), B), r) : 0;
+        mine += w[i];
+      }
+      u64 to = before + block_before(mine, s);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        here += threadIdx.x * PER + i < n && to < target;
+        to += w[i];
+      }
+      const int stay = (int)block_sum(here, s);
+      const u64 last = s.list.order[stay - 1];
+      c.key = (uint32_t)(last >> 32);
+      c.index = (int)(0xFFFFFFFFu - (uint32_t)last);
+      __syncthreads();
+      return c;
+    }
+    u64 above;
+    const uint32_t key = select_key<B>([&](auto f) { keys([&](uint32_t k, float a) { f(k, weight(a, r)); }); }, bin, LOW, before, target, &above, s);
+    // of the equal logits at the border those with less than the target in front of them
+    u64 w = 0;
+    keys([&](uint32_t k, float a) { if (k == key) w = weight(a, r); });
+    __syncthreads();
+    if (threadIdx.x == 0) s.found[2] = 1;
+    __syncthreads();
+    if (w) s.found[2] = w;
+    __syncthreads();
+    const u64 stay = (target - above + s.found[2] - 1) / s.found[2];
+    if (key > c.key || !cut_k) ties = stay;
+    else ties = min(ties, stay);
+    c.key = key;
+  }
+  if (ties != ~0ull) c.index = find_index([&](int v) { return key_of<T>(x[v]) == c.key ? 1ull : 0ull; }, V, ties - 1, s, false);
+  return c;
+}
+
+template <typename T>
+__device__ __forceinline__ bool is_kept(float a, int v, const Cut& c, const Row& r) {
+  const uint32_t k = key_of<T>(a);
+  if (!k || k < c.key || (k == c.key && v > c.index)) return false;
+  return exponent(a, r) >= c.least;
+}
+
+// the row into LDS, where it fits, and its maximum
+template <typename T, typename L>
+__device__ float load_row(const T* x, int V, bool cached, L& s) {
+  float m = -INFINITY;
+  T* row = reinterpret_cast<T*>(s.row);
+  constexpr int U = 8;
+  for (int v0 = threadIdx.x; v0 < V; v0 += U * L::kThreads) {
+    T a[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) a[i] = x[min(v0 + i * L::kThreads, V - 1)];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int v = v0 + i * L::kThreads;
+      if (cached && v < V) row[v] = a[i];
+      m = fmaxf(m, Logit<T>::value(a[i]));
+    }
+  }
+  m = wave_max(m);
+  if ((threadIdx.x & 63) == 0) s.fpart[threadIdx.x >> 6] = m;
+  __syncthreads();
+  for (int w = 0; w < L::kWaves; ++w) m = fmaxf(m, s.fpart[w]);
+  return m;
+}
+
+template <typename T, int NT, int CACHE>
+__global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
+  typedef Lds<NT, CACHE> L;
+  __shared__ L s;
+  const int row = blockIdx.x, V = a.vocab;
+  unsigned long long* lgp = reinterpret_cast<unsigned long long*>(a.workspace);
+  TICK(0);
+  const T* p = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
+  const Values<T, L> x{p, &s, V <= (int)(CACHE / sizeof(T))};
+  const float t = a.temperature ? a.temperature[row] : 1.f;
+  const int top_k = a.top_k ? a.top_k[row] : 0;
+  const float top_p = a.top_p ? a.top_p[row] : 1.f, min_p = a.min_p ? a.min_p[row] : 0.f, uniform = a.uniform ? a.uniform[row] : 0.f;
+  Row r{load_row(p, V, x.cached, s), fmax(1.0 / (double)t, 1e-300)};   // (an infinite temperature: all finite logits alike)
+  TICK(1);
+  int token = -1, kept = 0;
+  float lp = -INFINITY;
+  if (r.max == -INFINITY) {
+  } else if (!(t > 0.f)) {
+    token = find_index([&](int v) { return x[v] == r.max ? 1ull : 0ull; }, V, 0, s, false);
+    kept = 1;
+    lp = 0.f;
+  } else {
+    const Cut c = find_cut(x, V, r, top_k, top_p, min_p, s, lgp);
+    TICK(8);
+    // weight and number of what is kept, a piece of the row a wave (find_index's first cut)
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int piece = V > 64 ? (V + L::kWaves - 1) / L::kWaves : V, begin = wave * piece, end = min(V, begin + piece);
+    u64 z = 0, n = 0;
+    auto add = [&](int v, float b) {
+      if (is_kept<T>(b, v, c, r)) {
+        z += weight(b, r);
+        ++n;
+      }
+    };
+    int v = begin + lane;
+    for (; v + 3 * 64 < end; v += 4 * 64) {
+      float b[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) b[i] = x[v + i * 64];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) add(v + i * 64, b[i]);
+    }
+    for (; v < end; v += 64) add(v, x[v]);
+    z = wave_sum_u64(z);
+    n = wave_sum_u64(n);
+    __syncthreads();
+    if (lane == 0) {
+      s.part[wave] = z;
+      s.part2[wave] = n;
+    }
+    __syncthreads();
+    z = n = 0;
+    for (int w = 0; w < L::kWaves; ++w) {
+      z += s.part[w];
+      n += s.part2[w];
+    }
+    kept = (int)n;
+    TICK(9);
+    // (the lowest index whose sum exceeds u z: the sums are whole numbers, so it exceeds floor(u z) too; u below 1 by 2^-24 at
+    // least, u z below z by one at least; a u outside [0, 1) or not a number is brought inside)
+    const double u = fmin(fmax((double)uniform, 0.0), 1.0);
+    const u64 target = min((u64)(u * (double)z), z - 1);
+    token = find_index([&](int v) {
+      const float b = x[v];
+      return is_kept<T>(b, v, c, r) ? weight(b, r) : 0ull;
+    }, V, target, s, true);
+    lp = (float)(exponent(x[token], r) - log((double)z * (1.0 / kOne)));
+  }
+  TICK(10);
+  if (threadIdx.x == 0) {
+    a.token[row] = token;
+    if (a.logprob) a.logprob[row] = lp;
+    if (a.kept) a.kept[row] = kept;
+  }
+}
+
+// -infinity at the tokens of rows [.., ld] of floats that the rules do not keep
+template <int NT, int CACHE>
+__global__ __launch_bounds__(NT) void k_truncate(float* logits, int ld, int V, const SampleParams* sp) {
+  typedef Lds<NT, CACHE> L;
+  __shared__ L s;
+  float* p = logits + (size_t)blockIdx.x * ld;
+  const Values<float, L> x{p, &s, V <= (int)(CACHE / sizeof(float))};
+  const Row r{load_row(p, V, x.cached, s), (double)sp->inv_temp};
+  if (r.max == -INFINITY) return;
+  const Cut c = find_cut(x, V, r, sp->top_k, sp->top_p, sp->min_p, s);
+  __syncthreads();
+  each(x, V, [&](int v, float a) {
+    if (!is_kept<float>(a, v, c, r)) p[v] = -INFINITY;
+  });
+}
+
+// Up to 4096 logits: 256 threads, three work-groups to a CU; more: a CU's threads and LDS, 32128 floats or twice as many halves of it
+// (what is behind them is read again from L2 at every step).
+constexpr int kSmallRow = 4096, kSmallThreads = 256, kSmallCache = 16384;
+constexpr int kLargeThreads = 1024, kLargeCache = 128512;
+static_assert(sizeof(Lds<kLargeThreads, kLargeCache>) <= 160 * 1024, "one work-group's LDS");
+static_assert(sizeof(Lds<kSmallThreads, kSmallCache>) <= 52 * 1024, "three work-groups");
+
+}  // namespace
+
+void launch_truncate(float* logits, int rows, int ld, int V, const SampleParams* sp, hipStream_t st) {
+  if (V <= kSmallRow)
+    hipLaunchKernelGGL((k_truncate<kSmallThreads, kSmallCache>), dim3(rows), dim3(kSmallThreads), 0, st, logits, ld, V, sp);
+  else
+    hipLaunchKernelGGL((k_truncate<kLargeThreads, kLargeCache>), dim3(rows), dim3(kLargeThreads), 0, st, logits, ld, V, sp);
+}
+
+}  // namespace stairs
+
+using namespace stairs;
+
+static const char* check_sampling(const stairs_sampling* a) {
+  if (!a) return "sampling is NULL";
+  const int dt = a->dtype;
+  if (dt != STAIRS_DTYPE_FP32 && dt != STAIRS_DTYPE_BF16 && dt != STAIRS_DTYPE_FP16) return "unknown dtype";
+  if (a->rows < 0 || a->vocab < 1 || a->vocab > STAIRS_SAMPLE_MAX_VOCAB || a->ld < a->vocab) return "rows, vocab or ld out of range";
+  return nullptr;
+}
+
+extern "C" int64_t stairs_sample_workspace(const stairs_sampling* a) {
+  if (check_sampling(a)) return STAIRS_EINVAL;
+  return a->rows * 128;
+}
+
+extern "C" int stairs_sample_device(const stairs_sampling* a, void* hip_stream) {
+  if (check_sampling(a)) return STAIRS_EINVAL;
+  if (a->rows == 0) return STAIRS_OK;
+  if (!a->logits || !a->token) return STAIRS_EINVAL;
+  const size_t align = a->dtype == STAIRS_DTYPE_FP32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(a->logits) % align) return STAIRS_EINVAL;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (const int rc = check_stream(st)) return rc;
+  const dim3 grid(a->rows);
+  auto launch = [&](auto type) {
+    typedef decltype(type) T;
+    if (a->vocab <= kSmallRow) hipLaunchKernelGGL((k_sample_rows<T, kSmallThreads, kSmallCache>), grid, dim3(kSmallThreads), 0, st, *a);
+    else hipLaunchKernelGGL((k_sample_rows<T, kLargeThreads, kLargeCache>), grid, dim3(kLargeThreads), 0, st, *a);
+  };
+  if (a->dtype == STAIRS_DTYPE_FP32) launch(float{});
+  else if (a->dtype == STAIRS_DTYPE_BF16) launch(uint16_t{});
+  else launch(_Float16{});
+  return hipGetLastError() == hipSuccess ? STAIRS_OK : STAIRS_EHIP;
+}
