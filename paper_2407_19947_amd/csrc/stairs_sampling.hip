@@ -16,6 +16,8 @@
 #include "../../include/stairs.h"
 #include "stairs_device.h"
 
+#include <type_traits>
+
 namespace stairs {
 namespace {
 
@@ -117,14 +119,17 @@ struct Lds {
   unsigned lowest;
 };
 
-// the row's values: what is in LDS from there
-template <typename T, typename L>
+// the row's values, from LDS or from memory
+template <typename T, typename L, bool CACHED>
 struct Values {
+  typedef T Type;
+  typedef L Shared;
+  static constexpr bool kCached = CACHED;
   const T* x;
   const L* lds;
-  bool cached;
   __device__ __forceinline__ float operator[](int v) const {
-    return Logit<T>::value(cached ? reinterpret_cast<const T*>(lds->row)[v] : x[v]);
+    if constexpr (CACHED) return Logit<T>::value(reinterpret_cast<const T*>(lds->row)[v]);
+    else return Logit<T>::value(x[v]);
   }
 };
 // f(v, value) for the thread's share of the indices begin .. end, in no order; several loads at a time, more where they come from memory
@@ -140,10 +145,9 @@ __device__ __forceinline__ void walk(const X& x, int begin, int end, int step, F
   }
   for (; v < end; v += step) f(v, x[v]);
 }
-template <typename T, typename L, typename F>
-__device__ __forceinline__ void each(const Values<T, L>& x, int V, F f) {
-  if (x.cached) walk<4>(x, threadIdx.x, V, L::kThreads, f);
-  else walk<12>(x, threadIdx.x, V, L::kThreads, f);
+template <typename X, typename F>
+__device__ __forceinline__ void each(const X& x, int V, F f) {
+  walk<X::kCached ? 4 : 12>(x, threadIdx.x, V, X::Shared::kThreads, f);
 }
 
 template <typename L>
@@ -250,15 +254,15 @@ __device__ int find_index(Measure measure, int V, u64 target, L& s, bool have_pa
 
 
 // The tokens of the bins first .. last, sorted into s.list.order, the first in front; how many, or -1: too many
-template <typename T, typename L>
-__device__ int sort_bins(const Values<T, L>& x, int V, const Row& r, int first, int last, L& s) {
+template <typename X, typename L>
+__device__ int sort_bins(const X& x, int V, const Row& r, int first, int last, L& s) {
   __syncthreads();
   if (threadIdx.x == 0) s.count = 0;
   __syncthreads();
   each(x, V, [&](int v, float a) {
     const int b = bin_of(a, r);
     if (b >= first && b <= last) {
-      const uint32_t k = key_of<T>(a);
+      const uint32_t k = key_of<typename X::Type>(a);
       if (k) {
         const int at = atomicAdd(&s.count, 1);
         if (at < kList) s.list.order[at] = ((u64)k << 32) | (0xFFFFFFFFu - (uint32_t)v);
@@ -352,41 +356,24 @@ __device__ Cut cut_list(int n, int top_k, float top_p, u64 before, u64 target, c
   auto logit = [&](int i) { return value_of_key((uint32_t)(s.list.order[i] >> 32), B); };
   int stay;
   if (all <= kShort) {
-    constexpr int PER = kShort / 64;
-    u64 w[PER], mine = 0;
-    int strong = 0;                                 // of the lane's tokens, by their exponent
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int at = lane * PER + i;
-      w[i] = 0;
-      if (at < all) {
-        const double d = exponent(logit(at), r);
-        w[i] = fixed_exp(d);
-        strong += d >= c.least;
-      }
-      mine += w[i];
+    u64 z = 0;
+    for (int i = lane; i < all; i += 64) {          // (every wave writes the same numbers, and reads its own)
+      const u64 w = fixed_exp(exponent(logit(i), r));
+      s.list.weight[i] = w;
+      z += w;
     }
-    const u64 to = wave_scan_u64(mine), z = __shfl(to, 63);
-    u64 front = before + to - mine;
-    int here = 0;
-    if (top_p < 1.f && target == 0) target = border(top_p, z);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      here += lane * PER + i < all && (!(top_p < 1.f) || front < target);
-      front += w[i];
-    }
-    for (int off = 32; off >= 1; off >>= 1) {       // (weights do not grow along the order: prefixes)
-      here += __shfl_xor(here, off);
-      strong += __shfl_xor(strong, off);
-    }
-    stay = __builtin_amdgcn_readfirstlane(here);
-    const int kept = min(stay, __builtin_amdgcn_readfirstlane(strong));
-    u64 sum = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int at = lane * PER + i;
-      if (at < kept) sum += w[i];
-      if (threadIdx.x < 64 && at < all) s.list.weight[at] = w[i];
+    if (top_p < 1.f && target == 0) target = border(top_p, wave_sum_u64(z));
+    u64 front = before, sum = 0;
+    int kept = 0;
+    stay = 0;
+    for (int i0 = 0; i0 < all; i0 += 64) {          // (weights do not grow along the order: what stays is a prefix)
+      const int i = i0 + lane;
+      const u64 w = i < all ? s.list.weight[i] : 0, to = wave_scan_u64(w);
+      const bool here = i < all && (!(top_p < 1.f) || front + to - w < target), strong = here && exponent(logit(min(i, all - 1)), r) >= c.least;
+      stay += __popcll(__ballot(here));
+      kept += __popcll(__ballot(strong));
+      if (strong) sum += w;
+      front += __shfl(to, 63);
     }
     if (before == 0) {
       c.listed = kept;
@@ -418,8 +405,9 @@ __device__ Cut cut_list(int n, int top_k, float top_p, u64 before, u64 target, c
   return c;
 }
 
-template <typename T, typename L>
-__device__ Cut find_cut(const Values<T, L>& x, int V, const Row& r, float mine, int top_k, float top_p, float min_p, L& s) {
+template <typename X, typename L>
+__device__ Cut find_cut(const X& x, int V, const Row& r, float mine, int top_k, float top_p, float min_p, L& s) {
+  typedef typename X::Type T;
   constexpr int B = Logit<T>::kBits;
   Cut c{1u, 0x7fffffff, min_p > 0.f ? fmax(kNoWeight, log((double)fminf(min_p, 1.f))) : kNoWeight, 0, 0};
   u64 ties = ~0ull;                                 // kept of the tokens with key c.key, where c.index does not say it
@@ -532,8 +520,8 @@ __device__ __forceinline__ bool is_kept(float a, int v, const Cut& c, const Row&
 }
 
 // the row into LDS, where it fits, its maximum and the thread's own
-template <typename T, typename L>
-__device__ float load_row(const T* x, int V, bool cached, float* mine, L& s) {
+template <bool CACHED, typename T, typename L>
+__device__ float load_row(const T* x, int V, float* mine, L& s) {
   float m = -INFINITY;
   T* row = reinterpret_cast<T*>(s.row);
   constexpr int U = 16;
@@ -545,7 +533,7 @@ __device__ float load_row(const T* x, int V, bool cached, float* mine, L& s) {
     for (int i = 0; i < U; ++i) {
       const int v = v0 + i * L::kThreads;
       if (v >= V) continue;                        // (a logit is one thread's: find_cut counts on it)
-      if (cached) row[v] = a[i];
+      if constexpr (CACHED) row[v] = a[i];
       m = fmaxf(m, Logit<T>::value(a[i]));
     }
   }
@@ -557,18 +545,18 @@ __device__ float load_row(const T* x, int V, bool cached, float* mine, L& s) {
   return m;
 }
 
-template <typename T, int NT, int CACHE>
+template <typename T, int NT, int CACHE, bool CACHED>
 __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
   typedef Lds<NT, CACHE> L;
   __shared__ L s;
   const int row = blockIdx.x, V = a.vocab;
   const T* p = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
-  const Values<T, L> x{p, &s, V <= (int)(CACHE / sizeof(T))};
+  const Values<T, L, CACHED> x{p, &s};
   const float t = a.temperature ? a.temperature[row] : 1.f;
   const int top_k = a.top_k ? a.top_k[row] : 0;
   const float top_p = a.top_p ? a.top_p[row] : 1.f, min_p = a.min_p ? a.min_p[row] : 0.f, uniform = a.uniform ? a.uniform[row] : 0.f;
   float mine;
-  Row r{load_row(p, V, x.cached, &mine, s), fmax(1.0 / (double)t, 1e-300), kBinsPerNat / t};   // (an infinite temperature: all finite logits alike)
+  Row r{load_row<CACHED>(p, V, &mine, s), fmax(1.0 / (double)t, 1e-300), kBinsPerNat / t};   // (an infinite temperature: all finite logits alike)
   int token = -1, kept = 0;
   float lp = -INFINITY;
   if (r.max == -INFINITY) {
@@ -597,8 +585,7 @@ __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
           ++n;
         }
       };
-      if (x.cached) walk<4>(x, begin + lane, end, 64, add);
-      else walk<12>(x, begin + lane, end, 64, add);
+      walk<CACHED ? 4 : 12>(x, begin + lane, end, 64, add);
       z = wave_sum_u64(z);
       n = wave_sum_u64(n);
       __syncthreads();
@@ -628,14 +615,14 @@ __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
 }
 
 // -infinity at the tokens of rows [.., ld] of floats that the rules do not keep
-template <int NT, int CACHE>
+template <int NT, int CACHE, bool CACHED>
 __global__ __launch_bounds__(NT) void k_truncate(float* logits, int ld, int V, const SampleParams* sp) {
   typedef Lds<NT, CACHE> L;
   __shared__ L s;
   float* p = logits + (size_t)blockIdx.x * ld;
-  const Values<float, L> x{p, &s, V <= (int)(CACHE / sizeof(float))};
+  const Values<float, L, CACHED> x{p, &s};
   float mine;
-  const Row r{load_row(p, V, x.cached, &mine, s), (double)sp->inv_temp, kBinsPerNat * sp->inv_temp};
+  const Row r{load_row<CACHED>(p, V, &mine, s), (double)sp->inv_temp, kBinsPerNat * sp->inv_temp};
   if (r.max == -INFINITY) return;
   const Cut c = find_cut(x, V, r, mine, sp->top_k, sp->top_p, sp->min_p, s);
   __syncthreads();
@@ -647,17 +634,24 @@ __global__ __launch_bounds__(NT) void k_truncate(float* logits, int ld, int V, c
 // Up to 4096 logits: 256 threads, three work-groups to a CU; more: a CU's threads and LDS, 32128 floats or twice as many halves of it
 // (what is behind them is read again from L2 at every step).
 constexpr int kSmallRow = 4096, kSmallThreads = 256, kSmallCache = 16384;
-constexpr int kLargeThreads = 1024, kLargeCache = 128512;
+constexpr int kLargeThreads = 1024, kLargeCache = 128512, kNoCache = 16;
 static_assert(sizeof(Lds<kLargeThreads, kLargeCache>) <= 160 * 1024, "one work-group's LDS");
 static_assert(sizeof(Lds<kSmallThreads, kSmallCache>) <= 52 * 1024, "three work-groups");
 
 }  // namespace
 
+// f(threads, bytes of LDS for the row, whether it fits) for rows of V logits of so many bytes
+template <typename F>
+static void by_size(int V, size_t bytes, F f) {
+  if (V <= kSmallRow) f(std::integral_constant<int, kSmallThreads>{}, std::integral_constant<int, kSmallCache>{}, std::true_type{});
+  else if (V * bytes <= kLargeCache) f(std::integral_constant<int, kLargeThreads>{}, std::integral_constant<int, kLargeCache>{}, std::true_type{});
+  else f(std::integral_constant<int, kLargeThreads>{}, std::integral_constant<int, kNoCache>{}, std::false_type{});
+}
 void launch_truncate(float* logits, int rows, int ld, int V, const SampleParams* sp, hipStream_t st) {
-  if (V <= kSmallRow)
-    hipLaunchKernelGGL((k_truncate<kSmallThreads, kSmallCache>), dim3(rows), dim3(kSmallThreads), 0, st, logits, ld, V, sp);
-  else
-    hipLaunchKernelGGL((k_truncate<kLargeThreads, kLargeCache>), dim3(rows), dim3(kLargeThreads), 0, st, logits, ld, V, sp);
+  by_size(V, sizeof(float), [&](auto threads, auto cache, auto cached) {
+    constexpr int NT = decltype(threads)::value, C = decltype(cache)::value;
+    hipLaunchKernelGGL((k_truncate<NT, C, decltype(cached)::value>), dim3(rows), dim3(NT), 0, st, logits, ld, V, sp);
+  });
 }
 
 }  // namespace stairs
@@ -688,8 +682,10 @@ extern "C" int stairs_sample_device(const stairs_sampling* a, void* hip_stream) 
   const dim3 grid(a->rows);
   auto launch = [&](auto type) {
     typedef decltype(type) T;
-    if (a->vocab <= kSmallRow) hipLaunchKernelGGL((k_sample_rows<T, kSmallThreads, kSmallCache>), grid, dim3(kSmallThreads), 0, st, *a);
-    else hipLaunchKernelGGL((k_sample_rows<T, kLargeThreads, kLargeCache>), grid, dim3(kLargeThreads), 0, st, *a);
+    by_size(a->vocab, sizeof(T), [&](auto threads, auto cache, auto cached) {
+      constexpr int NT = decltype(threads)::value, C = decltype(cache)::value;
+      hipLaunchKernelGGL((k_sample_rows<T, NT, C, decltype(cached)::value>), grid, dim3(NT), 0, st, *a);
+    });
   };
   if (a->dtype == STAIRS_DTYPE_FP32) launch(float{});
   else if (a->dtype == STAIRS_DTYPE_BF16) launch(uint16_t{});

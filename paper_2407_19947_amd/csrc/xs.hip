@@ -2,28 +2,31 @@
 // (stairs_sample_device), and the same cut applied to the rows of the sampled generation path (launch_truncate).
 //
 // Tokens are ordered by (logit, index); what the rules keep is a prefix of that order, and its end a key (the logit's bits in an
-// order-preserving form) with, among equal logits, an index.  It is found by a histogram of the keys' leading bits, by count (top-k)
-// or by weight (top-p), which names the bin it is in, and by sorting that bin's tokens; a bin that is too full (equal logits by
-// the thousand) is cut by radix selection instead, bin by bin down to one key, and the equal ones by index.  Weights are
-// multiples of 2^-44 of the largest, held in 64-bit integers: their sums do not depend on the order of additions, so neither the
-// histograms' atomics nor the split of a row over threads change a result, and equal borders are equal.  (2^-44 against sums of 1
-// and more: a border moves by about 1e-11 of the whole against sums in double; a 24-bit random number falls between
-// the two never in practice.)
+// order-preserving form) with, among equal logits, an index.  A histogram over the distance from the largest logit (1/128 of a
+// temperature a bin), by count or by weight, says how far down it can be; the tokens down to there are listed and sorted, and
+// the draw is made among them.  For top-k up to a work-group's threads the histogram is of each thread's largest logit
+// alone: the k-th of these is not above the k-th of all.  Where the list would be too long (flat rows, equal logits by the thousand) the
+// end is found in one bin, or by radix selection, and the draw goes over the row.  Weights are multiples of 2^-44 of the largest,
+// held in 64-bit integers: their sums do not depend on the order of additions, so neither the histograms' atomics nor the
+// split of a row over threads change a result, and equal borders are equal.  (2^-44 against sums of 1 and more: a border moves by
+// about 1e-11 of the whole against sums in double; a 24-bit random number falls between the two never in practice.)
 //
 // A row is one work-group's, read from memory once: up to 125 KiB of it stay in LDS beside the histogram.  Bound by
 // latencies (a dozen steps that wait for each other), and with top-p alone by the exponentials in double, one a logit.
 #include "../../include/stairs.h"
 #include "stairs_device.h"
 
+#include <type_traits>
+
 namespace stairs {
 namespace {
-__device__ unsigned long long* g_lg;
 #define TICK(i) do { __syncthreads(); if (threadIdx.x == 0 && lgp) lgp[blockIdx.x * 16 + i] = __builtin_amdgcn_s_memrealtime(); } while (0)
 
 
 typedef unsigned long long u64;
 constexpr int kBinBits = 12, kBins = 1 << kBinBits;
-constexpr int kList = 2048;                        // tokens that are sorted
+constexpr int kList = 2048;                        // tokens that are listed
+constexpr int kShort = 512;                        // ... and drawn from without another look at the row
 constexpr double kOne = 17592186044416.0;          // 2^44: the weight of the largest logit
 
 // Order-preserving keys: larger logit, larger key; -0 and +0 alike; NaN and -infinity are key 0 (never kept, never counted).
@@ -51,7 +54,11 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 struct Row {
   float max;
   double inv_temp;
+  float bins;                                      // bins of the distance histogram to one of the logit
 };
+// a logit's bin: larger logits never a later one
+__device__ __forceinline__ int bin_of(float x, const Row& r) { return x == r.max ? 0 : (int)fminf((r.max - x) * r.bins, (float)(kBins - 1)); }
+constexpr float kBinsPerNat = kBins / 32.f;        // weights below e^-32 are 0 in multiples of 2^-44
 // logarithm of the weight: 0 for the largest logits (infinite ones too)
 __device__ __forceinline__ double exponent(float x, const Row& r) { return x == r.max ? 0.0 : ((double)x - (double)r.max) * r.inv_temp; }
 constexpr double kNoWeight = -745.13;              // below it a weight is 0 in double
@@ -102,36 +109,47 @@ struct Lds {
   alignas(16) unsigned char row[CACHE];
   union {
     u64 bin[kBins];                                // histogram
-    struct { u64 order[kList]; } list;             // tokens of a bin, (key, index from the end)
+    struct {
+      u64 order[kList], other[kShort];             // listed tokens, (key, index from the end)
+      u64 weight[kShort];
+    } list;
   };
   u64 part[kWaves], part2[kWaves];
   u64 found[3];
   float fpart[kWaves];
   int count;
+  unsigned lowest;
 };
 
-// the row's values: what is in LDS from there
-template <typename T, typename L>
+// the row's values, from LDS or from memory
+template <typename T, typename L, bool CACHED>
 struct Values {
+  typedef T Type;
+  typedef L Shared;
+  static constexpr bool kCached = CACHED;
   const T* x;
   const L* lds;
-  bool cached;
   __device__ __forceinline__ float operator[](int v) const {
-    return Logit<T>::value(cached ? reinterpret_cast<const T*>(lds->row)[v] : x[v]);
+    if constexpr (CACHED) return Logit<T>::value(reinterpret_cast<const T*>(lds->row)[v]);
+    else return Logit<T>::value(x[v]);
   }
 };
-// f(v, value) for the thread's share of the row, in no order; four loads at a time
-template <typename T, typename L, typename F>
-__device__ __forceinline__ void each(const Values<T, L>& x, int V, F f) {
-  int v = threadIdx.x;
-  for (; v + 3 * L::kThreads < V; v += 4 * L::kThreads) {
-    float a[4];
+// f(v, value) for the thread's share of the indices begin .. end, in no order; several loads at a time, more where they come from memory
+template <int U, typename X, typename F>
+__device__ __forceinline__ void walk(const X& x, int begin, int end, int step, F f) {
+  int v = begin;
+  for (; v + (U - 1) * step < end; v += U * step) {
+    float a[U];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a[i] = x[v + i * L::kThreads];
+    for (int i = 0; i < U; ++i) a[i] = x[v + i * step];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f(v + i * L::kThreads, a[i]);
+    for (int i = 0; i < U; ++i) f(v + i * step, a[i]);
   }
-  for (; v < V; v += L::kThreads) f(v, x[v]);
+  for (; v < end; v += step) f(v, x[v]);
+}
+template <typename X, typename F>
+__device__ __forceinline__ void each(const X& x, int V, F f) {
+  walk<X::kCached ? 4 : 12>(x, threadIdx.x, V, X::Shared::kThreads, f);
 }
 
 template <typename L>
@@ -156,20 +174,20 @@ __device__ u64 block_before(u64 v, L& s) {
   return before;
 }
 
-// Of the histogram's n bins, from the top: the first at which `over` and the bins so far reach the target -> s.found[0], what is
-// in front of it -> s.found[1]; s.found[0] is n if none does
-template <typename L>
+// Of the histogram's n bins, in order (DOWN: from the last): the first at which `over` and the bins so far reach the target ->
+// s.found[0], what is in front of it -> s.found[1]; s.found[0] is n if none does
+template <bool DOWN, typename L>
 __device__ void find_bin(int n, u64 over, u64 target, L& s) {
   const int per = (n + L::kThreads - 1) / L::kThreads, first = threadIdx.x * per;
   if (threadIdx.x == 0) s.found[0] = n;
   u64 mine = 0;
-  for (int i = first; i < min(first + per, n); ++i) mine += s.bin[n - 1 - i];
+  for (int i = first; i < min(first + per, n); ++i) mine += s.bin[DOWN ? n - 1 - i : i];
   u64 before = over + block_before(mine, s);
   if (before < target && before + mine >= target) {
     for (int i = first; i < min(first + per, n); ++i) {
-      const u64 b = s.bin[n - 1 - i];
+      const u64 b = s.bin[DOWN ? n - 1 - i : i];
       if (before < target && before + b >= target) {
-        s.found[0] = (u64)(n - 1 - i);
+        s.found[0] = (u64)(DOWN ? n - 1 - i : i);
         s.found[1] = before;
       }
       before += b;
@@ -236,23 +254,21 @@ __device__ int find_index(Measure measure, int V, u64 target, L& s, bool have_pa
   return over ? lo + __builtin_ctzll(over) : V;
 }
 
-struct Cut {                       // kept: key > key, or key == key and index <= index; and exponent >= least
-  uint32_t key;
-  int index;
-  double least;
-};
 
-// The tokens with low <= key < high, sorted into s.list.order; how many, or -1: too many
-template <typename T, typename L>
-__device__ int sort_bin(const Values<T, L>& x, int V, uint32_t low, u64 high, L& s) {
+// The tokens of the bins first .. last, sorted into s.list.order, the first in front; how many, or -1: too many
+template <typename X, typename L>
+__device__ int sort_bins(const X& x, int V, const Row& r, int first, int last, L& s) {
   __syncthreads();
   if (threadIdx.x == 0) s.count = 0;
   __syncthreads();
   each(x, V, [&](int v, float a) {
-    const uint32_t k = key_of<T>(a);
-    if (k >= low && k < high && k) {
-      const int at = atomicAdd(&s.count, 1);
-      if (at < kList) s.list.order[at] = ((u64)k << 32) | (0xFFFFFFFFu - (uint32_t)v);
+    const int b = bin_of(a, r);
+    if (b >= first && b <= last) {
+      const uint32_t k = key_of<typename X::Type>(a);
+      if (k) {
+        const int at = atomicAdd(&s.count, 1);
+        if (at < kList) s.list.order[at] = ((u64)k << 32) | (0xFFFFFFFFu - (uint32_t)v);
+      }
     }
   });
   __syncthreads();
@@ -260,6 +276,19 @@ __device__ int sort_bin(const Values<T, L>& x, int V, uint32_t low, u64 high, L&
   if (c > kList) return -1;
   int n = 64;                                      // a power of two
   while (n < c) n *= 2;
+  if (n <= kShort && n <= L::kThreads) {
+    // a token's place is the number of those in front of it, NT / n threads to a token (no two are equal)
+    const int per = L::kThreads / n, mine = threadIdx.x / per, part = threadIdx.x % per;
+    const u64 a = mine < c ? s.list.order[mine] : 0;
+    int ahead = 0;
+    for (int i = part; i < c; i += per) ahead += s.list.order[i] > a;
+    for (int off = 1; off < per; off <<= 1) ahead += __shfl_xor(ahead, off);
+    if (mine < c && part == 0) s.list.other[ahead] = a;
+    __syncthreads();
+    for (int i = threadIdx.x; i < c; i += L::kThreads) s.list.order[i] = s.list.other[i];
+    __syncthreads();
+    return c;
+  }
   for (int i = c + threadIdx.x; i < n; i += L::kThreads) s.list.order[i] = 0;
   __syncthreads();
   // bitonic, largest first; pairs up to 64 apart stay within the 128 entries of a wave
@@ -284,19 +313,22 @@ __device__ __forceinline__ float value_of_key(uint32_t k, int bits) {
   return __uint_as_float(k >> 31 ? k ^ 0x80000000u : ~k);
 }
 
-// The largest key K with (measure of the keys >= K) >= target, among those whose bits above `below` are prefix; over: the measure of
-// the keys above those; -> what is above K too.  each_key(f): f(key, measure) for every token of the row.
+// The largest key K with (measure of the keys >= K) >= target; *above: of the keys above it.  each_key(f): f(key, measure()) for every
+// token of the row.
 template <int KEYBITS, typename L, typename Each>
-__device__ uint32_t select_key(Each each_key, uint32_t prefix, int below, u64 over, u64 target, u64* above, L& s) {
+__device__ uint32_t select_key(Each each_key, u64 target, u64* above, L& s) {
+  uint32_t prefix = 0;
+  u64 over = 0;
+  int below = KEYBITS;
   while (below > 0) {
-    const int bits = below > kBinBits ? (below + 1) / 2 : below, shift = below - bits, n = 1 << bits;
+    const int bits = below > 2 * kBinBits ? kBinBits : below > kBinBits ? (below + 1) / 2 : below, shift = below - bits, n = 1 << bits;
     clear_bins(n, s);
-    each_key([&](uint32_t key, u64 m) {
-      if ((key >> below) == prefix) add_to_bin((key >> shift) & (n - 1), m, s);
+    each_key([&](uint32_t key, auto m) {
+      if (below >= 32 || (key >> below) == prefix) add_to_bin((key >> shift) & (n - 1), m(), s);
     });
     __syncthreads();
-    find_bin(n, over, target, s);
-    prefix = prefix << bits | (uint32_t)s.found[0];
+    find_bin<true>(n, over, target, s);
+    prefix = (below >= 32 ? 0u : prefix << bits) | (uint32_t)s.found[0];
     over = s.found[1];
     below = shift;
     __syncthreads();
@@ -305,80 +337,131 @@ __device__ uint32_t select_key(Each each_key, uint32_t prefix, int below, u64 ov
   return prefix;
 }
 
-// the cut of the rules
-template <typename T, typename L>
-__device__ Cut find_cut(const Values<T, L>& x, int V, const Row& r, int top_k, float top_p, float min_p, L& s, unsigned long long* lgp = nullptr) {
-  constexpr int B = Logit<T>::kBits, LOW = B - kBinBits;
-  Cut c{1u, 0x7fffffff, min_p > 0.f ? fmax(kNoWeight, log((double)fminf(min_p, 1.f))) : kNoWeight};
+// What the rules keep: the tokens up to a cut, and, where they are few, the tokens themselves.
+struct Cut {                       // kept: key > key, or key == key and index <= index; and exponent >= least
+  uint32_t key;
+  int index;
+  double least;
+  int listed;                      // > 0: the first so many of s.list.order, their weights in s.list.weight; 0: not listed
+  u64 sum;                         // ... and their weight
+};
+__device__ __forceinline__ u64 border(float top_p, u64 z) {       // tokens with less than this in front of them stay
+  const double t = ceil((double)top_p * (double)z);
+  return t < 1.0 ? 1ull : (u64)t;
+}
+
+// The cut among the n listed tokens, sorted, of which the first top_k are in question; `before`: weight in front of the list; target:
+// 0 to form it from the listed tokens' own weight.  Up to kShort of them every wave does it for itself.
+template <int B, typename L>
+__device__ Cut cut_list(int n, int top_k, float top_p, u64 before, u64 target, const Row& r, Cut c, L& s) {
+  const int lane = threadIdx.x & 63, all = min(n, top_k);
+  auto logit = [&](int i) { return value_of_key((uint32_t)(s.list.order[i] >> 32), B); };
+  int stay;
+  if (all <= kShort) {
+    u64 z = 0;
+    for (int i = lane; i < all; i += 64) {          // (every wave writes the same numbers, and reads its own)
+      const u64 w = fixed_exp(exponent(logit(i), r));
+      s.list.weight[i] = w;
+      z += w;
+    }
+    if (top_p < 1.f && target == 0) target = border(top_p, wave_sum_u64(z));
+    u64 front = before, sum = 0;
+    int kept = 0;
+    stay = 0;
+    for (int i0 = 0; i0 < all; i0 += 64) {          // (weights do not grow along the order: what stays is a prefix)
+      const int i = i0 + lane;
+      const u64 w = i < all ? s.list.weight[i] : 0, to = wave_scan_u64(w);
+      const bool here = i < all && (!(top_p < 1.f) || front + to - w < target), strong = here && exponent(logit(min(i, all - 1)), r) >= c.least;
+      stay += __popcll(__ballot(here));
+      kept += __popcll(__ballot(strong));
+      if (strong) sum += w;
+      front += __shfl(to, 63);
+    }
+    if (before == 0) {
+      c.listed = kept;
+      c.sum = wave_sum_u64(sum);
+    }
+  } else {
+    constexpr int PER = kList / L::kThreads;
+    u64 w[PER], mine = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int at = threadIdx.x * PER + i;
+      w[i] = at < all ? fixed_exp(exponent(logit(at), r)) : 0;
+      mine += w[i];
+    }
+    u64 front = before + block_before(mine, s), z = 0, here = 0;
+    for (int k = 0; k < L::kWaves; ++k) z += s.part[k];
+    if (top_p < 1.f && target == 0) target = border(top_p, z);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      here += threadIdx.x * PER + i < all && (!(top_p < 1.f) || front < target);
+      front += w[i];
+    }
+    stay = (int)block_sum(here, s);
+  }
+  const u64 last = s.list.order[stay - 1];
+  c.key = (uint32_t)(last >> 32);
+  c.index = (int)(0xFFFFFFFFu - (uint32_t)last);
+  __syncthreads();
+  return c;
+}
+
+template <typename X, typename L>
+__device__ Cut find_cut(const X& x, int V, const Row& r, float mine, int top_k, float top_p, float min_p, L& s, unsigned long long* lgp = nullptr) {
+  typedef typename X::Type T;
+  constexpr int B = Logit<T>::kBits;
+  Cut c{1u, 0x7fffffff, min_p > 0.f ? fmax(kNoWeight, log((double)fminf(min_p, 1.f))) : kNoWeight, 0, 0};
   u64 ties = ~0ull;                                 // kept of the tokens with key c.key, where c.index does not say it
-  u64 z = 0;                                        // weight of the first top_k
-  bool cut_k = false;
   auto keys = [&](auto f) {
     each(x, V, [&](int, float a) {
       const uint32_t k = key_of<T>(a);
       if (k) f(k, a);
     });
   };
+  bool cut_k = false;
   if (top_k > 0 && top_k < V) {
-    clear_bins(kBins, s);
-    keys([&](uint32_t k, float) { add_to_bin(k >> LOW, 1, s); });
-    __syncthreads();
-    TICK(2);
-    find_bin(kBins, 0, (u64)top_k, s);
-    TICK(3);
-    const uint32_t bin = (uint32_t)s.found[0];
-    const u64 before = s.found[1];
-    if (bin < kBins) {                              // (else there are fewer tokens)
-      cut_k = true;
-      // everything down to that bin, so that the weights of all of the first top_k are at hand
-      const int n = sort_bin(x, V, bin << LOW, 1ull << B, s);
-      TICK(4);
-      if (n >= 0) {
-        constexpr int PER = kList / L::kThreads;
-        u64 w[PER], mine = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          const int at = threadIdx.x * PER + i;
-          w[i] = at < top_k && at < n ? weight(value_of_key((uint32_t)(s.list.order[at] >> 32), B), r) : 0;
-          mine += w[i];
-        }
-        u64 to = block_before(mine, s);
-        z = 0;
-        for (int k = 0; k < L::kWaves; ++k) z += s.part[k];
-        int stay = top_k;
-        if (top_p < 1.f) {
-          const double t = ceil((double)top_p * (double)z);
-          const u64 target = t < 1.0 ? 1ull : (u64)t;
-          u64 here = 0;
-#pragma unroll
-          for (int i = 0; i < PER; ++i) {
-            here += threadIdx.x * PER + i < top_k && to < target;
-            to += w[i];
-          }
-          stay = (int)block_sum(here, s);           // (weights do not grow along the order: a prefix)
-        }
-        const u64 last = s.list.order[stay - 1];
-        c.key = (uint32_t)(last >> 32);
-        c.index = (int)(0xFFFFFFFFu - (uint32_t)last);
-        __syncthreads();
-        return c;
+    for (int full = top_k > L::kThreads; full < 2; ++full) {       // (the threads' largest, then all)
+      clear_bins(kBins, s);
+      if (!full && mine > -INFINITY) atomicAdd(&s.bin[bin_of(mine, r)], 1ull);
+      if (full) each(x, V, [&](int, float a) { if (a > -INFINITY) add_to_bin(bin_of(a, r), 1, s); });
+      __syncthreads();
+      TICK(2);
+      find_bin<false>(kBins, 0, (u64)top_k, s);
+      TICK(3);
+      const int bin = (int)s.found[0];
+      if (bin == kBins) {                           // so many there are not (of the threads' largest: look at all)
+        if (full) break;
+        continue;
       }
+      const int n = sort_bins(x, V, r, 0, bin, s);
+      TICK(4); if (threadIdx.x == 0) lgp[blockIdx.x * 16 + 12] = n;
+      if (n >= 0) return cut_list<B>(n, top_k, top_p, 0, 0, r, c, s);
+      cut_k = full;
+    }
+    if (cut_k) {
       u64 above;
-      c.key = select_key<B>([&](auto f) { keys([&](uint32_t k, float) { f(k, 1); }); }, bin, LOW, before, (u64)top_k, &above, s);
+      c.key = select_key<B>([&](auto f) { keys([&](uint32_t k, float) { f(k, [] { return 1ull; }); }); }, (u64)top_k, &above, s);
       ties = (u64)top_k - above;
     }
   }
   if (top_p < 1.f) {                                // (not for NaN)
     clear_bins(kBins, s);
     u64 sum = 0, tie = 0;
-    keys([&](uint32_t k, float a) {
+    each(x, V, [&](int, float a) {
+      if (!(a > -INFINITY)) return;
       const u64 w = weight(a, r);
-      if (!cut_k || k > c.key) sum += w;
-      else if (k == c.key) tie = w;
-      add_to_bin(k >> LOW, w, s);
+      if (cut_k) {
+        const uint32_t k = key_of<T>(a);
+        if (k > c.key) sum += w;
+        else if (k == c.key) tie = w;
+      } else {
+        sum += w;
+      }
+      add_to_bin(bin_of(a, r), w, s);
     });
     TICK(5);
-    z = block_sum(sum, s);
+    u64 z = block_sum(sum, s);                      // weight of the first top_k
     if (cut_k) {
       if (threadIdx.x == 0) s.found[2] = 0;
       __syncthreads();
@@ -386,38 +469,20 @@ __device__ Cut find_cut(const Values<T, L>& x, int V, const Row& r, int top_k, f
       __syncthreads();
       z += ties * s.found[2];
     }
-    const double t = ceil((double)top_p * (double)z);
-    const u64 target = t < 1.0 ? 1ull : (u64)t;
-    find_bin(kBins, 0, target, s);
+    const u64 target = border(top_p, z);
+    find_bin<false>(kBins, 0, target, s);
     TICK(6);
-    const uint32_t bin = (uint32_t)s.found[0];
+    const int bin = (int)s.found[0];
     const u64 before = s.found[1];
-    const int n = cut_k ? -1 : sort_bin(x, V, bin << LOW, ((u64)bin + 1) << LOW, s);
-    TICK(7);
-    if (n >= 0) {
-      constexpr int PER = kList / L::kThreads;
-      u64 w[PER], mine = 0, here = 0;
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int at = threadIdx.x * PER + i;
-        w[i] = at < n ? weight(value_of_key((uint32_t)(s.list.order[at] >> 32), B), r) : 0;
-        mine += w[i];
-      }
-      u64 to = before + block_before(mine, s);
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        here += threadIdx.x * PER + i < n && to < target;
-        to += w[i];
-      }
-      const int stay = (int)block_sum(here, s);
-      const u64 last = s.list.order[stay - 1];
-      c.key = (uint32_t)(last >> 32);
-      c.index = (int)(0xFFFFFFFFu - (uint32_t)last);
-      __syncthreads();
-      return c;
+    if (!cut_k) {
+      int n = sort_bins(x, V, r, 0, bin, s);
+      TICK(7); if (threadIdx.x == 0) lgp[blockIdx.x * 16 + 12] = n;
+      if (n >= 0) return cut_list<B>(n, n, top_p, 0, target, r, c, s);
+      n = sort_bins(x, V, r, bin, bin, s);
+      if (n >= 0) return cut_list<B>(n, n, top_p, before, target, r, c, s);
     }
     u64 above;
-    const uint32_t key = select_key<B>([&](auto f) { keys([&](uint32_t k, float a) { f(k, weight(a, r)); }); }, bin, LOW, before, target, &above, s);
+    const uint32_t key = select_key<B>([&](auto f) { keys([&](uint32_t k, float a) { f(k, [&] { return weight(a, r); }); }); }, target, &above, s);
     // of the equal logits at the border those with less than the target in front of them
     u64 w = 0;
     keys([&](uint32_t k, float a) { if (k == key) w = weight(a, r); });
@@ -435,6 +500,26 @@ __device__ Cut find_cut(const Values<T, L>& x, int V, const Row& r, int top_k, f
   return c;
 }
 
+// the lowest index among the listed tokens at which their weights, by index, exceed the target
+template <typename L>
+__device__ int draw_listed(const Cut& c, u64 target, L& s) {
+  if (threadIdx.x == 0) s.lowest = 0xFFFFFFFFu;
+  __syncthreads();
+  int n = 1;
+  while (n < c.listed) n *= 2;
+  const int per = n < L::kThreads ? min(64, L::kThreads / n) : 1;
+  for (int i = threadIdx.x / per; i < c.listed; i += L::kThreads / per) {
+    const uint32_t from_end = (uint32_t)s.list.order[i];
+    u64 to = 0;
+    for (int k = threadIdx.x % per; k < c.listed; k += per)
+      if ((uint32_t)s.list.order[k] >= from_end) to += s.list.weight[k];
+    for (int off = 1; off < per; off <<= 1) to += __shfl_xor(to, off);
+    if (to > target) atomicMin(&s.lowest, 0xFFFFFFFFu - from_end);
+  }
+  __syncthreads();
+  return (int)s.lowest;
+}
+
 template <typename T>
 __device__ __forceinline__ bool is_kept(float a, int v, const Cut& c, const Row& r) {
   const uint32_t k = key_of<T>(a);
@@ -442,12 +527,12 @@ __device__ __forceinline__ bool is_kept(float a, int v, const Cut& c, const Row&
   return exponent(a, r) >= c.least;
 }
 
-// the row into LDS, where it fits, and its maximum
-template <typename T, typename L>
-__device__ float load_row(const T* x, int V, bool cached, L& s) {
+// the row into LDS, where it fits, its maximum and the thread's own
+template <bool CACHED, typename T, typename L>
+__device__ float load_row(const T* x, int V, float* mine, L& s) {
   float m = -INFINITY;
   T* row = reinterpret_cast<T*>(s.row);
-  constexpr int U = 8;
+  constexpr int U = 16;
   for (int v0 = threadIdx.x; v0 < V; v0 += U * L::kThreads) {
     T a[U];
 #pragma unroll
@@ -455,10 +540,12 @@ __device__ float load_row(const T* x, int V, bool cached, L& s) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int v = v0 + i * L::kThreads;
-      if (cached && v < V) row[v] = a[i];
+      if (v >= V) continue;                        // (a logit is one thread's: find_cut counts on it)
+      if constexpr (CACHED) row[v] = a[i];
       m = fmaxf(m, Logit<T>::value(a[i]));
     }
   }
+  *mine = m;
   m = wave_max(m);
   if ((threadIdx.x & 63) == 0) s.fpart[threadIdx.x >> 6] = m;
   __syncthreads();
@@ -466,7 +553,7 @@ __device__ float load_row(const T* x, int V, bool cached, L& s) {
   return m;
 }
 
-template <typename T, int NT, int CACHE>
+template <typename T, int NT, int CACHE, bool CACHED>
 __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
   typedef Lds<NT, CACHE> L;
   __shared__ L s;
@@ -474,11 +561,12 @@ __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
   unsigned long long* lgp = reinterpret_cast<unsigned long long*>(a.workspace);
   TICK(0);
   const T* p = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
-  const Values<T, L> x{p, &s, V <= (int)(CACHE / sizeof(T))};
+  const Values<T, L, CACHED> x{p, &s};
   const float t = a.temperature ? a.temperature[row] : 1.f;
   const int top_k = a.top_k ? a.top_k[row] : 0;
   const float top_p = a.top_p ? a.top_p[row] : 1.f, min_p = a.min_p ? a.min_p[row] : 0.f, uniform = a.uniform ? a.uniform[row] : 0.f;
-  Row r{load_row(p, V, x.cached, s), fmax(1.0 / (double)t, 1e-300)};   // (an infinite temperature: all finite logits alike)
+  float mine;
+  Row r{load_row<CACHED>(p, V, &mine, s), fmax(1.0 / (double)t, 1e-300), kBinsPerNat / t};   // (an infinite temperature: all finite logits alike)
   TICK(1);
   int token = -1, kept = 0;
   float lp = -INFINITY;
@@ -488,54 +576,52 @@ __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
     kept = 1;
     lp = 0.f;
   } else {
-    const Cut c = find_cut(x, V, r, top_k, top_p, min_p, s, lgp);
+    const Cut c = find_cut(x, V, r, mine, top_k, top_p, min_p, s, lgp);
     TICK(8);
-    // weight and number of what is kept, a piece of the row a wave (find_index's first cut)
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int piece = V > 64 ? (V + L::kWaves - 1) / L::kWaves : V, begin = wave * piece, end = min(V, begin + piece);
-    u64 z = 0, n = 0;
-    auto add = [&](int v, float b) {
-      if (is_kept<T>(b, v, c, r)) {
-        z += weight(b, r);
-        ++n;
-      }
-    };
-    int v = begin + lane;
-    for (; v + 3 * 64 < end; v += 4 * 64) {
-      float b[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) b[i] = x[v + i * 64];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) add(v + i * 64, b[i]);
-    }
-    for (; v < end; v += 64) add(v, x[v]);
-    z = wave_sum_u64(z);
-    n = wave_sum_u64(n);
-    __syncthreads();
-    if (lane == 0) {
-      s.part[wave] = z;
-      s.part2[wave] = n;
-    }
-    __syncthreads();
-    z = n = 0;
-    for (int w = 0; w < L::kWaves; ++w) {
-      z += s.part[w];
-      n += s.part2[w];
-    }
-    kept = (int)n;
-    TICK(9);
     // (the lowest index whose sum exceeds u z: the sums are whole numbers, so it exceeds floor(u z) too; u below 1 by 2^-24 at
     // least, u z below z by one at least; a u outside [0, 1) or not a number is brought inside)
     const double u = fmin(fmax((double)uniform, 0.0), 1.0);
-    const u64 target = min((u64)(u * (double)z), z - 1);
-    token = find_index([&](int v) {
-      const float b = x[v];
-      return is_kept<T>(b, v, c, r) ? weight(b, r) : 0ull;
-    }, V, target, s, true);
+    auto target_of = [&](u64 z) { return min((u64)(u * (double)z), z - 1); };
+    u64 z = 0, n = 0;
+    if (c.listed > 0) {
+      z = c.sum;
+      kept = c.listed;
+      token = draw_listed(c, target_of(z), s);
+    } else {
+      // weight and number of what is kept, a piece of the row a wave (find_index's first cut)
+      const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+      const int piece = V > 64 ? (V + L::kWaves - 1) / L::kWaves : V, begin = wave * piece, end = min(V, begin + piece);
+      auto add = [&](int v, float b) {
+        if (is_kept<T>(b, v, c, r)) {
+          z += weight(b, r);
+          ++n;
+        }
+      };
+      walk<CACHED ? 4 : 12>(x, begin + lane, end, 64, add);
+      z = wave_sum_u64(z);
+      n = wave_sum_u64(n);
+      __syncthreads();
+      if (lane == 0) {
+        s.part[wave] = z;
+        s.part2[wave] = n;
+      }
+      __syncthreads();
+      z = n = 0;
+      for (int w = 0; w < L::kWaves; ++w) {
+        z += s.part[w];
+        n += s.part2[w];
+      }
+      kept = (int)n;
+      token = find_index([&](int v) {
+        const float b = x[v];
+        return is_kept<T>(b, v, c, r) ? weight(b, r) : 0ull;
+      }, V, target_of(z), s, true);
+    }
     lp = (float)(exponent(x[token], r) - log((double)z * (1.0 / kOne)));
   }
   TICK(10);
   if (threadIdx.x == 0) {
+    if (lgp) { lgp[row*16+11] = kept; }
     a.token[row] = token;
     if (a.logprob) a.logprob[row] = lp;
     if (a.kept) a.kept[row] = kept;
@@ -543,15 +629,16 @@ __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
 }
 
 // -infinity at the tokens of rows [.., ld] of floats that the rules do not keep
-template <int NT, int CACHE>
+template <int NT, int CACHE, bool CACHED>
 __global__ __launch_bounds__(NT) void k_truncate(float* logits, int ld, int V, const SampleParams* sp) {
   typedef Lds<NT, CACHE> L;
   __shared__ L s;
   float* p = logits + (size_t)blockIdx.x * ld;
-  const Values<float, L> x{p, &s, V <= (int)(CACHE / sizeof(float))};
-  const Row r{load_row(p, V, x.cached, s), (double)sp->inv_temp};
+  const Values<float, L, CACHED> x{p, &s};
+  float mine;
+  const Row r{load_row<CACHED>(p, V, &mine, s), (double)sp->inv_temp, kBinsPerNat * sp->inv_temp};
   if (r.max == -INFINITY) return;
-  const Cut c = find_cut(x, V, r, sp->top_k, sp->top_p, sp->min_p, s);
+  const Cut c = find_cut(x, V, r, mine, sp->top_k, sp->top_p, sp->min_p, s);
   __syncthreads();
   each(x, V, [&](int v, float a) {
     if (!is_kept<float>(a, v, c, r)) p[v] = -INFINITY;
@@ -561,17 +648,24 @@ __global__ __launch_bounds__(NT) void k_truncate(float* logits, int ld, int V, c
 // Up to 4096 logits: 256 threads, three work-groups to a CU; more: a CU's threads and LDS, 32128 floats or twice as many halves of it
 // (what is behind them is read again from L2 at every step).
 constexpr int kSmallRow = 4096, kSmallThreads = 256, kSmallCache = 16384;
-constexpr int kLargeThreads = 1024, kLargeCache = 128512;
+constexpr int kLargeThreads = 1024, kLargeCache = 128512, kNoCache = 16;
 static_assert(sizeof(Lds<kLargeThreads, kLargeCache>) <= 160 * 1024, "one work-group's LDS");
 static_assert(sizeof(Lds<kSmallThreads, kSmallCache>) <= 52 * 1024, "three work-groups");
 
 }  // namespace
 
+// f(threads, bytes of LDS for the row, whether it fits) for rows of V logits of so many bytes
+template <typename F>
+static void by_size(int V, size_t bytes, F f) {
+  if (V <= kSmallRow) f(std::integral_constant<int, kSmallThreads>{}, std::integral_constant<int, kSmallCache>{}, std::true_type{});
+  else if (V * bytes <= kLargeCache) f(std::integral_constant<int, kLargeThreads>{}, std::integral_constant<int, kLargeCache>{}, std::true_type{});
+  else f(std::integral_constant<int, kLargeThreads>{}, std::integral_constant<int, kNoCache>{}, std::false_type{});
+}
 void launch_truncate(float* logits, int rows, int ld, int V, const SampleParams* sp, hipStream_t st) {
-  if (V <= kSmallRow)
-    hipLaunchKernelGGL((k_truncate<kSmallThreads, kSmallCache>), dim3(rows), dim3(kSmallThreads), 0, st, logits, ld, V, sp);
-  else
-    hipLaunchKernelGGL((k_truncate<kLargeThreads, kLargeCache>), dim3(rows), dim3(kLargeThreads), 0, st, logits, ld, V, sp);
+  by_size(V, sizeof(float), [&](auto threads, auto cache, auto cached) {
+    constexpr int NT = decltype(threads)::value, C = decltype(cache)::value;
+    hipLaunchKernelGGL((k_truncate<NT, C, decltype(cached)::value>), dim3(rows), dim3(NT), 0, st, logits, ld, V, sp);
+  });
 }
 
 }  // namespace stairs
@@ -602,8 +696,10 @@ extern "C" int stairs_sample_device(const stairs_sampling* a, void* hip_stream) 
   const dim3 grid(a->rows);
   auto launch = [&](auto type) {
     typedef decltype(type) T;
-    if (a->vocab <= kSmallRow) hipLaunchKernelGGL((k_sample_rows<T, kSmallThreads, kSmallCache>), grid, dim3(kSmallThreads), 0, st, *a);
-    else hipLaunchKernelGGL((k_sample_rows<T, kLargeThreads, kLargeCache>), grid, dim3(kLargeThreads), 0, st, *a);
+    by_size(a->vocab, sizeof(T), [&](auto threads, auto cache, auto cached) {
+      constexpr int NT = decltype(threads)::value, C = decltype(cache)::value;
+      hipLaunchKernelGGL((k_sample_rows<T, NT, C, decltype(cached)::value>), grid, dim3(NT), 0, st, *a);
+    });
   };
   if (a->dtype == STAIRS_DTYPE_FP32) launch(float{});
   else if (a->dtype == STAIRS_DTYPE_BF16) launch(uint16_t{});
