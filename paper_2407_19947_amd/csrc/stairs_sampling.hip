@@ -2,7 +2,7 @@
 // (stairs_sample_device), and the same cut applied to the rows of the sampled generation path (launch_truncate).
 //
 // Tokens are ordered by (logit, index); what the rules keep is a prefix of that order, and its end a key (the logit's bits in an
-// order-preserving form) with, among equal logits, an index.  A histogram over the distance from the largest logit (1/128 of a
+// order-preserving form) with, among equal logits, an index.  A histogram over the distance from the largest logit (1/64 of a
 // temperature a bin), by count or by weight, says how far down it can be; the tokens down to there are listed and sorted, and
 // the draw is made among them.  For top-k up to a work-group's threads the histogram is of each thread's largest logit
 // alone: the k-th of these is not above the k-th of all.  Where the list would be too long (flat rows, equal logits by the thousand) the
@@ -11,7 +11,7 @@
 // split of a row over threads change a result, and equal borders are equal.  (2^-44 against sums of 1 and more: a border moves by
 // about 1e-11 of the whole against sums in double; a 24-bit random number falls between the two never in practice.)
 //
-// A row is one work-group's, read from memory once: up to 125 KiB of it stay in LDS beside the histogram.  Bound by
+// A row is one work-group's, read from memory once: up to 140 KiB of it stay in LDS beside the histogram.  Bound by
 // latencies (a dozen steps that wait for each other), and with top-p alone by the exponentials in double, one a logit.
 #include "../../include/stairs.h"
 #include "stairs_device.h"
@@ -22,8 +22,8 @@ namespace stairs {
 namespace {
 
 typedef unsigned long long u64;
-constexpr int kBinBits = 12, kBins = 1 << kBinBits;
-constexpr int kList = 2048;                        // tokens that are listed
+constexpr int kBinBits = 11, kBins = 1 << kBinBits;
+constexpr int kList = 1024;                        // tokens that are listed
 constexpr int kShort = 512;                        // ... and drawn from without another look at the row
 constexpr double kOne = 17592186044416.0;          // 2^44: the weight of the largest logit
 
@@ -57,14 +57,17 @@ struct Row {
 // a logit's bin: larger logits never a later one
 __device__ __forceinline__ int bin_of(float x, const Row& r) { return x == r.max ? 0 : (int)fminf((r.max - x) * r.bins, (float)(kBins - 1)); }
 constexpr float kBinsPerNat = kBins / 32.f;        // weights below e^-32 are 0 in multiples of 2^-44
-// logarithm of the weight: 0 for the largest logits (infinite ones too)
-__device__ __forceinline__ double exponent(float x, const Row& r) { return x == r.max ? 0.0 : ((double)x - (double)r.max) * r.inv_temp; }
+// logarithm of the weight: 0 for the largest logits; where those are infinite nothing else has any
+__device__ __forceinline__ double exponent(float x, const Row& r) {
+  if (r.max == INFINITY) return x == INFINITY ? 0.0 : -INFINITY;
+  return ((double)x - (double)r.max) * r.inv_temp;
+}
 constexpr double kNoWeight = -745.13;              // below it a weight is 0 in double
 
 // exp(d) for d <= 0 in multiples of 2^-44.  d = n ln 2 + r with |r| <= ln 2 / 2; exp(r / 4) by its series up to the 8th power
 // (the next term is 8e-16), squared twice; the number and the place of its last bit come from one multiply-add.
 __device__ __forceinline__ u64 fixed_exp(double d) {
-  d = fmax(d, -64.0);                              // (weights below 2^-45 are 0 here)
+  d = fmax(d, -64.0);                              // (weights below 2^-45 are 0 here; NaN is the least too)
   const double big = 6755399441055744.0;           // 1.5 * 2^52: adding it rounds to a whole number
   const double nb = fma(d, 1.4426950408889634074, big), n = nb - big;
   const double x = fma(n, -0.17328679513998632735, 0.25 * d);   // ln 2 / 4
@@ -112,11 +115,11 @@ struct Lds {
       u64 weight[kShort];
     } list;
   };
+  u64 piece[64];
   u64 part[kWaves], part2[kWaves];
   u64 found[3];
   float fpart[kWaves];
   int count;
-  unsigned lowest;
 };
 
 // the row's values, from LDS or from memory
@@ -145,9 +148,9 @@ __device__ __forceinline__ void walk(const X& x, int begin, int end, int step, F
   }
   for (; v < end; v += step) f(v, x[v]);
 }
-template <typename X, typename F>
+template <int U = 8, typename X, typename F>
 __device__ __forceinline__ void each(const X& x, int V, F f) {
-  walk<X::kCached ? 4 : 12>(x, threadIdx.x, V, X::Shared::kThreads, f);
+  walk<X::kCached ? 4 : U>(x, threadIdx.x, V, X::Shared::kThreads, f);
 }
 
 template <typename L>
@@ -340,7 +343,7 @@ struct Cut {                       // kept: key > key, or key == key and index <
   uint32_t key;
   int index;
   double least;
-  int listed;                      // > 0: the first so many of s.list.order, their weights in s.list.weight; 0: not listed
+  int listed;                      // > 0: the first so many of s.list.order; 0: not listed
   u64 sum;                         // ... and their weight
 };
 __device__ __forceinline__ u64 border(float top_p, u64 z) {       // tokens with less than this in front of them stay
@@ -388,15 +391,26 @@ __device__ Cut cut_list(int n, int top_k, float top_p, u64 before, u64 target, c
       w[i] = at < all ? fixed_exp(exponent(logit(at), r)) : 0;
       mine += w[i];
     }
-    u64 front = before + block_before(mine, s), z = 0, here = 0;
+    u64 front = before + block_before(mine, s), z = 0, here = 0, strong = 0, sum = 0;
     for (int k = 0; k < L::kWaves; ++k) z += s.part[k];
     if (top_p < 1.f && target == 0) target = border(top_p, z);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      here += threadIdx.x * PER + i < all && (!(top_p < 1.f) || front < target);
+      const int at = threadIdx.x * PER + i;
+      if (at < all && (!(top_p < 1.f) || front < target)) {
+        ++here;
+        if (exponent(logit(at), r) >= c.least) {
+          ++strong;
+          sum += w[i];
+        }
+      }
       front += w[i];
     }
     stay = (int)block_sum(here, s);
+    if (before == 0) {
+      c.listed = (int)block_sum(strong, s);
+      c.sum = block_sum(sum, s);
+    }
   }
   const u64 last = s.list.order[stay - 1];
   c.key = (uint32_t)(last >> 32);
@@ -410,52 +424,69 @@ __device__ Cut find_cut(const X& x, int V, const Row& r, float mine, int top_k, 
   typedef typename X::Type T;
   constexpr int B = Logit<T>::kBits;
   Cut c{1u, 0x7fffffff, min_p > 0.f ? fmax(kNoWeight, log((double)fminf(min_p, 1.f))) : kNoWeight, 0, 0};
-  u64 ties = ~0ull;                                 // kept of the tokens with key c.key, where c.index does not say it
+  // tokens that min_p may keep are in the bins up to this one
+  const int weak = (int)fmin(1.0 - c.least * (double)kBinsPerNat, (double)(kBins - 1));
+  const bool by_p = top_p < 1.f;                    // (not for NaN)
+  // ways to list the tokens in question, one after the other until one gives a list that is short enough (one place for each step:
+  // the code runs once and comes from memory)
+  enum { kThreadsLargest, kCount, kWeight, kOneBin, kWeak, kNone };
+  auto behind_k = [&] { return by_p ? kWeight : weak < kBins - 1 ? kWeak : kNone; };
+  int way = top_k > 0 && top_k < V ? (top_k > L::kThreads ? kCount : kThreadsLargest) : behind_k();
+  bool cut_k = false;                               // top_k cuts, and found no list
+  int bin = weak;
+  u64 before = 0, target = 0;
+  while (way != kNone) {
+    if (way <= kWeight) {
+      clear_bins(kBins, s);
+      u64 sum = 0;
+      if (way == kThreadsLargest) {
+        if (mine > -INFINITY) atomicAdd(&s.bin[bin_of(mine, r)], 1ull);
+      } else if (way == kCount) {
+        each(x, V, [&](int, float a) { if (a > -INFINITY) add_to_bin(bin_of(a, r), 1, s); });
+      } else {
+        each(x, V, [&](int, float a) {
+          const u64 w = weight(a, r);               // (0 for NaN and -infinity)
+          sum += w;
+          if (w) atomicAdd(&s.bin[bin_of(a, r)], w);
+        });
+      }
+      __syncthreads();
+      if (way == kWeight) target = border(top_p, block_sum(sum, s));
+      find_bin<false>(kBins, 0, way == kWeight ? target : (u64)top_k, s);
+      bin = (int)s.found[0];
+      before = s.found[1];
+      if (bin == kBins) {                           // so many there are not: of the threads' largest, or of all
+        way = way == kThreadsLargest ? kCount : behind_k();
+        bin = weak;
+        continue;
+      }
+    }
+    // (under top_k with top_p all of the first top_k count, else what min_p keeps of them)
+    const int n = sort_bins(x, V, r, way == kOneBin ? bin : 0, way == kOneBin || (way < kWeight && by_p) ? bin : min(bin, weak), s);
+    if (n >= 0) return cut_list<B>(n, way < kWeight ? top_k : n, way == kWeak ? 1.f : top_p, way == kOneBin ? before : 0, way < kWeight ? 0 : target, r, c, s);
+    cut_k = way == kCount;
+    way = way == kThreadsLargest ? kCount : way == kWeight ? kOneBin : kNone;
+  }
+  // flat rows: bit by bit
   auto keys = [&](auto f) {
     each(x, V, [&](int, float a) {
       const uint32_t k = key_of<T>(a);
       if (k) f(k, a);
     });
   };
-  bool cut_k = false;
-  if (top_k > 0 && top_k < V) {
-    for (int full = top_k > L::kThreads; full < 2; ++full) {       // (the threads' largest, then all)
-      clear_bins(kBins, s);
-      if (!full && mine > -INFINITY) atomicAdd(&s.bin[bin_of(mine, r)], 1ull);
-      if (full) each(x, V, [&](int, float a) { if (a > -INFINITY) add_to_bin(bin_of(a, r), 1, s); });
-      __syncthreads();
-      find_bin<false>(kBins, 0, (u64)top_k, s);
-      const int bin = (int)s.found[0];
-      if (bin == kBins) {                           // so many there are not (of the threads' largest: look at all)
-        if (full) break;
-        continue;
-      }
-      const int n = sort_bins(x, V, r, 0, bin, s);
-      if (n >= 0) return cut_list<B>(n, top_k, top_p, 0, 0, r, c, s);
-      cut_k = full;
-    }
-    if (cut_k) {
-      u64 above;
-      c.key = select_key<B>([&](auto f) { keys([&](uint32_t k, float) { f(k, [] { return 1ull; }); }); }, (u64)top_k, &above, s);
-      ties = (u64)top_k - above;
-    }
+  u64 ties = ~0ull;                                 // kept of the tokens with key c.key, where c.index does not say it
+  if (cut_k) {
+    u64 above;
+    c.key = select_key<B>([&](auto f) { keys([&](uint32_t k, float) { f(k, [] { return 1ull; }); }); }, (u64)top_k, &above, s);
+    ties = (u64)top_k - above;
   }
-  if (top_p < 1.f) {                                // (not for NaN)
-    clear_bins(kBins, s);
-    u64 sum = 0, tie = 0;
-    each(x, V, [&](int, float a) {
-      if (!(a > -INFINITY)) return;
-      const u64 w = weight(a, r);
-      if (cut_k) {
-        const uint32_t k = key_of<T>(a);
-        if (k > c.key) sum += w;
-        else if (k == c.key) tie = w;
-      } else {
-        sum += w;
-      }
-      add_to_bin(bin_of(a, r), w, s);
+  if (by_p) {
+    u64 sum = 0, tie = 0;                           // weight of the first top_k; of one of the last of them
+    keys([&](uint32_t k, float a) {
+      if (!cut_k || k > c.key) sum += weight(a, r);
+      else if (k == c.key) tie = weight(a, r);
     });
-    u64 z = block_sum(sum, s);                      // weight of the first top_k
+    u64 z = block_sum(sum, s);
     if (cut_k) {
       if (threadIdx.x == 0) s.found[2] = 0;
       __syncthreads();
@@ -463,16 +494,7 @@ __device__ Cut find_cut(const X& x, int V, const Row& r, float mine, int top_k, 
       __syncthreads();
       z += ties * s.found[2];
     }
-    const u64 target = border(top_p, z);
-    find_bin<false>(kBins, 0, target, s);
-    const int bin = (int)s.found[0];
-    const u64 before = s.found[1];
-    if (!cut_k) {
-      int n = sort_bins(x, V, r, 0, bin, s);
-      if (n >= 0) return cut_list<B>(n, n, top_p, 0, target, r, c, s);
-      n = sort_bins(x, V, r, bin, bin, s);
-      if (n >= 0) return cut_list<B>(n, n, top_p, before, target, r, c, s);
-    }
+    target = border(top_p, z);
     u64 above;
     const uint32_t key = select_key<B>([&](auto f) { keys([&](uint32_t k, float a) { f(k, [&] { return weight(a, r); }); }); }, target, &above, s);
     // of the equal logits at the border those with less than the target in front of them
@@ -492,24 +514,41 @@ __device__ Cut find_cut(const X& x, int V, const Row& r, float mine, int top_k, 
   return c;
 }
 
-// the lowest index among the listed tokens at which their weights, by index, exceed the target
-template <typename L>
-__device__ int draw_listed(const Cut& c, u64 target, L& s) {
-  if (threadIdx.x == 0) s.lowest = 0xFFFFFFFFu;
-  __syncthreads();
-  int n = 1;
-  while (n < c.listed) n *= 2;
-  const int per = n < L::kThreads ? min(64, L::kThreads / n) : 1;
-  for (int i = threadIdx.x / per; i < c.listed; i += L::kThreads / per) {
-    const uint32_t from_end = (uint32_t)s.list.order[i];
-    u64 to = 0;
-    for (int k = threadIdx.x % per; k < c.listed; k += per)
-      if ((uint32_t)s.list.order[k] >= from_end) to += s.list.weight[k];
-    for (int off = 1; off < per; off <<= 1) to += __shfl_xor(to, off);
-    if (to > target) atomicMin(&s.lowest, 0xFFFFFFFFu - from_end);
+// The lowest index among the listed tokens at which their weights, by index, exceed the target: six bits of the index at a time, the
+// weights of the tokens with the bits found so far summed by the next six.
+template <int B, typename L>
+__device__ int draw_listed(const Cut& c, int V, u64 target, const Row& r, L& s) {
+  constexpr int PER = kList / L::kThreads;
+  const int lane = threadIdx.x & 63;
+  u64 w[PER];
+  uint32_t v[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int at = threadIdx.x + i * L::kThreads;
+    w[i] = 0;
+    v[i] = 0;
+    if (at < c.listed) {
+      const u64 o = s.list.order[at];
+      v[i] = 0xFFFFFFFFu - (uint32_t)o;
+      w[i] = fixed_exp(exponent(value_of_key((uint32_t)(o >> 32), B), r));
+    }
   }
-  __syncthreads();
-  return (int)s.lowest;
+  uint32_t found = 0;
+  u64 before = 0;
+  for (int shift = (31 - __builtin_clz(V | 1)) / 6 * 6; shift >= 0; shift -= 6) {
+    if (threadIdx.x < 64) s.piece[lane] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (w[i] && (v[i] >> shift >> 6) == found) atomicAdd(&s.piece[(v[i] >> shift) & 63], w[i]);
+    __syncthreads();
+    const u64 p = s.piece[lane], to = before + wave_scan_u64(p);
+    const int l = __builtin_ctzll(__ballot(to > target));
+    before = __shfl(to, l) - __shfl(p, l);
+    found = found << 6 | (uint32_t)l;
+    __syncthreads();
+  }
+  return (int)found;
 }
 
 template <typename T>
@@ -574,7 +613,7 @@ __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
     if (c.listed > 0) {
       z = c.sum;
       kept = c.listed;
-      token = draw_listed(c, target_of(z), s);
+      token = draw_listed<Logit<T>::kBits>(c, V, target_of(z), r, s);
     } else {
       // weight and number of what is kept, a piece of the row a wave (find_index's first cut)
       const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -585,7 +624,7 @@ __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
           ++n;
         }
       };
-      walk<CACHED ? 4 : 12>(x, begin + lane, end, 64, add);
+      walk<CACHED ? 4 : 8>(x, begin + lane, end, 64, add);
       z = wave_sum_u64(z);
       n = wave_sum_u64(n);
       __syncthreads();
@@ -631,24 +670,25 @@ __global__ __launch_bounds__(NT) void k_truncate(float* logits, int ld, int V, c
   });
 }
 
-// Up to 4096 logits: 256 threads, three work-groups to a CU; more: a CU's threads and LDS, 32128 floats or twice as many halves of it
-// (what is behind them is read again from L2 at every step).
+// Up to 4096 logits: 256 threads, several work-groups to a CU; up to 140 KB of them: a CU's threads, or, if there are more rows than CUs
+// and they take 63 KB at most, half of them for each of two work-groups; more is read again from L2 at every step.
 constexpr int kSmallRow = 4096, kSmallThreads = 256, kSmallCache = 16384;
-constexpr int kLargeThreads = 1024, kLargeCache = 128512, kNoCache = 16;
-static_assert(sizeof(Lds<kLargeThreads, kLargeCache>) <= 160 * 1024, "one work-group's LDS");
-static_assert(sizeof(Lds<kSmallThreads, kSmallCache>) <= 52 * 1024, "three work-groups");
+constexpr int kCus = 256, kHalfThreads = 512, kHalfCache = 64256;
+constexpr int kLargeThreads = 1024, kLargeCache = 142848, kNoCache = 16;
+static_assert(sizeof(Lds<kLargeThreads, kLargeCache>) <= 160 * 1024 && sizeof(Lds<kHalfThreads, kHalfCache>) <= 80 * 1024, "work-groups on a CU");
 
 }  // namespace
 
 // f(threads, bytes of LDS for the row, whether it fits) for rows of V logits of so many bytes
 template <typename F>
-static void by_size(int V, size_t bytes, F f) {
+static void by_size(int rows, int V, size_t bytes, F f) {
   if (V <= kSmallRow) f(std::integral_constant<int, kSmallThreads>{}, std::integral_constant<int, kSmallCache>{}, std::true_type{});
+  else if (rows > kCus && V * bytes <= kHalfCache) f(std::integral_constant<int, kHalfThreads>{}, std::integral_constant<int, kHalfCache>{}, std::true_type{});
   else if (V * bytes <= kLargeCache) f(std::integral_constant<int, kLargeThreads>{}, std::integral_constant<int, kLargeCache>{}, std::true_type{});
   else f(std::integral_constant<int, kLargeThreads>{}, std::integral_constant<int, kNoCache>{}, std::false_type{});
 }
 void launch_truncate(float* logits, int rows, int ld, int V, const SampleParams* sp, hipStream_t st) {
-  by_size(V, sizeof(float), [&](auto threads, auto cache, auto cached) {
+  by_size(rows, V, sizeof(float), [&](auto threads, auto cache, auto cached) {
     constexpr int NT = decltype(threads)::value, C = decltype(cache)::value;
     hipLaunchKernelGGL((k_truncate<NT, C, decltype(cached)::value>), dim3(rows), dim3(NT), 0, st, logits, ld, V, sp);
   });
@@ -682,7 +722,7 @@ extern "C" int stairs_sample_device(const stairs_sampling* a, void* hip_stream) 
   const dim3 grid(a->rows);
   auto launch = [&](auto type) {
     typedef decltype(type) T;
-    by_size(a->vocab, sizeof(T), [&](auto threads, auto cache, auto cached) {
+    by_size(a->rows, a->vocab, sizeof(T), [&](auto threads, auto cache, auto cached) {
       constexpr int NT = decltype(threads)::value, C = decltype(cache)::value;
       hipLaunchKernelGGL((k_sample_rows<T, NT, C, decltype(cached)::value>), grid, dim3(NT), 0, st, *a);
     });
