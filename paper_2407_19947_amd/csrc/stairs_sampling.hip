@@ -24,7 +24,9 @@ namespace {
 typedef unsigned long long u64;
 constexpr int kBinBits = 11, kBins = 1 << kBinBits;
 constexpr int kList = 1024;                        // tokens that are listed
-constexpr int kShort = 512;                        // ... and drawn from without another look at the row
+constexpr int kAllListed = 16384;                  // tokens in question that a row from memory is read for once
+constexpr int kRanked = 512;                       // ... and sorted by counting
+constexpr int kShort = 128;                        // ... and cut by every wave for itself
 constexpr double kOne = 17592186044416.0;          // 2^44: the weight of the largest logit
 
 // Order-preserving keys: larger logit, larger key; -0 and +0 alike; NaN and -infinity are key 0 (never kept, never counted).
@@ -103,15 +105,17 @@ __device__ __forceinline__ u64 wave_scan_u64(u64 v) {              // inclusive,
   return v;
 }
 
-// A work-group of NT threads; CACHE bytes of the row in LDS.  Small vocabularies take small work-groups, several to a CU.
-template <int NT, int CACHE>
+// A work-group of NT threads; CACHE bytes of the row in LDS, or up to ALL tokens of it.  Small vocabularies take small work-groups,
+// several to a CU.
+template <int NT, int CACHE, int ALL>
 struct Lds {
-  static constexpr int kThreads = NT, kWaves = NT / 64, kCache = CACHE;
+  static constexpr int kThreads = NT, kWaves = NT / 64, kCache = CACHE, kAll = ALL;
   alignas(16) unsigned char row[CACHE];
+  u64 all[ALL];                                    // rows that are not in LDS: the tokens in question, unsorted
   union {
     u64 bin[kBins];                                // histogram
     struct {
-      u64 order[kList], other[kShort];             // listed tokens, (key, index from the end)
+      u64 order[kList], other[kRanked];            // listed tokens, (key, index from the end)
       u64 weight[kShort];
     } list;
   };
@@ -151,6 +155,19 @@ __device__ __forceinline__ void walk(const X& x, int begin, int end, int step, F
 template <int U = 8, typename X, typename F>
 __device__ __forceinline__ void each(const X& x, int V, F f) {
   walk<X::kCached ? 4 : U>(x, threadIdx.x, V, X::Shared::kThreads, f);
+}
+__device__ __forceinline__ uint32_t index_of(u64 entry) { return 0xFFFFFFFFu - (uint32_t)entry; }
+__device__ __forceinline__ float value_of_key(uint32_t k, int bits) {
+  if (bits == 16) k = (k << 16) | ((k >> 15) ? 0u : 0xFFFFu);
+  return __uint_as_float(k >> 31 ? k ^ 0x80000000u : ~k);
+}
+// ... of the n tokens in s.all
+template <int B, typename L, typename F>
+__device__ __forceinline__ void each_listed(int n, const L& s, F f) {
+  for (int i = threadIdx.x; i < n; i += L::kThreads) {
+    const u64 e = s.all[i];
+    f((int)index_of(e), value_of_key((uint32_t)(e >> 32), B));
+  }
 }
 
 template <typename L>
@@ -256,39 +273,48 @@ __device__ int find_index(Measure measure, int V, u64 target, L& s, bool have_pa
 }
 
 
-// The tokens of the bins first .. last, sorted into s.list.order, the first in front; how many, or -1: too many
-template <typename X, typename L>
-__device__ int sort_bins(const X& x, int V, const Row& r, int first, int last, L& s) {
+// The tokens of the bins first .. last among those of each_token(f) -> to, in no order, up to `most` of them; how many there are
+template <typename T, typename L, typename Each>
+__device__ int gather(Each each_token, const Row& r, int first, int last, u64* to, int most, L& s) {
   __syncthreads();
   if (threadIdx.x == 0) s.count = 0;
   __syncthreads();
-  each(x, V, [&](int v, float a) {
+  each_token([&](int v, float a) {
     const int b = bin_of(a, r);
     if (b >= first && b <= last) {
-      const uint32_t k = key_of<typename X::Type>(a);
+      const uint32_t k = key_of<T>(a);
       if (k) {
         const int at = atomicAdd(&s.count, 1);
-        if (at < kList) s.list.order[at] = ((u64)k << 32) | (0xFFFFFFFFu - (uint32_t)v);
+        if (at < most) to[at] = ((u64)k << 32) | (0xFFFFFFFFu - (uint32_t)v);
       }
     }
   });
   __syncthreads();
-  const int c = s.count;
-  if (c > kList) return -1;
+  return s.count;
+}
+// s.list.order[0 .. c), c <= kList, sorted, the first in front
+template <typename L>
+__device__ void sort_list(int c, L& s) {
   int n = 64;                                      // a power of two
   while (n < c) n *= 2;
-  if (n <= kShort && n <= L::kThreads) {
+  if (n <= kRanked && n <= L::kThreads) {
     // a token's place is the number of those in front of it, NT / n threads to a token (no two are equal)
     const int per = L::kThreads / n, mine = threadIdx.x / per, part = threadIdx.x % per;
     const u64 a = mine < c ? s.list.order[mine] : 0;
     int ahead = 0;
-    for (int i = part; i < c; i += per) ahead += s.list.order[i] > a;
+    for (int i0 = part; i0 < c; i0 += 8 * per) {    // (eight reads on their way at a time)
+      u64 b[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) b[i] = s.list.order[min(i0 + i * per, kList - 1)];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ahead += i0 + i * per < c && b[i] > a;
+    }
     for (int off = 1; off < per; off <<= 1) ahead += __shfl_xor(ahead, off);
     if (mine < c && part == 0) s.list.other[ahead] = a;
     __syncthreads();
     for (int i = threadIdx.x; i < c; i += L::kThreads) s.list.order[i] = s.list.other[i];
     __syncthreads();
-    return c;
+    return;
   }
   for (int i = c + threadIdx.x; i < n; i += L::kThreads) s.list.order[i] = 0;
   __syncthreads();
@@ -307,13 +333,7 @@ __device__ int sort_bins(const X& x, int V, const Row& r, int first, int last, L
       else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
   __syncthreads();
-  return c;
 }
-__device__ __forceinline__ float value_of_key(uint32_t k, int bits) {
-  if (bits == 16) k = (k << 16) | ((k >> 15) ? 0u : 0xFFFFu);
-  return __uint_as_float(k >> 31 ? k ^ 0x80000000u : ~k);
-}
-
 // The largest key K with (measure of the keys >= K) >= target; *above: of the keys above it.  each_key(f): f(key, measure()) for every
 // token of the row.
 template <int KEYBITS, typename L, typename Each>
@@ -344,6 +364,7 @@ struct Cut {                       // kept: key > key, or key == key and index <
   int index;
   double least;
   int listed;                      // > 0: the first so many of s.list.order; 0: not listed
+  int in_all;                      // > 0: they are among the first so many of s.all
   u64 sum;                         // ... and their weight
 };
 __device__ __forceinline__ u64 border(float top_p, u64 z) {       // tokens with less than this in front of them stay
@@ -423,7 +444,7 @@ template <typename X, typename L>
 __device__ Cut find_cut(const X& x, int V, const Row& r, float mine, int top_k, float top_p, float min_p, L& s) {
   typedef typename X::Type T;
   constexpr int B = Logit<T>::kBits;
-  Cut c{1u, 0x7fffffff, min_p > 0.f ? fmax(kNoWeight, log((double)fminf(min_p, 1.f))) : kNoWeight, 0, 0};
+  Cut c{1u, 0x7fffffff, min_p > 0.f ? fmax(kNoWeight, log((double)fminf(min_p, 1.f))) : kNoWeight, 0, 0, 0};
   // tokens that min_p may keep are in the bins up to this one
   const int weak = (int)fmin(1.0 - c.least * (double)kBinsPerNat, (double)(kBins - 1));
   const bool by_p = top_p < 1.f;                    // (not for NaN)
@@ -462,12 +483,28 @@ __device__ Cut find_cut(const X& x, int V, const Row& r, float mine, int top_k, 
       }
     }
     // (under top_k with top_p all of the first top_k count, else what min_p keeps of them)
-    const int n = sort_bins(x, V, r, way == kOneBin ? bin : 0, way == kOneBin || (way < kWeight && by_p) ? bin : min(bin, weak), s);
-    if (n >= 0) return cut_list<B>(n, way < kWeight ? top_k : n, way == kWeak ? 1.f : top_p, way == kOneBin ? before : 0, way < kWeight ? 0 : target, r, c, s);
+    const int first = way == kOneBin ? bin : 0, last = way == kOneBin || (way < kWeight && by_p) ? bin : min(bin, weak);
+    int n;
+    if (L::kAll == 0 || (way == kOneBin && !c.in_all)) {
+      n = gather<T>([&](auto f) { each(x, V, f); }, r, first, last, s.list.order, kList, s);
+    } else {
+      // a row that is read from memory is read once for all tokens in question
+      if (way != kOneBin) {
+        n = gather<T>([&](auto f) { each(x, V, f); }, r, first, last, s.all, L::kAll, s);
+        c.in_all = n <= L::kAll ? n : 0;
+      }
+      n = c.in_all ? gather<T>([&](auto f) { each_listed<B>(c.in_all, s, f); }, r, first, last, s.list.order, kList, s) : kList + 1;
+    }
+    if (n <= kList) {
+      sort_list(n, s);
+      return cut_list<B>(n, way < kWeight ? top_k : n, way == kWeak ? 1.f : top_p, way == kOneBin ? before : 0, way < kWeight ? 0 : target, r, c, s);
+    }
+    if (way == kWeak && c.in_all) return c;
     cut_k = way == kCount;
     way = way == kThreadsLargest ? kCount : way == kWeight ? kOneBin : kNone;
   }
   // flat rows: bit by bit
+  c.in_all = 0;
   auto keys = [&](auto f) {
     each(x, V, [&](int, float a) {
       const uint32_t k = key_of<T>(a);
@@ -514,33 +551,29 @@ __device__ Cut find_cut(const X& x, int V, const Row& r, float mine, int top_k, 
   return c;
 }
 
-// The lowest index among the listed tokens at which their weights, by index, exceed the target: six bits of the index at a time, the
-// weights of the tokens with the bits found so far summed by the next six.
-template <int B, typename L>
-__device__ int draw_listed(const Cut& c, int V, u64 target, const Row& r, L& s) {
-  constexpr int PER = kList / L::kThreads;
+template <typename T>
+__device__ __forceinline__ bool is_kept(float a, int v, const Cut& c, const Row& r) {
+  const uint32_t k = key_of<T>(a);
+  if (!k || k < c.key || (k == c.key && v > c.index)) return false;
+  return exponent(a, r) >= c.least;
+}
+
+// The lowest index among listed tokens at which their weights, by index, exceed the target: six bits of the index at a time, the
+// weights of the tokens with the bits found so far summed by the next six.  each_weight(f): f(index, weight) for every token.
+template <typename L, typename Each>
+__device__ int draw_listed(Each each_weight, int V, u64 target, L& s) {
   const int lane = threadIdx.x & 63;
-  u64 w[PER];
-  uint32_t v[PER];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int at = threadIdx.x + i * L::kThreads;
-    w[i] = 0;
-    v[i] = 0;
-    if (at < c.listed) {
-      const u64 o = s.list.order[at];
-      v[i] = 0xFFFFFFFFu - (uint32_t)o;
-      w[i] = fixed_exp(exponent(value_of_key((uint32_t)(o >> 32), B), r));
-    }
-  }
   uint32_t found = 0;
   u64 before = 0;
   for (int shift = (31 - __builtin_clz(V | 1)) / 6 * 6; shift >= 0; shift -= 6) {
     if (threadIdx.x < 64) s.piece[lane] = 0;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      if (w[i] && (v[i] >> shift >> 6) == found) atomicAdd(&s.piece[(v[i] >> shift) & 63], w[i]);
+    each_weight([&](uint32_t v, auto w) {
+      if ((v >> shift >> 6) == found) {
+        const u64 x = w();
+        if (x) atomicAdd(&s.piece[(v >> shift) & 63], x);
+      }
+    });
     __syncthreads();
     const u64 p = s.piece[lane], to = before + wave_scan_u64(p);
     const int l = __builtin_ctzll(__ballot(to > target));
@@ -549,13 +582,6 @@ __device__ int draw_listed(const Cut& c, int V, u64 target, const Row& r, L& s) 
     __syncthreads();
   }
   return (int)found;
-}
-
-template <typename T>
-__device__ __forceinline__ bool is_kept(float a, int v, const Cut& c, const Row& r) {
-  const uint32_t k = key_of<T>(a);
-  if (!k || k < c.key || (k == c.key && v > c.index)) return false;
-  return exponent(a, r) >= c.least;
 }
 
 // the row into LDS, where it fits, its maximum and the thread's own
@@ -586,7 +612,7 @@ __device__ float load_row(const T* x, int V, float* mine, L& s) {
 
 template <typename T, int NT, int CACHE, bool CACHED>
 __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
-  typedef Lds<NT, CACHE> L;
+  typedef Lds<NT, CACHE, CACHED ? 0 : kAllListed> L;
   __shared__ L s;
   const int row = blockIdx.x, V = a.vocab;
   const T* p = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
@@ -613,7 +639,28 @@ __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
     if (c.listed > 0) {
       z = c.sum;
       kept = c.listed;
-      token = draw_listed<Logit<T>::kBits>(c, V, target_of(z), r, s);
+      constexpr int B = Logit<T>::kBits;
+      token = draw_listed([&](auto f) {
+        for (int i = threadIdx.x; i < c.listed; i += L::kThreads) {
+          const u64 e = s.list.order[i];
+          f(index_of(e), [&] { return weight(value_of_key((uint32_t)(e >> 32), B), r); });
+        }
+      }, V, target_of(z), s);
+    } else if (L::kAll > 0 && c.in_all) {
+      constexpr int B = Logit<T>::kBits;
+      each_listed<B>(c.in_all, s, [&](int v, float b) {
+        if (is_kept<T>(b, v, c, r)) {
+          z += weight(b, r);
+          ++n;
+        }
+      });
+      z = block_sum(z, s);
+      kept = (int)block_sum(n, s);
+      token = draw_listed([&](auto f) {
+        each_listed<B>(c.in_all, s, [&](int v, float b) {
+          if (is_kept<T>(b, v, c, r)) f((uint32_t)v, [&] { return weight(b, r); });
+        });
+      }, V, target_of(z), s);
     } else {
       // weight and number of what is kept, a piece of the row a wave (find_index's first cut)
       const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -656,7 +703,7 @@ __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
 // -infinity at the tokens of rows [.., ld] of floats that the rules do not keep
 template <int NT, int CACHE, bool CACHED>
 __global__ __launch_bounds__(NT) void k_truncate(float* logits, int ld, int V, const SampleParams* sp) {
-  typedef Lds<NT, CACHE> L;
+  typedef Lds<NT, CACHE, CACHED ? 0 : kAllListed> L;
   __shared__ L s;
   float* p = logits + (size_t)blockIdx.x * ld;
   const Values<float, L, CACHED> x{p, &s};
@@ -675,7 +722,7 @@ __global__ __launch_bounds__(NT) void k_truncate(float* logits, int ld, int V, c
 constexpr int kSmallRow = 4096, kSmallThreads = 256, kSmallCache = 16384;
 constexpr int kCus = 256, kHalfThreads = 512, kHalfCache = 64256;
 constexpr int kLargeThreads = 1024, kLargeCache = 142848, kNoCache = 16;
-static_assert(sizeof(Lds<kLargeThreads, kLargeCache>) <= 160 * 1024 && sizeof(Lds<kHalfThreads, kHalfCache>) <= 80 * 1024, "work-groups on a CU");
+static_assert(sizeof(Lds<kLargeThreads, kLargeCache, 0>) <= 160 * 1024 && sizeof(Lds<kHalfThreads, kHalfCache, 0>) <= 80 * 1024, "work-groups on a CU");
 
 }  // namespace
 
