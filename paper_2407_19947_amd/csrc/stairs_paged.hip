@@ -142,53 +142,116 @@ template <> struct Elem<_Float16> {
   static __device__ __forceinline__ _Float16 down(float v) { return (_Float16)v; }
 };
 
-// a block per row: q and k rotated, k and v stored
+// sine and cosine of `turns` whole turns: the nearest quarter turn, and the series for what is left, |x| <= pi / 4 (the next terms are
+// below 2^-28)
+__device__ __forceinline__ float2 cos_sin(double turns) {
+  const double t = 4.0 * (turns - rint(turns)), quarter = rint(t), x = (t - quarter) * 1.57079632679489661923, y = x * x;
+  double s = 1.0 / 362880;
+  s = fma(s, y, -1.0 / 5040);
+  s = fma(s, y, 1.0 / 120);
+  s = fma(s, y, -1.0 / 6);
+  s = fma(s * y, x, x);
+  double c = -1.0 / 3628800;
+  c = fma(c, y, 1.0 / 40320);
+  c = fma(c, y, -1.0 / 720);
+  c = fma(c, y, 1.0 / 24);
+  c = fma(c, y, -0.5);
+  c = fma(c, y, 1.0);
+  const int q = (int)quarter;
+  const float fc = (float)c, fs = (float)s;
+  const float2 r = q & 1 ? make_float2(-fs, fc) : make_float2(fc, fs);      // (a quarter turn on: (cos, sin) -> (-sin, cos))
+  return q & 2 ? make_float2(-r.x, -r.y) : r;
+}
+
+// Bound by memory, with few rows by latency.  A work-group has 32 rows and some of the n_heads + 2 n_kv_heads heads (so many
+// groups of them that there are work for all CUs); the rows' rotations are formed once for all its heads.  q and k: a thread takes 8
+// pairs of a row, 16 bytes of either half; in a key tile the same 8 dims of 8 rows are one line.  v: four rows whose positions are a
+// quad of a value tile are transposed in registers and stored as 8 bytes a dim, other rows as single values.
+constexpr int kAppendRows = 32;
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stairs_paged_rows a) {
-  __shared__ float2 s_cs[HD / 2];
-  const int t = blockIdx.x;
-  const int slot = a.slot[t];
+__global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stairs_paged_rows a, double log2_theta, int heads_a_group) {
+  __shared__ float2 s_cs[kAppendRows][HD / 2];
+  __shared__ int s_slot[kAppendRows], s_pos[kAppendRows], s_unit[kAppendRows], s_units;
+  const int t0 = blockIdx.x * kAppendRows, n = min(kAppendRows, a.rows - t0);
+  const int nq = a.n_heads, nk = c.n_kv_heads, h0 = blockIdx.y * heads_a_group, h1 = min(nq + 2 * nk, h0 + heads_a_group);
   const bool rotate = a.rope_theta > 0.f;
-  const int pos = rotate ? a.position[t] : 0;
-  if (rotate && threadIdx.x < HD / 2) {
-    const double angle = (double)pos * exp2(-(2.0 * threadIdx.x / HD) * log2((double)a.rope_theta));
-    double s, co;
-    sincos(angle, &s, &co);
-    s_cs[threadIdx.x] = make_float2((float)co, (float)s);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const unsigned slots = (unsigned)c.n_pages * (unsigned)c.page_size;
+  if (tid < 64) {
+    const int slot = lane < n ? a.slot[t0 + lane] : -1, pos = lane < n ? (rotate ? a.position[t0 + lane] : 0) : -1;
+    const bool there = (unsigned)slot < slots;
+    // rows that begin four of one quad, rows that are in one, the others
+    bool leads = there && (slot & 3) == 0 && lane < kAppendRows - 3;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) leads &= __shfl(slot, lane + i) == slot + i;
+    const unsigned long long lead = __ballot(leads), in = lead | lead << 1 | lead << 2 | lead << 3;
+    const unsigned long long units = lead | (__ballot(there) & ~in);
+    if (lane < kAppendRows) {
+      s_slot[lane] = there ? slot : -1;
+      s_pos[lane] = pos;
+      if (units >> lane & 1) s_unit[__popcll(units & ((1ull << lane) - 1))] = lane << 1 | (int)leads;
+    }
+    if (lane == 0) s_units = __popcll(units);
   }
   __syncthreads();
-  const bool store = (unsigned)slot < (unsigned)c.n_pages * (unsigned)c.page_size;
-  const int page = store ? slot / c.page_size : 0, p = store ? slot % c.page_size : 0;
+  if (rotate && h0 < nq + nk) {
+    const int i = tid % (HD / 2);
+    const double turn = exp2(-(2.0 * i / HD) * log2_theta) * 0.15915494309189533577;   // of a position, in whole turns
+    for (int r = tid / (HD / 2); r < n; r += 256 / (HD / 2)) s_cs[r][i] = cos_sin((double)s_pos[r] * turn);
+    __syncthreads();
+  }
   const size_t head_elems = (size_t)c.page_size * HD;
-  const int nq = a.n_heads, nk = c.n_kv_heads;
-  for (int i = threadIdx.x; i < (nq + nk) * (HD / 2); i += 256) {
-    const int h = i / (HD / 2), e = i % (HD / 2);
+  const int ps_shift = __builtin_ctz(c.page_size);
+  typedef typename Elem<T>::x8 x8;
+  constexpr int PAIRS = HD / 16;                                // units of 8 pairs
+  for (int i = tid; i < (min(h1, nq + nk) - h0) * kAppendRows * PAIRS; i += 256) {
+    const int e = i % PAIRS * 8, r = i / PAIRS % kAppendRows, h = h0 + i / (PAIRS * kAppendRows);
     const bool is_q = h < nq;
-    if (is_q ? pos < 0 : !store) continue;
-    const T* src = is_q ? static_cast<const T*>(a.q) + (size_t)t * a.q_stride + h * HD
-                        : static_cast<const T*>(a.k) + (size_t)t * a.k_stride + (h - nq) * HD;
-    T lo = src[e], hi = src[e + HD / 2];
+    const int slot = s_slot[r];
+    if (r >= n || (is_q ? s_pos[r] < 0 : slot < 0)) continue;
+    const T* src = is_q ? static_cast<const T*>(a.q) + (size_t)(t0 + r) * a.q_stride + h * HD + e
+                        : static_cast<const T*>(a.k) + (size_t)(t0 + r) * a.k_stride + (h - nq) * HD + e;
+    x8 lo = *reinterpret_cast<const x8*>(src), hi = *reinterpret_cast<const x8*>(src + HD / 2);
     if (rotate) {
-      const float2 r = rope_rotate(Elem<T>::up(lo), Elem<T>::up(hi), s_cs[e]);
-      lo = Elem<T>::down(r.x);
-      hi = Elem<T>::down(r.y);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float2 v = rope_rotate(Elem<T>::up(lo[k]), Elem<T>::up(hi[k]), s_cs[r][e + k]);
+        lo[k] = Elem<T>::down(v.x);
+        hi[k] = Elem<T>::down(v.y);
+      }
     }
     if (is_q) {
-      T* dst = static_cast<T*>(a.q_out) + (size_t)t * a.q_out_stride + h * HD;
-      dst[e] = lo;
-      dst[e + HD / 2] = hi;
+      T* dst = static_cast<T*>(a.q_out) + (size_t)(t0 + r) * a.q_out_stride + h * HD + e;
+      *reinterpret_cast<x8*>(dst) = lo;
+      *reinterpret_cast<x8*>(dst + HD / 2) = hi;
     } else {
-      T* dst = static_cast<T*>(c.k) + ((size_t)page * nk + (h - nq)) * head_elems;
-      dst[k_cache_off(p, e, HD)] = lo;
-      dst[k_cache_off(p, e + HD / 2, HD)] = hi;
+      T* dst = static_cast<T*>(c.k) + ((size_t)(slot >> ps_shift) * nk + (h - nq)) * head_elems;
+      const int p = slot & (c.page_size - 1);
+      *reinterpret_cast<x8*>(dst + k_cache_off(p, e, HD)) = lo;
+      *reinterpret_cast<x8*>(dst + k_cache_off(p, e + HD / 2, HD)) = hi;
     }
   }
-  if (store)
-    for (int i = threadIdx.x; i < nk * HD; i += 256) {
-      const int h = i / HD, e = i % HD;
-      T* dst = static_cast<T*>(c.v) + ((size_t)page * nk + h) * head_elems;
-      dst[v_cache_off(p, e, HD)] = static_cast<const T*>(a.v)[(size_t)t * a.v_stride + i];
+  const int v0 = max(h0 - nq - nk, 0), v1 = h1 - nq - nk, units = s_units;
+  for (int i = tid; i < (v1 - v0) * units * (HD / 8); i += 256) {
+    const int e = i % (HD / 8) * 8, u = i / (HD / 8), h = v0 + u / units, r = s_unit[u % units] >> 1;
+    const int slot = s_slot[r], p = slot & (c.page_size - 1);
+    const T* src = static_cast<const T*>(a.v) + (size_t)(t0 + r) * a.v_stride + h * HD + e;
+    T* dst = static_cast<T*>(c.v) + ((size_t)(slot >> ps_shift) * nk + h) * head_elems + v_cache_off(p, e, HD);
+    if (s_unit[u % units] & 1) {
+      x8 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const x8*>(src + k * a.v_stride);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        T q[4] = {v[0][k], v[1][k], v[2][k], v[3][k]};
+        *reinterpret_cast<uint2*>(dst + k * 8) = *reinterpret_cast<const uint2*>(q);
+      }
+    } else {
+      const x8 v = *reinterpret_cast<const x8*>(src);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) dst[k * 8] = v[k];
     }
+  }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -982,6 +1045,8 @@ using namespace stairs;
 
 namespace {
 
+constexpr int kCus = 256;
+
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 bool cache_ok(const stairs_paged_cache* c) {
@@ -1044,8 +1109,12 @@ extern "C" int stairs_paged_append(const stairs_paged_cache* c, const stairs_pag
   if (const int rc = check_stream(st)) return rc;
   stairs_paged_rows r = *a;
   if (r.rope_theta == 0.f && r.q == r.q_out) r.n_heads = 0;       // nothing happens to q
+  const int heads = r.n_heads + 2 * c->n_kv_heads, tiles = (r.rows + kAppendRows - 1) / kAppendRows;
+  const int groups = std::max(1, std::min((4 * kCus + tiles - 1) / tiles, heads));
+  const int per = (heads + groups - 1) / groups;
+  const double log2_theta = r.rope_theta > 0.f ? std::log2((double)r.rope_theta) : 0.0;
   by_type(c, [&](auto type, auto hd) {
-    hipLaunchKernelGGL((k_paged_append<decltype(type), decltype(hd)::value>), dim3(r.rows), dim3(256), 0, st, *c, r);
+    hipLaunchKernelGGL((k_paged_append<decltype(type), decltype(hd)::value>), dim3(tiles, (heads + per - 1) / per), dim3(256), 0, st, *c, r, log2_theta, per);
   });
   return launched();
 }
@@ -1056,7 +1125,7 @@ namespace {
 // A sequence's columns are its rows times the query heads of a key head.  Up to 32 of them (16 in one tile) go to attend_rows, more to
 // attend_chunk; max_fresh says which of the two a call needs, and with one sequence, or none with more, one kernel
 // takes whatever it finds.
-constexpr int kCus = 256, kFewCols = 32;
+constexpr int kFewCols = 32;
 struct Launch {
   int ct;                      // column tiles of the rows' part, 0: there is none
   bool chunk;
