@@ -163,93 +163,131 @@ __device__ __forceinline__ float2 cos_sin(double turns) {
   return q & 2 ? make_float2(-r.x, -r.y) : r;
 }
 
+// (streaming hint, for what is read once: 8190 rows of 16 + 16 heads of q and k 36.7 -> 30.5 us; on the stores it costs 9)
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <typename X>
+__device__ __forceinline__ X ld_once_as(const void* p) {
+  return __builtin_bit_cast(X, __builtin_nontemporal_load(static_cast<const u32x4*>(p)));
+}
+
 // Bound by memory, with few rows by latency.  A work-group has 32 rows and some of the n_heads + 2 n_kv_heads heads (so many
 // groups of them that there are work for all CUs); the rows' rotations are formed once for all its heads.  q and k: a thread takes 8
-// pairs of a row, 16 bytes of either half; in a key tile the same 8 dims of 8 rows are one line.  v: four rows whose positions are a
-// quad of a value tile are transposed in registers and stored as 8 bytes a dim, other rows as single values.
+// pairs of a row, 16 bytes of either half; in a key tile the same 8 dims of 8 rows are one line.  v: a head's rows go through LDS;
+// the eight positions of a value tile that are 16 adjacent bytes a dim (two quads, 16 apart) are stored together where they are rows
+// of this call, so that a wave's store is a whole tile row; rows that have not all of them as quads of 8 bytes or single
+// values.  (Quads transposed in registers, 8 bytes here and there: 8190 rows of 48 heads 75 us, 40 of them for the values.)
 constexpr int kAppendRows = 32;
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stairs_paged_rows a, double log2_theta, int heads_a_group) {
-  __shared__ float2 s_cs[kAppendRows][HD / 2];
-  __shared__ int s_slot[kAppendRows], s_pos[kAppendRows], s_unit[kAppendRows], s_units;
+__global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stairs_paged_rows a, double log2_theta) {
+  constexpr int AHEAD = 19, BEHIND = 16;                        // rows around these that decide how theirs are stored
+  __shared__ union {
+    float2 cs[kAppendRows][HD / 2];
+    T v[kAppendRows + AHEAD][HD];
+  } lds;
+  __shared__ int s_slots[BEHIND + kAppendRows + AHEAD], s_pos[kAppendRows], s_unit[kAppendRows], s_units, s_end;
+  const int* const s_slot = s_slots + BEHIND;
   const int t0 = blockIdx.x * kAppendRows, n = min(kAppendRows, a.rows - t0);
-  const int nq = a.n_heads, nk = c.n_kv_heads, h0 = blockIdx.y * heads_a_group, h1 = min(nq + 2 * nk, h0 + heads_a_group);
+  // its heads: a run of q's, one of k's and v's
+  const int nq = a.n_heads, nk = c.n_kv_heads, y = blockIdx.y, groups = gridDim.y;
+  const int only = gridDim.z == 1 ? -1 : (int)blockIdx.z;      // (few rows: q, k and v each a work-group of their own)
+  const int q0 = nq * y / groups, q1 = only > 0 ? q0 : nq * (y + 1) / groups, k0 = nk * y / groups, k1 = only == 0 ? k0 : nk * (y + 1) / groups;
   const bool rotate = a.rope_theta > 0.f;
   const int tid = threadIdx.x, lane = tid & 63;
   const unsigned slots = (unsigned)c.n_pages * (unsigned)c.page_size;
+  if (tid < BEHIND + kAppendRows + AHEAD) {
+    const int t = t0 - BEHIND + tid, slot = t >= 0 && t < a.rows ? a.slot[t] : -1;
+    s_slots[tid] = (unsigned)slot < slots ? slot : -1;
+  }
+  if (tid < kAppendRows) s_pos[tid] = tid < n ? (rotate ? a.position[t0 + tid] : 0) : -1;
+  __syncthreads();
   if (tid < 64) {
-    const int slot = lane < n ? a.slot[t0 + lane] : -1, pos = lane < n ? (rotate ? a.position[t0 + lane] : 0) : -1;
-    const bool there = (unsigned)slot < slots;
-    // rows that begin four of one quad, rows that are in one, the others
-    bool leads = there && (slot & 3) == 0 && lane < kAppendRows - 3;
-#pragma unroll
-    for (int i = 1; i < 4; ++i) leads &= __shfl(slot, lane + i) == slot + i;
-    const unsigned long long lead = __ballot(leads), in = lead | lead << 1 | lead << 2 | lead << 3;
-    const unsigned long long units = lead | (__ballot(there) & ~in);
-    if (lane < kAppendRows) {
-      s_slot[lane] = there ? slot : -1;
-      s_pos[lane] = pos;
-      if (units >> lane & 1) s_unit[__popcll(units & ((1ull << lane) - 1))] = lane << 1 | (int)leads;
+    // whether row r begins four of one quad; whether that and row r + 16 begin the two quads that are stored together
+    auto quad = [&](int r) { return s_slot[r] >= 0 && (s_slot[r] & 3) == 0 && s_slot[r + 1] == s_slot[r] + 1 && s_slot[r + 2] == s_slot[r] + 2 && s_slot[r + 3] == s_slot[r] + 3; };
+    auto pair = [&](int r) { return quad(r) && (s_slot[r] & 16) == 0 && s_slot[r + 16] == s_slot[r] + 16 && quad(r + 16); };
+    int kind = 0;                                               // 3: two quads, 2: one, 1: a single row, 0: stored with another
+    if (lane < n && s_slot[lane] >= 0) {
+      const int first = lane - (s_slot[lane] & 3);
+      if (first < -BEHIND || !quad(first)) kind = 1;
+      else if (first == lane) kind = pair(lane) ? 3 : (s_slot[lane] & 16) && lane >= 16 - BEHIND && pair(lane - 16) ? 0 : 2;
     }
-    if (lane == 0) s_units = __popcll(units);
+    const unsigned long long units = __ballot(kind > 0);
+    if (kind > 0) s_unit[__popcll(units & ((1ull << lane) - 1))] = lane << 2 | kind;
+    int end = kind == 3 ? lane + 20 : kind == 2 ? lane + 4 : lane + 1;   // rows that the units read
+    if (kind == 0) end = 0;
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) end = max(end, __shfl_xor(end, off));
+    if (lane == 0) {
+      s_units = __popcll(units);
+      s_end = end;
+    }
   }
   __syncthreads();
-  if (rotate && h0 < nq + nk) {
+  if (rotate && (q1 > q0 || (k1 > k0 && only < 2))) {
     const int i = tid % (HD / 2);
     const double turn = exp2(-(2.0 * i / HD) * log2_theta) * 0.15915494309189533577;   // of a position, in whole turns
-    for (int r = tid / (HD / 2); r < n; r += 256 / (HD / 2)) s_cs[r][i] = cos_sin((double)s_pos[r] * turn);
+    for (int r = tid / (HD / 2); r < n; r += 256 / (HD / 2)) lds.cs[r][i] = cos_sin((double)s_pos[r] * turn);
     __syncthreads();
   }
   const size_t head_elems = (size_t)c.page_size * HD;
   const int ps_shift = __builtin_ctz(c.page_size);
   typedef typename Elem<T>::x8 x8;
   constexpr int PAIRS = HD / 16;                                // units of 8 pairs
-  for (int i = tid; i < (min(h1, nq + nk) - h0) * kAppendRows * PAIRS; i += 256) {
-    const int e = i % PAIRS * 8, r = i / PAIRS % kAppendRows, h = h0 + i / (PAIRS * kAppendRows);
-    const bool is_q = h < nq;
-    const int slot = s_slot[r];
-    if (r >= n || (is_q ? s_pos[r] < 0 : slot < 0)) continue;
-    const T* src = is_q ? static_cast<const T*>(a.q) + (size_t)(t0 + r) * a.q_stride + h * HD + e
-                        : static_cast<const T*>(a.k) + (size_t)(t0 + r) * a.k_stride + (h - nq) * HD + e;
-    x8 lo = *reinterpret_cast<const x8*>(src), hi = *reinterpret_cast<const x8*>(src + HD / 2);
-    if (rotate) {
+  auto turn = [&](x8& lo, x8& hi, int r, int e) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float2 v = rope_rotate(Elem<T>::up(lo[k]), Elem<T>::up(hi[k]), s_cs[r][e + k]);
-        lo[k] = Elem<T>::down(v.x);
-        hi[k] = Elem<T>::down(v.y);
-      }
+    for (int k = 0; k < 8; ++k) {
+      const float2 v = rope_rotate(Elem<T>::up(lo[k]), Elem<T>::up(hi[k]), lds.cs[r][e + k]);
+      lo[k] = Elem<T>::down(v.x);
+      hi[k] = Elem<T>::down(v.y);
     }
-    if (is_q) {
-      T* dst = static_cast<T*>(a.q_out) + (size_t)(t0 + r) * a.q_out_stride + h * HD + e;
-      *reinterpret_cast<x8*>(dst) = lo;
-      *reinterpret_cast<x8*>(dst + HD / 2) = hi;
-    } else {
-      T* dst = static_cast<T*>(c.k) + ((size_t)(slot >> ps_shift) * nk + (h - nq)) * head_elems;
-      const int p = slot & (c.page_size - 1);
-      *reinterpret_cast<x8*>(dst + k_cache_off(p, e, HD)) = lo;
-      *reinterpret_cast<x8*>(dst + k_cache_off(p, e + HD / 2, HD)) = hi;
-    }
+  };
+  const int nqh = q1 - q0, nkh = only < 2 ? k1 - k0 : 0;
+  for (int i = tid; i < nqh * n * PAIRS; i += 256) {            // (a row's heads one behind the other in memory)
+    const int e = i % PAIRS * 8, h = q0 + i / PAIRS % nqh, r = i / (PAIRS * nqh);
+    if (s_pos[r] < 0) continue;
+    const T* src = static_cast<const T*>(a.q) + (size_t)(t0 + r) * a.q_stride + h * HD + e;
+    x8 lo = ld_once_as<x8>(src), hi = ld_once_as<x8>(src + HD / 2);
+    if (rotate) turn(lo, hi, r, e);
+    T* dst = static_cast<T*>(a.q_out) + (size_t)(t0 + r) * a.q_out_stride + h * HD + e;
+    *reinterpret_cast<x8*>(dst) = lo;
+    *reinterpret_cast<x8*>(dst + HD / 2) = hi;
   }
-  const int v0 = max(h0 - nq - nk, 0), v1 = h1 - nq - nk, units = s_units;
-  for (int i = tid; i < (v1 - v0) * units * (HD / 8); i += 256) {
-    const int e = i % (HD / 8) * 8, u = i / (HD / 8), h = v0 + u / units, r = s_unit[u % units] >> 1;
-    const int slot = s_slot[r], p = slot & (c.page_size - 1);
-    const T* src = static_cast<const T*>(a.v) + (size_t)(t0 + r) * a.v_stride + h * HD + e;
-    T* dst = static_cast<T*>(c.v) + ((size_t)(slot >> ps_shift) * nk + h) * head_elems + v_cache_off(p, e, HD);
-    if (s_unit[u % units] & 1) {
-      x8 v[4];
+  for (int i = tid; i < nkh * kAppendRows * PAIRS; i += 256) {  // (rows that are neighbours in a tile one behind the other)
+    const int e = i % PAIRS * 8, r = i / PAIRS % kAppendRows, h = k0 + i / (PAIRS * kAppendRows), slot = s_slot[r];
+    if (r >= n || slot < 0) continue;
+    const T* src = static_cast<const T*>(a.k) + (size_t)(t0 + r) * a.k_stride + h * HD + e;
+    x8 lo = ld_once_as<x8>(src), hi = ld_once_as<x8>(src + HD / 2);
+    if (rotate) turn(lo, hi, r, e);
+    T* dst = static_cast<T*>(c.k) + ((size_t)(slot >> ps_shift) * nk + h) * head_elems;
+    const int p = slot & (c.page_size - 1);
+    *reinterpret_cast<x8*>(dst + k_cache_off(p, e, HD)) = lo;
+    *reinterpret_cast<x8*>(dst + k_cache_off(p, e + HD / 2, HD)) = hi;
+  }
+  const int units = only == 1 ? 0 : s_units, staged = s_end;
+  if (units == 0) return;
+  for (int h = k0; h < k1; ++h) {
+    __syncthreads();
+    for (int i = tid; i < staged * (HD / 8); i += 256) {
+      const int r = i / (HD / 8), e = i % (HD / 8) * 8;
+      *reinterpret_cast<x8*>(&lds.v[r][e]) = ld_once_as<x8>(static_cast<const T*>(a.v) + (size_t)(t0 + r) * a.v_stride + h * HD + e);
+    }
+    __syncthreads();
+    for (int i = tid; i < units * HD; i += 256) {
+      const int e = i % HD, r = s_unit[i / HD] >> 2, kind = s_unit[i / HD] & 3, slot = s_slot[r];
+      T* dst = static_cast<T*>(c.v) + ((size_t)(slot >> ps_shift) * nk + h) * head_elems + v_cache_off(slot & (c.page_size - 1), e, HD);
+      if (kind == 1) {
+        *dst = lds.v[r][e];
+      } else {
+        T v[8];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const x8*>(src + k * a.v_stride);
+        for (int k = 0; k < 4; ++k) v[k] = lds.v[r + k][e];
+        if (kind == 2) {
+          *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(v);
+        } else {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        T q[4] = {v[0][k], v[1][k], v[2][k], v[3][k]};
-        *reinterpret_cast<uint2*>(dst + k * 8) = *reinterpret_cast<const uint2*>(q);
+          for (int k = 0; k < 4; ++k) v[4 + k] = lds.v[r + 16 + k][e];
+          *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(v);
+        }
       }
-    } else {
-      const x8 v = *reinterpret_cast<const x8*>(src);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) dst[k * 8] = v[k];
     }
   }
 }
@@ -459,7 +497,6 @@ __device__ __forceinline__ void store_out(const stairs_paged_cache& c, const sta
 }
 __device__ __forceinline__ float weight_of(float m, float all) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - all); }
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // 16 bytes past the caches that XCDs do not share (what ld_dev and st_dev do for 4 and 8)
 __device__ __forceinline__ float4 ld_dev4(const float* base, int offset) {
   const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0, 0xFFFFFFFFu, 0x00027000);
@@ -580,10 +617,6 @@ __device__ __forceinline__ void join_waves(const stairs_paged_cache& c, const st
 // wave), no LDS, and are joined at the end.  Values are requested before the scores they wait for, the next block's keys as
 // soon as this block's are used.
 constexpr int kRowUnit = 32 * 4;
-__device__ __forceinline__ uint4 ld_once(const void* p) {        // (streaming hint: 3 x 32 heads of up to 59999 keys 384 -> 366 us)
-  const u32x4 v = __builtin_nontemporal_load(static_cast<const u32x4*>(p));
-  return make_uint4(v[0], v[1], v[2], v[3]);
-}
 template <int HD, int CT>
 struct RowsLds {
   float o[4][16 * CT][HD + 4], m[4][16 * CT], l[4][16 * CT];
@@ -658,7 +691,7 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
   };
   auto load_keys = [&](size_t at) {
 #pragma unroll
-    for (int i = 0; i < 2 * KK; ++i) kf[i] = ld_once(K + at + (i * 64 + lane) * 8);
+    for (int i = 0; i < 2 * KK; ++i) kf[i] = ld_once_as<uint4>(K + at + (i * 64 + lane) * 8);
   };
   if (w.u0 < u1) fetch_pages(w.u0);
   int u = next_block(w.u0);
@@ -669,7 +702,7 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
   }
   while (u < u1) {
 #pragma unroll
-    for (int i = 0; i < ET; ++i) vf[i] = ld_once(V + at + (i * 64 + lane) * 8);
+    for (int i = 0; i < ET; ++i) vf[i] = ld_once_as<uint4>(V + at + (i * 64 + lane) * 8);
     f32x4 s[CT][2];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
@@ -1109,12 +1142,11 @@ extern "C" int stairs_paged_append(const stairs_paged_cache* c, const stairs_pag
   if (const int rc = check_stream(st)) return rc;
   stairs_paged_rows r = *a;
   if (r.rope_theta == 0.f && r.q == r.q_out) r.n_heads = 0;       // nothing happens to q
-  const int heads = r.n_heads + 2 * c->n_kv_heads, tiles = (r.rows + kAppendRows - 1) / kAppendRows;
+  const int heads = std::max(r.n_heads, c->n_kv_heads), tiles = (r.rows + kAppendRows - 1) / kAppendRows;
   const int groups = std::max(1, std::min((4 * kCus + tiles - 1) / tiles, heads));
-  const int per = (heads + groups - 1) / groups;
   const double log2_theta = r.rope_theta > 0.f ? std::log2((double)r.rope_theta) : 0.0;
   by_type(c, [&](auto type, auto hd) {
-    hipLaunchKernelGGL((k_paged_append<decltype(type), decltype(hd)::value>), dim3(tiles, (heads + per - 1) / per), dim3(256), 0, st, *c, r, log2_theta, per);
+    hipLaunchKernelGGL((k_paged_append<decltype(type), decltype(hd)::value>), dim3(tiles, groups, tiles * groups < 2 * kCus ? 3 : 1), dim3(256), 0, st, *c, r, log2_theta);
   });
   return launched();
 }

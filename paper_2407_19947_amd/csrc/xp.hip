@@ -142,53 +142,158 @@ template <> struct Elem<_Float16> {
   static __device__ __forceinline__ _Float16 down(float v) { return (_Float16)v; }
 };
 
-// a block per row: q and k rotated, k and v stored
+// sine and cosine of `turns` whole turns: the nearest quarter turn, and the series for what is left, |x| <= pi / 4 (the next terms are
+// below 2^-28)
+__device__ __forceinline__ float2 cos_sin(double turns) {
+  const double t = 4.0 * (turns - rint(turns)), quarter = rint(t), x = (t - quarter) * 1.57079632679489661923, y = x * x;
+  double s = 1.0 / 362880;
+  s = fma(s, y, -1.0 / 5040);
+  s = fma(s, y, 1.0 / 120);
+  s = fma(s, y, -1.0 / 6);
+  s = fma(s * y, x, x);
+  double c = -1.0 / 3628800;
+  c = fma(c, y, 1.0 / 40320);
+  c = fma(c, y, -1.0 / 720);
+  c = fma(c, y, 1.0 / 24);
+  c = fma(c, y, -0.5);
+  c = fma(c, y, 1.0);
+  const int q = (int)quarter;
+  const float fc = (float)c, fs = (float)s;
+  const float2 r = q & 1 ? make_float2(-fs, fc) : make_float2(fc, fs);      // (a quarter turn on: (cos, sin) -> (-sin, cos))
+  return q & 2 ? make_float2(-r.x, -r.y) : r;
+}
+
+// Bound by memory, with few rows by latency.  A work-group has 32 rows and some of the n_heads + 2 n_kv_heads heads (so many
+// groups of them that there are work for all CUs); the rows' rotations are formed once for all its heads.  q and k: a thread takes 8
+// pairs of a row, 16 bytes of either half; in a key tile the same 8 dims of 8 rows are one line.  v: a head's rows go through LDS;
+// the eight positions of a value tile that are 16 adjacent bytes a dim (two quads, 16 apart) are stored together where they are rows
+// of this call, so that a wave's store is a whole tile row; rows that have not all of them as quads of 8 bytes or single
+// values.  (Quads transposed in registers, 8 bytes here and there: 8190 rows of 48 heads 75 us, 40 of them for the values.)
+constexpr int kAppendRows = X_R;
+template <typename X> __device__ __forceinline__ X ldn(const void* p) {
+  typedef unsigned u4 __attribute__((ext_vector_type(4)));
+  if (X_NT & 1) return __builtin_bit_cast(X, __builtin_nontemporal_load(static_cast<const u4*>(p)));
+  return *static_cast<const X*>(p);
+}
+template <typename X> __device__ __forceinline__ void stn(void* p, X v) {
+  typedef unsigned u4 __attribute__((ext_vector_type(4)));
+  if (X_NT & 2) __builtin_nontemporal_store(__builtin_bit_cast(u4, v), static_cast<u4*>(p));
+  else *static_cast<X*>(p) = v;
+}
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stairs_paged_rows a) {
-  __shared__ float2 s_cs[HD / 2];
-  const int t = blockIdx.x;
-  const int slot = a.slot[t];
+__global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stairs_paged_rows a, double log2_theta) {
+  constexpr int AHEAD = 19, BEHIND = 16;                        // rows around these that decide how theirs are stored
+  __shared__ union {
+    float2 cs[kAppendRows][HD / 2];
+    T v[kAppendRows + AHEAD][HD];
+  } lds;
+  __shared__ int s_slots[BEHIND + kAppendRows + AHEAD], s_pos[kAppendRows], s_unit[kAppendRows], s_units, s_end;
+  const int* const s_slot = s_slots + BEHIND;
+  const int t0 = blockIdx.x * kAppendRows, n = min(kAppendRows, a.rows - t0);
+  // its heads: a run of q's, one of k's and v's
+  const int nq = a.n_heads, nk = c.n_kv_heads, y = blockIdx.y, groups = gridDim.y;
+  const int q0 = nq * y / groups, q1 = nq * (y + 1) / groups, k0 = nk * y / groups, k1 = nk * (y + 1) / groups;
   const bool rotate = a.rope_theta > 0.f;
-  const int pos = rotate ? a.position[t] : 0;
-  if (rotate && threadIdx.x < HD / 2) {
-    const double angle = (double)pos * exp2(-(2.0 * threadIdx.x / HD) * log2((double)a.rope_theta));
-    double s, co;
-    sincos(angle, &s, &co);
-    s_cs[threadIdx.x] = make_float2((float)co, (float)s);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const unsigned slots = (unsigned)c.n_pages * (unsigned)c.page_size;
+  if (tid < BEHIND + kAppendRows + AHEAD) {
+    const int t = t0 - BEHIND + tid, slot = t >= 0 && t < a.rows ? a.slot[t] : -1;
+    s_slots[tid] = (unsigned)slot < slots ? slot : -1;
+  }
+  if (tid < kAppendRows) s_pos[tid] = tid < n ? (rotate ? a.position[t0 + tid] : 0) : -1;
+  __syncthreads();
+  if (tid < 64) {
+    // whether row r begins four of one quad; whether that and row r + 16 begin the two quads that are stored together
+    auto quad = [&](int r) { return s_slot[r] >= 0 && (s_slot[r] & 3) == 0 && s_slot[r + 1] == s_slot[r] + 1 && s_slot[r + 2] == s_slot[r] + 2 && s_slot[r + 3] == s_slot[r] + 3; };
+    auto pair = [&](int r) { return quad(r) && (s_slot[r] & 16) == 0 && s_slot[r + 16] == s_slot[r] + 16 && quad(r + 16); };
+    int kind = 0;                                               // 3: two quads, 2: one, 1: a single row, 0: stored with another
+    if (lane < n && s_slot[lane] >= 0) {
+      const int first = lane - (s_slot[lane] & 3);
+      if (first < -BEHIND || !quad(first)) kind = 1;
+      else if (first == lane) kind = pair(lane) ? 3 : (s_slot[lane] & 16) && lane >= 16 - BEHIND && pair(lane - 16) ? 0 : 2;
+    }
+    const unsigned long long units = __ballot(kind > 0);
+    if (kind > 0) s_unit[__popcll(units & ((1ull << lane) - 1))] = lane << 2 | kind;
+    int end = kind == 3 ? lane + 20 : kind == 2 ? lane + 4 : lane + 1;   // rows that the units read
+    if (kind == 0) end = 0;
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) end = max(end, __shfl_xor(end, off));
+    if (lane == 0) {
+      s_units = __popcll(units);
+      s_end = end;
+    }
   }
   __syncthreads();
-  const bool store = (unsigned)slot < (unsigned)c.n_pages * (unsigned)c.page_size;
-  const int page = store ? slot / c.page_size : 0, p = store ? slot % c.page_size : 0;
+  if (rotate && (q1 > q0 || k1 > k0)) {
+    const int i = tid % (HD / 2);
+    const double turn = exp2(-(2.0 * i / HD) * log2_theta) * 0.15915494309189533577;   // of a position, in whole turns
+    for (int r = tid / (HD / 2); r < n; r += 256 / (HD / 2)) lds.cs[r][i] = cos_sin((double)s_pos[r] * turn);
+    __syncthreads();
+  }
   const size_t head_elems = (size_t)c.page_size * HD;
-  const int nq = a.n_heads, nk = c.n_kv_heads;
-  for (int i = threadIdx.x; i < (nq + nk) * (HD / 2); i += 256) {
-    const int h = i / (HD / 2), e = i % (HD / 2);
-    const bool is_q = h < nq;
-    if (is_q ? pos < 0 : !store) continue;
-    const T* src = is_q ? static_cast<const T*>(a.q) + (size_t)t * a.q_stride + h * HD
-                        : static_cast<const T*>(a.k) + (size_t)t * a.k_stride + (h - nq) * HD;
-    T lo = src[e], hi = src[e + HD / 2];
-    if (rotate) {
-      const float2 r = rope_rotate(Elem<T>::up(lo), Elem<T>::up(hi), s_cs[e]);
-      lo = Elem<T>::down(r.x);
-      hi = Elem<T>::down(r.y);
+  const int ps_shift = __builtin_ctz(c.page_size);
+  typedef typename Elem<T>::x8 x8;
+  constexpr int PAIRS = HD / 16;                                // units of 8 pairs
+  auto turn = [&](x8& lo, x8& hi, int r, int e) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float2 v = rope_rotate(Elem<T>::up(lo[k]), Elem<T>::up(hi[k]), lds.cs[r][e + k]);
+      lo[k] = Elem<T>::down(v.x);
+      hi[k] = Elem<T>::down(v.y);
     }
-    if (is_q) {
-      T* dst = static_cast<T*>(a.q_out) + (size_t)t * a.q_out_stride + h * HD;
-      dst[e] = lo;
-      dst[e + HD / 2] = hi;
-    } else {
-      T* dst = static_cast<T*>(c.k) + ((size_t)page * nk + (h - nq)) * head_elems;
-      dst[k_cache_off(p, e, HD)] = lo;
-      dst[k_cache_off(p, e + HD / 2, HD)] = hi;
+  };
+  const int nqh = q1 - q0, nkh = k1 - k0;
+_Pragma("unroll X_U")
+  for (int i = tid; i < nqh * n * PAIRS; i += 256) {            // (a row's heads one behind the other in memory)
+    const int e = i % PAIRS * 8, h = q0 + i / PAIRS % nqh, r = i / (PAIRS * nqh);
+    if (s_pos[r] < 0) continue;
+    const T* src = static_cast<const T*>(a.q) + (size_t)(t0 + r) * a.q_stride + h * HD + e;
+    x8 lo = ldn<x8>(src), hi = ldn<x8>(src + HD / 2);
+    if (rotate) turn(lo, hi, r, e);
+    T* dst = static_cast<T*>(a.q_out) + (size_t)(t0 + r) * a.q_out_stride + h * HD + e;
+    stn<x8>(dst, lo);
+    stn<x8>(dst + HD / 2, hi);
+  }
+_Pragma("unroll X_U")
+  for (int i = tid; i < nkh * kAppendRows * PAIRS; i += 256) {  // (rows that are neighbours in a tile one behind the other)
+    const int e = i % PAIRS * 8, r = i / PAIRS % kAppendRows, h = k0 + i / (PAIRS * kAppendRows), slot = s_slot[r];
+    if (r >= n || slot < 0) continue;
+    const T* src = static_cast<const T*>(a.k) + (size_t)(t0 + r) * a.k_stride + h * HD + e;
+    x8 lo = ldn<x8>(src), hi = ldn<x8>(src + HD / 2);
+    if (rotate) turn(lo, hi, r, e);
+    T* dst = static_cast<T*>(c.k) + ((size_t)(slot >> ps_shift) * nk + h) * head_elems;
+    const int p = slot & (c.page_size - 1);
+    stn<x8>(dst + k_cache_off(p, e, HD), lo);
+    stn<x8>(dst + k_cache_off(p, e + HD / 2, HD), hi);
+  }
+  if (X_SKIP & 1) return;
+  const int units = s_units, staged = s_end;
+  for (int h = k0; h < k1; ++h) {
+    __syncthreads();
+    for (int i = tid; i < staged * (HD / 8); i += 256) {
+      const int r = i / (HD / 8), e = i % (HD / 8) * 8;
+      *reinterpret_cast<x8*>(&lds.v[r][e]) = *reinterpret_cast<const x8*>(static_cast<const T*>(a.v) + (size_t)(t0 + r) * a.v_stride + h * HD + e);
+    }
+    __syncthreads();
+    for (int i = tid; i < units * HD; i += 256) {
+      const int e = i % HD, r = s_unit[i / HD] >> 2, kind = s_unit[i / HD] & 3, slot = s_slot[r];
+      T* dst = static_cast<T*>(c.v) + ((size_t)(slot >> ps_shift) * nk + h) * head_elems + v_cache_off(slot & (c.page_size - 1), e, HD);
+      if (kind == 1) {
+        *dst = lds.v[r][e];
+      } else {
+        T v[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = lds.v[r + k][e];
+        if (kind == 2) {
+          *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(v);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[4 + k] = lds.v[r + 16 + k][e];
+          *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(v);
+        }
+      }
     }
   }
-  if (store)
-    for (int i = threadIdx.x; i < nk * HD; i += 256) {
-      const int h = i / HD, e = i % HD;
-      T* dst = static_cast<T*>(c.v) + ((size_t)page * nk + h) * head_elems;
-      dst[v_cache_off(p, e, HD)] = static_cast<const T*>(a.v)[(size_t)t * a.v_stride + i];
-    }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -413,7 +518,7 @@ template <typename T, int HD, int COLS>
 __device__ __forceinline__ void join_pieces(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, const Piece& w, float2* s_ml, int* s_last) {
   int* counter = tickets(a, sp) + w.first;
   if (!last_arrival(counter, w.pieces, s_last)) return;
-  constexpr int NT = 256, TB = COLS <= 32 ? 1 : 4, PB = X_PB / TB;
+  constexpr int NT = 256, TB = COLS <= 32 ? 1 : 4, PB = 16 / TB;
   const size_t step = piece_floats<HD>(COLS) * c.n_kv_heads;
   float* base = partials(a, sp) + (size_t)w.first * piece_floats<HD>(COLS);
   const int G = a.n_heads / c.n_kv_heads, col0 = w.group * COLS, cols = min(COLS, w.rows * G - col0);
@@ -982,6 +1087,8 @@ using namespace stairs;
 
 namespace {
 
+constexpr int kCus = 256;
+
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 bool cache_ok(const stairs_paged_cache* c) {
@@ -1044,8 +1151,11 @@ extern "C" int stairs_paged_append(const stairs_paged_cache* c, const stairs_pag
   if (const int rc = check_stream(st)) return rc;
   stairs_paged_rows r = *a;
   if (r.rope_theta == 0.f && r.q == r.q_out) r.n_heads = 0;       // nothing happens to q
+  const int heads = std::max(r.n_heads, c->n_kv_heads), tiles = (r.rows + kAppendRows - 1) / kAppendRows;
+  const int groups = std::max(1, std::min((X_G * kCus + tiles - 1) / tiles, heads));
+  const double log2_theta = r.rope_theta > 0.f ? std::log2((double)r.rope_theta) : 0.0;
   by_type(c, [&](auto type, auto hd) {
-    hipLaunchKernelGGL((k_paged_append<decltype(type), decltype(hd)::value>), dim3(r.rows), dim3(256), 0, st, *c, r);
+    hipLaunchKernelGGL((k_paged_append<decltype(type), decltype(hd)::value>), dim3(tiles, groups), dim3(256), 0, st, *c, r, log2_theta);
   });
   return launched();
 }
@@ -1056,7 +1166,7 @@ namespace {
 // A sequence's columns are its rows times the query heads of a key head.  Up to 32 of them (16 in one tile) go to attend_rows, more to
 // attend_chunk; max_fresh says which of the two a call needs, and with one sequence, or none with more, one kernel
 // takes whatever it finds.
-constexpr int kCus = 256, kFewCols = 32;
+constexpr int kFewCols = 32;
 struct Launch {
   int ct;                      // column tiles of the rows' part, 0: there is none
   bool chunk;
@@ -1079,12 +1189,12 @@ Launch plan_attention(const stairs_paged_cache* c, const stairs_paged_attn* a) {
     l.work_bytes += most_pieces(s.slots) * (int64_t)(sizeof(int) + s.tile_cols * (c->head_dim + 2) * sizeof(float));
   };
   if (l.chunk) {
-    l.chunks = Span{l.ct ? kFewCols + 1 : 1, INT32_MAX, kChunkCols, kChunkUnit, X_C, X_CM, X_CW, 0, 0};
+    l.chunks = Span{l.ct ? kFewCols + 1 : 1, INT32_MAX, kChunkCols, kChunkUnit, 2 * kCus, 8, 400, 0, 0};
     add(l.chunks);
   }
   if (l.ct) {
     // pieces of 4 units and more: shorter ones cost more to join than they save (8000 keys of 8 heads alone: 25 us with 2, 19 with 4)
-    l.rows = Span{1, l.chunk ? kFewCols : INT32_MAX, 16 * l.ct, kRowUnit, l.chunk ? X_R : 2 * kCus, X_RM, 200, 0, 0};
+    l.rows = Span{1, l.chunk ? kFewCols : INT32_MAX, 16 * l.ct, kRowUnit, 2 * kCus, 4, 200, 0, 0};
     add(l.rows);
   }
   return l;
