@@ -499,7 +499,8 @@ __device__ Cut find_cut(const X& x, int V, const Row& r, float mine, int top_k, 
       sort_list(n, s);
       return cut_list<B>(n, way < kWeight ? top_k : n, way == kWeak ? 1.f : top_p, way == kOneBin ? before : 0, way < kWeight ? 0 : target, r, c, s);
     }
-    if (way == kWeak && c.in_all) return c;
+    // (all that min_p keeps is in s.all, and top_p's border, where there is one, behind it)
+    if (c.in_all && (way == kWeak || (way == kWeight && weak < bin))) return c;
     cut_k = way == kCount;
     way = way == kThreadsLargest ? kCount : way == kWeight ? kOneBin : kNone;
   }

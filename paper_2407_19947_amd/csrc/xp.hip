@@ -163,6 +163,13 @@ __device__ __forceinline__ float2 cos_sin(double turns) {
   return q & 2 ? make_float2(-r.x, -r.y) : r;
 }
 
+// (streaming hint, for what is read once: 8190 rows of 16 + 16 heads of q and k 36.7 -> 30.5 us; on the stores it costs 9)
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <typename X>
+__device__ __forceinline__ X ld_once_as(const void* p) {
+  return __builtin_bit_cast(X, __builtin_nontemporal_load(static_cast<const u32x4*>(p)));
+}
+
 // Bound by memory, with few rows by latency.  A work-group has 32 rows and some of the n_heads + 2 n_kv_heads heads (so many
 // groups of them that there are work for all CUs); the rows' rotations are formed once for all its heads.  q and k: a thread takes 8
 // pairs of a row, 16 bytes of either half; in a key tile the same 8 dims of 8 rows are one line.  v: a head's rows go through LDS;
@@ -170,16 +177,6 @@ __device__ __forceinline__ float2 cos_sin(double turns) {
 // of this call, so that a wave's store is a whole tile row; rows that have not all of them as quads of 8 bytes or single
 // values.  (Quads transposed in registers, 8 bytes here and there: 8190 rows of 48 heads 75 us, 40 of them for the values.)
 constexpr int kAppendRows = X_R;
-template <typename X> __device__ __forceinline__ X ldn(const void* p) {
-  typedef unsigned u4 __attribute__((ext_vector_type(4)));
-  if (X_NT & 1) return __builtin_bit_cast(X, __builtin_nontemporal_load(static_cast<const u4*>(p)));
-  return *static_cast<const X*>(p);
-}
-template <typename X> __device__ __forceinline__ void stn(void* p, X v) {
-  typedef unsigned u4 __attribute__((ext_vector_type(4)));
-  if (X_NT & 2) __builtin_nontemporal_store(__builtin_bit_cast(u4, v), static_cast<u4*>(p));
-  else *static_cast<X*>(p) = v;
-}
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stairs_paged_rows a, double log2_theta) {
   constexpr int AHEAD = 19, BEHIND = 16;                        // rows around these that decide how theirs are stored
@@ -192,7 +189,8 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
   const int t0 = blockIdx.x * kAppendRows, n = min(kAppendRows, a.rows - t0);
   // its heads: a run of q's, one of k's and v's
   const int nq = a.n_heads, nk = c.n_kv_heads, y = blockIdx.y, groups = gridDim.y;
-  const int q0 = nq * y / groups, q1 = nq * (y + 1) / groups, k0 = nk * y / groups, k1 = nk * (y + 1) / groups;
+  const int only = gridDim.z == 1 ? -1 : (int)blockIdx.z;      // (few rows: q, k and v each a work-group of their own)
+  const int q0 = nq * y / groups, q1 = only > 0 ? q0 : nq * (y + 1) / groups, k0 = nk * y / groups, k1 = only == 0 ? k0 : nk * (y + 1) / groups;
   const bool rotate = a.rope_theta > 0.f;
   const int tid = threadIdx.x, lane = tid & 63;
   const unsigned slots = (unsigned)c.n_pages * (unsigned)c.page_size;
@@ -224,7 +222,7 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
     }
   }
   __syncthreads();
-  if (rotate && (q1 > q0 || k1 > k0)) {
+  if (rotate && (q1 > q0 || (k1 > k0 && only < 2))) {
     const int i = tid % (HD / 2);
     const double turn = exp2(-(2.0 * i / HD) * log2_theta) * 0.15915494309189533577;   // of a position, in whole turns
     for (int r = tid / (HD / 2); r < n; r += 256 / (HD / 2)) lds.cs[r][i] = cos_sin((double)s_pos[r] * turn);
@@ -242,37 +240,35 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
       hi[k] = Elem<T>::down(v.y);
     }
   };
-  const int nqh = q1 - q0, nkh = k1 - k0;
-_Pragma("unroll X_U")
+  const int nqh = q1 - q0, nkh = only < 2 ? k1 - k0 : 0;
   for (int i = tid; i < nqh * n * PAIRS; i += 256) {            // (a row's heads one behind the other in memory)
     const int e = i % PAIRS * 8, h = q0 + i / PAIRS % nqh, r = i / (PAIRS * nqh);
     if (s_pos[r] < 0) continue;
     const T* src = static_cast<const T*>(a.q) + (size_t)(t0 + r) * a.q_stride + h * HD + e;
-    x8 lo = ldn<x8>(src), hi = ldn<x8>(src + HD / 2);
+    x8 lo = ld_once_as<x8>(src), hi = ld_once_as<x8>(src + HD / 2);
     if (rotate) turn(lo, hi, r, e);
     T* dst = static_cast<T*>(a.q_out) + (size_t)(t0 + r) * a.q_out_stride + h * HD + e;
-    stn<x8>(dst, lo);
-    stn<x8>(dst + HD / 2, hi);
+    *reinterpret_cast<x8*>(dst) = lo;
+    *reinterpret_cast<x8*>(dst + HD / 2) = hi;
   }
-_Pragma("unroll X_U")
   for (int i = tid; i < nkh * kAppendRows * PAIRS; i += 256) {  // (rows that are neighbours in a tile one behind the other)
     const int e = i % PAIRS * 8, r = i / PAIRS % kAppendRows, h = k0 + i / (PAIRS * kAppendRows), slot = s_slot[r];
     if (r >= n || slot < 0) continue;
     const T* src = static_cast<const T*>(a.k) + (size_t)(t0 + r) * a.k_stride + h * HD + e;
-    x8 lo = ldn<x8>(src), hi = ldn<x8>(src + HD / 2);
+    x8 lo = ld_once_as<x8>(src), hi = ld_once_as<x8>(src + HD / 2);
     if (rotate) turn(lo, hi, r, e);
     T* dst = static_cast<T*>(c.k) + ((size_t)(slot >> ps_shift) * nk + h) * head_elems;
     const int p = slot & (c.page_size - 1);
-    stn<x8>(dst + k_cache_off(p, e, HD), lo);
-    stn<x8>(dst + k_cache_off(p, e + HD / 2, HD), hi);
+    *reinterpret_cast<x8*>(dst + k_cache_off(p, e, HD)) = lo;
+    *reinterpret_cast<x8*>(dst + k_cache_off(p, e + HD / 2, HD)) = hi;
   }
-  if (X_SKIP & 1) return;
-  const int units = s_units, staged = s_end;
+  const int units = only == 1 ? 0 : s_units, staged = s_end;
+  if (units == 0) return;
   for (int h = k0; h < k1; ++h) {
     __syncthreads();
     for (int i = tid; i < staged * (HD / 8); i += 256) {
       const int r = i / (HD / 8), e = i % (HD / 8) * 8;
-      *reinterpret_cast<x8*>(&lds.v[r][e]) = *reinterpret_cast<const x8*>(static_cast<const T*>(a.v) + (size_t)(t0 + r) * a.v_stride + h * HD + e);
+      *reinterpret_cast<x8*>(&lds.v[r][e]) = ld_once_as<x8>(static_cast<const T*>(a.v) + (size_t)(t0 + r) * a.v_stride + h * HD + e);
     }
     __syncthreads();
     for (int i = tid; i < units * HD; i += 256) {
@@ -501,7 +497,6 @@ __device__ __forceinline__ void store_out(const stairs_paged_cache& c, const sta
 }
 __device__ __forceinline__ float weight_of(float m, float all) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - all); }
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // 16 bytes past the caches that XCDs do not share (what ld_dev and st_dev do for 4 and 8)
 __device__ __forceinline__ float4 ld_dev4(const float* base, int offset) {
   const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0, 0xFFFFFFFFu, 0x00027000);
@@ -622,10 +617,6 @@ __device__ __forceinline__ void join_waves(const stairs_paged_cache& c, const st
 // wave), no LDS, and are joined at the end.  Values are requested before the scores they wait for, the next block's keys as
 // soon as this block's are used.
 constexpr int kRowUnit = 32 * 4;
-__device__ __forceinline__ uint4 ld_once(const void* p) {        // (streaming hint: 3 x 32 heads of up to 59999 keys 384 -> 366 us)
-  const u32x4 v = __builtin_nontemporal_load(static_cast<const u32x4*>(p));
-  return make_uint4(v[0], v[1], v[2], v[3]);
-}
 template <int HD, int CT>
 struct RowsLds {
   float o[4][16 * CT][HD + 4], m[4][16 * CT], l[4][16 * CT];
@@ -700,7 +691,7 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
   };
   auto load_keys = [&](size_t at) {
 #pragma unroll
-    for (int i = 0; i < 2 * KK; ++i) kf[i] = ld_once(K + at + (i * 64 + lane) * 8);
+    for (int i = 0; i < 2 * KK; ++i) kf[i] = ld_once_as<uint4>(K + at + (i * 64 + lane) * 8);
   };
   if (w.u0 < u1) fetch_pages(w.u0);
   int u = next_block(w.u0);
@@ -711,7 +702,7 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
   }
   while (u < u1) {
 #pragma unroll
-    for (int i = 0; i < ET; ++i) vf[i] = ld_once(V + at + (i * 64 + lane) * 8);
+    for (int i = 0; i < ET; ++i) vf[i] = ld_once_as<uint4>(V + at + (i * 64 + lane) * 8);
     f32x4 s[CT][2];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
@@ -1155,7 +1146,7 @@ extern "C" int stairs_paged_append(const stairs_paged_cache* c, const stairs_pag
   const int groups = std::max(1, std::min((X_G * kCus + tiles - 1) / tiles, heads));
   const double log2_theta = r.rope_theta > 0.f ? std::log2((double)r.rope_theta) : 0.0;
   by_type(c, [&](auto type, auto hd) {
-    hipLaunchKernelGGL((k_paged_append<decltype(type), decltype(hd)::value>), dim3(tiles, groups), dim3(256), 0, st, *c, r, log2_theta);
+    hipLaunchKernelGGL((k_paged_append<decltype(type), decltype(hd)::value>), dim3(tiles, groups, tiles * groups < 2 * kCus ? 3 : 1), dim3(256), 0, st, *c, r, log2_theta);
   });
   return launched();
 }

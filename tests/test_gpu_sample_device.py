@@ -53,6 +53,20 @@ def test_large_vocabularies(V):
             check(x, dtype, rng.random(3).astype(np.float32), **rules)
 
 
+@pytest.mark.parametrize("V,dtype", [(3000, "fp32"), (30000, "bf16"), (32000, "fp32"), (60000, "fp32"), (100003, "fp32"), (100003, "bf16")])
+@pytest.mark.parametrize("spread", [0.01, 0.5, 2.0])
+def test_flat_rows_that_keep_thousands_of_tokens(V, dtype, spread):
+    """More tokens than are listed, between the borders of the rules in every order: min_p in front of top_p, top_p in front of
+    min_p, top_k in front of either."""
+    import torch
+    rng = np.random.default_rng([V, int(100 * spread)])
+    x = torch.from_numpy(rng.standard_normal((3, V)).astype(np.float32)) * spread
+    for rules in (dict(min_p=0.1), dict(min_p=0.01), dict(top_p=0.95, min_p=0.3), dict(top_p=0.99, min_p=0.02), dict(top_p=0.3, min_p=0.001), dict(top_p=0.7),
+                  dict(top_k=1500), dict(top_k=V // 2, top_p=0.9), dict(top_k=V // 3, min_p=0.2), dict(top_k=1100, top_p=0.8, min_p=0.1),
+                  dict(top_k=1000, top_p=0.999), dict(top_p=0.999, temperature=3.0), dict(min_p=0.5, temperature=0.3)):
+        check(x, dtype, rng.random(3).astype(np.float32), **rules)
+
+
 def test_rows_with_rules_of_their_own():
     rng = np.random.default_rng(1)
     n, V = 200, 5000
