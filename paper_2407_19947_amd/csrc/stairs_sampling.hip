@@ -66,10 +66,10 @@ __device__ __forceinline__ double exponent(float x, const Row& r) {
 }
 constexpr double kNoWeight = -745.13;              // below it a weight is 0 in double
 
-// exp(d) for d <= 0 in multiples of 2^-44.  d = n ln 2 + r with |r| <= ln 2 / 2; exp(r / 4) by its series up to the 8th power
+// exp(d) for least <= d <= 0, or of `least`, in multiples of 2^-bits, where that is below 2^51.  d = n ln 2 + r with |r| <= ln 2 / 2; exp(r / 4) by its series up to the 8th power
 // (the next term is 8e-16), squared twice; the number and the place of its last bit come from one multiply-add.
-__device__ __forceinline__ u64 fixed_exp(double d) {
-  d = fmax(d, -64.0);                              // (weights below 2^-45 are 0 here; NaN is the least too)
+__device__ __forceinline__ u64 fixed_exp(double d, int bits = 44, double least = -64.0) {
+  d = fmax(d, least);                              // (weights below 2^-45 are 0 in multiples of 2^-44; NaN is the least too)
   const double big = 6755399441055744.0;           // 1.5 * 2^52: adding it rounds to a whole number
   const double nb = fma(d, 1.4426950408889634074, big), n = nb - big;
   const double x = fma(n, -0.17328679513998632735, 0.25 * d);   // ln 2 / 4
@@ -85,7 +85,7 @@ __device__ __forceinline__ u64 fixed_exp(double d) {
   p *= p;
   p *= p;
   const int e = (int)(uint32_t)__double_as_longlong(nb);        // n, in the low bits
-  const double scale = __longlong_as_double((long long)(1023 + 44 + e) << 52);
+  const double scale = __longlong_as_double((long long)(1023 + bits + e) << 52);
   return (u64)__double_as_longlong(fma(p, scale, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;   // + 2^52
 }
 __device__ __forceinline__ u64 weight(float x, const Row& r) { return fixed_exp(exponent(x, r)); }
@@ -692,7 +692,36 @@ __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
         return is_kept<T>(b, v, c, r) ? weight(b, r) : 0ull;
       }, V, target_of(z), s, true);
     }
-    lp = (float)(exponent(x[token], r) - log((double)z * (1.0 / kOne)));
+    double log_z = log((double)z * (1.0 / kOne));
+    if ((z & ((1ull << 44) - 1)) < 1ull << 34) {
+      // Perhaps little beside the largest logits (2^-10 of them): then that is summed again in multiples of 2^-50 of itself, or the
+      // logarithm would be the roundings' sum.
+      constexpr int B = Logit<T>::kBits;
+      auto each_kept = [&](auto f) {
+        if (c.listed > 0) {
+          for (int i = threadIdx.x; i < c.listed; i += L::kThreads) f(value_of_key((uint32_t)(s.list.order[i] >> 32), B));
+        } else if (L::kAll > 0 && c.in_all) {
+          each_listed<B>(c.in_all, s, [&](int v, float b) { if (is_kept<T>(b, v, c, r)) f(b); });
+        } else {
+          each(x, V, [&](int v, float b) { if (is_kept<T>(b, v, c, r)) f(b); });
+        }
+      };
+      u64 tops = 0;
+      each_kept([&](float b) { tops += b == r.max; });
+      tops = block_sum(tops, s);
+      const u64 little = z - tops * (1ull << 44);
+      if (little < 1ull << 34) {
+        const int bits = 94 - (little ? 64 - __builtin_clzll(little) : 0);
+        u64 rest = 0;
+        each_kept([&](float b) {
+          const double d = exponent(b, r);
+          if (b != r.max && d >= -100.0) rest += fixed_exp(d, bits, -100.0);
+        });
+        rest = block_sum(rest, s);
+        log_z = log((double)tops) + log1p(ldexp((double)rest, -bits) / (double)tops);
+      }
+    }
+    lp = (float)(exponent(x[token], r) - log_z);
   }
   if (threadIdx.x == 0) {
     a.token[row] = token;

@@ -137,6 +137,25 @@ def test_a_row_does_not_depend_on_the_others_and_outputs_are_optional():
     assert np.array_equal(only, token) and none is None and nothing is None
 
 
+@pytest.mark.parametrize("V,rules", [(700, dict()), (700, dict(top_k=50)), (40000, dict()), (40000, dict(top_p=1.0, min_p=1e-30))])
+def test_logprob_of_a_token_that_is_nearly_certain(V, rules):
+    """What is beside one logit, or three equal ones, is 1e-6 .. 1e-15 of it: the logarithm to a float's half step all the same (sums of
+    equal logits add equal roundings: 900 of them here)."""
+    rng = np.random.default_rng(V)
+    import torch
+    for gap in (14.0, 20.0, 27.0, 34.0):
+        for tops in (1, 3):
+            x = torch.from_numpy(np.minimum(rng.standard_normal((1, V)).astype(np.float32), 2.0))
+            x[0, [5, 17, 300][:tops]] = gap + 3
+            token, lp, _, xs = ou.sample_call(x, "fp32", np.float32(0.5), **rules)
+            keep, w = ou.keep_reference(xs[0], 1.0, rules.get("top_k", 0), rules.get("top_p", 1.0), rules.get("min_p", 0.0))
+            rest = float(np.sum(np.sort(w[keep & (w < 1)])))
+            want = -np.log(tops) - np.log1p(rest / tops)
+            assert token[0] in (5, 17, 300)
+            # half a step of float, and V roundings: to 2^-51 of what is beside the largest, or to 2^-45 where that is more than 2^-10
+            assert abs(lp[0] - want) <= 2.0 ** -24 * abs(want) + V * (2.0 ** -51 * 2 * rest if rest < 2.0 ** -10 else 2.0 ** -45), (gap, tops, lp[0], want)
+
+
 def test_drawn_tokens_follow_the_probabilities():
     """Evenly spaced numbers: each token's count is its share to within one, by the definition."""
     import torch
