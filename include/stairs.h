@@ -372,12 +372,12 @@ int stairs_paged_append(const stairs_paged_cache *cache, const stairs_paged_rows
  * probabilities rounded to the cache's type for the product with v; scale <= 0: 1 / sqrt(head_dim).  Positions whose page
  * number lies outside the pool are not seen, and a row that sees nothing gives zeros.  Masked positions may hold anything,
  * infinities and NaN included.  Rows of out that no sequence has are left as they were.  rows: rows of the q and out buffers;
- * max_fresh: most rows any sequence has (only the choice of kernels depends on it).  The result does not depend on which
- * sequences share a call only up to the last bits: the split of a long sequence follows the whole batch.
- * workspace: stairs_paged_attention_workspace bytes (0 <= result; depends on n_heads, head_dim, n_kv_heads and max_fresh alone),
- * 16-byte aligned, all zeros before its first use, left fit for the next call; calls that may overlap need one each.
+ * max_fresh: most rows any sequence has (only the choice of kernels depends on it).  Which sequences share a
+ * call shows in the last bits of their results alone (a long sequence is split by the whole batch); the same call gives the same bits.
+ * workspace: stairs_paged_attention_workspace bytes (at most about 90 MB; not fewer for more sequences or rows), 16-byte aligned, all
+ * zeros before its first use, left fit for the next call, of other sizes and types too; calls that may overlap need one each.
  * 0 <= n_seqs <= STAIRS_PAGED_MAX_SEQS; row_start ascending; n_heads a multiple of n_kv_heads; rows * n_heads / n_kv_heads at most
- * 2^24; pointers 16-byte aligned, strides multiples of 8. */
+ * 2^24, work-groups (a tile of 16, 32 or 128 such columns and a key head) fewer than 2^24; pointers 16-byte aligned, strides multiples of 8. */
 typedef struct {
   int32_t n_seqs, max_blocks, rows, n_heads, max_fresh;
   const void *q;                   /* [rows][n_heads][head_dim] */
@@ -405,7 +405,7 @@ int stairs_paged_attention(const stairs_paged_cache *cache, const stairs_paged_a
  * rule off; uniform may be NULL only if temperature is 0 everywhere, else 0 is taken.  A NaN logit is never drawn; if a logit is +INFINITY,
  * those alone have weight; a token whose weight is 0 in double is not kept.  A row of -INFINITY and NaN alone gives token
  * -1, logprob -INFINITY, kept 0.  logprob (natural logarithm of the drawn token's share of the kept weight) and kept (tokens
- * kept) may be NULL.  1 <= vocab <= STAIRS_SAMPLE_MAX_VOCAB, ld >= vocab; logits aligned to their type.
+ * kept) may be NULL.  0 <= rows <= 2^21, 1 <= vocab <= STAIRS_SAMPLE_MAX_VOCAB, ld >= vocab; logits aligned to their type.
  * workspace: stairs_sample_workspace bytes (may be 0), on the terms of stairs_paged_attention's. */
 #define STAIRS_SAMPLE_MAX_VOCAB 524288
 typedef struct {

@@ -365,7 +365,8 @@ struct Span {
   int slots;
   int min_units, whole;       // of a piece; tiles that are not cut (find_piece)
   int first_block;            // the launch's work-groups from here on
-  int64_t work;               // bytes in front of its part of the workspace
+  int tickets;                // its first in the workspace
+  int64_t partials;           // bytes in front of its partial results there
 };
 constexpr int kMaxPieces = 32;        // of a tile: whoever joins them reads them all
 struct Piece {
@@ -481,9 +482,11 @@ __device__ __forceinline__ bool find_piece(const stairs_paged_cache& c, const st
 __host__ __device__ constexpr int most_pieces(int slots) { return 2 * slots; }
 
 // ---- joining ------------------------------------------------------------------------------------------------------------
-// Partial results of a piece: [tile_cols][HD] outputs relative to the column's maximum, then [tile_cols] (maximum, sum) pairs.
-__device__ __forceinline__ int* tickets(const stairs_paged_attn& a, const Span& sp) { return reinterpret_cast<int*>(static_cast<char*>(a.workspace) + sp.work); }
-__device__ __forceinline__ float* partials(const stairs_paged_attn& a, const Span& sp) { return reinterpret_cast<float*>(tickets(a, sp) + most_pieces(sp.slots)); }
+// Partial results of a piece: [tile_cols][HD] outputs relative to the column's maximum, then [tile_cols] (maximum, sum) pairs.  The
+// workspace begins with all tickets, chunks' and rows', whichever of them a call needs: calls of other head sizes, head counts and
+// rows may follow in the same workspace, and none finds partial results where its tickets are.
+__device__ __forceinline__ int* tickets(const stairs_paged_attn& a, const Span& sp) { return static_cast<int*>(a.workspace) + sp.tickets; }
+__device__ __forceinline__ float* partials(const stairs_paged_attn& a, const Span& sp) { return reinterpret_cast<float*>(static_cast<char*>(a.workspace) + sp.partials); }
 template <int HD>
 __host__ __device__ constexpr size_t piece_floats(int tile_cols) { return (size_t)tile_cols * (HD + 2); }
 
@@ -671,7 +674,7 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
   const int u1 = min(w.u1, last_last < 0 ? 0 : (last_last - 32 * wave) / kRowUnit + (last_last >= 32 * wave));
   auto fetch_pages = [&](int u) {
     pages_at = u;
-    const int key = (u + lane) * kRowUnit + wave * 32;
+    const unsigned key = (unsigned)(u + lane) * kRowUnit + wave * 32;
     pages = u + lane < u1 ? table[key >> ps_shift] : -1;
     if ((unsigned)pages >= (unsigned)c.n_pages) pages = -1;
   };
@@ -889,8 +892,8 @@ __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const 
   int pages = -1, pages_at = w.u0;                              // of the blocks 2 pages_at .., a lane each
   auto fetch_pages = [&](int u) {
     pages_at = u;
-    const int key = u * kChunkUnit + lane * 32;
-    pages = key <= last_group ? table[key >> ps_shift] : -1;
+    const unsigned key = u * kChunkUnit + lane * 32u;           // (lanes behind the last key: past 2^31 perhaps)
+    pages = key <= (unsigned)last_group ? table[key >> ps_shift] : -1;
     if ((unsigned)pages >= (unsigned)c.n_pages) pages = -1;
   };
   auto page_of = [&](int u, int block) { return __builtin_amdgcn_readlane(pages, (u - pages_at) * 2 + block); };
@@ -1124,7 +1127,7 @@ extern "C" int stairs_paged_plan(const stairs_page_plan* p, void* hip_stream) {
   if (const int rc = check_stream(st)) return rc;
   const bool one = p->max_rows <= 4 * kPlanThreads;
   hipLaunchKernelGGL(k_paged_plan, dim3(1), dim3(kPlanThreads), 0, st, *p, one ? p->max_rows : 0);
-  if (!one) hipLaunchKernelGGL(k_paged_slots, dim3((p->max_rows + 255) / 256), dim3(256), 0, st, *p);
+  if (!one) hipLaunchKernelGGL(k_paged_slots, dim3((p->max_rows - 1) / 256 + 1), dim3(256), 0, st, *p);
   return launched();
 }
 
@@ -1142,7 +1145,7 @@ extern "C" int stairs_paged_append(const stairs_paged_cache* c, const stairs_pag
   if (const int rc = check_stream(st)) return rc;
   stairs_paged_rows r = *a;
   if (r.rope_theta == 0.f && r.q == r.q_out) r.n_heads = 0;       // nothing happens to q
-  const int heads = std::max(r.n_heads, c->n_kv_heads), tiles = (r.rows + kAppendRows - 1) / kAppendRows;
+  const int heads = std::max(r.n_heads, c->n_kv_heads), tiles = (r.rows - 1) / kAppendRows + 1;
   const int groups = std::max(1, std::min((4 * kCus + tiles - 1) / tiles, heads));
   const double log2_theta = r.rope_theta > 0.f ? std::log2((double)r.rope_theta) : 0.0;
   by_type(c, [&](auto type, auto hd) {
@@ -1162,30 +1165,32 @@ struct Launch {
   int ct;                      // column tiles of the rows' part, 0: there is none
   bool chunk;
   Span rows, chunks;
-  int64_t work_bytes;
-  unsigned grid;
+  int64_t work_bytes, grid;
 };
+constexpr int64_t kMostGroups = (1ll << 24) - 1;     // work-groups of 256 threads in a launch
 Launch plan_attention(const stairs_paged_cache* c, const stairs_paged_attn* a) {
   const int G = a->n_heads / c->n_kv_heads;
   const int64_t cols = (int64_t)a->max_fresh * G;
   Launch l{};
   l.chunk = cols > kFewCols;
   l.ct = cols <= 16 ? 1 : !l.chunk || a->n_seqs > 1 ? 2 : 0;
+  constexpr int kSlots = 2 * kCus;
+  l.work_bytes = 2 * most_pieces(kSlots) * (int64_t)sizeof(int);
   auto add = [&](Span& s) {
     s.first_block = (int)l.grid;
-    s.work = l.work_bytes;
+    s.partials = l.work_bytes;
     // at most `slots` pieces and one a tile
     const int64_t tiles = a->n_seqs + (int64_t)a->rows * G / s.tile_cols;
-    l.grid += (unsigned)(s.slots + tiles * c->n_kv_heads);
-    l.work_bytes += most_pieces(s.slots) * (int64_t)(sizeof(int) + s.tile_cols * (c->head_dim + 2) * sizeof(float));
+    l.grid += s.slots + tiles * c->n_kv_heads;
+    l.work_bytes += most_pieces(s.slots) * (int64_t)(s.tile_cols * (c->head_dim + 2) * sizeof(float));
   };
   if (l.chunk) {
-    l.chunks = Span{l.ct ? kFewCols + 1 : 1, INT32_MAX, kChunkCols, kChunkUnit, 2 * kCus, 8, 400, 0, 0};
+    l.chunks = Span{l.ct ? kFewCols + 1 : 1, INT32_MAX, kChunkCols, kChunkUnit, kSlots, 8, 400, 0, 0, 0};
     add(l.chunks);
   }
   if (l.ct) {
     // pieces of 4 units and more: shorter ones cost more to join than they save (8000 keys of 8 heads alone: 25 us with 2, 19 with 4)
-    l.rows = Span{1, l.chunk ? kFewCols : INT32_MAX, 16 * l.ct, kRowUnit, 2 * kCus, 4, 200, 0, 0};
+    l.rows = Span{1, l.chunk ? kFewCols : INT32_MAX, 16 * l.ct, kRowUnit, kSlots, 4, 200, 0, most_pieces(kSlots), 0};
     add(l.rows);
   }
   return l;
@@ -1195,7 +1200,8 @@ Launch plan_attention(const stairs_paged_cache* c, const stairs_paged_attn* a) {
 
 extern "C" int64_t stairs_paged_attention_workspace(const stairs_paged_cache* c, const stairs_paged_attn* a) {
   if (!attn_sizes_ok(c, a)) return STAIRS_EINVAL;
-  return plan_attention(c, a).work_bytes;
+  const Launch l = plan_attention(c, a);
+  return l.grid <= kMostGroups ? l.work_bytes : (int64_t)STAIRS_EINVAL;
 }
 
 extern "C" int stairs_paged_attention(const stairs_paged_cache* c, const stairs_paged_attn* a, void* hip_stream) {
@@ -1206,6 +1212,7 @@ extern "C" int stairs_paged_attention(const stairs_paged_cache* c, const stairs_
     return STAIRS_EINVAL;
   if (!a->workspace || !aligned16(a->workspace)) return STAIRS_EINVAL;
   const Launch l = plan_attention(c, a);
+  if (l.grid > kMostGroups) return STAIRS_EINVAL;
   if (a->workspace_bytes < l.work_bytes) return STAIRS_ECAPACITY;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (const int rc = check_stream(st)) return rc;
@@ -1213,7 +1220,7 @@ extern "C" int stairs_paged_attention(const stairs_paged_cache* c, const stairs_
   by_type(c, [&](auto type, auto hd) {
     typedef decltype(type) T;
     constexpr int HD = decltype(hd)::value;
-    const dim3 grid(l.grid), block(256);
+    const dim3 grid((unsigned)l.grid), block(256);
     if (l.chunk && l.ct) hipLaunchKernelGGL((k_paged_mixed<T, HD>), grid, block, 0, st, *c, *a, l.chunks, l.rows, scale2);
     else if (l.chunk) hipLaunchKernelGGL((k_paged_chunk<T, HD>), grid, block, 0, st, *c, *a, l.chunks, scale2);
     else if (l.ct == 1) hipLaunchKernelGGL((k_paged_rows<T, HD, 1>), grid, block, 0, st, *c, *a, l.rows, scale2);

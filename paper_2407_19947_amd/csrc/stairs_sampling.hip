@@ -775,21 +775,18 @@ void launch_truncate(float* logits, int rows, int ld, int V, const SampleParams*
 
 using namespace stairs;
 
-static const char* check_sampling(const stairs_sampling* a) {
-  if (!a) return "sampling is NULL";
-  const int dt = a->dtype;
-  if (dt != STAIRS_DTYPE_FP32 && dt != STAIRS_DTYPE_BF16 && dt != STAIRS_DTYPE_FP16) return "unknown dtype";
-  if (a->rows < 0 || a->vocab < 1 || a->vocab > STAIRS_SAMPLE_MAX_VOCAB || a->ld < a->vocab) return "rows, vocab or ld out of range";
-  return nullptr;
+static bool sampling_ok(const stairs_sampling* a) {
+  if (!a || (a->dtype != STAIRS_DTYPE_FP32 && a->dtype != STAIRS_DTYPE_BF16 && a->dtype != STAIRS_DTYPE_FP16)) return false;
+  return a->rows >= 0 && a->rows <= 1 << 21 && a->vocab >= 1 && a->vocab <= STAIRS_SAMPLE_MAX_VOCAB && a->ld >= a->vocab;   // (a row, 2^10 threads)
 }
 
 extern "C" int64_t stairs_sample_workspace(const stairs_sampling* a) {
-  if (check_sampling(a)) return STAIRS_EINVAL;
+  if (!sampling_ok(a)) return STAIRS_EINVAL;
   return 0;
 }
 
 extern "C" int stairs_sample_device(const stairs_sampling* a, void* hip_stream) {
-  if (check_sampling(a)) return STAIRS_EINVAL;
+  if (!sampling_ok(a)) return STAIRS_EINVAL;
   if (a->rows == 0) return STAIRS_OK;
   if (!a->logits || !a->token) return STAIRS_EINVAL;
   const size_t align = a->dtype == STAIRS_DTYPE_FP32 ? 4 : 2;

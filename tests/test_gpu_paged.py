@@ -198,6 +198,13 @@ def test_append(dtype, Hq, Hkv, hd, page, slots):
     append_case(dtype, SLOT_SETS[slots], Hq, Hkv, hd, page, 1100 // page + 2, 10000.0)
 
 
+@pytest.mark.parametrize("first", range(0, 32, 3))
+def test_append_of_runs_longer_than_a_work_groups_rows(first):
+    """A run that begins anywhere in a block of 32 positions, another behind it whose rows meet the next 32 rows elsewhere."""
+    append_case("bf16", [*range(first, first + 70), *range(320 - first, 320 - first + 45)], 2, 2, 64, 32, 14, 10000.0)
+    append_case("fp16", [*range(601, 601 + first), *range(first + 64, first + 64 + 97)], 2, 1, 128, 64, 12, 10000.0)
+
+
 @pytest.mark.parametrize("theta", [0.0, 1.0, 500000.0])
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("pad", [0, 24])
@@ -384,6 +391,37 @@ def test_calls_one_after_the_other_share_a_workspace_and_give_the_same_bits():
     for _ in range(3):
         assert np.array_equal(a.call(workspace=work), first_a)
         assert np.array_equal(b.call(workspace=work), first_b)
+
+
+def test_calls_of_other_head_sizes_rows_and_types_share_a_workspace():
+    """A draft model's and its target's, prompts and single tokens: a call's partial results lie where another's were, no call's
+    where another looks for tickets."""
+    import torch
+    calls = [ou.Attend("bf16", [400, 6000, 3000], [130, 300, 2], 8, 2, 128, 64), ou.Attend("fp16", [5000, 200, 2500], [1, 150, 5], 4, 4, 64, 32),
+             ou.Attend("bf16", [9000, 300, 64], [1, 5, 2], 8, 2, 128, 64), ou.Attend("fp16", [7000], [300], 2, 2, 64, 256),
+             ou.Attend("bf16", [9000, 8000], [1, 1], 4, 4, 128, 128), ou.Attend("bf16", [7000, 20], [7, 1], 40, 2, 64, 64)]
+    alone = [x.call() for x in calls]
+    work = torch.zeros(max(x.dev["work"].numel() for x in calls), dtype=torch.uint8).cuda()
+    for order in ([0, 1, 2, 3, 4, 5], [3, 0, 5, 1, 4, 2], [5, 4, 3, 2, 1, 0], [0, 3, 1, 0, 1, 5]):
+        for i in order:
+            assert np.array_equal(calls[i].call(workspace=work), alone[i]), (order, i)
+
+
+def test_two_calls_at_once_with_a_workspace_each():
+    import torch
+    a = ou.Attend("bf16", [20000, 3000], [1, 5], 8, 2, 128, 64)
+    b = ou.Attend("bf16", [2000, 6000], [130, 300], 8, 2, 128, 64)
+    first = [a.call(), b.call()]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for x in (a, b):
+        x.dev["out"].fill_(7.0)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for x, st in zip((a, b), streams):
+            pkg.stairs_paged_attention(x.cache, x.args, st.cuda_stream)
+    torch.cuda.synchronize()
+    for x, want in zip((a, b), first):
+        assert np.array_equal(x.result(), want)
 
 
 def test_a_workspace_that_is_too_small_is_refused():

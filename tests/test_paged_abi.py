@@ -67,15 +67,28 @@ def test_append_refuses(bad):
 @pytest.mark.parametrize("bad", [dict(n_seqs=-1), dict(n_seqs=1025), dict(max_blocks=0), dict(rows=-1), dict(n_heads=6), dict(n_heads=0), dict(max_fresh=-1),
                                  dict(q=None), dict(out=None), dict(out=P), dict(block_table=None), dict(row_start=None), dict(seq_len=None),
                                  dict(q=P + 8), dict(out=2 * P + 2), dict(q_stride=1000), dict(out_stride=1025), dict(scale=float("nan")),
-                                 dict(scale=float("inf")), dict(max_blocks=1 << 25)])
+                                 dict(scale=float("inf")), dict(max_blocks=1 << 25), dict(rows=1 << 25)])
 def test_attention_refuses(bad):
     refused(lambda: pkg.stairs_paged_attention(cache(), attn(**bad)))
 
 
-@pytest.mark.parametrize("bad", [dict(dtype=3), dict(rows=-1), dict(vocab=0), dict(vocab=524289, ld=524289), dict(ld=99), dict(logits=None),
+@pytest.mark.parametrize("bad", [dict(dtype=3), dict(rows=-1), dict(rows=(1 << 21) + 1), dict(vocab=0), dict(vocab=524289, ld=524289), dict(ld=99), dict(logits=None),
                                  dict(token=None), dict(logits=P + 2), dict(dtype=pkg.DTYPE_FP16, logits=P + 1)])
 def test_sampling_refuses(bad):
     refused(lambda: pkg.stairs_sample_device(sampling(**bad)))
+
+
+def test_attention_refuses_more_work_groups_than_a_launch_has():
+    many = dict(n_heads=4096, q_stride=4096 * 64, out_stride=4096 * 64, max_fresh=1)
+    heads = cache(n_kv_heads=4096, head_dim=64)
+    assert pkg.stairs_paged_attention_workspace(heads, attn(rows=4000, **many)) > 0
+    refused(lambda: pkg.stairs_paged_attention_workspace(heads, attn(rows=1 << 20, **many)))
+    refused(lambda: pkg.stairs_paged_attention(heads, attn(rows=1 << 20, **many)))
+
+
+def test_a_workspace_does_not_shrink_with_the_call():
+    sizes = [pkg.stairs_paged_attention_workspace(cache(), attn(n_seqs=n, rows=r)) for n, r in ((1, 2), (2, 4), (1024, 2048))]
+    assert sizes == sorted(sizes)
 
 
 def test_nothing_to_do_is_no_error():
