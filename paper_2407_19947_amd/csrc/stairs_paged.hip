@@ -17,114 +17,136 @@ namespace {
 constexpr int kPlanThreads = 1024;
 static_assert(kPlanThreads >= STAIRS_PAGED_MAX_SEQS, "a thread per sequence");
 
-// exclusive sum over the threads of the block
-__device__ __forceinline__ long long block_scan(long long v, long long* s_part, long long* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  long long x = v;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const long long o = __shfl_up(x, off);
-    if (lane >= off) x += o;
-  }
-  __syncthreads();
-  if (lane == 63) s_part[wave] = x;
-  __syncthreads();
-  long long before = 0, all = 0;
-  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) {
-    if (w < wave) before += s_part[w];
-    all += s_part[w];
-  }
-  *total = all;
-  return before + x - v;
-}
+// Sums that stop at 2^31 - 1: counts that make no sense stay counts, ascending, and whatever is compared with fewer pages than that
+// compares as it would in the integers.
+struct Counts { unsigned rows, ask, drop; };
+__device__ __forceinline__ unsigned capped(unsigned a, unsigned b) { return min(a + b, (unsigned)INT32_MAX); }
+__device__ __forceinline__ Counts plus(const Counts& a, const Counts& b) { return {capped(a.rows, b.rows), capped(a.ask, b.ask), capped(a.drop, b.drop)}; }
 
-// the last index b < n with first[b] <= i, first ascending, first[0] <= i
+// the last index b < n with first[b] <= i, first ascending, first[0] <= i; ten steps for any n up to 1024, so that several searches
+// run side by side
 __device__ __forceinline__ int find_seq(const int* first, int n, int i) {
-  int lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (first[mid] <= i) lo = mid;
-    else hi = mid;
+  int b = 0;
+#pragma unroll
+  for (int step = STAIRS_PAGED_MAX_SEQS / 2; step >= 1; step >>= 1) {
+    const int next = b + step;
+    if (first[min(next, n - 1)] <= i && next < n) b = next;
   }
-  return lo;
+  return b;
+}
+// f(i, sequence of i) for the thread's share of 0 .. n - 1, U searches at a time
+template <int U, typename F>
+__device__ __forceinline__ void each_of(int n, const int* first, int n_seqs, int begin, int step, F f) {
+  for (int i0 = begin; i0 < n; i0 += U * step) {
+    int b[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) b[k] = find_seq(first, n_seqs, i0 + k * step);
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (i0 + k * step < n) f(i0 + k * step, b[k]);
+    if (n - i0 <= U * step) break;                  // (i0 stays an int)
+  }
 }
 
-// position and slot of row t, from what the plan has left
-__device__ __forceinline__ void row_slot(const stairs_page_plan& p, const int* row_start, int t, int total) {
-  int pos = -1, slot = -1;
-  if (t < total) {
-    const int b = find_seq(row_start, p.n_seqs, t);
-    const int len = p.seq_len[b];
-    if (len > 0) {
-      pos = len - (row_start[b + 1] - t);
-      if (pos < 0 || pos >= len) pos = -1;          // (counts whose sum is no int)
-      const int page = pos < 0 ? -1 : p.block_table[(size_t)b * p.max_blocks + pos / p.page_size];
-      if ((unsigned)page < (unsigned)p.n_pages) slot = page * p.page_size + pos % p.page_size;
-    }
-  }
-  p.position[t] = pos;
-  p.slot[t] = slot;
+// positions and slots of the thread's rows, by the sequences' first rows and lengths
+template <int U>
+__device__ __forceinline__ void row_slots(const stairs_page_plan& p, const int* first, const int* lens, int rows, int begin, int step) {
+  const int total = first[p.n_seqs], shift = __builtin_ctz(p.page_size);
+  each_of<U>(min(total, rows), first, p.n_seqs, begin, step, [&](int t, int b) {
+    const int len = lens[b];
+    int pos = len > 0 ? len - (first[b + 1] - t) : -1, slot = -1;
+    if (pos < 0 || pos >= len) pos = -1;            // (counts whose sum is no int)
+    const int page = pos < 0 ? -1 : p.block_table[(size_t)b * p.max_blocks + (pos >> shift)];
+    if ((unsigned)page < (unsigned)p.n_pages) slot = (page << shift) + (pos & (p.page_size - 1));
+    p.position[t] = pos;
+    p.slot[t] = slot;
+  });
+  for (long long t = begin; t < rows; t += step)
+    if (t >= total) p.position[t] = p.slot[t] = -1;
 }
 
-// One block: a thread per sequence counts, three sums over the sequences say where everything goes, then the pages that change
-// hands and the rows are spread over all threads (a sequence that ends with a thousand pages is not one thread's work).
+// One block, bound by the latency of its steps: a thread per sequence counts, sums over the sequences say where everything goes, then the
+// pages that change hands and the rows are spread over all threads (a sequence that ends with a thousand pages is not one
+// thread's work).  Requests are served in order without overtaking, so whoever gets pages stands behind nobody who asked and got
+// none: its pages begin where its share of the asks does.  (16 requests 6.8 us, of which a launch with nothing to do is most; 1000
+// requests with thousands of rows 19.8 us with k_paged_slots; a sum at a time and a search at a time 25.7.)
 __global__ __launch_bounds__(kPlanThreads) void k_paged_plan(stairs_page_plan p, int rows_here) {
-  __shared__ long long s_part[kPlanThreads / 64];
-  __shared__ int s_rows[STAIRS_PAGED_MAX_SEQS + 1], s_drop[STAIRS_PAGED_MAX_SEQS + 1], s_ask[STAIRS_PAGED_MAX_SEQS + 1];
-  __shared__ int s_need[STAIRS_PAGED_MAX_SEQS], s_held[STAIRS_PAGED_MAX_SEQS];
-  const int b = threadIdx.x;
+  constexpr int kWaves = kPlanThreads / 64;
+  __shared__ Counts s_wave[kWaves];
+  __shared__ int s_rows[STAIRS_PAGED_MAX_SEQS + 1], s_drop[STAIRS_PAGED_MAX_SEQS], s_ask[STAIRS_PAGED_MAX_SEQS];
+  __shared__ int s_need[STAIRS_PAGED_MAX_SEQS], s_held[STAIRS_PAGED_MAX_SEQS], s_granted;
+  const int b = threadIdx.x, lane = b & 63, wave = b >> 6;
   const bool here = b < p.n_seqs;
   const int cached = here ? max(p.cached[b], 0) : 0, fresh = here ? max(p.fresh[b], 0) : 0;
   const int held = here ? min(max(p.held[b], 0), p.max_blocks) : 0;
   const int n_free = min(max(p.n_free[0], 0), p.n_pages);
-  const long long wants = ((long long)cached + fresh + p.page_size - 1) / p.page_size;
-  const bool fits = wants <= p.max_blocks;
-  const int need = fits ? (int)wants : held;
+  const unsigned len = (unsigned)cached + (unsigned)fresh;
+  const bool fits = len <= (unsigned)p.max_blocks * (unsigned)p.page_size;
+  const int need = fits ? (int)((len + p.page_size - 1) >> __builtin_ctz(p.page_size)) : held;
   const int ask = max(need - held, 0), drop = held - min(need, held);
-  long long rows_l, asked, dropped_l, granted_l;
-  const int row0 = (int)block_scan(fresh, s_part, &rows_l);
-  const long long ask0 = block_scan(ask, s_part, &asked);
-  const int drop0 = (int)min(block_scan(drop, s_part, &dropped_l), (long long)INT32_MAX);
-  const int dropped = (int)min(dropped_l, (long long)(p.n_pages - n_free)), avail = n_free + dropped;
-  const bool ok = fits && (ask == 0 || ask0 + ask <= avail);
-  const int grant0 = (int)block_scan(ok ? ask : 0, s_part, &granted_l);     // (at most avail)
-  const int rows = (int)rows_l, granted = (int)granted_l;
+  const Counts mine{(unsigned)fresh, (unsigned)ask, (unsigned)drop};
+  Counts to = mine;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const Counts o{__shfl_up(to.rows, off), __shfl_up(to.ask, off), __shfl_up(to.drop, off)};
+    if (lane >= off) to = plus(to, o);
+  }
+  if (lane == 63) s_wave[wave] = to;
+  if (b == 0) s_granted = 0;
+  __syncthreads();
+  Counts front{0, 0, 0}, all{0, 0, 0};
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const Counts o = s_wave[w];
+    all = plus(all, o);
+    if (w < wave) front = plus(front, o);
+  }
+  const Counts before = plus(front, {(unsigned)__shfl_up(to.rows, 1), (unsigned)__shfl_up(to.ask, 1), (unsigned)__shfl_up(to.drop, 1)});
+  const Counts at = lane == 0 ? front : before;
+  const int rows = (int)all.rows, dropped = min((int)all.drop, p.n_pages - n_free), avail = n_free + dropped;
+  const bool ok = fits && (ask == 0 || (long long)at.ask + ask <= avail);
+  const unsigned long long takers = __ballot(ok && ask > 0);
+  if (takers && lane == 63 - __builtin_clzll(takers)) atomicMax(&s_granted, (int)at.ask + ask);   // (the wave's last)
   if (here) {
-    s_rows[b] = row0;
-    s_drop[b] = drop0;
-    s_ask[b] = grant0;
+    s_rows[b] = (int)at.rows;
+    s_drop[b] = (int)at.drop;
+    s_ask[b] = (int)at.ask;
     s_need[b] = need;
     s_held[b] = held;
   }
   if (b == 0) s_rows[p.n_seqs] = rows;
   __syncthreads();
+  const int granted = s_granted;
   // pages given back, behind the free ones
-  for (int i = threadIdx.x; i < dropped; i += kPlanThreads) {
-    const int q = find_seq(s_drop, p.n_seqs, i);
+  each_of<4>(dropped, s_drop, p.n_seqs, b, kPlanThreads, [&](int i, int q) {
     p.free_pages[n_free + i] = p.block_table[(size_t)q * p.max_blocks + s_need[q] + (i - s_drop[q])];
-  }
+  });
   __syncthreads();
   // pages taken, from the end of the stack
-  for (int i = threadIdx.x; i < granted; i += kPlanThreads) {
-    const int q = find_seq(s_ask, p.n_seqs, i);
+  each_of<4>(granted, s_ask, p.n_seqs, b, kPlanThreads, [&](int i, int q) {
     p.block_table[(size_t)q * p.max_blocks + s_held[q] + (i - s_ask[q])] = p.free_pages[avail - 1 - i];
-  }
+  });
   if (here) {
     p.held_out[b] = ok ? need : held;
-    p.row_start[b] = row0;
-    p.seq_len[b] = ok ? cached + fresh : 0;
+    p.row_start[b] = s_rows[b];
+    p.seq_len[b] = s_need[b] = ok ? (int)len : 0;    // (s_need: of no more use)
   }
   if (b == 0) {
     p.n_free_out[0] = avail - granted;
     p.row_start[p.n_seqs] = rows;
   }
   __syncthreads();
-  for (int t = threadIdx.x; t < rows_here; t += kPlanThreads) row_slot(p, s_rows, t, rows);
+  row_slots<4>(p, s_rows, s_need, rows_here, b, kPlanThreads);
 }
 
 __global__ __launch_bounds__(256) void k_paged_slots(stairs_page_plan p) {
-  const int t = blockIdx.x * 256 + threadIdx.x;
-  if (t < p.max_rows) row_slot(p, p.row_start, t, p.row_start[p.n_seqs]);
+  __shared__ int s_rows[STAIRS_PAGED_MAX_SEQS + 1], s_len[STAIRS_PAGED_MAX_SEQS];
+  for (int b = threadIdx.x; b <= p.n_seqs; b += 256) {
+    s_rows[b] = p.row_start[b];
+    if (b < p.n_seqs) s_len[b] = p.seq_len[b];
+  }
+  __syncthreads();
+  row_slots<1>(p, s_rows, s_len, p.max_rows, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -1127,7 +1149,7 @@ extern "C" int stairs_paged_plan(const stairs_page_plan* p, void* hip_stream) {
   if (const int rc = check_stream(st)) return rc;
   const bool one = p->max_rows <= 4 * kPlanThreads;
   hipLaunchKernelGGL(k_paged_plan, dim3(1), dim3(kPlanThreads), 0, st, *p, one ? p->max_rows : 0);
-  if (!one) hipLaunchKernelGGL(k_paged_slots, dim3((p->max_rows - 1) / 256 + 1), dim3(256), 0, st, *p);
+  if (!one) hipLaunchKernelGGL(k_paged_slots, dim3(std::min((p->max_rows - 1) / 256 + 1, 8 * kCus)), dim3(256), 0, st, *p);
   return launched();
 }
 
