@@ -67,6 +67,16 @@ def test_flat_rows_that_keep_thousands_of_tokens(V, dtype, spread):
         check(x, dtype, rng.random(3).astype(np.float32), **rules)
 
 
+@pytest.mark.parametrize("V,dtype", [(2000, "fp32"), (20000, "bf16"), (120000, "fp32")])
+def test_lists_of_every_length(V, dtype):
+    """Tokens listed and kept around every size at which they are sorted, cut or drawn from another way; equal logits among them."""
+    rng = np.random.default_rng(V)
+    k = np.array([1, 2, 3, 31, 32, 33, 63, 64, 65, 66, 127, 128, 129, 130, 255, 256, 257, 261, 511, 512, 513, 514, 1023, 1024, 1025, 1026], np.int32)
+    x = logits_like_a_model(len(k), V, V + 1)
+    for rules in (dict(), dict(temperature=3.0), dict(temperature=2.0, top_p=0.9), dict(min_p=0.01)):
+        check(x, dtype, rng.random(len(k)).astype(np.float32), top_k=k, **rules)
+
+
 def test_rows_with_rules_of_their_own():
     rng = np.random.default_rng(1)
     n, V = 200, 5000
