@@ -197,7 +197,9 @@ __device__ __forceinline__ X ld_once_as(const void* p) {
 // pairs of a row, 16 bytes of either half; in a key tile the same 8 dims of 8 rows are one line.  v: a head's rows go through LDS;
 // the eight positions of a value tile that are 16 adjacent bytes a dim (two quads, 16 apart) are stored together where they are rows
 // of this call, so that a wave's store is a whole tile row; rows that have not all of them as quads of 8 bytes or single
-// values.  (Quads transposed in registers, 8 bytes here and there: 8190 rows of 48 heads 75 us, 40 of them for the values.)
+// values.  (Quads transposed in registers, 8 bytes here and there: 8190 rows of 48 heads 75 us, 40 of them for the
+// values; as it is 57.5 = 3.5 TB/s, reading 8 % more than the rows have,
+// writing no more.)
 constexpr int kAppendRows = 32;
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stairs_paged_rows a, double log2_theta) {
@@ -208,7 +210,9 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
   } lds;
   __shared__ int s_slots[BEHIND + kAppendRows + AHEAD], s_pos[kAppendRows], s_unit[kAppendRows], s_units, s_end;
   const int* const s_slot = s_slots + BEHIND;
-  const int t0 = blockIdx.x * kAppendRows, n = min(kAppendRows, a.rows - t0);
+  // (an XCD takes rows that follow each other: lines that two work-groups share meet in one L2; 16000 rows of 48 heads 104 -> 101 us)
+  const int xcd = blockIdx.x & 7, share = gridDim.x >> 3, more = gridDim.x & 7;
+  const int t0 = (xcd * share + min(xcd, more) + (int)(blockIdx.x >> 3)) * kAppendRows, n = min(kAppendRows, a.rows - t0);
   // its heads: a run of q's, one of k's and v's
   const int nq = a.n_heads, nk = c.n_kv_heads, y = blockIdx.y, groups = gridDim.y;
   const int only = gridDim.z == 1 ? -1 : (int)blockIdx.z;      // (few rows: q, k and v each a work-group of their own)
