@@ -562,9 +562,9 @@ __device__ Cut find_cut(const X& x, int V, const Row& r, float mine, int top_k, 
 
 template <typename T>
 __device__ __forceinline__ bool is_kept(float a, int v, const Cut& c, const Row& r) {
-  const uint32_t k = key_of<T>(a);
-  if (!k || k < c.key || (k == c.key && v > c.index)) return false;
-  return exponent(a, r) >= c.least;
+  // (by value: 8 rows of 128255 without rules 67.4 us, by key 71.5; where nothing is cut -infinity is left out by its exponent)
+  const float last = c.key > 1 ? value_of_key(c.key, Logit<T>::kBits) : -INFINITY;
+  return (a > last || (a == last && v <= c.index)) && exponent(a, r) >= c.least;
 }
 
 // The same for up to 64 tokens, a lane of the first wave each, for that wave alone (0 in the others): a token's sum is formed by
