@@ -68,8 +68,8 @@ __device__ __forceinline__ void row_slots(const stairs_page_plan& p, const int* 
 // One block, bound by the latency of its steps: a thread per sequence counts, sums over the sequences say where everything goes, then the
 // pages that change hands and the rows are spread over all threads (a sequence that ends with a thousand pages is not one
 // thread's work).  Requests are served in order without overtaking, so whoever gets pages stands behind nobody who asked and got
-// none: its pages begin where its share of the asks does.  (16 requests 6.8 us, of which a launch with nothing to do is most; 1000
-// requests with thousands of rows 19.8 us with k_paged_slots; a sum at a time and a search at a time 25.7.)
+// none: its pages begin where its share of the asks does.  (16 requests 5.0 us; 1000
+// requests, a quarter of them chunks of up to 600 rows, 14.9 and k_paged_slots 4.8; a sum and a search at a time 20 and 5.6.)
 __global__ __launch_bounds__(kPlanThreads) void k_paged_plan(stairs_page_plan p, int rows_here) {
   constexpr int kWaves = kPlanThreads / 64;
   __shared__ Counts s_wave[kWaves];
@@ -644,7 +644,8 @@ __device__ __forceinline__ void join_waves(const stairs_paged_cache& c, const st
 // Bound by the bytes of the cache.  A work-group takes a piece of a tile of 16 CT columns; its four waves take 32-key blocks in
 // turn, straight from memory into the matrix operands (a block of a head is 2 x 64 HD contiguous bytes, every load 1 KiB of a
 // wave), no LDS, and are joined at the end.  Values are requested before the scores they wait for, the next block's keys as
-// soon as this block's are used.
+// soon as this block's are used.  (3 sequences of 9 rows and 23456 .. 59999 positions, 32 heads of 128: 300 us = 6.6 TB/s; 32 of 5 rows and
+// 200 .. 8000 positions, 8 key heads: 66 us = 4.3 TB/s, the rest goes into starting and joining pieces; 300 positions alone 6.5 us.)
 constexpr int kRowUnit = 32 * 4;
 template <int HD, int CT>
 struct RowsLds {
@@ -855,7 +856,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_rows(stairs_paged_cache c, sta
 // Bound by the matrix units and by the exponentials beside them.  A wave has 32 columns, the work-group's four waves read 64
 // keys at a time, copied to LDS while the 64 before are used.  On the 32 x 32 instruction the tiled page layout fits as it is: a
 // lane's 16 scores of 32 keys are two operands of the value product (keys 4 h + i and 16 + 4 h + i, and 8 further, of lane
-// half h), whose other operand is one 16-byte read of a value tile.
+// half h), whose other operand is one 16-byte read of a value tile.  (2048 rows that end at 8200, 32 heads of 128 on 8 key heads: 235 ..
+// 246 us by card, 980 .. 1020 TFLOP/s, where a bf16 product of 8192^3 reaches 1181.)
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mma(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
@@ -1082,7 +1084,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(stairs_paged_cache c, st
   __shared__ ChunkLds<HD> lds;
   attend_chunk<T, HD>(c, a, sp, scale2, lds);
 }
-// both in one launch: the chunks' work-groups first, the few rows of the others where there is room
+// both in one launch: the chunks' work-groups first, the few rows of the others where there is room (2 chunks of 509 rows among 22
+// sequences of 3, 90 .. 5000 positions, 16 heads of 128: 78 us = 3.3 TB/s)
 template <typename T, int HD>
 __global__ __launch_bounds__(256, 2) void k_paged_mixed(stairs_paged_cache c, stairs_paged_attn a, Span chunk, Span rows, float scale2) {
   __shared__ union { ChunkLds<HD> chunk; RowsLds<HD, 2> rows; } lds;
