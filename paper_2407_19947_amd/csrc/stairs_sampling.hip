@@ -69,10 +69,10 @@ __device__ __forceinline__ double exponent(float x, const Row& r) {
 }
 constexpr double kNoWeight = -745.13;              // below it a weight is 0 in double
 
-// exp(d) for least <= d <= 0, or of `least`, in multiples of 2^-bits, where that is below 2^51.  d = n ln 2 + r with |r| <= ln 2 / 2; exp(r / 4) by its series up to the 8th power
-// (the next term is 8e-16), squared twice; the number and the place of its last bit come from one multiply-add.
-__device__ __forceinline__ u64 fixed_exp(double d, int bits = 44, double least = -64.0) {
-  d = fmax(d, least);                              // (weights below 2^-45 are 0 in multiples of 2^-44; NaN is the least too)
+// exp(d) for d <= 0 in multiples of 2^-44.  d = n ln 2 + r with |r| <= ln 2 / 2; exp(r / 4) by its series up to the 8th power (the next
+// term is 8e-16), squared twice; the number and the place of its last bit come from one multiply-add.
+__device__ __forceinline__ u64 fixed_exp(double d) {
+  d = fmax(d, -64.0);                              // (weights below 2^-45 are 0 in multiples of 2^-44; NaN is the least too)
   const double big = 6755399441055744.0;           // 1.5 * 2^52: adding it rounds to a whole number
   const double nb = fma(d, 1.4426950408889634074, big), n = nb - big;
   const double x = fma(n, -0.17328679513998632735, 0.25 * d);   // ln 2 / 4
@@ -88,7 +88,7 @@ __device__ __forceinline__ u64 fixed_exp(double d, int bits = 44, double least =
   p *= p;
   p *= p;
   const int e = (int)(uint32_t)__double_as_longlong(nb);        // n, in the low bits
-  const double scale = __longlong_as_double((long long)(1023 + bits + e) << 52);
+  const double scale = __longlong_as_double((long long)(1023 + 44 + e) << 52);
   return (u64)__double_as_longlong(fma(p, scale, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;   // + 2^52
 }
 __device__ __forceinline__ u64 weight(float x, const Row& r) { return fixed_exp(exponent(x, r)); }
@@ -182,6 +182,15 @@ __device__ u64 block_sum(u64 v, L& s) {
   u64 t = 0;
   for (int w = 0; w < L::kWaves; ++w) t += s.part[w];
   return t;
+}
+template <typename L>
+__device__ float block_max(float v, L& s) {
+  v = wave_max(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) s.fpart[threadIdx.x >> 6] = v;
+  __syncthreads();
+  for (int w = 0; w < L::kWaves; ++w) v = fmaxf(v, s.fpart[w]);
+  return v;
 }
 // sum of the threads in front
 template <typename L>
@@ -634,11 +643,7 @@ __device__ float load_row(const T* x, int V, float* mine, L& s) {
     }
   }
   *mine = m;
-  m = wave_max(m);
-  if ((threadIdx.x & 63) == 0) s.fpart[threadIdx.x >> 6] = m;
-  __syncthreads();
-  for (int w = 0; w < L::kWaves; ++w) m = fmaxf(m, s.fpart[w]);
-  return m;
+  return block_max(m, s);
 }
 
 template <typename T, int NT, int CACHE, bool CACHED>
@@ -725,8 +730,8 @@ __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
     }
     double log_z = log((double)z * (1.0 / kOne));
     if ((z & ((1ull << 44) - 1)) < 1ull << 34) {
-      // Perhaps little beside the largest logits (2^-10 of them): then that is summed again in multiples of 2^-50 of itself, or the
-      // logarithm would be the roundings' sum.
+      // Perhaps little beside the largest logits (2^-10 of them): then that is summed again in multiples of 2^-44 of the largest of it
+      // (2^19 tokens at most: sums stay below 2^64 however little it is), or the logarithm would be the roundings' sum.
       constexpr int B = Logit<T>::kBits;
       auto each_kept = [&](auto f) {
         if (c.listed > 0) {
@@ -738,18 +743,19 @@ __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
         }
       };
       u64 tops = 0;
-      each_kept([&](float b) { tops += b == r.max; });
+      float second = -INFINITY;
+      each_kept([&](float b) {
+        if (b == r.max) ++tops;
+        else second = fmaxf(second, b);
+      });
       tops = block_sum(tops, s);
-      const u64 little = z - tops * (1ull << 44);
-      if (little < 1ull << 34) {
-        const int bits = 94 - (little ? 64 - __builtin_clzll(little) : 0);
+      if (z - tops * (1ull << 44) < 1ull << 34) {
+        const Row low{block_max(second, s), r.inv_temp, r.bins};
         u64 rest = 0;
-        each_kept([&](float b) {
-          const double d = exponent(b, r);
-          if (b != r.max && d >= -100.0) rest += fixed_exp(d, bits, -100.0);
-        });
+        each_kept([&](float b) { rest += b == r.max ? 0 : weight(b, low); });
         rest = block_sum(rest, s);
-        log_z = log((double)tops) + log1p(ldexp((double)rest, -bits) / (double)tops);
+        const double share = rest ? (double)rest * (1.0 / kOne) * exp(exponent(low.max, r)) : 0.0;
+        log_z = log((double)tops) + log1p(share / (double)tops);
       }
     }
     lp = (float)(exponent(x[token], r) - log_z);

@@ -166,6 +166,27 @@ def test_logprob_of_a_token_that_is_nearly_certain(V, rules):
             assert abs(lp[0] - want) <= 2.0 ** -24 * abs(want) + V * (2.0 ** -51 * 2 * rest if rest < 2.0 ** -10 else 2.0 ** -45), (gap, tops, lp[0], want)
 
 
+@pytest.mark.parametrize("V", [1000, 128255, 200001, 524288])
+@pytest.mark.parametrize("tops", [1, 3])
+@pytest.mark.parametrize("rules", [dict(), dict(min_p=1e-37)], ids=str)
+def test_logprob_beside_a_flat_rest_of_any_size(V, tops, rules):
+    """Hundreds of thousands of equal logits, each below 2^-45 of the largest or just above it, alone and with one among them that is not:
+    their sum neither wraps nor is lost."""
+    import torch
+    gaps = np.float32([30.9, 31.2, 31.5, 32.0, 33.0, 33.5, 36.0, 50.0, 70.0, 84.0])
+    x = torch.zeros(2 * len(gaps), V)
+    x[:, [7, V // 3, V - 1][:tops]] = torch.from_numpy(np.concatenate([gaps, gaps]))[:, None]
+    x[len(gaps):, 11] = 2.0
+    token, lp, kept, _ = ou.sample_call(x, "fp32", np.float32(0.5), **rules)
+    for i, gap in enumerate(np.concatenate([gaps, gaps]).astype(np.float64)):
+        one = i >= len(gaps)
+        rest = (V - tops - one) * np.exp(-gap) + one * np.exp(2.0 - gap)
+        want = -np.log(tops) - np.log1p(rest / tops)
+        assert token[i] in (7, V // 3, V - 1) and kept[i] == V, (i, token[i], kept[i])
+        # half a step of float; V roundings to 2^-45 of the largest of what is beside the top (rest / exp(2 - gap) is one at least)
+        assert abs(lp[i] - want) <= (2.0 ** -24 + 2.0 ** -50) * abs(want) + V * 2.0 ** -45 * np.exp(2.0 - gap), (gap, one, lp[i], want)
+
+
 def test_drawn_tokens_follow_the_probabilities():
     """Evenly spaced numbers: each token's count is its share to within one, by the definition."""
     import torch
