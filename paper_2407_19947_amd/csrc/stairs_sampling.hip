@@ -67,7 +67,7 @@ __device__ __forceinline__ double exponent(float x, const Row& r) {
   if (r.max == INFINITY) return x == INFINITY ? 0.0 : -INFINITY;
   return ((double)x - (double)r.max) * r.inv_temp;
 }
-constexpr double kNoWeight = -745.13;              // below it a weight is 0 in double
+constexpr double kNoWeight = -745.13321910194118;  // -1075 ln 2: below it a weight is 0 in double
 
 // exp(d) for d <= 0 in multiples of 2^-44.  d = n ln 2 + r with |r| <= ln 2 / 2; exp(r / 4) by its series up to the 8th power (the next
 // term is 8e-16), squared twice; the number and the place of its last bit come from one multiply-add.

@@ -187,6 +187,20 @@ def test_logprob_beside_a_flat_rest_of_any_size(V, tops, rules):
         assert abs(lp[i] - want) <= (2.0 ** -24 + 2.0 ** -50) * abs(want) + V * 2.0 ** -45 * np.exp(2.0 - gap), (gap, one, lp[i], want)
 
 
+@pytest.mark.parametrize("V", [40, 1000, 5000, 40000])
+def test_kept_are_the_weights_that_are_not_0_in_double(V):
+    """exp(d) is the smallest double down to d = -1075 ln 2 = -745.13322, and 0 below."""
+    import torch
+    d = np.float32([-745.0, -745.1299, -745.1301, -745.1310, -745.1330, -745.1332, -745.1333, -745.1340, -745.2, -746.0])
+    x = torch.full((2, V), -float("inf"))
+    x[:, 3] = 0.0
+    x[:, 5:5 + len(d)] = torch.from_numpy(d)
+    want = 1 + int((d.astype(np.float64) > -1075 * np.log(2.0)).sum())
+    for rules in (dict(), dict(top_k=30), dict(top_p=1.0, top_k=V)):
+        token, lp, kept, _ = ou.sample_call(x, "fp32", np.float32(0.5), **rules)
+        assert kept.tolist() == [want] * 2 and token.tolist() == [3, 3] and lp.tolist() == [0.0, 0.0]
+
+
 def test_drawn_tokens_follow_the_probabilities():
     """Evenly spaced numbers: each token's count is its share to within one, by the definition."""
     import torch
