@@ -876,6 +876,7 @@ __device__ __forceinline__ void copy_tile(const void* base, uint32_t offset, uin
                                            lane_bytes, offset, 0, 0);
 }
 constexpr int kChunkCols = 128, kChunkUnit = 64;
+constexpr float kFarScore = 4096.f;   // in powers of two; below it the reference point's product is off by 2^-13 of one at most
 template <int HD>
 struct ChunkLds {
   union {
@@ -956,7 +957,7 @@ __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const 
       for (int b = 0; b < 2; ++b) s[b] = mma(__builtin_bit_cast(x8, kt[b * 8 * HD + (k >> 1) * 64 + 32 * (k & 1)]), q[k], s[b]);
   };
   // (m: the reference point in units of the raw score)
-  auto probabilities = [&](const f32x16 (&s)[2], x8 (&p)[2][2]) {
+  auto probabilities = [&](f32x16 (&s)[2], x8 (&p)[2][2]) {
     // (the maximum that passes NaN on, one instruction for three values; a NaN makes the column's sum NaN whatever m is)
     float mx = __builtin_elementwise_maximum(s[0][0], s[1][0]);
 #pragma unroll
@@ -969,7 +970,14 @@ __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const 
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] *= f;
     }
-    const float mr = m == -INFINITY ? 0.f : -m * scale2;
+    float mr = m == -INFINITY ? 0.f : -m * scale2;
+    if (__any(fabsf(mr) > kFarScore)) {
+      // Far from 0 the reference point's product is rounded by whole powers of two (probabilities past the largest half, in bfloat16 ones
+      // that are none of 1): there it is taken off the raw scores.
+#pragma unroll
+      for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] -= m == -INFINITY ? 0.f : m;
+      mr = 0.f;
+    }
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 32; ++i) {

@@ -351,6 +351,33 @@ def test_scores_of_every_size():
     a.check(a.call())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows", [1, 9, 140])
+def test_scores_of_the_largest_halves(dtype, rows):
+    """Scores up to 3e8, hundreds apart: each row's result is the value of one key, to the last bit."""
+    import torch
+    a = ou.Attend(dtype, [700, 150, 333], [rows, rows, rows], 4, 2, 64, 64, seed=rows)
+    a.q[:], a.K[:] = 0, 0
+    at = np.concatenate([n - rows + np.arange(rows) for n in a.lens] + [[0, 0]])
+    a.q[:, :, 5] = torch.where(torch.from_numpy(at % 3 == 0), -30000.0, 30000.0)[:, None].to(a.dt)
+    rng = np.random.default_rng(rows)
+    order = torch.from_numpy(rng.permutation(a.n_pages * 2 * 64).reshape(a.n_pages, 2, 64))
+    a.K[..., 5] = (10000 * (2.0 * (order % 128) / 127 - 1)).to(a.dt)
+    out = a.call(scale=1.0)
+    q, K, V = (t.double().numpy() for t in (a.q, a.K, a.V))
+    t = 0
+    for b, n in enumerate(a.lens):
+        page, p = a.table[b, np.arange(n) // 64], np.arange(n) % 64
+        for i in range(n - rows, n):
+            for h in range(4):
+                x = q[t, h, 5] * K[page, h // 2, p, 5][:i + 1]
+                best = x == x.max()
+                want = V[page, h // 2, p][:i + 1][best].mean(0)
+                # (equal keys share: their mean, rounded, the probabilities exact powers of two)
+                assert (np.abs(out[t, h] - want) <= ou.HALF_STEP[dtype] * (np.abs(want) + (best.sum() > 1) * 2.0 ** -10) + ou.SMALLEST[dtype]).all(), (b, i, h)
+            t += 1
+
+
 def test_a_cache_beyond_32_bit_offsets():
     """Pages far into pools of more than 2^32 bytes each."""
     import torch
