@@ -328,8 +328,14 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
 __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kMaxSlack = 8.f;      // the running maximum follows once a score exceeds it by 2^8: sums and rounded
-                                      // probabilities keep their relative precision whatever the reference point is
+// The running maximum m follows once a score exceeds it by 2^slack; probabilities are exp2(score + lift - m).  A bfloat16 has a float's
+// range: rounded, they keep their relative precision wherever they lie.  A half's steps are 2^-24 all the way below 2^-14, so the largest
+// are put next to its end (2^15, and room for what rounding adds): full precision down to 2^-27 of the largest, and keys below that are
+// off by 2^-38 of it, 60000 of them together by 2^-22.  (Without the lift the others' share beside keys 13 .. 18 nats above them
+// was up to 23 times as far off as roundings of half a step explain.)
+template <typename T> struct Headroom;
+template <> struct Headroom<__bf16> { static constexpr float slack = 8.f, lift = 0.f; };
+template <> struct Headroom<_Float16> { static constexpr float slack = 2.f, lift = 13.f; };
 
 // (a lane's value, those of the lanes 16, 32 and 48 further) -> the largest / the sum, in all four
 __device__ __forceinline__ float groups_max(float v) {
@@ -761,7 +767,7 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
         for (int i = 0; i < 8; ++i) x[i] = key0 + (i >> 2) * 16 + g * 4 + (i & 3) <= last[ct] ? x[i] : -INFINITY;
       }
       float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-      if (__any(mx > m[ct] + kMaxSlack)) {
+      if (__any(mx - m[ct] > Headroom<T>::slack)) {             // (the difference is exact where the scores are far from 0)
         const float mn = fmaxf(m[ct], groups_max(mx));
         const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[ct] - mn);
         m[ct] = mn;
@@ -772,7 +778,7 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
       const float mr = m[ct] == -INFINITY ? 0.f : m[ct];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[i] = __builtin_amdgcn_exp2f(x[i] - mr);
+        x[i] = __builtin_amdgcn_exp2f(x[i] - mr + Headroom<T>::lift);
         l[ct] += x[i];
         p[ct][i] = Elem<T>::down(x[i]);
       }
@@ -962,7 +968,7 @@ __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const 
     float mx = __builtin_elementwise_maximum(s[0][0], s[1][0]);
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = __builtin_elementwise_maximum(mx, __builtin_elementwise_maximum(s[0][i], s[1][i]));
-    if (__any(mx * scale2 > m * scale2 + kMaxSlack)) {
+    if (__any((mx - m) * scale2 > Headroom<T>::slack)) {
       const float mn = fmaxf(m, halves_max(mx));
       const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * scale2);
       m = mn;
@@ -970,13 +976,13 @@ __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const 
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] *= f;
     }
-    float mr = m == -INFINITY ? 0.f : -m * scale2;
+    float mr = m == -INFINITY ? 0.f : Headroom<T>::lift - m * scale2;
     if (__any(fabsf(mr) > kFarScore)) {
       // Far from 0 the reference point's product is rounded by whole powers of two (probabilities past the largest half, in bfloat16 ones
       // that are none of 1): there it is taken off the raw scores.
 #pragma unroll
       for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] -= m == -INFINITY ? 0.f : m;
-      mr = 0.f;
+      mr = Headroom<T>::lift;
     }
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll

@@ -351,6 +351,28 @@ def test_scores_of_every_size():
     a.check(a.call())
 
 
+def beside_sinks(dtype, rows, nats, n=6000):
+    """A key of 32 whose score is so many nats above the others', a number for each key head; its value is 0, the others' thousands: what
+    comes out is the others' share alone, and is to be right relative to that."""
+    import torch
+    a = ou.Attend(dtype, [n, 40 + rows], [rows, rows], len(nats), len(nats), 64, 64, seed=rows)
+    a.q[:], a.K[:] = 0, 0
+    a.q[:, :, 0] = 4
+    a.V = (a.V.float().abs() * 2048 + 2048).to(a.dt)
+    sink = torch.arange(0, 64, 32)
+    a.V[:, :, sink] = 0
+    for h, x in enumerate(nats):
+        a.K[:, h, sink, 0] = x / 4                           # (whole quarters: exact in both types)
+    a.check(a.call(scale=1.0), scale=1.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows", [1, 9, 40])
+def test_many_keys_far_below_a_few(dtype, rows):
+    beside_sinks(dtype, rows, [9.0, 12.0, 13.0, 15.0])
+    beside_sinks(dtype, rows, [14.0, 16.0, 17.0, 18.0])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("rows", [1, 9, 140])
 def test_scores_of_the_largest_halves(dtype, rows):
@@ -376,6 +398,23 @@ def test_scores_of_the_largest_halves(dtype, rows):
                 # (equal keys share: their mean, rounded, the probabilities exact powers of two)
                 assert (np.abs(out[t, h] - want) <= ou.HALF_STEP[dtype] * (np.abs(want) + (best.sum() > 1) * 2.0 ** -10) + ou.SMALLEST[dtype]).all(), (b, i, h)
             t += 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows", [1, 9, 140])
+def test_far_scores_that_rise_by_steps_of_a_float(dtype, rows):
+    """Scores from 2.5e7 to 2e8 that rise by one step of a float every 128 positions, past where the reference point follows: with all
+    values 1 every row gives 1 (two roundings of half a step)."""
+    a = ou.Attend(dtype, [2000, 900], [rows, rows], 4, 4, 64, 32, seed=rows)
+    a.q[:], a.K[:], a.V[:] = 0, 0, 1
+    a.q[..., 0], a.q[..., 1] = 4992, 2
+    for b, n in enumerate(a.lens):
+        for j in range(-(-n // 32)):
+            for h, step in enumerate((2, 4, 8, 16)):
+                a.K[a.table[b, j], h, :, 0] = 4992 * step / 2
+                a.K[a.table[b, j], h, :, 1] = step / 2 * (32 * j // 128)
+    out = a.call(scale=1.0)[:a.row_start[-1]]
+    assert (np.abs(out - 1) <= 2 * ou.HALF_STEP[dtype] + 2.0 ** -12).all()
 
 
 def test_a_cache_beyond_32_bit_offsets():
