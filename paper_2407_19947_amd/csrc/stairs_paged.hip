@@ -337,6 +337,33 @@ template <typename T> struct Headroom;
 template <> struct Headroom<__bf16> { static constexpr float slack = 8.f, lift = 0.f; };
 template <> struct Headroom<_Float16> { static constexpr float slack = 2.f, lift = 13.f; };
 
+// x >= 0 as two numbers of the type, the one below it and what that leaves, for two products with the values: results are then off by
+// their own rounding (with probabilities rounded once they were 1.3 to 1.5 times as far off).  Where the first is not 0 neither is the rest (an
+// infinite value times 0 would be NaN): in bfloat16 2^-23 of x is added to it, in half it is the smallest step at least.  The matrix units
+// wait for memory in attend_rows, the second product costs 0 .. 1.5 % there (32 verifications 66.4 -> 66.6 us, the mixed batch 78.5 -> 79.0);
+// in attend_chunk, which they bound, a third (2048 rows over 8200 positions 241 -> 325 us, 256 over 8000 56 -> 70): probabilities stay
+// rounded once there, half a step of the type each.
+__device__ __forceinline__ void split(const float (&x)[8], bf16x8& first, bf16x8& rest) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t top = __float_as_uint(x[i]) & 0xFFFF0000u;
+    first[i] = __builtin_bit_cast(__bf16, (uint16_t)(top >> 16));
+    rest[i] = (__bf16)fmaf(x[i], 1.f + 0x1p-23f, -__uint_as_float(top));
+  }
+}
+__device__ __forceinline__ void split(const float (&x)[8], f16x8& first, f16x8& rest) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    const auto top = __builtin_amdgcn_cvt_pkrtz(x[i], x[i + 1]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float t = (float)top[k];
+      first[i + k] = (_Float16)t;
+      rest[i + k] = (_Float16)fmaxf(x[i + k] - t, fminf(t, 0x1p-24f));
+    }
+  }
+}
+
 // (a lane's value, those of the lanes 16, 32 and 48 further) -> the largest / the sum, in all four
 __device__ __forceinline__ float groups_max(float v) {
   auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -756,7 +783,7 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
       load_keys(at);
     }
     const bool full = key0 + 31 <= first_last;
-    x8 p[CT];
+    x8 p[CT], rest[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
       float x[8];
@@ -780,8 +807,8 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
       for (int i = 0; i < 8; ++i) {
         x[i] = __builtin_amdgcn_exp2f(x[i] - mr + Headroom<T>::lift);
         l[ct] += x[i];
-        p[ct][i] = Elem<T>::down(x[i]);
       }
+      split(x, p[ct], rest[ct]);
     }
     if (!full) {
       // Some keys of the block are not seen by all columns.  Their probability is 0, and 0 times what is there must be 0: what
@@ -826,7 +853,10 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
 #pragma unroll
     for (int et = 0; et < ET; ++et)
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) o[ct][et] = mma(__builtin_bit_cast(x8, vf[et]), p[ct], o[ct][et]);
+      for (int ct = 0; ct < CT; ++ct) {
+        o[ct][et] = mma(__builtin_bit_cast(x8, vf[et]), rest[ct], o[ct][et]);
+        o[ct][et] = mma(__builtin_bit_cast(x8, vf[et]), p[ct], o[ct][et]);
+      }
     u = un;
   }
 

@@ -351,6 +351,24 @@ def test_scores_of_every_size():
     a.check(a.call())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("Hq,Hkv,hd", [(4, 4, 64), (8, 2, 128), (5, 1, 128)])
+@pytest.mark.parametrize("lens,fresh", [([1, 40, 333, 3000], [1, 1, 1, 1]), ([6, 33, 700, 6000], [5, 3, 2, 6]), ([300, 900, 64], [150, 5, 1])])
+def test_few_rows_are_off_by_one_rounding_of_the_result(dtype, Hq, Hkv, hd, lens, fresh):
+    """Probabilities are two numbers of the type, the second rounded: 2^-8 of a rest of 2^-7 (bfloat16); 2^-11 of 2^-10, or a smallest step of 2^-24
+    beside the largest of 2^13 and more (half)."""
+    a = ou.Attend(dtype, lens, fresh, Hq, Hkv, hd, 64)
+    out = a.call()
+    half = ou.HALF_STEP[dtype]
+    lost = max(lens) * 2.0 ** -37 * float(a.V.abs().max()) if dtype == "fp16" else 0.0
+    want, tol = ou.attention_reference(a.q.double().numpy(), a.K.double().numpy(), a.V.double().numpy(), a.table, a.row_start, a.lens, a.scale,
+                                       2.0 ** -15 if dtype == "bf16" else 2.0 ** -21, ou.SMALLEST[dtype] + lost)
+    for b, f in enumerate(fresh):
+        if f * Hq // Hkv <= 32:
+            r = slice(a.row_start[b], a.row_start[b + 1])
+            ou.check_close(out[r], want[r], tol[r] + half * np.abs(want[r]), (b, f))
+
+
 def beside_sinks(dtype, rows, nats, n=6000):
     """A key of 32 whose score is so many nats above the others', a number for each key head; its value is 0, the others' thousands: what
     comes out is the others' share alone, and is to be right relative to that."""
