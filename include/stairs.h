@@ -355,7 +355,7 @@ int stairs_paged_plan(const stairs_page_plan *plan, void *hip_stream);
  * q_out (which may be q itself with the same stride), k and v to the row's slot.  A row whose slot is outside the pool is not
  * stored; one whose position is negative leaves q_out as it was.  n_heads = 0: k and v only.  rope_theta = 0: no rotation,
  * position not read (q_out is written for every row, or nowhere when it is q).  Two rows of a call have different slots.
- * Pointers 16-byte aligned, strides multiples of 8. */
+ * Pointers 16-byte aligned, strides multiples of 8; 0 <= rows <= 2^29 - 32. */
 typedef struct {
   int32_t rows, n_heads;
   const void *q, *k, *v;

@@ -1155,6 +1155,7 @@ using namespace stairs;
 namespace {
 
 constexpr int kCus = 256;
+constexpr int64_t kMostGroups = (1ll << 24) - 1;     // work-groups of 256 threads in a launch
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
@@ -1205,7 +1206,7 @@ extern "C" int stairs_paged_plan(const stairs_page_plan* p, void* hip_stream) {
 }
 
 extern "C" int stairs_paged_append(const stairs_paged_cache* c, const stairs_paged_rows* a, void* hip_stream) {
-  if (!cache_ok(c) || !a || a->rows < 0 || a->n_heads < 0 || a->n_heads > 4096) return STAIRS_EINVAL;
+  if (!cache_ok(c) || !a || a->rows < 0 || a->rows > kMostGroups * kAppendRows || a->n_heads < 0 || a->n_heads > 4096) return STAIRS_EINVAL;
   if (!(a->rope_theta >= 0.f) || std::isinf(a->rope_theta)) return STAIRS_EINVAL;
   if (a->rows == 0) return STAIRS_OK;
   if (!a->k || !a->v || !a->slot || (a->rope_theta > 0.f && !a->position)) return STAIRS_EINVAL;
@@ -1240,7 +1241,6 @@ struct Launch {
   Span rows, chunks;
   int64_t work_bytes, grid;
 };
-constexpr int64_t kMostGroups = (1ll << 24) - 1;     // work-groups of 256 threads in a launch
 Launch plan_attention(const stairs_paged_cache* c, const stairs_paged_attn* a) {
   const int G = a->n_heads / c->n_kv_heads;
   const int64_t cols = (int64_t)a->max_fresh * G;

@@ -86,6 +86,11 @@ def test_attention_refuses_more_work_groups_than_a_launch_has():
     refused(lambda: pkg.stairs_paged_attention(heads, attn(rows=1 << 20, **many)))
 
 
+@pytest.mark.parametrize("n", [(1 << 29) - 31, 1 << 30, 2 ** 31 - 1])
+def test_append_refuses_more_work_groups_than_a_launch_has(n):
+    refused(lambda: pkg.stairs_paged_append(cache(), rows(rows=n)))
+
+
 def test_a_workspace_does_not_shrink_with_the_call():
     sizes = [pkg.stairs_paged_attention_workspace(cache(), attn(n_seqs=n, rows=r)) for n, r in ((1, 2), (2, 4), (1024, 2048))]
     assert sizes == sorted(sizes)
