@@ -795,16 +795,21 @@ static_assert(sizeof(Lds<kLargeThreads, kLargeCache, 0>) <= 160 * 1024 && sizeof
 
 }  // namespace
 
-// f(threads, bytes of LDS for the row, whether it fits) for rows of V logits of so many bytes
+// f(threads, bytes of LDS for the row, whether it fits) for rows of V logits of so many bytes; no more rows than CUs
 template <typename F>
-static void by_size(int rows, int V, size_t bytes, F f) {
+static void by_size(int V, size_t bytes, F f) {
   if (V <= kSmallRow) f(std::integral_constant<int, kSmallThreads>{}, std::integral_constant<int, kSmallCache>{}, std::true_type{});
-  else if (rows > kCus && V * bytes <= kHalfCache) f(std::integral_constant<int, kHalfThreads>{}, std::integral_constant<int, kHalfCache>{}, std::true_type{});
   else if (V * bytes <= kLargeCache) f(std::integral_constant<int, kLargeThreads>{}, std::integral_constant<int, kLargeCache>{}, std::true_type{});
   else f(std::integral_constant<int, kLargeThreads>{}, std::integral_constant<int, kNoCache>{}, std::false_type{});
 }
+// ... any number of rows
+template <typename F>
+static void by_size(int rows, int V, size_t bytes, F f) {
+  if (rows > kCus && V > kSmallRow && V * bytes <= kHalfCache) f(std::integral_constant<int, kHalfThreads>{}, std::integral_constant<int, kHalfCache>{}, std::true_type{});
+  else by_size(V, bytes, f);
+}
 void launch_truncate(float* logits, int rows, int ld, int V, const SampleParams* sp, hipStream_t st) {
-  by_size(rows, V, sizeof(float), [&](auto threads, auto cache, auto cached) {
+  by_size(V, sizeof(float), [&](auto threads, auto cache, auto cached) {
     constexpr int NT = decltype(threads)::value, C = decltype(cache)::value;
     hipLaunchKernelGGL((k_truncate<NT, C, decltype(cached)::value>), dim3(rows), dim3(NT), 0, st, logits, ld, V, sp);
   });
