@@ -276,6 +276,28 @@ def test_attention_of_many_sequences():
     a.check(a.call())
 
 
+@pytest.mark.parametrize("B", [65, 130, 1000])
+@pytest.mark.parametrize("chunks", [False, True])
+def test_attention_cuts_long_sequences_behind_the_first_64(B, chunks):
+    """Few long sequences among short ones, in the second 64 sequences and later ones as in the first: their tiles are cut, and their pieces'
+    numbers go on from those in front."""
+    import torch
+    rng = np.random.default_rng([B, chunks])
+    lens = rng.integers(1, 60, B)
+    fresh = np.minimum(lens, rng.integers(1, 4, B))
+    for at, n in ((40, 3000), (64, 9000), (B - 1, 7001), (B // 2 + 31, 5120), (B * 3 // 4, 2500)):
+        lens[at], fresh[at] = n, 2
+    if chunks:
+        fresh[64], fresh[B - 2], lens[B - 2], fresh[40] = 130, 40, 4000, 17
+    a = ou.Attend("bf16", lens.tolist(), fresh.tolist(), 4, 2, 64, 32, seed=B)
+    first = a.call()
+    a.check(first)
+    work = torch.zeros_like(a.dev["work"])
+    for _ in range(2):
+        assert np.array_equal(a.call(workspace=work), first)
+    assert int(work[:8192].sum()) == 0                       # every ticket is 0 again
+
+
 def test_attention_with_strides_scale_and_a_hint_that_is_too_small():
     a = ou.Attend("bf16", [300, 64, 5, 900], [70, 3, 5, 300], 8, 2, 128, 64)
     a.check(a.call(scale=0.3, q_pad=40, out_pad=8), scale=0.3)

@@ -246,6 +246,103 @@ def test_proposals_and_verifications_keep_what_the_rules_keep(rules):
         assert np.all(emitted[:n] == d[:n])
 
 
+def _models(vocab):
+    w = si.scaled_workload("cfg2_125m", target=dict(n_layers=2, d_model=256, n_heads=4, d_ffn=512, vocab=vocab), draft=dict(kind="prefix", n_layers=1), P=20, G=60)
+    return (*si.make_pair(w), si.make_prompt(w))
+
+
+def kept_of(x, T, rules):
+    return ou.keep_reference(x.astype(np.float64), 1 / float(np.float32(1) / np.float32(T)), rules.get("top_k", 0), rules.get("top_p", 1.0), rules.get("min_p", 0.0))[0]
+
+
+def is_cut(row, free, T, rules):
+    kept = kept_of(free, T, rules)
+    assert np.array_equal(row > -np.inf, kept) and np.array_equal(row[kept], free[kept])
+
+
+@pytest.mark.parametrize("vocab", [272, 2064, 32000, 40000, 70000])
+@pytest.mark.parametrize("rules", RULE_SETS, ids=str)
+def test_rows_are_cut_and_tokens_follow_the_cut_rows(vocab, rules):
+    """The assistant's first row and all the main model's, at vocabularies in and out of LDS: the rows without rules, cut.  Later rows of the
+    assistant: cut at the borders that the same prefix has in a context of its own (to what its other launches may change).  Draws, what is
+    kept and what replaces it: the oracle's, from the rows handed out."""
+    from oracle import sampling_oracle as sa
+    target, draft, prompt = _models(vocab)
+    T, k, seed, tol = 0.3, 4, 23, 5e-3
+    key = sa.key_from_seed(seed)
+    n_all = near = 0
+    with pkg.Stairs(target, draft, k_max=k, max_seq=160) as s, pkg.Stairs(draft, None, k_max=0, max_seq=160) as alone:
+        seq = [int(t) for t in prompt]
+        for it in range(6):
+            s.set_truncation()
+            s.prefill(seq)
+            _, free_draft = s.propose_sampled(k, T, seed)
+            s.prefill(seq)
+            s.set_truncation(**rules)
+            d, dl = s.propose_sampled(k, T, seed)
+            emitted, n, tl = s.verify_sampled(k, T, seed)
+            d, emitted = [int(t) for t in d], [int(t) for t in emitted]
+            s.set_truncation()
+            s.prefill(seq)
+            free = s.verify_tokens(d, logits=True)[2]
+            for r in range(k + 1):
+                is_cut(tl[r], free[r], T, rules)
+            is_cut(dl[0], free_draft[0], T, rules)
+            for j in range(1, k):
+                alone.prefill(seq + d[:j])
+                x = alone.verify_tokens([], logits=True)[2][0].astype(np.float64)
+                kept = dl[j] > -np.inf
+                y = np.where(kept, dl[j], x).astype(np.float64)
+                assert np.abs(dl[j][kept] - x[kept]).max() <= tol
+                assert x[~kept].max(initial=-np.inf) <= y[kept].min() + tol
+                w = np.exp((y - y.max()) / T)
+                last, band = w[kept].min(), 2 * tol / T
+                if rules.get("top_k"):
+                    assert kept.sum() <= rules["top_k"]
+                    count = kept.sum() == rules["top_k"]
+                else:
+                    count = False
+                base = np.sort(w)[::-1][:rules.get("top_k") or vocab].sum()
+                p, m = rules.get("top_p", 1.0), rules.get("min_p", 0.0)
+                assert (w[kept].sum() - last) <= p * base * np.exp(band)          # what is in front of the last one
+                assert last >= m * np.exp(-band)
+                out = w[~kept].max(initial=0.0)                                   # ... and why no more are kept
+                assert count or w[kept].sum() >= p * base * np.exp(-band) or out <= m * np.exp(band)
+            L = len(seq)
+            for j in range(k):
+                score = dl[j].astype(np.float64) / T + sa.gumbel(L + j, sa.STREAM_DRAFT, vocab, key)
+                assert score[d[j]] >= score.max() - 1e-5
+            want_n, want, us, ratios = sa.validate_sampled(L, d, tl.astype(np.float64), dl.astype(np.float64), T, key)
+            if min(abs(np.log(u) - np.log(max(r, 1e-300))) for u, r in zip(us, ratios)) > 1e-4:
+                assert (n, emitted[:n]) == (want_n, want[:n])
+                near += emitted[n] != want[n]
+                n_all += 1
+            seq = seq + emitted
+    assert n_all >= 4 and near <= 1                                               # (a draw may be a near tie)
+
+
+@pytest.mark.parametrize("rules", [dict(top_k=4), dict(top_p=0.6), dict(min_p=0.25, top_k=6)], ids=str)
+def test_tokens_come_as_often_as_the_cut_main_model_has_them(rules):
+    """The first emitted token over many seeds, whatever the assistant proposes: the main model's probabilities among what the rules
+    keep, each count within five standard deviations, and nothing else."""
+    target, draft, prompt, w = _pair()
+    T, n = 1.0, 1500
+    with pkg.Stairs(target, draft, k_max=2, max_seq=w["P"] + 16) as s:
+        s.prefill(prompt)
+        free = s.verify_tokens([], logits=True)[2][0]
+        kept = kept_of(free, T, rules)
+        p = np.where(kept, np.exp((free.astype(np.float64) - free.max()) / T), 0)
+        p /= p.sum()
+        s.set_truncation(**rules)
+        count = np.zeros(len(p))
+        for seed in range(n):
+            s.prefill(prompt)
+            s.propose_sampled(2, T, seed, logits=False)
+            count[s.verify_sampled(2, T, seed, logits=False)[0][0]] += 1
+    assert count[~kept].sum() == 0 and kept.sum() >= 2
+    assert (np.abs(count - n * p) <= 5 * np.sqrt(n * p * (1 - p)) + 1).all()
+
+
 @pytest.mark.parametrize("k", [0, 3])
 def test_generation_with_rules(k):
     """Graphs and single launches give the same tokens, a repeated call too; one token is greedy decoding; rules turned off
