@@ -371,7 +371,7 @@ int stairs_paged_append(const stairs_paged_cache *cache, const stairs_paged_rows
  * Head h reads key head h / (n_heads / n_kv_heads).  out = softmax(scale * q . k) . v, sums and softmax in float; the
  * probabilities enter the product with v as sums of two numbers of the cache's type (16 bits and more) where a sequence has up to 32
  * rows times query heads of a key head, rounded to one where it has more; scale <= 0: 1 / sqrt(head_dim).  Positions whose page
- * number lies outside the pool are not seen, and a row that sees nothing gives zeros.  Masked positions may hold anything,
+ * number lies outside the pool are not seen, and a row that sees nothing, or whose scores are all -INFINITY, gives zeros.  Masked positions may hold anything,
  * infinities and NaN included.  Rows of out that no sequence has are left as they were.  rows: rows of the q and out buffers;
  * max_fresh: most rows any sequence has (only the choice of kernels depends on it, and with it how probabilities are rounded).  Which sequences share a
  * call shows in the last bits of their results alone (a long sequence is split by the whole batch); the same call gives the same bits.

@@ -315,6 +315,22 @@ def test_rows_that_see_nothing_and_pages_that_are_none(rows, lens):
     a.check(a.call())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows", [1, 5, 140])
+def test_rows_whose_scores_are_all_minus_infinity(dtype, rows):
+    """They give zeros, as rows that see nothing; one finite score takes all."""
+    a = ou.Attend(dtype, [700, 180, 300], [rows] * 3, 4, 2, 128, 64, seed=rows)
+    a.q = a.q.abs() + 0.5
+    a.K[..., 3] = -float("inf")
+    out = a.call()
+    assert (out[:a.row_start[-1]] == 0).all()
+    a.K[a.table[0, 2], :, 5, 3] = 0                          # position 133 of the first sequence
+    out = a.call()
+    sees = 700 - rows + np.arange(rows) >= 133
+    want = np.repeat(a.V[a.table[0, 2], :, 5].double().numpy(), 2, axis=0)
+    assert sees.all() and (out[:rows] == want).all() and (out[rows:a.row_start[-1]] == 0).all()
+
+
 def test_more_rows_than_positions_and_more_positions_than_blocks():
     a = ou.Attend("fp16", [3, 40, 200], [7, 60, 2], 8, 2, 64, 32, extra_blocks=0)
     a.check(a.call())                                        # rows in front of position 0 see nothing

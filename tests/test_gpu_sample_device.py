@@ -363,6 +363,23 @@ def test_generation_with_rules(k):
         assert np.array_equal(s.generate_sampled(prompt, G, k, 0.8, 5)[0], plain)
 
 
+def test_rules_in_an_encoder_decoder_context():
+    w = si.scaled_encdec_workload("t5_tiny")
+    target, draft = si.make_encdec_pair(w)
+    src = si.make_source(w)
+    with pkg.StairsEncDec(target, draft, k_max=4, max_src=64, max_seq=64) as s:
+        s.encode(src)
+        greedy, _ = s.decode(32, 3)
+        s.encode(src)
+        warm, _ = s.decode_sampled(32, 3, 0.2, 9)
+        s.set_truncation(top_k=1)
+        s.encode(src)
+        assert np.array_equal(s.decode_sampled(32, 3, 0.2, 9)[0], greedy)
+        s.set_truncation(min_p=1e-30)                                             # nothing is cut at this temperature
+        s.encode(src)
+        assert np.array_equal(s.decode_sampled(32, 3, 0.2, 9)[0], warm)
+
+
 def test_rules_that_are_refused():
     target, draft, prompt, w = _pair()
     with pkg.Stairs(target, draft, k_max=4, max_seq=w["P"] + 40) as s:
