@@ -401,8 +401,8 @@ int stairs_paged_attention(const stairs_paged_cache *cache, const stairs_paged_a
  *      top_p times the whole                 (1 and more: all; the first token always stays)
  *   3. of these the tokens with w_v >= min_p (0: all; more than 1 counts as 1)
  * and the token drawn is the lowest index at which the kept weights, summed by index, exceed uniform times their sum.
- * Weights are formed in double and summed exactly (multiples of 2^-44 of the largest), so a row's result does not depend on the
- * other rows or on the launch.  temperature <= 0 or NaN: the largest logit, lowest index.  Per-row arrays may be NULL: temperature 1, the
+ * Weights are formed in double, rounded to multiples of 2^-44 of the largest and summed exactly, so a row's result does not depend on the
+ * other rows or on the launch; a token below 2^-45 of the largest is never drawn (kept counts it where the rules keep it).  temperature <= 0 or NaN: the largest logit, lowest index.  Per-row arrays may be NULL: temperature 1, the
  * rule off; uniform may be NULL only if temperature is 0 everywhere, else 0 is taken.  A NaN logit is never drawn; if a logit is +INFINITY,
  * those alone have weight; a token whose weight is 0 in double is not kept.  A row of -INFINITY and NaN alone gives token
  * -1, logprob -INFINITY, kept 0.  logprob (natural logarithm of the drawn token's share of the kept weight) and kept (tokens

@@ -678,7 +678,8 @@ __device__ __forceinline__ void join_waves(const stairs_paged_cache& c, const st
 // turn, straight from memory into the matrix operands (a block of a head is 2 x 64 HD contiguous bytes, every load 1 KiB of a
 // wave), no LDS, and are joined at the end.  Values are requested before the scores they wait for, the next block's keys as
 // soon as this block's are used.  (3 sequences of 9 rows and 23456 .. 59999 positions, 32 heads of 128: 300 us = 6.6 TB/s; 32 of 5 rows and
-// 200 .. 8000 positions, 8 key heads: 66 us = 4.3 TB/s, the rest goes into starting and joining pieces; 300 positions alone 6.5 us.)
+// 200 .. 8000 positions, 8 key heads: 66.6 us = 4.3 TB/s, the rest goes into starting and joining pieces; 300 positions alone 6.6 us, one sequence of
+// 8000 and 8 key heads 13 us with 1 row, 19 with 5.)
 constexpr int kRowUnit = 32 * 4;
 template <int HD, int CT>
 struct RowsLds {
@@ -892,8 +893,9 @@ __global__ __launch_bounds__(256, 2) void k_paged_rows(stairs_paged_cache c, sta
 // Bound by the matrix units and by the exponentials beside them.  A wave has 32 columns, the work-group's four waves read 64
 // keys at a time, copied to LDS while the 64 before are used.  On the 32 x 32 instruction the tiled page layout fits as it is: a
 // lane's 16 scores of 32 keys are two operands of the value product (keys 4 h + i and 16 + 4 h + i, and 8 further, of lane
-// half h), whose other operand is one 16-byte read of a value tile.  (2048 rows that end at 8200, 32 heads of 128 on 8 key heads: 235 ..
-// 246 us by card, 980 .. 1020 TFLOP/s, where a bf16 product of 8192^3 reaches 1181.)
+// half h), whose other operand is one 16-byte read of a value tile.  (2048 rows that end at 8200, 32 heads of 128 on 8 key heads: 233 ..
+// 249 us by card, 970 .. 1030 TFLOP/s, where a bf16 product of 8192^3 reaches 1181; 2048 rows alone 53.8 us = 640, 256 rows that end at 8000 56.8 =
+// 580: partial results of pieces and their joins.)
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mma(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
@@ -1129,7 +1131,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(stairs_paged_cache c, st
   attend_chunk<T, HD>(c, a, sp, scale2, lds);
 }
 // both in one launch: the chunks' work-groups first, the few rows of the others where there is room (2 chunks of 509 rows among 22
-// sequences of 3, 90 .. 5000 positions, 16 heads of 128: 78 us = 3.3 TB/s)
+// sequences of 3, 90 .. 5000 positions, 16 heads of 128: 79 us = 3.3 TB/s)
 template <typename T, int HD>
 __global__ __launch_bounds__(256, 2) void k_paged_mixed(stairs_paged_cache c, stairs_paged_attn a, Span chunk, Span rows, float scale2) {
   __shared__ union { ChunkLds<HD> chunk; RowsLds<HD, 2> rows; } lds;

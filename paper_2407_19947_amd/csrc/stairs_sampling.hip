@@ -8,13 +8,15 @@
 // alone: the k-th of these is not above the k-th of all.  Where the list would be too long (flat rows, equal logits by the thousand) the
 // end is found in one bin, or by radix selection, and the draw goes over the row.  Weights are multiples of 2^-44 of the largest,
 // held in 64-bit integers: their sums do not depend on the order of additions, so neither the histograms' atomics nor the
-// split of a row over threads change a result, and equal borders are equal.  (2^-44 against sums of 1 and more: a border moves by
-// about 1e-11 of the whole against sums in double; a 24-bit random number falls between the two never in practice.)
+// split of a row over threads change a result, and equal borders are equal.  Against sums in double a border moves by 2^-45 of the largest
+// weight for each token at most: about sqrt(V) of them where their roundings differ (1e-11 of the whole), all where logits are equal and round alike
+// (4e-9 of 128255, 1.5e-8 of the largest vocabulary; a 24-bit random number's step is 6e-8).  Tokens below 2^-45 of the largest weigh nothing in
+// the sums: they count as kept and are not drawn.
 //
 // A row is one work-group's, read from memory once: up to 140 KiB of it stay in LDS beside the histogram.  Bound by
 // latencies (a dozen steps that wait for each other: 1 row of 32000 floats with all rules 16 .. 22 us by inputs, 320 rows of 32000
-// bfloat16 with top-k and top-p 31), and with top-p alone by the exponentials in double, one a logit (64 rows of 128255 floats 107 .. 140
-// us by inputs, 42 of them for a row's histogram by weight).  Several work-groups a row, joined over three launches, gained
+// bfloat16 with top-k and top-p 31), and with top-p alone by the exponentials in double, one a logit (64 rows of 128255 floats 95 .. 175
+// us by inputs, 42 of them for a row's histogram by weight).  Without rules 25 us for a row of 32000 and 68 for 8 of 128255, temperature 0 12 and 35.  Several work-groups a row, joined over three launches, gained
 // 14 % there and cost 40 % where top-k is in front.
 #include "../../include/stairs.h"
 #include "stairs_device.h"
@@ -767,7 +769,9 @@ __global__ __launch_bounds__(NT) void k_sample_rows(stairs_sampling a) {
   }
 }
 
-// -infinity at the tokens of rows [.., ld] of floats that the rules do not keep
+// -infinity at the tokens of rows [.., ld] of floats that the rules do not keep.  A launch a draft token and one for the main model's rows:
+// with 4 draft tokens and 32000 logits an iteration is 85 .. 110 us longer (125M pair 650 -> 742 .. 749 us, 1B 1645 -> 1731 .. 1756), with top-p
+// alone 215 (866, 1856).
 template <int NT, int CACHE, bool CACHED>
 __global__ __launch_bounds__(NT) void k_truncate(float* logits, int ld, int V, const SampleParams* sp) {
   typedef Lds<NT, CACHE, CACHED ? 0 : kAllListed> L;
