@@ -373,8 +373,8 @@ int stairs_paged_append(const stairs_paged_cache *cache, const stairs_paged_rows
  * rows times query heads of a key head, rounded to one where it has more; scale <= 0: 1 / sqrt(head_dim).  Positions whose page
  * number lies outside the pool are not seen, and a row that sees nothing, or whose scores are all -INFINITY, gives zeros.  Masked positions may hold anything,
  * infinities and NaN included.  Rows of out that no sequence has are left as they were.  rows: rows of the q and out buffers;
- * max_fresh: most rows any sequence has (only the choice of kernels depends on it, and with it how probabilities are rounded).  Which sequences share a
- * call shows in the last bits of their results alone (a long sequence is split by the whole batch); the same call gives the same bits.
+ * max_fresh: most rows any sequence has (only the choice of kernels depends on it, and with it how probabilities are rounded).  Which
+ * sequences share a call shows in the last bits of their results alone (a long sequence is split by the whole batch); the same call gives the same bits.
  * workspace: stairs_paged_attention_workspace bytes (at most about 90 MB; not fewer for more sequences or rows), 16-byte aligned, all
  * zeros before its first use, left fit for the next call, of other sizes and types too; calls that may overlap need one each.
  * 0 <= n_seqs <= STAIRS_PAGED_MAX_SEQS; row_start ascending; n_heads a multiple of n_kv_heads; rows * n_heads / n_kv_heads at most

@@ -16,8 +16,9 @@
 // A row is one work-group's, read from memory once: up to 140 KiB of it stay in LDS beside the histogram.  Bound by
 // latencies (a dozen steps that wait for each other: 1 row of 32000 floats with all rules 16 .. 22 us by inputs, 320 rows of 32000
 // bfloat16 with top-k and top-p 31), and with top-p alone by the exponentials in double, one a logit (64 rows of 128255 floats 95 .. 175
-// us by inputs, 42 of them for a row's histogram by weight).  Without rules 25 us for a row of 32000 and 68 for 8 of 128255, temperature 0 12 and 35.  Several work-groups a row, joined over three launches, gained
-// 14 % there and cost 40 % where top-k is in front.
+// us by inputs, 42 of them for a row's histogram by weight).  Without rules a row of 32000 takes 25 us and 8 of 128255 take 68, at
+// temperature 0 12 and 35.  Several work-groups a row, joined over three launches, gained 14 % with top-p alone and cost 40 % where
+// top-k is in front.
 #include "../../include/stairs.h"
 #include "stairs_device.h"
 
