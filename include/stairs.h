@@ -42,6 +42,7 @@ extern "C" {
 #define STAIRS_DTYPE_FP32  0     /* matrices are float                                     */
 #define STAIRS_DTYPE_BF16  1     /* matrices are bfloat16 bit patterns (uint16_t)          */
 #define STAIRS_DTYPE_FP16  2     /* IEEE half bit patterns (operators on device buffers)   */
+#define STAIRS_DTYPE_E4M3  3     /* 8-bit floats, 4 exponent and 3 mantissa bits, 448 the largest (held in pages) */
 
 #define STAIRS_MAX_ROWS    32    /* most rows one forward takes: k + 1 <= STAIRS_MAX_ROWS  */
 #define STAIRS_MAX_BATCH        128   /* most sequences stairs_reserve_batch makes room for          */
@@ -300,8 +301,13 @@ int stairs_get_tokens(stairs_ctx *ctx, int32_t *out, int32_t cap, int32_t *len);
  *   stairs_paged_plan       pages for the requests' new rows, and where each row goes
  *   stairs_paged_append     new rows: q and k rotated, k and v into their pages
  *   stairs_paged_attention  attention of the new rows over the pages
+ *   stairs_paged_read       rows out of their pages
  *   stairs_sample_device    a token from each row of logits
  * A verification of k draft tokens is k + 1 new rows of a request; its rollback is a smaller `cached` in the next plan.
+ * Drafts that branch: the new rows of a request are a tree, the last token that is certain and drafted ones behind it, each behind its parent:
+ *   stairs_tree_plan        the rows' positions, and which of the new rows each sees (stairs_paged_attn.sees)
+ *   stairs_tree_walk        the path of each tree that the model's own predictions follow
+ *   stairs_paged_compact    the path's rows to the positions behind the context, in the pools of all layers
  * All pointers inside the structures are DEVICE pointers the caller owns, on the device that is current and that hip_stream
  * (a hipStream_t or NULL) belongs to; the structures themselves are host memory and may go after the call.  Calls allocate
  * nothing, keep nothing from one call to the next, and do not wait: results are valid once the stream has reached the end of
@@ -315,10 +321,22 @@ int stairs_get_tokens(stairs_ctx *ctx, int32_t *out, int32_t cap, int32_t *len);
  *   keys   is at (((p / 16) * (head_dim / 32) + e / 32) * 64 + p % 16 + 16 * (e % 32 / 8)) * 8 + e % 8
  *   values is at (((p / 32) * (head_dim / 16) + e / 16) * 64 + e % 16 + 16 * (p % 16 / 4)) * 8 + p % 4 + 4 * (p % 32 / 16)
  * (the operand order of the matrix instructions: a wave reads whole tiles of 1 KiB).  Slot = page * page_size + position in it.
- * k, v 16-byte aligned; dtype BF16 or FP16; page_size 32, 64, 128 or 256; head_dim 64 or 128; n_pages * page_size < 2^31. */
+ * k, v 16-byte aligned; dtype BF16 or FP16; page_size 32, 64, 128 or 256; head_dim 64 or 128; n_pages * page_size < 2^31.
+ *
+ * held = STAIRS_DTYPE_E4M3: rows go in and come out in dtype, pages hold them in 8 bits; a row of a head (its keys; its values) is codes times
+ * one power of two, 2^(b - 127) with a byte b, as it is stored the smallest from 1 to 254 for which the row's largest finite magnitude is at
+ * most 448 * 2^(b - 127), codes rounded to nearest even; infinities and NaN become NaN; in FP16, magnitudes past 61440 count as 61440.  A page is n_kv_heads * page_size * head_dim bytes; inside
+ * a head, element (p, e) of
+ *   keys   is at ((p / 16) * (head_dim / 64) + e / 64) * 1024 + (p % 16 + 16 * (e % 32 / 8)) * 16 + e % 64 / 32 * 8 + e % 8
+ *   values is at ((p / 32) * (head_dim / 32) + e / 32) * 1024 + (e % 16 + 16 * (p % 16 / 4)) * 16 + e % 32 / 16 * 8 + p % 4 + 4 * (p % 32 / 16)
+ * and scale, 16-byte aligned, has page_size * 2 bytes a page and head, the byte of position p's
+ *   keys   at p / 32 * 64 + p % 16 / 4 * 16 + p % 32 / 16 * 4 + p % 4,   values 8 bytes further.
+ * (Bytes 0 and 255, which no row is stored with, stand for no number.)  held = 0: pages hold dtype, scale is not read. */
 typedef struct {
   void *k, *v;
   int32_t dtype, n_pages, page_size, n_kv_heads, head_dim;
+  int32_t held;
+  void *scale;
 } stairs_paged_cache;
 
 #define STAIRS_PAGED_MAX_SEQS   1024
@@ -378,7 +396,11 @@ int stairs_paged_append(const stairs_paged_cache *cache, const stairs_paged_rows
  * workspace: stairs_paged_attention_workspace bytes (at most about 90 MB; not fewer for more sequences or rows), 16-byte aligned, all
  * zeros before its first use, left fit for the next call, of other sizes and types too; calls that may overlap need one each.
  * 0 <= n_seqs <= STAIRS_PAGED_MAX_SEQS; row_start ascending; n_heads a multiple of n_kv_heads; rows * n_heads / n_kv_heads at most
- * 2^24, work-groups (a tile of 16, 32 or 128 such columns and a key head) fewer than 2^24; pointers 16-byte aligned, strides multiples of 8. */
+ * 2^24, work-groups (a tile of 16, 32 or 128 such columns and a key head) fewer than 2^24; pointers 16-byte aligned, strides multiples of 8.
+ * Over E4M3 pages keys and values count as the numbers they stand for, in FP16 those past 65504 as infinite; where the probabilities are sums of two numbers,
+ * those are bfloat16.
+ * sees (8-byte aligned, or NULL): what the rows of a sequence with up to STAIRS_TREE_MAX_ROWS of them see of each other: bit i of a row's, the i-th new
+ * row of its sequence.  All positions in front of the new rows are seen.  Sequences with more rows are not trees: each row sees the positions up to its own. */
 typedef struct {
   int32_t n_seqs, max_blocks, rows, n_heads, max_fresh;
   const void *q;                   /* [rows][n_heads][head_dim] */
@@ -390,9 +412,73 @@ typedef struct {
   float scale;
   void *workspace;
   int64_t workspace_bytes;
+  const uint64_t *sees;            /* [rows] or NULL */
 } stairs_paged_attn;
 int64_t stairs_paged_attention_workspace(const stairs_paged_cache *cache, const stairs_paged_attn *attn);
 int stairs_paged_attention(const stairs_paged_cache *cache, const stairs_paged_attn *attn, void *hip_stream);
+
+/* Rows out of their pages, what stairs_paged_append stored: k, v [rows][n_kv_heads][head_dim] in the cache's dtype, rows *_stride elements
+ * apart.  8-bit rows come back as the numbers they stand for (in FP16 those past 65504 as 65504).  A row whose slot is outside the pool is left as it was;
+ * slots may come more than once.  k or v may be NULL.  Pointers 16-byte aligned, strides multiples of 8; 0 <= rows <= 2^29 - 32. */
+typedef struct {
+  int32_t rows;
+  void *k, *v;
+  int64_t k_stride, v_stride;
+  const int32_t *slot;             /* [rows] */
+} stairs_paged_out;
+int stairs_paged_read(const stairs_paged_cache *cache, const stairs_paged_out *out, void *hip_stream);
+
+/* Trees of drafted tokens.  The new rows row_start[b] .. row_start[b + 1] - 1 of request b (as stairs_paged_plan leaves them) are stored at the last
+ * positions of its seq_len[b], one behind the other; its context is what lies in front.  parent[r] is the number of r's parent among them, smaller
+ * than its own (which begins at 0 with every request); anything else: none, r comes right behind the context.  Row 0 is the last token
+ * that is certain.  A request with more than STAIRS_TREE_MAX_ROWS rows is a prompt's chunk: parent is not read, each row is behind the one in front of it.
+ *   position[r]   the context's length + parents in front of r: what r's q and k are rotated by, two rows of a tree may share it
+ *   sees[r]       bit i: r itself or in front of it on its path (stairs_paged_attn.sees; 0 in a chunk)
+ * Rows of a request whose seq_len is smaller than its rows (that got no pages) have position -1 and see none, those behind the last request likewise.
+ * 0 <= n_seqs <= STAIRS_PAGED_MAX_SEQS, rows >= 0; position may be NULL. */
+#define STAIRS_TREE_MAX_ROWS   64
+typedef struct {
+  int32_t n_seqs, rows;
+  const int32_t *row_start;        /* [n_seqs + 1] */
+  const int32_t *seq_len;          /* [n_seqs] */
+  const int32_t *parent;           /* [rows] */
+  int32_t *position;               /* [rows] or NULL */
+  uint64_t *sees;                  /* [rows] */
+} stairs_tree;
+int stairs_tree_plan(const stairs_tree *tree, void *hip_stream);
+
+/* Validation of a tree: predicted[r] is the token the model says comes behind row r (the argmax of its logits, say).  From row 0 on, a row
+ * whose token is the one predicted for its parent is kept, and so on from that row; of several such children the first.  A row with a
+ * negative token goes with its parent whatever is predicted (a prompt's rows).  A chain of parents is the stairs validation.
+ *   kept[b]       rows of the path, 1 and more (0: the request has none, or got no pages)
+ *   cached[b]     the context's length + kept: the next plan's (which may be the same array); left as it was if the request got no pages
+ *   path[row_start[b] + j], emitted[...]   the path's j-th row, ascending, and the token predicted for it; -1 behind the path and behind the
+ *                 last request
+ * All rows of a chunk are kept. */
+typedef struct {
+  int32_t n_seqs, rows;
+  const int32_t *row_start;        /* [n_seqs + 1] */
+  const int32_t *seq_len;          /* [n_seqs] */
+  const int32_t *parent;           /* [rows] */
+  const int32_t *token, *predicted;/* [rows] */
+  int32_t *kept, *cached;          /* [n_seqs] */
+  int32_t *path, *emitted;         /* [rows] */
+} stairs_tree_path;
+int stairs_tree_walk(const stairs_tree_path *walk, void *hip_stream);
+
+/* What the path's rows have in n_caches pools (HOST array; one shape, type and page numbering: a model's layers) to the positions behind the context:
+ * position context + path[row_start[b] + j] to context + j, j < kept[b], as they are held.  path ascending from 0 or more (as stairs_tree_walk
+ * leaves it; kept and path may be the caller's own); rows that stay, and those whose page or position is none, are not touched.  Requests with more
+ * than STAIRS_TREE_MAX_ROWS rows keep all of them: nothing moves.  0 <= n_caches <= 4096. */
+typedef struct {
+  int32_t n_seqs, max_blocks, rows;
+  const int32_t *block_table;      /* [n_seqs][max_blocks] */
+  const int32_t *row_start;        /* [n_seqs + 1] */
+  const int32_t *seq_len;          /* [n_seqs] */
+  const int32_t *path;             /* [rows] */
+  const int32_t *kept;             /* [n_seqs] */
+} stairs_paged_path;
+int stairs_paged_compact(const stairs_paged_cache *caches, int32_t n_caches, const stairs_paged_path *path, void *hip_stream);
 
 /* A token from each row of logits [rows][vocab] (FP32, BF16 or FP16; rows ld elements apart), with one uniform random number in
  * [0, 1) a row.  Tokens are ordered by logit, larger first, equal ones by index; weight w_v = exp((x_v - max) / temperature).

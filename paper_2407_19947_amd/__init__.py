@@ -11,4 +11,5 @@ from .binding import (  # noqa: F401
     EXPORTED_SYMBOLS, stairs_decode_sampled, stairs_generate_sampled, draft_propose_sampled, stairs_verify_sampled, StairsEncDec, stairs_encdec_init, stairs_encode, stairs_encdec_generate, stairs_rel_bucket,
     stairs_set_truncation, DTYPE_FP32, DTYPE_BF16, DTYPE_FP16, StairsPagedCache, StairsPagePlan, StairsPagedRows, StairsPagedAttention, StairsSampling,
     stairs_paged_plan, stairs_paged_append, stairs_paged_attention, stairs_paged_attention_workspace, stairs_sample_device, stairs_sample_workspace,
+    DTYPE_E4M3, StairsPagedRead, StairsTree, StairsTreeWalk, StairsPagedPath, stairs_paged_read, stairs_tree_plan, stairs_tree_walk, stairs_paged_compact,
 )

@@ -10,10 +10,10 @@ import numpy as np
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libstairs.so")
-_SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("stairs_kernels.hip", "stairs_block.hip", "stairs_api.hip", "stairs_paged.hip", "stairs_sampling.hip")]
+_SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("stairs_kernels.hip", "stairs_block.hip", "stairs_api.hip", "stairs_paged.hip", "stairs_tree.hip", "stairs_sampling.hip")]
 
 STAIRS_MAX_ROWS = 32
-DTYPE_FP32, DTYPE_BF16, DTYPE_FP16 = 0, 1, 2
+DTYPE_FP32, DTYPE_BF16, DTYPE_FP16, DTYPE_E4M3 = 0, 1, 2, 3
 
 EXPORTED_SYMBOLS = [
     "stairs_strerror", "stairs_last_error", "stairs_init", "stairs_free", "stairs_prefill",
@@ -24,6 +24,7 @@ EXPORTED_SYMBOLS = [
     "stairs_rel_bucket", "stairs_set_truncation",
     "stairs_paged_plan", "stairs_paged_append", "stairs_paged_attention", "stairs_paged_attention_workspace",
     "stairs_sample_device", "stairs_sample_workspace",
+    "stairs_paged_read", "stairs_tree_plan", "stairs_tree_walk", "stairs_paged_compact",
 ]
 
 
@@ -105,7 +106,7 @@ def _structure(name: str, doc: str, fields: str):
 # Arguments of the operators on device buffers; build one with keyword arguments, keep it as long as its buffers stay where
 # they are.  (The buffers are the caller's: an address does not keep a tensor alive.)
 StairsPagedCache = _structure("StairsPagedCache", "stairs_paged_cache: one layer's pool of pages.",
-                              "ptr k v; i32 dtype n_pages page_size n_kv_heads head_dim")
+                              "ptr k v; i32 dtype n_pages page_size n_kv_heads head_dim held; ptr scale")
 StairsPagePlan = _structure("StairsPagePlan", "stairs_page_plan: requests, pages and rows of a step.",
                             "i32 n_seqs max_blocks n_pages page_size max_rows; ptr cached fresh held n_free block_table free_pages held_out "
                             "n_free_out row_start seq_len position slot")
@@ -113,7 +114,14 @@ StairsPagedRows = _structure("StairsPagedRows", "stairs_paged_rows: new rows to 
                              "i32 rows n_heads; ptr q k v q_out; i64 q_stride k_stride v_stride q_out_stride; ptr position slot; f32 rope_theta")
 StairsPagedAttention = _structure("StairsPagedAttention", "stairs_paged_attn: attention of new rows over pages.",
                                   "i32 n_seqs max_blocks rows n_heads max_fresh; ptr q out; i64 q_stride out_stride; ptr block_table row_start "
-                                  "seq_len; f32 scale; ptr workspace; i64 workspace_bytes")
+                                  "seq_len; f32 scale; ptr workspace; i64 workspace_bytes; ptr sees")
+StairsPagedRead = _structure("StairsPagedRead", "stairs_paged_out: rows to read out of their pages.", "i32 rows; ptr k v; i64 k_stride v_stride; ptr slot")
+StairsTree = _structure("StairsTree", "stairs_tree: parents of drafted tokens, and what follows from them.",
+                        "i32 n_seqs rows; ptr row_start seq_len parent position sees")
+StairsTreeWalk = _structure("StairsTreeWalk", "stairs_tree_path: drafted and predicted tokens, and the path that is accepted.",
+                            "i32 n_seqs rows; ptr row_start seq_len parent token predicted kept cached path emitted")
+StairsPagedPath = _structure("StairsPagedPath", "stairs_paged_path: rows to move behind their contexts.",
+                             "i32 n_seqs max_blocks rows; ptr block_table row_start seq_len path kept")
 StairsSampling = _structure("StairsSampling", "stairs_sampling: rows of logits and the rules to draw from them.",
                             "i32 dtype rows vocab; i64 ld; ptr logits temperature top_k top_p min_p uniform token logprob kept workspace; "
                             "i64 workspace_bytes")
@@ -168,6 +176,10 @@ def lib() -> C.CDLL:
     L.stairs_paged_append.argtypes = [C.POINTER(StairsPagedCache), C.POINTER(StairsPagedRows), vp]
     L.stairs_paged_attention.argtypes = [C.POINTER(StairsPagedCache), C.POINTER(StairsPagedAttention), vp]
     L.stairs_paged_attention_workspace.argtypes = [C.POINTER(StairsPagedCache), C.POINTER(StairsPagedAttention)]
+    L.stairs_paged_read.argtypes = [C.POINTER(StairsPagedCache), C.POINTER(StairsPagedRead), vp]
+    L.stairs_tree_plan.argtypes = [C.POINTER(StairsTree), vp]
+    L.stairs_tree_walk.argtypes = [C.POINTER(StairsTreeWalk), vp]
+    L.stairs_paged_compact.argtypes = [C.POINTER(StairsPagedCache), i32, C.POINTER(StairsPagedPath), vp]
     L.stairs_sample_device.argtypes = [C.POINTER(StairsSampling), vp]
     L.stairs_sample_workspace.argtypes = [C.POINTER(StairsSampling)]
     for name in EXPORTED_SYMBOLS:
@@ -386,6 +398,28 @@ def _bytes(n: int, where: str) -> int:
 def stairs_paged_attention_workspace(cache: StairsPagedCache, attn: StairsPagedAttention) -> int:
     """Bytes of zeroed device memory that stairs_paged_attention takes as attn.workspace."""
     return _bytes(lib().stairs_paged_attention_workspace(cache, attn), "stairs_paged_attention_workspace")
+
+
+def stairs_paged_read(cache: StairsPagedCache, out: StairsPagedRead, stream: Optional[int] = None) -> None:
+    """Rows out of their pages."""
+    _check(lib().stairs_paged_read(cache, out, stream), "stairs_paged_read")
+
+
+def stairs_tree_plan(tree: StairsTree, stream: Optional[int] = None) -> None:
+    """Positions of drafted trees' rows, and which of the new rows each sees."""
+    _check(lib().stairs_tree_plan(tree, stream), "stairs_tree_plan")
+
+
+def stairs_tree_walk(walk: StairsTreeWalk, stream: Optional[int] = None) -> None:
+    """The path of each drafted tree that the predictions follow."""
+    _check(lib().stairs_tree_walk(walk, stream), "stairs_tree_walk")
+
+
+def stairs_paged_compact(caches: Sequence[StairsPagedCache], path: StairsPagedPath, stream: Optional[int] = None) -> None:
+    """The accepted rows to the positions behind their contexts, in the pools of all layers (a sequence, or a ctypes array of them)."""
+    n = len(caches)
+    array = caches if isinstance(caches, C.Array) else (StairsPagedCache * max(n, 1))(*caches)
+    _check(lib().stairs_paged_compact(array, n, path, stream), "stairs_paged_compact")
 
 
 def stairs_sample_device(sampling: StairsSampling, stream: Optional[int] = None) -> None:

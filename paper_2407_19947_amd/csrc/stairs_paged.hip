@@ -1,8 +1,7 @@
-// Operators over paged key/value caches: pages and slots for the requests of a step, storing the new rows, attention of the
-// new rows over the pages.  The page layout is the tiled layout of the framework's own half caches (k_cache_off, v_cache_off),
+// Operators over paged key/value caches: pages and slots for the requests of a step, storing the new rows and reading rows back,
+// attention of the new rows over the pages.  The page layout is the tiled layout of the framework's own half caches (k_cache_off, v_cache_off),
 // page by page.
-#include "../../include/stairs.h"
-#include "stairs_device.h"
+#include "stairs_paged.h"
 
 #include <algorithm>
 #include <cmath>
@@ -164,6 +163,68 @@ template <> struct Elem<_Float16> {
   static __device__ __forceinline__ _Float16 down(float v) { return (_Float16)v; }
 };
 
+// ---- rows in 8 bits -------------------------------------------------------------------------------------------------
+// A row of a head is codes times 2^(b - 127): b the smallest byte from 1 on with amax <= 448 * 2^(b - 127) = 1.75 * 2^(b - 119).  A float
+// amax = 1.f * 2^(E - 127) asks for b = E - 8, one more where its mantissa is past 1.75.  (A power of two loses nothing against a finer scale: codes are
+// floats themselves, with 4 bits down to 2^-14 of the largest, and products with it are exact.)
+__device__ __forceinline__ uint32_t finite_bits(float x) {       // of |x|; 0 for infinities and NaN
+  const uint32_t u = __float_as_uint(x) & 0x7FFFFFFFu;
+  return u < 0x7F800000u ? u : 0u;
+}
+// Rows of halves: magnitudes past 61440 are held as 61440 (within a half step, 2^-4; the next number is past the largest half).  -> what is then the
+// largest finite one
+constexpr uint32_t kHalfTop = 0x47700000u;
+__device__ __forceinline__ uint32_t cut(float* x, int n) {
+#pragma unroll
+  for (int i = 0; i < n; ++i)
+    if (finite_bits(x[i]) > kHalfTop) x[i] = copysignf(61440.f, x[i]);
+  return kHalfTop;
+}
+__device__ __forceinline__ uint32_t scale_byte(uint32_t amax_bits) {
+  const int b = (int)(amax_bits >> 23) - 8 + ((amax_bits & 0x7FFFFFu) > 0x600000u);
+  return (uint32_t)max(b, 1);
+}
+__device__ __forceinline__ float scale_inverse(uint32_t b) { return __uint_as_float((254u - b) << 23); }     // 2^(127 - b), b at most 247
+__device__ __forceinline__ float scale_of(uint32_t bytes, int i) {                                           // byte i of four
+  return __uint_as_float((i < 3 ? bytes << (23 - 8 * i) : bytes >> 1) & 0x7F800000u);
+}
+__device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d) {
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+}
+template <typename T> struct Wide;
+template <> struct Wide<__bf16> {
+  template <bool HI> static __device__ __forceinline__ uint32_t pair(uint32_t codes, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, HI));
+  }
+};
+template <> struct Wide<_Float16> {
+  template <bool HI> static __device__ __forceinline__ uint32_t pair(uint32_t codes, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, HI));
+  }
+};
+// eight codes as numbers of the type, times a power of two
+template <typename T>
+__device__ __forceinline__ uint4 widen(uint32_t lo, uint32_t hi, float scale) {
+  return make_uint4(Wide<T>::template pair<false>(lo, scale), Wide<T>::template pair<true>(lo, scale), Wide<T>::template pair<false>(hi, scale),
+                    Wide<T>::template pair<true>(hi, scale));
+}
+// the same, a power of two for each: a pair converted with either's
+__device__ __forceinline__ uint32_t low_high(uint32_t a, uint32_t b) { return (a & 0xFFFFu) | (b & 0xFFFF0000u); }
+template <typename T>
+__device__ __forceinline__ uint4 widen(uint32_t lo, uint32_t hi, const float (&f)[8]) {
+  typedef Wide<T> W;
+  return make_uint4(low_high(W::template pair<false>(lo, f[0]), W::template pair<false>(lo, f[1])), low_high(W::template pair<true>(lo, f[2]), W::template pair<true>(lo, f[3])),
+                    low_high(W::template pair<false>(hi, f[4]), W::template pair<false>(hi, f[5])), low_high(W::template pair<true>(hi, f[6]), W::template pair<true>(hi, f[7])));
+}
+__device__ __forceinline__ uint32_t group_max(uint32_t v, int lanes) {                                       // of 4, 8 or 16 adjacent lanes
+  auto step = [&](auto ctrl) { v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xF, 0xF, true)); };
+  step(std::integral_constant<int, kDppXor1>{});
+  step(std::integral_constant<int, kDppXor2>{});
+  if (lanes > 4) step(std::integral_constant<int, kDppHalfMirror>{});
+  if (lanes > 8) step(std::integral_constant<int, kDppRor8>{});
+  return v;
+}
+
 // sine and cosine of `turns` whole turns: the nearest quarter turn, and the series for what is left, |x| <= pi / 4 (the next terms are
 // below 2^-28)
 __device__ __forceinline__ float2 cos_sin(double turns) {
@@ -201,13 +262,15 @@ __device__ __forceinline__ X ld_once_as(const void* p) {
 // values; as it is 57.5 = 3.5 TB/s, reading 8 % more than the rows have,
 // writing no more.)
 constexpr int kAppendRows = 32;
-template <typename T, int HD>
+template <typename T, int HD, bool H8>
 __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stairs_paged_rows a, double log2_theta) {
   constexpr int AHEAD = 19, BEHIND = 16;                        // rows around these that decide how theirs are stored
   __shared__ union {
     float2 cs[kAppendRows][HD / 2];
     T v[kAppendRows + AHEAD][HD];
+    uint8_t v8[kAppendRows + AHEAD][HD];
   } lds;
+  __shared__ uint8_t s_vb[H8 ? kAppendRows + AHEAD : 1];        // the values' powers of two
   __shared__ int s_slots[BEHIND + kAppendRows + AHEAD], s_pos[kAppendRows], s_unit[kAppendRows], s_units, s_end;
   const int* const s_slot = s_slots + BEHIND;
   // (an XCD takes rows that follow each other: lines that two work-groups share meet in one L2; 16000 rows of 48 heads 104 -> 101 us)
@@ -277,6 +340,53 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
     *reinterpret_cast<x8*>(dst) = lo;
     *reinterpret_cast<x8*>(dst + HD / 2) = hi;
   }
+  const size_t head_scales = (size_t)c.page_size * 2;
+  uint8_t* const scales = static_cast<uint8_t*>(c.scale);
+  if constexpr (H8) {
+    // four lanes have a row: each 8 dims of every 32, so that what it stores are whole places of 16 bytes
+    constexpr int NX = HD / 32;
+    for (int i = tid; i < nkh * kAppendRows * 4; i += 256) {
+      const int g = i & 3, r = i / 4 % kAppendRows, h = k0 + i / (4 * kAppendRows), slot = s_slot[r];
+      if (r >= n || slot < 0) continue;
+      const T* src = static_cast<const T*>(a.k) + (size_t)(t0 + r) * a.k_stride + h * HD + 8 * g;
+      x8 in[NX];
+#pragma unroll
+      for (int j = 0; j < NX; ++j) in[j] = ld_once_as<x8>(src + 32 * j);
+      float x[NX][8];
+#pragma unroll
+      for (int j = 0; j < NX; ++j)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[j][k] = Elem<T>::up(in[j][k]);
+      if (rotate) {
+#pragma unroll
+        for (int j = 0; j < NX / 2; ++j)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float2 v = rope_rotate(x[j][k], x[j + NX / 2][k], lds.cs[r][32 * j + 8 * g + k]);
+            x[j][k] = v.x;
+            x[j + NX / 2][k] = v.y;
+          }
+      }
+      uint32_t top = 0;
+#pragma unroll
+      for (int j = 0; j < NX; ++j)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = max(top, finite_bits(x[j][k]));
+      if (__is_same(T, _Float16) && top > kHalfTop) top = cut(x[0], NX * 8);
+      const uint32_t b = scale_byte(group_max(top, 4));
+      const float f = scale_inverse(b);
+      uint2 code[NX];
+#pragma unroll
+      for (int j = 0; j < NX; ++j)
+        code[j] = make_uint2(codes_of(x[j][0] * f, x[j][1] * f, x[j][2] * f, x[j][3] * f), codes_of(x[j][4] * f, x[j][5] * f, x[j][6] * f, x[j][7] * f));
+      const int p = slot & (c.page_size - 1);
+      const size_t head = (size_t)(slot >> ps_shift) * nk + h;
+      uint8_t* dst = static_cast<uint8_t*>(c.k) + head * head_elems + k_held_off(p, 8 * g, HD);
+#pragma unroll
+      for (int t = 0; t < HD / 64; ++t) *reinterpret_cast<uint4*>(dst + t * 1024) = make_uint4(code[2 * t].x, code[2 * t].y, code[2 * t + 1].x, code[2 * t + 1].y);
+      if (g == 0) scales[head * head_scales + scale_off(p)] = (uint8_t)b;
+    }
+  } else
   for (int i = tid; i < nkh * kAppendRows * PAIRS; i += 256) {  // (rows that are neighbours in a tile one behind the other)
     const int e = i % PAIRS * 8, r = i / PAIRS % kAppendRows, h = k0 + i / (PAIRS * kAppendRows), slot = s_slot[r];
     if (r >= n || slot < 0) continue;
@@ -294,9 +404,48 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
     __syncthreads();
     for (int i = tid; i < staged * (HD / 8); i += 256) {
       const int r = i / (HD / 8), e = i % (HD / 8) * 8;
-      *reinterpret_cast<x8*>(&lds.v[r][e]) = ld_once_as<x8>(static_cast<const T*>(a.v) + (size_t)(t0 + r) * a.v_stride + h * HD + e);
+      const x8 in = ld_once_as<x8>(static_cast<const T*>(a.v) + (size_t)(t0 + r) * a.v_stride + h * HD + e);
+      if constexpr (H8) {
+        float x[8];
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          x[k] = Elem<T>::up(in[k]);
+          top = max(top, finite_bits(x[k]));
+        }
+        if (__is_same(T, _Float16) && top > kHalfTop) top = cut(x, 8);
+        const uint32_t b = scale_byte(group_max(top, HD / 8));
+        const float f = scale_inverse(b);
+        *reinterpret_cast<uint2*>(&lds.v8[r][e]) = make_uint2(codes_of(x[0] * f, x[1] * f, x[2] * f, x[3] * f), codes_of(x[4] * f, x[5] * f, x[6] * f, x[7] * f));
+        if (e == 0) s_vb[r] = (uint8_t)b;
+      } else {
+        *reinterpret_cast<x8*>(&lds.v[r][e]) = in;
+      }
     }
     __syncthreads();
+    if constexpr (H8) {
+      // a place of 16 bytes: dims e and e + 16, eight positions of either
+      for (int i = tid; i < units * (HD / 2); i += 256) {
+        const int j = i % (HD / 2), e = (j >> 4) * 32 + (j & 15), u = s_unit[i / (HD / 2)], r = u >> 2, kind = u & 3, slot = s_slot[r], p = slot & (c.page_size - 1);
+        const size_t head = (size_t)(slot >> ps_shift) * nk + h;
+        uint8_t* dst = static_cast<uint8_t*>(c.v) + head * head_elems + v_held_off(p, e, HD);
+        uint8_t* sdst = scales + head * head_scales + scale_off(p) + 8;
+        auto four = [&](int row, int dim) { return lds.v8[row][dim] | lds.v8[row + 1][dim] << 8 | lds.v8[row + 2][dim] << 16 | (uint32_t)lds.v8[row + 3][dim] << 24; };
+        auto bytes = [&](int row) { return s_vb[row] | s_vb[row + 1] << 8 | s_vb[row + 2] << 16 | (uint32_t)s_vb[row + 3] << 24; };
+        if (kind == 1) {
+          dst[0] = lds.v8[r][e];
+          dst[8] = lds.v8[r][e + 16];
+          if (j == 0) *sdst = s_vb[r];
+        } else if (kind == 2) {
+          *reinterpret_cast<uint32_t*>(dst) = four(r, e);
+          *reinterpret_cast<uint32_t*>(dst + 8) = four(r, e + 16);
+          if (j == 0) *reinterpret_cast<uint32_t*>(sdst) = bytes(r);
+        } else {
+          *reinterpret_cast<uint4*>(dst) = make_uint4(four(r, e), four(r + 16, e), four(r, e + 16), four(r + 16, e + 16));
+          if (j == 0) *reinterpret_cast<uint2*>(sdst) = make_uint2(bytes(r), bytes(r + 16));
+        }
+      }
+    } else
     for (int i = tid; i < units * HD; i += 256) {
       const int e = i % HD, r = s_unit[i / HD] >> 2, kind = s_unit[i / HD] & 3, slot = s_slot[r];
       T* dst = static_cast<T*>(c.v) + ((size_t)(slot >> ps_shift) * nk + h) * head_elems + v_cache_off(slot & (c.page_size - 1), e, HD);
@@ -314,6 +463,138 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
           *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(v);
         }
       }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// reading rows back
+// ---------------------------------------------------------------------------------------
+// As k_paged_append the other way: a work-group has 32 rows and some of the heads; keys go from a tile's places to the rows directly, values through
+// LDS, the eight positions of a place at once where they are rows of the work-group in that order, four or one otherwise.
+__device__ __forceinline__ uint16_t half_bits(__bf16, float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+__device__ __forceinline__ uint16_t half_bits(_Float16, float x) {   // (a row's largest half may have been rounded up to 2^16)
+  return __builtin_bit_cast(uint16_t, (_Float16)(fabsf(x) > 65504.f && fabsf(x) < INFINITY ? copysignf(65504.f, x) : x));
+}
+// eight codes times powers of two, as bits of the type
+template <typename T>
+__device__ __forceinline__ uint4 plain_row(uint32_t lo, uint32_t hi, float f) {
+  uint32_t out[4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t u = i ? hi : lo;
+    const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8(u, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
+    out[2 * i] = half_bits(T{}, a.x * f) | (uint32_t)half_bits(T{}, a.y * f) << 16;
+    out[2 * i + 1] = half_bits(T{}, b.x * f) | (uint32_t)half_bits(T{}, b.y * f) << 16;
+  }
+  return make_uint4(out[0], out[1], out[2], out[3]);
+}
+template <typename T, int HD, bool H8>
+__global__ __launch_bounds__(256) void k_paged_read(stairs_paged_cache c, stairs_paged_out a) {
+  constexpr int R = kAppendRows;
+  __shared__ uint16_t s_v[R][HD + 8];
+  __shared__ int s_slot[R], s_unit[R], s_units;
+  const int xcd = blockIdx.x & 7, share = gridDim.x >> 3, more = gridDim.x & 7;
+  const int t0 = (xcd * share + min(xcd, more) + (int)(blockIdx.x >> 3)) * R, n = min(R, a.rows - t0);
+  const int nk = c.n_kv_heads, h0 = nk * (int)blockIdx.y / (int)gridDim.y, h1 = nk * ((int)blockIdx.y + 1) / (int)gridDim.y;
+  const int tid = threadIdx.x, lane = tid & 63, ps_shift = __builtin_ctz(c.page_size);
+  const unsigned slots = (unsigned)c.n_pages * (unsigned)c.page_size;
+  if (tid < R) {
+    const int slot = tid < n ? a.slot[t0 + tid] : -1;
+    s_slot[tid] = (unsigned)slot < slots ? slot : -1;
+  }
+  __syncthreads();
+  if (tid < 64) {
+    auto quad = [&](int r) { return r + 3 < n && s_slot[r] >= 0 && (s_slot[r] & 3) == 0 && s_slot[r + 1] == s_slot[r] + 1 && s_slot[r + 2] == s_slot[r] + 2 && s_slot[r + 3] == s_slot[r] + 3; };
+    auto pair = [&](int r) { return r + 19 < n && quad(r) && (s_slot[r] & 16) == 0 && s_slot[r + 16] == s_slot[r] + 16 && quad(r + 16); };
+    int kind = 0;                                               // 3: two quads, 2: one, 1: a single row, 0: read with another
+    if (lane < n && s_slot[lane] >= 0) {
+      const int first = lane - (s_slot[lane] & 3);
+      if (first < 0 || !quad(first)) kind = 1;
+      else if (first == lane) kind = pair(lane) ? 3 : (s_slot[lane] & 16) && lane >= 16 && pair(lane - 16) ? 0 : 2;
+    }
+    const unsigned long long units = __ballot(kind > 0);
+    if (kind > 0) s_unit[__popcll(units & ((1ull << lane) - 1))] = lane << 2 | kind;
+    if (lane == 0) s_units = __popcll(units);
+  }
+  const size_t head_bytes = (size_t)c.page_size * HD * (H8 ? 1 : 2), head_scales = (size_t)c.page_size * 2;
+  const uint8_t* const scales = static_cast<const uint8_t*>(c.scale);
+  if (a.k && blockIdx.z == 0) {
+    for (int i = tid; i < (h1 - h0) * R * 4; i += 256) {
+      const int g = i & 3, r = i / 4 % R, h = h0 + i / (4 * R), slot = s_slot[r];
+      if (r >= n || slot < 0) continue;
+      const int p = slot & (c.page_size - 1);
+      const size_t head = (size_t)(slot >> ps_shift) * nk + h;
+      const uint8_t* src = static_cast<const uint8_t*>(c.k) + head * head_bytes;
+      uint16_t* dst = static_cast<uint16_t*>(a.k) + (size_t)(t0 + r) * a.k_stride + h * HD + 8 * g;
+      if constexpr (H8) {
+        const float f = scale_of(scales[head * head_scales + scale_off(p)], 0);
+#pragma unroll
+        for (int t = 0; t < HD / 64; ++t) {
+          const uint4 v = *reinterpret_cast<const uint4*>(src + k_held_off(p, 8 * g, HD) + t * 1024);
+          *reinterpret_cast<uint4*>(dst + 64 * t) = plain_row<T>(v.x, v.y, f);
+          *reinterpret_cast<uint4*>(dst + 64 * t + 32) = plain_row<T>(v.z, v.w, f);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < HD / 32; ++j) *reinterpret_cast<uint4*>(dst + 32 * j) = *reinterpret_cast<const uint4*>(src + 2 * k_cache_off(p, 32 * j + 8 * g, HD));
+      }
+    }
+  }
+  if (!a.v || (gridDim.z > 1 && blockIdx.z == 0)) return;
+  constexpr int D = H8 ? HD / 2 : HD;                           // places of 16 bytes of a unit
+  for (int h = h0; h < h1; ++h) {
+    __syncthreads();
+    const int units = s_units;
+    for (int i = tid; i < units * D; i += 256) {
+      const int j = i % D, e = H8 ? (j >> 4) * 32 + (j & 15) : j, r = s_unit[i / D] >> 2, kind = s_unit[i / D] & 3, slot = s_slot[r], p = slot & (c.page_size - 1);
+      const size_t head = (size_t)(slot >> ps_shift) * nk + h;
+      if constexpr (H8) {
+        const uint8_t* src = static_cast<const uint8_t*>(c.v) + head * head_bytes + v_held_off(p, e, HD);
+        const uint8_t* sc = scales + head * head_scales + scale_off(p) + 8;
+        auto put = [&](int row, uint32_t codes, uint32_t bytes, int dim, int count) {
+          const f32x2_t x = __builtin_amdgcn_cvt_pk_f32_fp8(codes, false), y = __builtin_amdgcn_cvt_pk_f32_fp8(codes, true);
+          const float v[4] = {x.x, x.y, y.x, y.y};
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (k < count) s_v[row + k][dim] = half_bits(T{}, v[k] * scale_of(bytes, k));
+        };
+        if (kind == 3) {
+          const uint4 v = *reinterpret_cast<const uint4*>(src);
+          const uint2 b = *reinterpret_cast<const uint2*>(sc);
+          put(r, v.x, b.x, e, 4);
+          put(r + 16, v.y, b.y, e, 4);
+          put(r, v.z, b.x, e + 16, 4);
+          put(r + 16, v.w, b.y, e + 16, 4);
+        } else if (kind == 2) {
+          const uint32_t b = *reinterpret_cast<const uint32_t*>(sc);
+          put(r, *reinterpret_cast<const uint32_t*>(src), b, e, 4);
+          put(r, *reinterpret_cast<const uint32_t*>(src + 8), b, e + 16, 4);
+        } else {
+          put(r, src[0], *sc, e, 1);
+          put(r, src[8], *sc, e + 16, 1);
+        }
+      } else {
+        const uint16_t* src = static_cast<const uint16_t*>(c.v) + head * (head_bytes / 2) + v_cache_off(p, e, HD);
+        if (kind == 1) {
+          s_v[r][e] = *src;
+        } else {
+          uint16_t v[8];
+          if (kind == 3) *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(src);
+          else *reinterpret_cast<uint2*>(v) = *reinterpret_cast<const uint2*>(src);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) s_v[r + k][e] = v[k];
+          if (kind == 3)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s_v[r + 16 + k][e] = v[4 + k];
+        }
+      }
+    }
+    __syncthreads();
+    for (int i = tid; i < n * (HD / 8); i += 256) {
+      const int r = i / (HD / 8), e = i % (HD / 8) * 8;
+      if (s_slot[r] < 0) continue;
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.v) + (size_t)(t0 + r) * a.v_stride + h * HD + e) = *reinterpret_cast<const uint4*>(&s_v[r][e]);
     }
   }
 }
@@ -673,6 +954,30 @@ __device__ __forceinline__ void join_waves(const stairs_paged_cache& c, const st
   if (w.pieces > 1) join_pieces<T, HD, COLS>(c, a, sp, w, reinterpret_cast<float2*>(s_o), s_last);
 }
 
+// ---- what a column sees -------------------------------------------------------------------------------------------
+// Kernels come in forms: keys and values of the cache's type and rows that see the positions up to their own (0); with what a column sees as a count
+// of keys in front and 64 bits for those behind them (kMasks: trees, and as bits or as a count every other row); over 8-bit pages (kHeld8, masks always:
+// they are looked at only in a sequence's last keys).
+constexpr int kMasks = 1, kHeld8 = 2;
+struct Sees {
+  int open;                   // keys in front of this one
+  unsigned long long bits;    // and of the 64 from it on
+};
+__device__ __forceinline__ bool is_tree(const stairs_paged_attn& a, const Piece& w) { return a.sees && w.rows <= STAIRS_TREE_MAX_ROWS; }
+__device__ __forceinline__ Sees sees_of(const stairs_paged_attn& a, const Piece& w, int row, int limit) {
+  const int pos0 = w.len - w.rows;
+  if (!is_tree(a, w)) return {max(min(pos0 + row, limit - 1) + 1, 0), 0};
+  unsigned long long bits = a.sees[w.row0 + row] & (~0ull >> (64 - w.rows));
+  if (pos0 < 0) bits = pos0 > -64 ? bits >> -pos0 : 0;           // (rows in front of position 0 are nowhere)
+  return {max(min(pos0, limit), 0), bits};
+}
+__device__ __forceinline__ uint32_t block_of(const Sees& s, int key0) {   // the 32 keys from key0 on
+  const int d = key0 - s.open;
+  if (d <= -32) return ~0u;
+  if (d < 0) return (~0u >> (32 + d)) | (uint32_t)(s.bits << -d);
+  return d < 64 ? (uint32_t)(s.bits >> d) : 0u;
+}
+
 // ---- few columns: a wave per 32 keys ----------------------------------------------------------------------------------
 // Bound by the bytes of the cache.  A work-group takes a piece of a tile of 16 CT columns; its four waves take 32-key blocks in
 // turn, straight from memory into the matrix operands (a block of a head is 2 x 64 HD contiguous bytes, every load 1 KiB of a
@@ -686,30 +991,41 @@ struct RowsLds {
   float o[4][16 * CT][HD + 4], m[4][16 * CT], l[4][16 * CT];
   int last;
 };
-template <typename T, int HD, int CT>
+template <typename T, int HD, int CT, int F>
 __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, float scale2, RowsLds<HD, CT>& lds) {
+  constexpr bool H8 = F & kHeld8, M = F & kMasks;
   typedef typename Elem<T>::x8 x8;
-  constexpr int KK = HD / 32, ET = HD / 16;
+  // Codes are numbers of either type.  A score is multiplied by its key's power of two, a probability by its value's: in bfloat16, so that whatever
+  // power of two that is stays in range; two numbers of it are as exact as half's two.
+  typedef std::conditional_t<H8, __bf16, T> VT;
+  typedef typename Elem<VT>::x8 vx8;
+  typedef std::conditional_t<H8, uint8_t, T> PT;
+  constexpr int KK = HD / 32, ET = HD / 16, NK = H8 ? KK : 2 * KK, NV = H8 ? ET / 2 : ET;
   Piece w;
   if (!find_piece(c, a, sp, w)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, g = lane >> 4;
   const int G = a.n_heads / c.n_kv_heads, cols = w.rows * G, col0 = w.group * 16 * CT;
   const int limit = a.max_blocks * c.page_size;
   const int pos0 = w.len - w.rows;                              // position of the sequence's first row
-  const int first_last = min(pos0 + col0 / G, limit - 1);        // last position the tile's first and last column see
-  const int last_last = min(pos0 + (min(cols, col0 + 16 * CT) - 1) / G, limit - 1);
+  const bool tree = M && is_tree(a, w);
+  // last position that all of the tile's columns see, that any does
+  const int first_last = tree ? min(pos0, limit) - 1 : min(pos0 + col0 / G, limit - 1);
+  const int last_last = tree ? min(w.len, limit) - 1 : min(pos0 + (min(cols, col0 + 16 * CT) - 1) / G, limit - 1);
   int last[CT];
+  Sees sees[CT];
   x8 q[CT][KK];
   bool had_odd = false;                                         // the wave has left infinities or NaNs in its part of lds.o
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
     const int col = col0 + ct * 16 + j;
     last[ct] = -1;
+    sees[ct] = {0, 0};
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) q[ct][kk] = x8{};
     if (col < cols) {
       const int r = col / G;
       last[ct] = min(pos0 + r, limit - 1);
+      if constexpr (M) sees[ct] = sees_of(a, w, r, limit);
       const T* qp = static_cast<const T*>(a.q) + (size_t)(w.row0 + r) * a.q_stride + (w.kvh * G + col - r * G) * HD + g * 8;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) q[ct][kk] = *reinterpret_cast<const x8*>(qp + kk * 32);
@@ -725,8 +1041,10 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
     for (int et = 0; et < ET; ++et) o[ct][et] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const size_t head_elems = (size_t)c.page_size * HD, page_elems = head_elems * c.n_kv_heads;
-  const T* K = static_cast<const T*>(c.k) + w.kvh * head_elems;
-  const T* V = static_cast<const T*>(c.v) + w.kvh * head_elems;
+  const PT* K = static_cast<const PT*>(c.k) + w.kvh * head_elems;
+  const PT* V = static_cast<const PT*>(c.v) + w.kvh * head_elems;
+  constexpr int PER = 16 / sizeof(PT);                          // elements of a load
+  const uint8_t* S = H8 ? static_cast<const uint8_t*>(c.scale) + w.kvh * (size_t)c.page_size * 2 : nullptr;
   const int* table = a.block_table + (size_t)w.seq * a.max_blocks;
   const int ps_shift = __builtin_ctz(c.page_size);
 
@@ -748,14 +1066,15 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
       u = pages_at + 64;
     }
   };
-  uint4 kf[2 * KK], vf[ET];
+  uint4 kf[NK], vf[NV], scales{};                               // (scales: of the lane's eight keys, then of their values)
   auto block_at = [&](int u) -> size_t {                        // elements in front of the block in its pool
     const int key = u * kRowUnit + wave * 32;
     return (size_t)__builtin_amdgcn_readlane(pages, u - pages_at) * page_elems + (size_t)(key & (c.page_size - 1)) * HD;
   };
   auto load_keys = [&](size_t at) {
 #pragma unroll
-    for (int i = 0; i < 2 * KK; ++i) kf[i] = ld_once_as<uint4>(K + at + (i * 64 + lane) * 8);
+    for (int i = 0; i < NK; ++i) kf[i] = ld_once_as<uint4>(K + at + (i * 64 + lane) * PER);
+    if constexpr (H8) scales = *reinterpret_cast<const uint4*>(S + at / (HD / 2) + g * 16);
   };
   if (w.u0 < u1) fetch_pages(w.u0);
   int u = next_block(w.u0);
@@ -766,7 +1085,15 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
   }
   while (u < u1) {
 #pragma unroll
-    for (int i = 0; i < ET; ++i) vf[i] = ld_once_as<uint4>(V + at + (i * 64 + lane) * 8);
+    for (int i = 0; i < NV; ++i) vf[i] = ld_once_as<uint4>(V + at + (i * 64 + lane) * PER);
+    float ks[8], vs[8];
+    if constexpr (H8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        ks[i] = scale_of(i < 4 ? scales.x : scales.y, i & 3) * scale2;
+        vs[i] = scale_of(i < 4 ? scales.z : scales.w, i & 3);
+      }
+    }
     f32x4 s[CT][2];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
@@ -774,7 +1101,16 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
       for (int t = 0; t < 2; ++t) {
         s[ct][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) s[ct][t] = mma(__builtin_bit_cast(x8, kf[t * KK + kk]), q[ct][kk], s[ct][t]);
+        for (int kk = 0; kk < KK; ++kk) {
+          uint4 k;
+          if constexpr (H8) {
+            const uint4 codes = kf[t * (KK / 2) + kk / 2];
+            k = kk & 1 ? widen<T>(codes.z, codes.w, 1.f) : widen<T>(codes.x, codes.y, 1.f);
+          } else {
+            k = kf[t * KK + kk];
+          }
+          s[ct][t] = mma(__builtin_bit_cast(x8, k), q[ct][kk], s[ct][t]);
+        }
       }
     const int key0 = u * kRowUnit + wave * 32;
     const int un = next_block(u + 1);
@@ -784,18 +1120,28 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
       load_keys(at);
     }
     const bool full = key0 + 31 <= first_last;
-    x8 p[CT], rest[CT];
+    vx8 p[CT], rest[CT];
+    uint32_t seen_bits[CT];                                     // of the lane's keys: (i >> 2) * 16 + (i & 3) for the i-th
+    if constexpr (M)
+      if (!full) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) seen_bits[ct] = block_of(sees[ct], key0) >> (g * 4);
+      }
+    auto sees_key = [&](int ct, int i) {
+      if constexpr (M) return (seen_bits[ct] >> ((i >> 2) * 16 + (i & 3)) & 1) != 0;
+      else return key0 + (i >> 2) * 16 + g * 4 + (i & 3) <= last[ct];
+    };
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
       float x[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = s[ct][i >> 2][i & 3] * scale2;
+      for (int i = 0; i < 8; ++i) x[i] = s[ct][i >> 2][i & 3] * (H8 ? ks[i] : scale2);
       if (!full) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = key0 + (i >> 2) * 16 + g * 4 + (i & 3) <= last[ct] ? x[i] : -INFINITY;
+        for (int i = 0; i < 8; ++i) x[i] = sees_key(ct, i) ? x[i] : -INFINITY;
       }
       float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-      if (__any(mx - m[ct] > Headroom<T>::slack)) {             // (the difference is exact where the scores are far from 0)
+      if (__any(mx - m[ct] > Headroom<VT>::slack)) {            // (the difference is exact where the scores are far from 0)
         const float mn = fmaxf(m[ct], groups_max(mx));
         const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[ct] - mn);
         m[ct] = mn;
@@ -806,11 +1152,23 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
       const float mr = m[ct] == -INFINITY ? 0.f : m[ct];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[i] = __builtin_amdgcn_exp2f(x[i] - mr + Headroom<T>::lift);
+        x[i] = __builtin_amdgcn_exp2f(x[i] - mr + Headroom<VT>::lift);
         l[ct] += x[i];
+        if constexpr (H8) x[i] = full || x[i] != 0.f ? x[i] * vs[i] : 0.f;   // (a power of two that nobody stored may be anything)
       }
       split(x, p[ct], rest[ct]);
     }
+    auto value = [&](int et) {
+      if constexpr (H8) return et & 1 ? widen<VT>(vf[et / 2].z, vf[et / 2].w, 1.f) : widen<VT>(vf[et / 2].x, vf[et / 2].y, 1.f);
+      else return vf[et];
+    };
+    auto add_value = [&](int et, uint4 v) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        o[ct][et] = mma(__builtin_bit_cast(vx8, v), rest[ct], o[ct][et]);
+        o[ct][et] = mma(__builtin_bit_cast(vx8, v), p[ct], o[ct][et]);
+      }
+    };
     if (!full) {
       // Some keys of the block are not seen by all columns.  Their probability is 0, and 0 times what is there must be 0: what
       // no column sees is cleared, and so are infinities and NaNs; those that some columns see are looked at again (odd_values).
@@ -822,42 +1180,43 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
       }
 #pragma unroll
       for (int et = 0; et < ET; ++et) {
-        odd |= clear_odd<T>(vf[et].x, keep[0]);
-        odd |= clear_odd<T>(vf[et].y, keep[1]);
-        odd |= clear_odd<T>(vf[et].z, keep[2]);
-        odd |= clear_odd<T>(vf[et].w, keep[3]);
+        uint4 held = value(et);
+        uint4& v = H8 ? held : vf[H8 ? 0 : et];
+        odd |= clear_odd<VT>(v.x, keep[0]);
+        odd |= clear_odd<VT>(v.y, keep[1]);
+        odd |= clear_odd<VT>(v.z, keep[2]);
+        odd |= clear_odd<VT>(v.w, keep[3]);
+        if constexpr (H8) add_value(et, v);
         __builtin_amdgcn_sched_barrier(0);                      // (one tile after the other: their temporaries share registers)
       }
       if (__any(odd != 0)) {
         if (!had_odd)
           for (int i = lane; i < 16 * CT * (HD + 4); i += 64) (&lds.o[wave][0][0])[i] = 0.f;
         had_odd = true;
-        x8 seen[CT];
+        vx8 seen[CT];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) seen[ct][i] = key0 + (i >> 2) * 16 + g * 4 + (i & 3) <= last[ct] ? (T)1.f : (T)0.f;
+          for (int i = 0; i < 8; ++i) seen[ct][i] = sees_key(ct, i) ? (VT)1.f : (VT)0.f;
 #pragma unroll 1
         for (int et = 0; et < ET; ++et) {
-          uint4 v = *reinterpret_cast<const uint4*>(V + at_here + (et * 64 + lane) * 8);
+          uint4 v = *reinterpret_cast<const uint4*>(V + at_here + ((H8 ? et / 2 : et) * 64 + lane) * PER);
+          if constexpr (H8) v = et & 1 ? widen<VT>(v.z, v.w, 1.f) : widen<VT>(v.x, v.y, 1.f);
           v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
-          const uint4 kinds = make_uint4(odd_kinds<T>(v.x), odd_kinds<T>(v.y), odd_kinds<T>(v.z), odd_kinds<T>(v.w));
+          const uint4 kinds = make_uint4(odd_kinds<VT>(v.x), odd_kinds<VT>(v.y), odd_kinds<VT>(v.z), odd_kinds<VT>(v.w));
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
-            const f32x4 count = mma(__builtin_bit_cast(x8, kinds), seen[ct], f32x4{0.f, 0.f, 0.f, 0.f});
+            const f32x4 count = mma(__builtin_bit_cast(vx8, kinds), seen[ct], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
             for (int i = 0; i < 4; ++i) lds.o[wave][ct * 16 + j][et * 16 + g * 4 + i] += odd_value(count[i]);
           }
         }
       }
     }
+    if (!H8 || full) {
 #pragma unroll
-    for (int et = 0; et < ET; ++et)
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        o[ct][et] = mma(__builtin_bit_cast(x8, vf[et]), rest[ct], o[ct][et]);
-        o[ct][et] = mma(__builtin_bit_cast(x8, vf[et]), p[ct], o[ct][et]);
-      }
+      for (int et = 0; et < ET; ++et) add_value(et, value(et));
+    }
     u = un;
   }
 
@@ -883,10 +1242,10 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
   __syncthreads();
   join_waves<T, HD, 16 * CT>(c, a, sp, w, lds.o, lds.m, lds.l, &lds.last);
 }
-template <typename T, int HD, int CT>
+template <typename T, int HD, int CT, int F>
 __global__ __launch_bounds__(256, 2) void k_paged_rows(stairs_paged_cache c, stairs_paged_attn a, Span sp, float scale2) {
   __shared__ RowsLds<HD, CT> lds;
-  attend_rows<T, HD, CT>(c, a, sp, scale2, lds);
+  attend_rows<T, HD, CT, F>(c, a, sp, scale2, lds);
 }
 
 // ---- many columns: tiles of 128 columns, keys and values shared through LDS ------------------------------------------
@@ -923,9 +1282,11 @@ struct ChunkLds {
   };
   int last;
 };
-template <typename T, int HD>
+template <typename T, int HD, int F>
 __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, float scale2, ChunkLds<HD>& lds) {
+  constexpr bool H8 = F & kHeld8, M = F & kMasks;
   typedef typename Elem<T>::x8 x8;
+  // (Over 8-bit pages the codes times their powers of two are what lies in LDS: numbers of T, exact but where a half has no steps any more.)
   constexpr int KS = HD / 16, DT = HD / 32;                     // steps of 16 dims, tiles of 32 dims
   Piece w;
   if (!find_piece(c, a, sp, w)) return;
@@ -933,11 +1294,16 @@ __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const 
   const int G = a.n_heads / c.n_kv_heads, cols = w.rows * G, col0 = w.group * kChunkCols, wcol = col0 + wave * 32;
   const int limit = a.max_blocks * c.page_size, pos0 = w.len - w.rows;
   // last positions that the work-group's, the wave's and the lane's columns see
-  const int last_group = min(pos0 + (min(cols, col0 + kChunkCols) - 1) / G, limit - 1);
-  const int first_wave = wcol < cols ? min(pos0 + wcol / G, limit - 1) : -1;
-  const int last_wave = wcol < cols ? min(pos0 + (min(cols, wcol + 32) - 1) / G, limit - 1) : -1;
+  const bool tree = M && is_tree(a, w);
+  const int last_tree = min(w.len, limit) - 1;
+  const int last_group = tree ? last_tree : min(pos0 + (min(cols, col0 + kChunkCols) - 1) / G, limit - 1);
+  const int first_wave = wcol >= cols ? -1 : tree ? min(pos0, limit) - 1 : min(pos0 + wcol / G, limit - 1);
+  const int last_wave = wcol >= cols ? -1 : tree ? last_tree : min(pos0 + (min(cols, wcol + 32) - 1) / G, limit - 1);
   const int col = wcol + n, row = col < cols ? col / G : 0;
   const int last = col < cols ? min(pos0 + row, limit - 1) : -1;
+  Sees sees{0, 0};
+  if constexpr (M)
+    if (col < cols) sees = sees_of(a, w, row, limit);
   const size_t at_row = (size_t)(w.row0 + row), at_head = (size_t)(w.kvh * G + (col < cols ? col - row * G : 0)) * HD;
   x8 q[KS];
   {
@@ -964,16 +1330,52 @@ __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const 
     if ((unsigned)pages >= (unsigned)c.n_pages) pages = -1;
   };
   auto page_of = [&](int u, int block) { return __builtin_amdgcn_readlane(pages, (u - pages_at) * 2 + block); };
+  // 8-bit pages: a wave takes 16 keys of a block and half of the dims of its values, through registers
+  constexpr int NS = HD / 64;
+  uint4 kr[NS], vr[NS];
+  uint32_t kb = 0;
+  uint2 vb{};
   auto request = [&](int u, int buf) {                          // (a block without a page: another's bytes, masked below)
     const int b = wave >> 1, key = u * kChunkUnit + b * 32;
-    const T* src = pool + (size_t)max(page_of(u, b), 0) * page_elems + (size_t)(key & (c.page_size - 1)) * HD;
+    const size_t at = (size_t)max(page_of(u, b), 0) * page_elems + (size_t)(key & (c.page_size - 1)) * HD;
+    if constexpr (H8) {
+      const size_t from = at + w.kvh * head_elems + (wave & 1) * NS * 1024;
+      const uint8_t* s = static_cast<const uint8_t*>(c.scale) + (at + w.kvh * head_elems) / (HD / 2);
 #pragma unroll
-    for (int i = 0; i < HD / 16; ++i) copy_tile(src, i * 1024, &lds.tile[buf][b][wave & 1][i * 64], lane * 16);
+      for (int i = 0; i < NS; ++i) {
+        kr[i] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(c.k) + from + i * 1024 + lane * 16);
+        vr[i] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(c.v) + from + i * 1024 + lane * 16);
+      }
+      kb = s[(lane & 15) / 4 * 16 + (wave & 1) * 4 + (lane & 3)];
+      vb = *reinterpret_cast<const uint2*>(s + (lane >> 4) * 16 + 8);
+    } else {
+      const T* src = pool + at;
+#pragma unroll
+      for (int i = 0; i < HD / 16; ++i) copy_tile(src, i * 1024, &lds.tile[buf][b][wave & 1][i * 64], lane * 16);
+    }
+  };
+  auto stage = [&](int buf) {                                   // what was requested, as it is used, into its buffer
+    if constexpr (H8) {
+      uint4* kd = &lds.tile[buf][wave >> 1][0][(wave & 1) * (HD / 32) * 64 + lane];
+      uint4* vd = &lds.tile[buf][wave >> 1][1][(wave & 1) * (HD / 32) * 64 + lane];
+      const float kf = __uint_as_float(kb << 23);
+      float vf[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) vf[i] = scale_of(i < 4 ? vb.x : vb.y, i & 3);
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        kd[2 * i * 64] = widen<T>(kr[i].x, kr[i].y, kf);
+        kd[(2 * i + 1) * 64] = widen<T>(kr[i].z, kr[i].w, kf);
+        vd[2 * i * 64] = widen<T>(vr[i].x, vr[i].y, vf);
+        vd[(2 * i + 1) * 64] = widen<T>(vr[i].z, vr[i].w, vf);
+      }
+    }
   };
   __syncthreads();
   if (w.u0 < u1) {
     fetch_pages(w.u0);
     request(w.u0, w.u0 & 1);
+    stage(w.u0 & 1);
   }
   // Two loops of one body: units that all of the wave's columns see, then those with masks (with both in one loop the 64 output
   // registers were copied twice a unit).  A wave goes from one to the other when it has to; barriers are one a unit in both.
@@ -1040,20 +1442,28 @@ __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const 
       for (int r = 0; r < 2; ++r)
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d] = mma(__builtin_bit_cast(x8, vt[b * 8 * HD + d * 128 + r * 32]), p[b][r], o[d]);
+    if (H8 && u + 1 < u1) stage((u + 1) & 1);
   }
 #pragma unroll 1
   for (; u < u1; ++u) {
     const int key0 = u * kChunkUnit;
     next_unit();
+    if (H8 && u + 1 < u1) stage((u + 1) & 1);
     if (key0 > last_wave) continue;                             // (nothing for this wave any more)
     f32x16 s[2];
     x8 p[2][2];
     scores(s);
+    uint32_t seen_bits[2];                                      // of the lane's keys of a block: (key - 4 h) of the 32
+    if constexpr (M) {
+      seen_bits[0] = page0 < 0 ? 0 : block_of(sees, key0) >> (4 * h);
+      seen_bits[1] = page1 < 0 ? 0 : block_of(sees, key0 + 32) >> (4 * h);
+    }
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
       const int key = key0 + (i >> 4) * 32 + (i >> 2 & 3) * 8 + h * 4 + (i & 3);
       float& x = reinterpret_cast<float*>(&s[i >> 4])[i & 15];
-      x = key <= last && (i < 16 ? page0 : page1) >= 0 ? x : -INFINITY;
+      if constexpr (M) x = seen_bits[i >> 4] >> ((i >> 2 & 3) * 8 + (i & 3)) & 1 ? x : -INFINITY;
+      else x = key <= last && (i < 16 ? page0 : page1) >= 0 ? x : -INFINITY;
     }
     probabilities(s, p);
     // as in attend_rows: what no column of the wave sees is cleared, infinities and NaNs go to the columns that see them
@@ -1079,7 +1489,10 @@ __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const 
         if (__any(odd != 0)) {
           x8 seen;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) seen[i] = key + (i >> 2) * 16 + (i & 3) <= mine ? (T)1.f : (T)0.f;
+          for (int i = 0; i < 8; ++i) {
+            const bool sees_key = M ? (seen_bits[b] >> (r * 8 + (i >> 2) * 16 + (i & 3)) & 1) != 0 : key + (i >> 2) * 16 + (i & 3) <= mine;
+            seen[i] = sees_key ? (T)1.f : (T)0.f;
+          }
 #pragma unroll
           for (int d = 0; d < DT; ++d) {
             uint4 v = vt[d * 128];
@@ -1125,18 +1538,18 @@ __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const 
   __syncthreads();                                              // (the tiles have been read: their place serves the join)
   join_pieces<T, HD, kChunkCols>(c, a, sp, w, reinterpret_cast<float2*>(lds.join), &lds.last);
 }
-template <typename T, int HD>
+template <typename T, int HD, int F>
 __global__ __launch_bounds__(256, 2) void k_paged_chunk(stairs_paged_cache c, stairs_paged_attn a, Span sp, float scale2) {
   __shared__ ChunkLds<HD> lds;
-  attend_chunk<T, HD>(c, a, sp, scale2, lds);
+  attend_chunk<T, HD, F>(c, a, sp, scale2, lds);
 }
 // both in one launch: the chunks' work-groups first, the few rows of the others where there is room (2 chunks of 509 rows among 22
 // sequences of 3, 90 .. 5000 positions, 16 heads of 128: 79 us = 3.3 TB/s)
-template <typename T, int HD>
+template <typename T, int HD, int F>
 __global__ __launch_bounds__(256, 2) void k_paged_mixed(stairs_paged_cache c, stairs_paged_attn a, Span chunk, Span rows, float scale2) {
   __shared__ union { ChunkLds<HD> chunk; RowsLds<HD, 2> rows; } lds;
-  if ((int)blockIdx.x < rows.first_block) attend_chunk<T, HD>(c, a, chunk, scale2, lds.chunk);
-  else attend_rows<T, HD, 2>(c, a, rows, scale2, lds.rows);
+  if ((int)blockIdx.x < rows.first_block) attend_chunk<T, HD, F>(c, a, chunk, scale2, lds.chunk);
+  else attend_rows<T, HD, 2, F>(c, a, rows, scale2, lds.rows);
 }
 
 }  // namespace
@@ -1161,13 +1574,18 @@ constexpr int64_t kMostGroups = (1ll << 24) - 1;     // work-groups of 256 threa
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
-bool cache_ok(const stairs_paged_cache* c) {
+}  // namespace
+
+bool stairs::paged_cache_ok(const stairs_paged_cache* c) {
   if (!c || (c->dtype != STAIRS_DTYPE_BF16 && c->dtype != STAIRS_DTYPE_FP16)) return false;
   if (c->page_size != 32 && c->page_size != 64 && c->page_size != 128 && c->page_size != 256) return false;
   if (c->head_dim != 64 && c->head_dim != 128) return false;
   if (c->n_kv_heads < 1 || c->n_kv_heads > 4096 || c->n_pages < 1 || (int64_t)c->n_pages * c->page_size > INT32_MAX) return false;
+  if (c->held != 0 && (c->held != STAIRS_DTYPE_E4M3 || !c->scale || !aligned16(c->scale))) return false;
   return c->k && c->v && aligned16(c->k) && aligned16(c->v);
 }
+
+namespace {
 
 // every stride holds a row and keeps its 16-byte alignment
 bool stride_ok(int64_t stride, int heads, int hd) { return stride >= (int64_t)heads * hd && stride % 8 == 0; }
@@ -1182,8 +1600,23 @@ void by_type(const stairs_paged_cache* c, F f) {
   else b ? f(__bf16{}, std::integral_constant<int, 128>{}) : f(_Float16{}, std::integral_constant<int, 128>{});
 }
 
+// f(type, head_dim, whether pages hold 8 bits)
+template <typename F>
+void by_pages(const stairs_paged_cache* c, F f) {
+  by_type(c, [&](auto type, auto hd) { c->held ? f(type, hd, std::true_type{}) : f(type, hd, std::false_type{}); });
+}
+// f(type, head_dim, form of the attention kernels)
+template <typename F>
+void by_form(const stairs_paged_cache* c, const stairs_paged_attn* a, F f) {
+  by_type(c, [&](auto type, auto hd) {
+    if (c->held) f(type, hd, std::integral_constant<int, kMasks | kHeld8>{});
+    else if (a->sees) f(type, hd, std::integral_constant<int, kMasks>{});
+    else f(type, hd, std::integral_constant<int, 0>{});
+  });
+}
+
 bool attn_sizes_ok(const stairs_paged_cache* c, const stairs_paged_attn* a) {
-  if (!cache_ok(c) || !a) return false;
+  if (!paged_cache_ok(c) || !a) return false;
   if (a->n_seqs < 0 || a->n_seqs > STAIRS_PAGED_MAX_SEQS || a->max_blocks < 1 || a->rows < 0 || a->max_fresh < 0) return false;
   if ((int64_t)a->max_blocks * c->page_size > INT32_MAX) return false;
   if (a->n_heads < 1 || (int64_t)a->rows * a->n_heads / c->n_kv_heads > 1 << 24) return false;   // (counts of tiles stay ints)
@@ -1208,7 +1641,7 @@ extern "C" int stairs_paged_plan(const stairs_page_plan* p, void* hip_stream) {
 }
 
 extern "C" int stairs_paged_append(const stairs_paged_cache* c, const stairs_paged_rows* a, void* hip_stream) {
-  if (!cache_ok(c) || !a || a->rows < 0 || a->rows > kMostGroups * kAppendRows || a->n_heads < 0 || a->n_heads > 4096) return STAIRS_EINVAL;
+  if (!paged_cache_ok(c) || !a || a->rows < 0 || a->rows > kMostGroups * kAppendRows || a->n_heads < 0 || a->n_heads > 4096) return STAIRS_EINVAL;
   if (!(a->rope_theta >= 0.f) || std::isinf(a->rope_theta)) return STAIRS_EINVAL;
   if (a->rows == 0) return STAIRS_OK;
   if (!a->k || !a->v || !a->slot || (a->rope_theta > 0.f && !a->position)) return STAIRS_EINVAL;
@@ -1224,8 +1657,23 @@ extern "C" int stairs_paged_append(const stairs_paged_cache* c, const stairs_pag
   const int heads = std::max(r.n_heads, c->n_kv_heads), tiles = (r.rows - 1) / kAppendRows + 1;
   const int groups = std::max(1, std::min((4 * kCus + tiles - 1) / tiles, heads));
   const double log2_theta = r.rope_theta > 0.f ? std::log2((double)r.rope_theta) : 0.0;
-  by_type(c, [&](auto type, auto hd) {
-    hipLaunchKernelGGL((k_paged_append<decltype(type), decltype(hd)::value>), dim3(tiles, groups, tiles * groups < 2 * kCus ? 3 : 1), dim3(256), 0, st, *c, r, log2_theta);
+  by_pages(c, [&](auto type, auto hd, auto h8) {
+    hipLaunchKernelGGL((k_paged_append<decltype(type), decltype(hd)::value, decltype(h8)::value>), dim3(tiles, groups, tiles * groups < 2 * kCus ? 3 : 1), dim3(256), 0, st, *c, r, log2_theta);
+  });
+  return launched();
+}
+
+extern "C" int stairs_paged_read(const stairs_paged_cache* c, const stairs_paged_out* a, void* hip_stream) {
+  if (!paged_cache_ok(c) || !a || a->rows < 0 || a->rows > kMostGroups * kAppendRows) return STAIRS_EINVAL;
+  if (a->rows == 0 || (!a->k && !a->v)) return STAIRS_OK;
+  if (!a->slot) return STAIRS_EINVAL;
+  if (a->k && (!aligned16(a->k) || !stride_ok(a->k_stride, c->n_kv_heads, c->head_dim))) return STAIRS_EINVAL;
+  if (a->v && (!aligned16(a->v) || !stride_ok(a->v_stride, c->n_kv_heads, c->head_dim))) return STAIRS_EINVAL;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (const int rc = check_stream(st)) return rc;
+  const int tiles = (a->rows - 1) / kAppendRows + 1, groups = std::max(1, std::min((4 * kCus + tiles - 1) / tiles, c->n_kv_heads));
+  by_pages(c, [&](auto type, auto hd, auto h8) {
+    hipLaunchKernelGGL((k_paged_read<decltype(type), decltype(hd)::value, decltype(h8)::value>), dim3(tiles, groups, a->k && a->v ? 2 : 1), dim3(256), 0, st, *c, *a);
   });
   return launched();
 }
@@ -1285,21 +1733,21 @@ extern "C" int stairs_paged_attention(const stairs_paged_cache* c, const stairs_
   if (!a->q || !a->out || a->q == a->out || !a->block_table || !a->row_start || !a->seq_len) return STAIRS_EINVAL;
   if (!aligned16(a->q) || !aligned16(a->out) || !stride_ok(a->q_stride, a->n_heads, c->head_dim) || !stride_ok(a->out_stride, a->n_heads, c->head_dim))
     return STAIRS_EINVAL;
-  if (!a->workspace || !aligned16(a->workspace)) return STAIRS_EINVAL;
+  if (!a->workspace || !aligned16(a->workspace) || reinterpret_cast<uintptr_t>(a->sees) % 8 != 0) return STAIRS_EINVAL;
   const Launch l = plan_attention(c, a);
   if (l.grid > kMostGroups) return STAIRS_EINVAL;
   if (a->workspace_bytes < l.work_bytes) return STAIRS_ECAPACITY;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (const int rc = check_stream(st)) return rc;
   const float scale2 = (a->scale > 0.f ? a->scale : 1.0f / sqrtf((float)c->head_dim)) * kLog2e;
-  by_type(c, [&](auto type, auto hd) {
+  by_form(c, a, [&](auto type, auto hd, auto form) {
     typedef decltype(type) T;
-    constexpr int HD = decltype(hd)::value;
+    constexpr int HD = decltype(hd)::value, F = decltype(form)::value;
     const dim3 grid((unsigned)l.grid), block(256);
-    if (l.chunk && l.ct) hipLaunchKernelGGL((k_paged_mixed<T, HD>), grid, block, 0, st, *c, *a, l.chunks, l.rows, scale2);
-    else if (l.chunk) hipLaunchKernelGGL((k_paged_chunk<T, HD>), grid, block, 0, st, *c, *a, l.chunks, scale2);
-    else if (l.ct == 1) hipLaunchKernelGGL((k_paged_rows<T, HD, 1>), grid, block, 0, st, *c, *a, l.rows, scale2);
-    else hipLaunchKernelGGL((k_paged_rows<T, HD, 2>), grid, block, 0, st, *c, *a, l.rows, scale2);
+    if (l.chunk && l.ct) hipLaunchKernelGGL((k_paged_mixed<T, HD, F>), grid, block, 0, st, *c, *a, l.chunks, l.rows, scale2);
+    else if (l.chunk) hipLaunchKernelGGL((k_paged_chunk<T, HD, F>), grid, block, 0, st, *c, *a, l.chunks, scale2);
+    else if (l.ct == 1) hipLaunchKernelGGL((k_paged_rows<T, HD, 1, F>), grid, block, 0, st, *c, *a, l.rows, scale2);
+    else hipLaunchKernelGGL((k_paged_rows<T, HD, 2, F>), grid, block, 0, st, *c, *a, l.rows, scale2);
   });
   return launched();
 }

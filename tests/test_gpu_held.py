@@ -1,0 +1,383 @@
+"""GPU: rows stored in 8 bits, read back, attended over; against plain implementations in 64 bits (trees_util.py)."""
+import numpy as np
+import pytest
+
+import paper_2407_19947_amd as pkg
+import operators_util as ou
+import trees_util as tu
+from test_gpu_paged import SLOT_SETS, rotate_reference
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- storing and reading -------------------------------------------------------------------------------------------------
+class Pool:
+    def __init__(self, dtype, n_pages, page, Hkv, hd, held=True, seed=0):
+        import torch
+        self.dtype, self.dt, self.n_pages, self.page, self.Hkv, self.hd, self.held = dtype, ou.torch_type(dtype), n_pages, page, Hkv, hd, held
+        rng = np.random.default_rng([seed, n_pages, page])
+        n = page * hd
+        if held:
+            raw = rng.integers(0, 127, (2, n_pages, Hkv, n)) | rng.integers(0, 2, (2, n_pages, Hkv, n)) << 7
+            self.k0, self.v0 = raw.astype(np.uint8)
+            # (as half rows come back: up to 448 * 2^7)
+            self.s0 = rng.integers(100, 135, (n_pages, Hkv, page * 2)).astype(np.uint8)
+            self.k, self.v, self.s = (torch.from_numpy(a.copy()).cuda() for a in (self.k0, self.v0, self.s0))
+        else:
+            self.k0, self.v0 = (torch.from_numpy(rng.standard_normal((n_pages, Hkv, n)).astype(np.float32)).to(self.dt) for _ in range(2))
+            self.k, self.v = self.k0.cuda(), self.v0.cuda()
+        self.cache = pkg.StairsPagedCache(k=self.k.data_ptr(), v=self.v.data_ptr(), dtype=ou.CODE[dtype], n_pages=n_pages, page_size=page, n_kv_heads=Hkv, head_dim=hd,
+                                          held=pkg.DTYPE_E4M3 if held else 0, scale=self.s.data_ptr() if held else None)
+
+    def codes(self):
+        """keys, values [pages, heads, page_size, hd] as codes, and their bytes [pages, heads, page_size]"""
+        k, v, s = (t.cpu().numpy() for t in (self.k, self.v, self.s))
+        p = np.arange(self.page)
+        return (ou.pages_to_rows(k, self.hd, tu.held_key_at), ou.pages_to_rows(v, self.hd, tu.held_value_at),
+                s[:, :, tu.held_scale_at(p, 0)], s[:, :, tu.held_scale_at(p, 1)])
+
+    def numbers(self):
+        if self.held:
+            k, v, kb, vb = self.codes()
+            return tu.values_of(k, kb), tu.values_of(v, vb)
+        k, v = (t.double().cpu().numpy() for t in (self.k, self.v))
+        return ou.pages_to_rows(k, self.hd, ou.key_at), ou.pages_to_rows(v, self.hd, ou.value_at)
+
+
+def append(pool, slots, Hq, theta, qkv, positions, pad=0):
+    import torch
+    hd, Hkv, n = pool.hd, pool.Hkv, len(slots)
+    dev = qkv.cuda()
+    wide, e, base = dev.stride(0), dev.element_size(), dev.data_ptr()
+    pos, slot = (torch.tensor(np.asarray(a), dtype=torch.int32).cuda() for a in (positions, slots))
+    q_out = torch.full((n, max(Hq, 1) * hd), 5.0, dtype=pool.dt).cuda()
+    r = pkg.StairsPagedRows(rows=n, n_heads=Hq, q=base if Hq else None, k=base + Hq * hd * e, v=base + (Hq + Hkv) * hd * e, q_out=q_out.data_ptr() if Hq else None,
+                            q_stride=wide, k_stride=wide, v_stride=wide, q_out_stride=q_out.stride(0), position=pos.data_ptr(), slot=slot.data_ptr(), rope_theta=theta)
+    torch.cuda.synchronize()
+    pkg.stairs_paged_append(pool.cache, r, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    return q_out.double().cpu().numpy()
+
+
+def check_append(dtype, slots, Hq, Hkv, hd, page, n_pages, theta=10000.0, pad=0, positions=None, seed=0, x=None):
+    """Values (not rotated) to the code; keys within half a step of the code's and what the rotation in float is off by: sine and cosine to half a
+    step, products and sum (6 * 2^-24 of the pair's length), the power of theta in double (2^-48 of the position's angle); the power of two is the
+    smallest that holds the largest of a row that is off by as much."""
+    import torch
+    n = len(slots)
+    g = torch.Generator().manual_seed(seed)
+    wide = (Hq + 2 * Hkv) * hd + pad
+    qkv = torch.randn(n, wide, generator=g) if x is None else x
+    # rows of many sizes
+    if x is None:
+        qkv *= torch.exp2(torch.randint(-9, 10, (n, 1), generator=g).float())
+    qkv = qkv.to(ou.torch_type(dtype))
+    pos = np.asarray(slots, np.int64) * 7 % 70000 if positions is None else np.asarray(positions, np.int64)
+    pool = Pool(dtype, n_pages, page, Hkv, hd)
+    before = pool.codes()
+    got_q = append(pool, slots, Hq, theta, qkv, pos)
+    kc, vc, kb, vb = pool.codes()
+    xs = qkv[:, :wide - pad].double().numpy()
+    q, k, v = (xs[:, a * hd:b * hd].reshape(n, b - a, hd) for a, b in ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, Hq + 2 * Hkv)))
+    with np.errstate(invalid="ignore"):
+        kt = rotate_reference(k, pos, theta) if theta > 0 else k
+        amp = np.concatenate([np.sqrt(k[..., :hd // 2] ** 2 + k[..., hd // 2:] ** 2)] * 2, -1)
+        off = (6 * 2.0 ** -24 + np.abs(pos)[:, None, None] * 2.0 ** -48) * amp if theta > 0 else np.zeros_like(amp)
+    want_v, want_vb = tu.quantise(v, dtype)
+    if dtype == "fp16":                                          # (past 61440: held as that)
+        with np.errstate(invalid="ignore"):
+            kt = np.where(np.isfinite(kt), np.clip(kt, -61440, 61440), kt)
+    touched = np.zeros((n_pages, page), bool)
+    for t, s in enumerate(slots):
+        if not 0 <= s < n_pages * page:
+            continue
+        pg, p = s // page, s % page
+        touched[pg, p] = True
+        assert np.array_equal(vb[pg, :, p], want_vb[t]), (t, vb[pg, :, p], want_vb[t])
+        bits = np.where(np.isfinite(v[t]), 255, 127)               # (the sign of what is no number says nothing)
+        assert np.array_equal(vc[pg, :, p] & bits, want_v[t] & bits), t
+        fin = np.isfinite(kt[t])
+        top = np.where(fin, np.abs(kt[t]), 0).max(-1)
+        room = np.where(fin, off[t], 0).max(-1)
+        b = kb[pg, :, p].astype(np.float64)
+        assert (top - room <= 448 * np.exp2(b - 127)).all() and ((b == 1) | (top + room > 448 * np.exp2(b - 128))).all(), (t, b, top)
+        num = tu.values_of(kc[pg, :, p], kb[pg, :, p])
+        assert np.array_equal(np.isnan(num), ~fin), t
+        step = np.maximum(np.abs(kt[t]) * 2.0 ** -4, np.exp2(b - 127)[:, None] * 2.0 ** -10)
+        ou.check_close(np.where(fin, num, 0), np.where(fin, kt[t], 0), np.where(fin, step + off[t] * (1 + 2.0 ** -4), 0), t)
+    for now, then in zip((kc, vc, kb, vb), before):
+        assert np.array_equal(np.moveaxis(now, 2, 1)[~touched], np.moveaxis(then, 2, 1)[~touched]), "other places were written"
+    if Hq and x is None:
+        want = rotate_reference(q, pos, theta) if theta > 0 else q
+        aq = np.concatenate([np.sqrt(q[..., :hd // 2] ** 2 + q[..., hd // 2:] ** 2)] * 2, -1)
+        ok = pos >= 0 if theta > 0 else np.ones(n, bool)
+        tol = ou.HALF_STEP[dtype] * np.abs(want) + ou.SMALLEST[dtype] + (6 * 2.0 ** -24 + np.abs(pos)[:, None, None] * 2.0 ** -48) * aq
+        ou.check_close(got_q.reshape(n, Hq, hd)[ok], want[ok], tol[ok])
+        assert (got_q.reshape(n, Hq, hd)[~ok] == 5.0).all()
+
+
+@pytest.mark.parametrize("slots", SLOT_SETS, ids=lambda s: s.replace(" ", "_"))
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("Hq,Hkv,hd,page", [(4, 4, 64, 32), (8, 2, 128, 64), (3, 1, 128, 256)])
+def test_append(dtype, Hq, Hkv, hd, page, slots):
+    check_append(dtype, SLOT_SETS[slots], Hq, Hkv, hd, page, 1100 // page + 2)
+
+
+@pytest.mark.parametrize("first", range(0, 32, 5))
+def test_append_of_runs_longer_than_a_work_groups_rows(first):
+    check_append("bf16", [*range(first, first + 70), *range(320 - first, 320 - first + 45)], 2, 2, 64, 32, 14)
+    check_append("fp16", [*range(601, 601 + first), *range(first + 64, first + 64 + 97)], 2, 1, 128, 64, 12)
+
+
+@pytest.mark.parametrize("theta", [0.0, 1.0, 500000.0])
+def test_append_rotations_and_strides(theta):
+    check_append("bf16", SLOT_SETS["runs of all alignments"], 8, 2, 128, 64, 20, theta, 24)
+    check_append("fp16", SLOT_SETS["some nowhere"], 8, 2, 64, 32, 20, theta, 0, positions=[3, -1, 0, 5, -7, 9, 1, 2, 3, 59999, -1, 2 ** 31 - 1, 6])
+    check_append("bf16", SLOT_SETS["run across pages"], 0, 4, 128, 64, 20, theta)
+    check_append("fp16", list(range(5, 1005)), 4, 40, 64, 128, 9, theta)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_append_of_rows_of_every_kind(dtype):
+    """Zeros, the smallest and largest numbers of the type, largest magnitudes at and next to 448 times a power of two, infinities and NaN."""
+    import torch
+    dt = ou.torch_type(dtype)
+    top = float(torch.finfo(dt).max)
+    hd, Hkv = 64, 2
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn(16, 2 * Hkv * hd, generator=g)
+    x[0] = 0
+    x[1] = torch.where(torch.rand(x.shape[1], generator=g) < 0.5, 0.0, float(torch.finfo(dt).smallest_normal))
+    x[2] = torch.sign(x[2]) * top
+    x[3, ::hd], x[4, ::hd], x[5, ::hd] = 448.0, 450.0, 446.0
+    x[6, ::hd], x[7, 5::hd] = 3.5, float(torch.tensor(3.5).to(dt) * (1 + torch.finfo(dt).eps))
+    x[8, 3::hd], x[9, 4::hd], x[10, ::hd] = float("inf"), -float("inf"), float("nan")
+    x[11] = float("inf")
+    x[12] = float("nan")
+    x[13, ::2] *= 2.0 ** -12
+    x[14] = -0.0
+    for theta in (0.0, 10000.0):
+        keep = x.clone()
+        if theta:
+            keep[2] /= 4                                          # (the largest of a pair turned would be past the type's)
+        check_append(dtype, list(range(20, 36)), 0, Hkv, hd, 32, 4, theta, x=keep)
+
+
+def read(pool, slots, which="kv", pad=0, stream=None):
+    import torch
+    n, w = len(slots), pool.Hkv * pool.hd
+    out = {k: torch.full((n, w + pad), 5.0, dtype=pool.dt).cuda() for k in "kv"}
+    slot = torch.tensor(np.asarray(slots), dtype=torch.int32).cuda()
+    r = pkg.StairsPagedRead(rows=n, k=out["k"].data_ptr() if "k" in which else None, v=out["v"].data_ptr() if "v" in which else None,
+                            k_stride=w + pad, v_stride=w + pad, slot=slot.data_ptr())
+    torch.cuda.synchronize()
+    pkg.stairs_paged_read(pool.cache, r, torch.cuda.current_stream().cuda_stream if stream is None else stream)
+    torch.cuda.synchronize()
+    return [out[k].double().cpu().numpy() for k in "kv"]
+
+
+def check_read(pool, slots, which="kv", pad=0):
+    import torch
+    w = pool.Hkv * pool.hd
+    for name, got, num in zip("kv", read(pool, slots, which, pad), pool.numbers()):
+        if pool.dtype == "fp16":
+            num = np.where(np.isnan(num), num, np.clip(num, -65504, 65504))
+        num = torch.from_numpy(num).to(pool.dt).double().numpy()
+        want = np.full((len(slots), w + pad), 5.0)
+        for t, s in enumerate(slots):
+            if 0 <= s < pool.n_pages * pool.page and name in which:
+                want[t, :w] = num[s // pool.page, :, s % pool.page].reshape(-1)
+        assert np.array_equal(got, want, equal_nan=True), (name, np.argwhere(got != want)[:4])
+
+
+@pytest.mark.parametrize("held", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("Hkv,hd,page", [(4, 64, 32), (2, 128, 64), (1, 128, 256), (40, 64, 128)])
+def test_read(dtype, Hkv, hd, page, held):
+    pool = Pool(dtype, 1100 // page + 2, page, Hkv, hd, held)
+    for slots in SLOT_SETS.values():
+        check_read(pool, slots)
+    check_read(pool, [7, 7, 7, 8, 8, 40, 7], pad=8)              # a slot more than once
+    check_read(pool, list(range(64, 900)), pad=24)
+    check_read(pool, SLOT_SETS["runs of all alignments"], "k")
+    check_read(pool, SLOT_SETS["runs of all alignments"], "v")
+
+
+def test_read_of_every_code_and_power():
+    """All 256 codes; fp16 where rounding up has left more than its largest number."""
+    for dtype, powers in (("bf16", [1, 2, 60, 127, 200, 246]), ("fp16", [100, 110, 127, 133, 134, 136])):
+        pool = Pool(dtype, 2, 32, 2, 128)
+        codes = np.arange(2 * 2 * 32 * 128).reshape(2, 2, -1) % 256
+        pool.k.copy_(pool.k.new_tensor(codes.astype(np.uint8).tolist()))
+        pool.v.copy_(pool.v.new_tensor(codes[..., ::-1].astype(np.uint8).tolist()))
+        pool.s.copy_(pool.s.new_tensor(np.resize(np.array(powers, np.uint8), (2, 2, 64)).tolist()))
+        check_read(pool, list(range(64)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_what_is_stored_comes_back(dtype):
+    """Within half a step of the 8-bit numbers, and storing what came back changes nothing."""
+    import torch
+    Hkv, hd, page = 4, 128, 64
+    pool = Pool(dtype, 8, page, Hkv, hd)
+    slots = list(range(37, 37 + 300))
+    x = torch.randn(300, 2 * Hkv * hd, generator=torch.Generator().manual_seed(1)).to(pool.dt)
+    append(pool, slots, 0, 0.0, x, slots)
+    k, v = read(pool, slots)
+    for got, want in zip((k, v), x.double().numpy().reshape(300, 2, -1).swapaxes(0, 1)):
+        top = np.abs(want).reshape(300, Hkv, hd).max(-1).repeat(hd, 1)
+        ou.check_close(got, want, np.maximum(np.abs(want) * 2.0 ** -4, top * 2.0 ** -17))   # (the smallest step 2^-9 of 224 and more, half of it)
+    append(pool, slots, 0, 0.0, torch.from_numpy(np.concatenate([k, v], 1)).to(pool.dt), slots)
+    k2, v2 = read(pool, slots)
+    assert np.array_equal(k, k2) and np.array_equal(v, v2)
+
+
+# ---- attention over 8-bit pages ------------------------------------------------------------------------------------------
+HEADS = [(4, 4, 64), (4, 4, 128), (8, 2, 128), (7, 1, 128), (40, 2, 64)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("Hq,Hkv,hd", HEADS)
+@pytest.mark.parametrize("page", [32, 256])
+def test_attention_of_single_rows_at_every_border(dtype, Hq, Hkv, hd, page):
+    lens = [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200, 257]
+    a = tu.Attend(dtype, lens, [1] * len(lens), Hq, Hkv, hd, page, powers=(-3, 3))
+    a.check(a.call())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("Hq,Hkv,hd", HEADS)
+@pytest.mark.parametrize("rows", [2, 5, 9, 17, 33])
+def test_attention_of_verifications(dtype, Hq, Hkv, hd, rows):
+    lens = [rows, rows + 1, 40 + rows, 129, 300]
+    a = tu.Attend(dtype, lens, [rows] * len(lens), Hq, Hkv, hd, 64, seed=rows)
+    a.check(a.call())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("Hq,Hkv,hd", [(2, 2, 64), (2, 2, 128), (8, 2, 128), (5, 1, 128)])
+@pytest.mark.parametrize("lens,fresh", [([130], [130]), ([300], [129]), ([700, 64, 333], [65, 64, 200])])
+def test_attention_of_chunks(dtype, Hq, Hkv, hd, lens, fresh):
+    a = tu.Attend(dtype, lens, fresh, Hq, Hkv, hd, 64)
+    a.check(a.call())
+
+
+@pytest.mark.parametrize("dtype,page", [("bf16", 32), ("fp16", 128)])
+def test_attention_of_a_mixed_batch(dtype, page):
+    a = tu.Attend(dtype, [300, 1, 77, 0, 500, 64, 33, 1000, 12, 250], [200, 1, 3, 0, 1, 64, 2, 150, 0, 5], 8, 2, 128, page)
+    a.check(a.call())
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,hd", [("bf16", 8, 2, 128), ("fp16", 2, 2, 64)])
+def test_attention_over_long_sequences_beside_short_ones(dtype, Hq, Hkv, hd):
+    a = tu.Attend(dtype, [20011, 3, 64, 9000, 257], [1, 3, 2, 5, 1], Hq, Hkv, hd, 128)
+    a.check(a.call())
+
+
+@pytest.mark.parametrize("powers", [(-40, -40), (-14, 0), (0, 7)])
+@pytest.mark.parametrize("rows", [3, 70])
+def test_rows_of_very_different_sizes(powers, rows):
+    """Powers of two far from 1, and different from key to key (queries made small where keys are large)."""
+    for dtype in ("bf16", "fp16"):
+        if dtype == "fp16" and powers[0] == -40:
+            continue                                             # (no row of halves is that small)
+        a = tu.Attend(dtype, [300, rows + 5], [rows, rows], 4, 2, 128, 64, powers=powers, q_scale=1.0 if powers[1] <= 0 else 2.0 ** -7)
+        a.check(a.call())
+
+
+@pytest.mark.parametrize("rows", [1, 40, 140])
+@pytest.mark.parametrize("byte", [0, 1, 254, 255])
+def test_masked_positions_may_hold_any_bytes(rows, byte):
+    """Behind the last position and in pages nobody has: codes that are no number, powers of two that nobody stores; later rows of a chunk
+    are not seen either."""
+    import torch
+    lens = [rows + 70, rows + 1, rows + 129]
+    for dtype in ("bf16", "fp16"):
+        a = tu.Attend(dtype, lens, [rows] * 3, 8, 2, 128, 32)
+        clean = a.call()
+        used = set()
+        for b, n in enumerate(lens):
+            for j in range(-(-n // 32)):
+                p = int(a.table[b, j])
+                used.add(p)
+                for t in (a.kc, a.vc):
+                    t[p, :, max(0, n - 32 * j):] = 0x7F
+                for t in (a.kb, a.vb):
+                    t[p, :, max(0, n - 32 * j):] = byte
+        for p in set(range(a.n_pages)) - used:
+            a.kc[p], a.vc[p], a.kb[p], a.vb[p] = 0xFF, 0xFF, byte, byte
+        assert np.array_equal(a.call(), clean)
+        a.check(clean)
+        # the last row's own value is no number: only it is off
+        for b, n in enumerate(lens):
+            a.vc[a.table[b, (n - 1) // 32], :, (n - 1) % 32] = 0x7F
+        out = a.call()
+        last = a.row_start[1:] - 1
+        others = np.setdiff1d(np.arange(a.row_start[-1]), last)
+        assert np.isnan(out[last]).all() and np.array_equal(out[others], clean[others])
+
+
+def test_pages_that_are_none_and_rows_that_see_nothing():
+    for rows in (1, 5, 140):
+        a = tu.Attend("bf16", [rows + 40, rows + 100, rows + 300], [rows] * 3, 8, 2, 128, 32)
+        a.table[0, :] = -1
+        a.table[1, 0] = a.n_pages
+        a.table[2, 1] = -2 ** 31
+        a.table[2, 3] = 2 ** 31 - 1
+        a.check(a.call())
+    a = tu.Attend("fp16", [3, 40, 200], [7, 60, 2], 8, 2, 64, 32, extra_blocks=0)
+    a.check(a.call())                                            # rows in front of position 0 see nothing
+
+
+def test_a_cache_beyond_32_bit_offsets():
+    """The last pages of pools of more than 2^32 bytes each: stored, attended over, read back."""
+    import torch
+    page, hd, n_pages = 256, 128, 140000                         # 140000 x 256 x 128 bytes = 4.6 GB
+    a = tu.Attend("fp16", [600, 300], [3, 130], 2, 1, hd, page, extra_blocks=0)
+    small = a.call()
+    d = a.dev
+    big = {k: torch.zeros(n_pages, n, dtype=torch.uint8, device="cuda") for k, n in (("k", page * hd), ("v", page * hd), ("scale", page * 2))}
+    far = n_pages - a.n_pages
+    for k, t in big.items():
+        t[far:] = d[k].view(a.n_pages, -1)
+    table = torch.where(d["table"] >= 0, d["table"] + far, d["table"])
+    a.cache.k, a.cache.v, a.cache.scale, a.cache.n_pages = big["k"].data_ptr(), big["v"].data_ptr(), big["scale"].data_ptr(), n_pages
+    a.args.block_table = table.data_ptr()
+    d["out"].fill_(7.0)
+    torch.cuda.synchronize()
+    pkg.stairs_paged_attention(a.cache, a.args, None)
+    torch.cuda.synchronize()
+    assert np.array_equal(a.result(), small)
+    slot = torch.tensor([n_pages * page - 1, n_pages * page], dtype=torch.int32).cuda()
+    rows = pkg.StairsPagedRows(rows=2, n_heads=0, k=d["q"].data_ptr(), v=d["q"].data_ptr(), k_stride=hd, v_stride=hd, slot=slot.data_ptr(), rope_theta=0.0)
+    pkg.stairs_paged_append(a.cache, rows, None)
+    k, v = torch.full((2, 2, hd), 5.0, dtype=a.dt, device="cuda")
+    out = pkg.StairsPagedRead(rows=2, k=k.data_ptr(), v=v.data_ptr(), k_stride=hd, v_stride=hd, slot=slot.data_ptr())
+    pkg.stairs_paged_read(a.cache, out, None)
+    torch.cuda.synchronize()
+    want = tu.values_of(*tu.quantise(a.q.double().numpy().reshape(-1, hd)[:1], "fp16"))
+    for t in (k, v):
+        assert np.array_equal(t[:1].double().cpu().numpy(), want) and bool((t[1] == 5).all())
+
+
+def test_calls_share_a_workspace_with_those_over_16_bit_pages_and_give_the_same_bits():
+    import torch
+    calls = [tu.Attend("bf16", [9000, 300, 64], [1, 5, 2], 8, 2, 128, 64), tu.Attend("bf16", [400, 6000], [130, 300], 8, 2, 128, 64, held=False),
+             tu.Attend("fp16", [5000, 200, 2500], [1, 150, 5], 4, 4, 64, 32), tu.Attend("fp16", [7000], [300], 2, 2, 64, 256)]
+    alone = [x.call() for x in calls]
+    for x, y in zip(calls, alone):
+        x.check(y)
+    work = torch.zeros(max(x.dev["work"].numel() for x in calls), dtype=torch.uint8).cuda()
+    for order in ([0, 1, 2, 3], [3, 0, 2, 1], [1, 1, 3, 3, 0]):
+        for i in order:
+            assert np.array_equal(calls[i].call(workspace=work), alone[i]), (order, i)
+
+
+def test_calls_on_a_stream_of_the_callers():
+    import torch
+    side = torch.cuda.Stream()
+    a = tu.Attend("fp16", [700, 20], [3, 20], 8, 2, 64, 32)
+    assert np.array_equal(a.call(), a.call(stream=side.cuda_stream))
+    pool = Pool("bf16", 4, 64, 2, 128)
+    one, two = read(pool, list(range(200))), read(pool, list(range(200)), stream=side.cuda_stream)
+    assert all(np.array_equal(x, y) for x, y in zip(one, two))

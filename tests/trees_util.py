@@ -1,0 +1,230 @@
+"""What the tests of drafted trees and of caches in 8 bits share: plain implementations in 64 bits (numpy, loops), page
+addressing by its formula, and calls with torch owning the buffers."""
+import numpy as np
+
+import paper_2407_19947_amd as pkg
+import operators_util as ou
+
+# the half step of the probabilities in the product with v: of two numbers of the type; of one
+TWO = {"bf16": 2.0 ** -15, "fp16": 2.0 ** -21}
+
+
+# ---- 8-bit rows --------------------------------------------------------------------------------------------------------
+def decode_table():
+    """The numbers of all 256 codes, from the format: sign, 4 bits of exponent (bias 7), 3 of mantissa; all ones: NaN."""
+    t = np.empty(256)
+    for c in range(256):
+        e, m = c >> 3 & 15, c & 7
+        v = np.nan if c & 127 == 127 else m * 2.0 ** -9 if e == 0 else (8 + m) * 2.0 ** (e - 10)
+        t[c] = -v if c & 128 else v
+    return t
+
+
+DECODE = decode_table()
+
+
+def encode(y):
+    """Nearest code of each number within +-448, ties to the even code; what is not finite: NaN."""
+    grid = DECODE[:127]                                      # ascending
+    a = np.abs(np.where(np.isfinite(y), y, 0.0))
+    hi = np.clip(np.searchsorted(grid, a), 1, 126)
+    lo = hi - 1
+    up = (grid[hi] - a < a - grid[lo]) | ((grid[hi] - a == a - grid[lo]) & (hi % 2 == 0))
+    code = np.where(up, hi, lo)
+    code = np.where(np.isfinite(y), code, 127)
+    return (code | np.where(np.signbit(y), 128, 0)).astype(np.uint8)
+
+
+def scale_byte(x):
+    """Rows [.., hd] -> the smallest byte b from 1 on with max |x| <= 448 * 2^(b - 127), over what is finite"""
+    top = np.max(np.where(np.isfinite(x), np.abs(x), 0.0), -1)
+    m, e = np.frexp(top)                                     # 448 * 2^(b - 127) = 0.875 * 2^(b - 118)
+    return np.clip(np.where(top > 0, e + 118 + (m > 0.875), 1), 1, 254).astype(np.uint8)
+
+
+def quantise(x, dtype="bf16"):
+    if dtype == "fp16":
+        with np.errstate(invalid="ignore"):
+            x = np.where(np.isfinite(x), np.clip(x, -61440, 61440), x)
+    b = scale_byte(x)
+    with np.errstate(invalid="ignore"):
+        return encode(x * np.exp2(127.0 - b)[..., None]), b
+
+
+def held_key_at(p, e, hd):
+    return ((p // 16) * (hd // 64) + e // 64) * 1024 + (p % 16 + 16 * (e % 32 // 8)) * 16 + e % 64 // 32 * 8 + e % 8
+
+
+def held_value_at(p, e, hd):
+    return ((p // 32) * (hd // 32) + e // 32) * 1024 + (e % 16 + 16 * (p % 16 // 4)) * 16 + e % 32 // 16 * 8 + p % 4 + 4 * (p % 32 // 16)
+
+
+def held_scale_at(p, values):
+    return p // 32 * 64 + p % 16 // 4 * 16 + p % 32 // 16 * 4 + p % 4 + 8 * values
+
+
+def scales_to_pages(kb, vb):
+    """Bytes [pages, heads, page_size] of keys and of values -> as a pool holds them"""
+    n, h, ps = kb.shape
+    raw = np.empty((n, h, ps * 2), np.uint8)
+    p = np.arange(ps)
+    raw[:, :, held_scale_at(p, 0)] = kb
+    raw[:, :, held_scale_at(p, 1)] = vb
+    return raw
+
+
+def values_of(codes, b):
+    return DECODE[codes] * np.exp2(b.astype(np.float64) - 127)[..., None]
+
+
+# ---- trees -------------------------------------------------------------------------------------------------------------
+def random_tree(rng, n):
+    return [-1] + [int(rng.integers(0, i)) for i in range(1, n)]
+
+
+def path_of(parent, i):
+    """The rows from the first to i; a parent that is none ends it."""
+    path = [i]
+    while 0 <= parent[path[0]] < path[0]:
+        path.insert(0, parent[path[0]])
+    return path
+
+
+def tree_reference(row_start, seq_len, parent, rows):
+    position, sees = np.full(rows, -1, np.int64), np.zeros(rows, np.uint64)
+    for b in range(len(seq_len)):
+        r0, n = row_start[b], row_start[b + 1] - row_start[b]
+        if seq_len[b] < n:
+            continue
+        for i in range(n):
+            path = path_of(parent[r0:r0 + n], i) if n <= 64 else list(range(i + 1))
+            position[r0 + i] = seq_len[b] - n + len(path) - 1
+            if n <= 64:
+                sees[r0 + i] = sum(1 << j for j in path)
+    return position, sees
+
+
+def walk_reference(row_start, seq_len, parent, token, predicted, rows, cached):
+    kept, cached = [], list(cached)
+    path, emitted = np.full(rows, -1, np.int64), np.full(rows, -1, np.int64)
+    for b in range(len(seq_len)):
+        r0, n = row_start[b], row_start[b + 1] - row_start[b]
+        way = []
+        if seq_len[b] >= n:
+            if n > 64:
+                way = list(range(n))
+            elif n > 0:
+                way = [0]
+                while True:
+                    say = predicted[r0 + way[-1]]
+                    nxt = [i for i in range(way[-1] + 1, n) if parent[r0 + i] == way[-1] and (token[r0 + i] == say or token[r0 + i] < 0)]
+                    if not nxt:
+                        break
+                    way.append(nxt[0])
+            cached[b] = seq_len[b] - n + len(way)
+        kept.append(len(way))
+        for j, i in enumerate(way):
+            path[r0 + j], emitted[r0 + j] = i, predicted[r0 + i]
+    return kept, cached, path, emitted
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------------
+def attention_reference(q, K, V, table, row_start, seq_len, scale, half, few, many, sees=None, smallest=2.0 ** -25, floor=0.0):
+    """As operators_util's, and with what trees' rows see.  few, many: the relative error of a probability in the product with v where a
+    sequence has up to 32 rows times heads of a key head, where it has more; floor: what a key's elements are off by beside their rounding."""
+    rows, Hq, hd = q.shape
+    n_pages, Hkv, ps, _ = K.shape
+    out, tol = np.full((rows, Hq, hd), np.nan), np.zeros((rows, Hq, hd))
+    for b in range(len(seq_len)):
+        f, n = row_start[b + 1] - row_start[b], int(seq_len[b])
+        blocks = np.array([table[b, j] if j < table.shape[1] else -1 for j in range(-(-max(n, 0) // ps))], int)
+        there = np.repeat((blocks >= 0) & (blocks < n_pages), ps)[:max(n, 0)]
+        at = np.where((blocks >= 0) & (blocks < n_pages), blocks, 0)
+        hp = few if f * Hq // Hkv <= 32 else many
+        for h in range(Hq):
+            k = K[at, h // (Hq // Hkv)].reshape(-1, hd)[:max(n, 0)]
+            v = V[at, h // (Hq // Hkv)].reshape(-1, hd)[:max(n, 0)]
+            for i in range(f):
+                t = row_start[b] + i
+                j = np.arange(max(n, 0))
+                if sees is not None and f <= 64:
+                    bits = np.array([int(sees[t]) >> x & 1 for x in range(f)], bool)
+                    see = there.copy()
+                    see[max(n - f, 0):] &= bits[max(f - n, 0):]
+                else:
+                    see = there & (j <= n - f + i)
+                if not see.any():
+                    out[t, h] = 0
+                    continue
+                ks, vs = k[see], v[see]
+                with np.errstate(invalid="ignore", over="ignore"):
+                    x = ks @ q[t, h] * scale
+                    p = np.exp(x - x.max())
+                    p /= p.sum()
+                    out[t, h] = p @ vs
+                    A = p @ np.abs(vs)
+                    d = 2 * ((hd + 2) * 2.0 ** -24 * (np.abs(ks) @ np.abs(q[t, h])).max() * scale + 2.0 ** -22 * (x.max() - x).max()
+                             + floor * np.abs(q[t, h]).sum() * scale) + 2 * (len(x) + 64) * 2.0 ** -24
+                    tol[t, h] = half * np.abs(out[t, h]) + A * (hp + d) + smallest
+    return out, tol
+
+
+class Attend(ou.Attend):
+    """Sequences over a random pool, in 8 bits if `held`; sees: a number for each row, or None."""
+
+    def __init__(self, dtype, lens, fresh, Hq, Hkv, hd, page, held=True, sees=None, powers=(0, 0), **kw):
+        super().__init__(dtype, lens, fresh, Hq, Hkv, hd, page, **kw)
+        self.held, self.sees = held, sees
+        if held:
+            # rows of different sizes: each times 2^(something of `powers`)
+            rng = np.random.default_rng(len(lens) + hd)
+            grow = lambda t: t.double().numpy() * np.exp2(rng.integers(powers[0], powers[1] + 1, t.shape[:3]))[..., None]  # noqa: E731
+            self.kc, self.kb = quantise(grow(self.K), dtype)
+            self.vc, self.vb = quantise(grow(self.V), dtype)
+
+    def numbers(self):
+        if not self.held:
+            return self.K.double().numpy(), self.V.double().numpy()
+        return values_of(self.kc, self.kb), values_of(self.vc, self.vb)
+
+    def call(self, scale=0.0, stream=None, max_fresh=None, workspace=None, poison=7.0, run=True):
+        import torch
+        hd, Hq = self.hd, self.Hq
+        dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+        d = self.dev = dict(q=self.q.view(self.rows, -1).cuda(), out=torch.full((self.rows, Hq * hd), poison, dtype=self.dt).cuda(), table=dev(self.table),
+                            row_start=dev(self.row_start), seq_len=torch.tensor(self.lens, dtype=torch.int32).cuda())
+        if self.held:
+            d.update(k=dev(ou.rows_to_pages(self.kc, held_key_at)), v=dev(ou.rows_to_pages(self.vc, held_value_at)), scale=dev(scales_to_pages(self.kb, self.vb)))
+        else:
+            d.update(k=self.raw(self.K, ou.key_at), v=self.raw(self.V, ou.value_at))
+        if self.sees is not None:
+            s = np.zeros(self.rows, np.uint64)
+            s[:len(self.sees)] = self.sees
+            d["sees"] = dev(s.view(np.int64))
+        at = lambda k: d[k].data_ptr() if k in d else None  # noqa: E731
+        self.cache = pkg.StairsPagedCache(k=at("k"), v=at("v"), dtype=ou.CODE[self.dtype], n_pages=self.n_pages, page_size=self.page, n_kv_heads=self.Hkv,
+                                          head_dim=hd, held=pkg.DTYPE_E4M3 if self.held else 0, scale=at("scale"))
+        a = self.args = pkg.StairsPagedAttention(n_seqs=len(self.lens), max_blocks=self.max_blocks, rows=self.rows, n_heads=Hq,
+                                                 max_fresh=max(self.fresh) if max_fresh is None else max_fresh, q=at("q"), out=at("out"), q_stride=Hq * hd,
+                                                 out_stride=Hq * hd, block_table=at("table"), row_start=at("row_start"), seq_len=at("seq_len"), scale=scale,
+                                                 sees=at("sees"))
+        need = pkg.stairs_paged_attention_workspace(self.cache, a)
+        d["work"] = torch.zeros(max(need, 16), dtype=torch.uint8).cuda() if workspace is None else workspace
+        a.workspace, a.workspace_bytes = d["work"].data_ptr(), d["work"].numel()
+        torch.cuda.synchronize()
+        if not run:
+            return None
+        pkg.stairs_paged_attention(self.cache, a, torch.cuda.current_stream().cuda_stream if stream is None else stream)
+        torch.cuda.synchronize()
+        return self.result(0, poison)
+
+    def reference(self, scale=None):
+        K, V = self.numbers()
+        half = ou.HALF_STEP[self.dtype]
+        # (two numbers over 8-bit pages: bfloat16; two halves: 2^-37 of a value for each key, where all of them are far below the largest)
+        few = TWO["bf16"] if self.held else TWO[self.dtype]
+        smallest = ou.SMALLEST[self.dtype]
+        if self.dtype == "fp16":
+            smallest += smallest if self.held else max(self.lens) * 2.0 ** -37 * float(self.V.abs().nan_to_num(0, 0, 0).max())
+        return attention_reference(self.q.double().numpy(), K, V, self.table, self.row_start, self.lens, self.scale if scale is None else scale, half, few, half,
+                                   self.sees, smallest, 2.0 ** -25 if self.held and self.dtype == "fp16" else 0.0)
