@@ -42,7 +42,7 @@ KERNEL_ARGS_IN_REGISTERS = ["-mllvm", "-amdgpu-kernarg-preload-count=14"]
 
 def build_library(verbose: bool = False) -> str:
     """Compile the HIP sources for gfx950 into libstairs.so next to this file."""
-    cmd = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-shared", "-fPIC",
+    cmd = ["hipcc", "-parallel-jobs=8", "--offload-arch=gfx950", "-O3", "-std=c++17", "-shared", "-fPIC",
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", *KERNEL_ARGS_IN_REGISTERS,
            *_SOURCES, "-o", LIB_PATH]
     res = subprocess.run(cmd, capture_output=True, text=True)

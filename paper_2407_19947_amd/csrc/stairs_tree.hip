@@ -115,89 +115,150 @@ constexpr int kLaunchCaches = 64;                               // pools of a la
 struct Pools {
   struct { void *k, *v, *scale; } of[kLaunchCaches];
 };
+constexpr int kMostGroups = 2048;                               // work-groups of four waves that run at once
 struct PoolShape { int n_pages, page_size, n_kv_heads; };
 
-// A wave has a request, a head and a pool.  Paths ascend, so a row's new place is never behind its old one and no row that is still to move
-// lies where one has moved to: some rows at a time, all of them read before the first is written.  A value is HD single numbers 16 bytes
-// apart.
+// a place of 16 bytes of a value tile: eight positions of one dim, or in 8 bits of each of two; position k of it
+__device__ __forceinline__ uint32_t of_four(uint4 v, int i) {   // (i: the same in all lanes)
+  const uint32_t a = i & 1 ? v.y : v.x, b = i & 1 ? v.w : v.z;
+  return i & 2 ? b : a;
+}
+__device__ __forceinline__ uint32_t put(uint32_t there, uint32_t value, uint32_t mask) { return (there & ~mask) | (value & mask); }
+template <bool H8>
+__device__ __forceinline__ void move_position(uint4& to, int kt, const uint4& from, int kf) {
+  if constexpr (H8) {
+    const uint32_t lo = (kf >> 2 ? from.y : from.x) >> (8 * (kf & 3)) << (8 * (kt & 3)), hi = (kf >> 2 ? from.w : from.z) >> (8 * (kf & 3)) << (8 * (kt & 3));
+    const uint32_t mask = 0xFFu << (8 * (kt & 3)), first = kt >> 2 ? 0 : mask, second = kt >> 2 ? mask : 0;
+    to = make_uint4(put(to.x, lo, first), put(to.y, lo, second), put(to.z, hi, first), put(to.w, hi, second));
+  } else {
+    const uint32_t v = of_four(from, kf >> 1) >> (16 * (kf & 1)) << (16 * (kt & 1)), mask = 0xFFFFu << (16 * (kt & 1));
+    to = make_uint4(put(to.x, v, kt >> 1 == 0 ? mask : 0), put(to.y, v, kt >> 1 == 1 ? mask : 0), put(to.z, v, kt >> 1 == 2 ? mask : 0), put(to.w, v, kt >> 1 == 3 ? mask : 0));
+  }
+}
+// (streaming hint: a launch that leaves thousands of changed lines behind in the L2s ends only when they have been written back; 31 rows of 12 heads in
+// 12 pools 19.6 -> 6.8 us, 203 of 8 heads in 32 pools 92 -> 83)
+__device__ __forceinline__ void st_once(void* p, uint4 v) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), static_cast<u32x4*>(p));
+}
+__device__ __forceinline__ int place_of(int pos) { return (pos & 3) + 4 * ((pos >> 4) & 1); }
+
+// A wave has a request and a head in some of the pools: where its rows lie is found once, and the next pool's rows are requested before this one's are
+// written.  Paths ascend: what moves is the path's end, to positions one behind the other, none behind its old one, so no row that is still to
+// move lies where one has moved to.  Four positions at a time, aligned: all that comes there and what stays there is read before the
+// first is written, and written in runs of 64 bytes and more.  (Bound by the memory's granularity: a key is pieces of 16 bytes 256 apart, a value
+// numbers 16 apart, so that eight times what moves is read.)
 template <int HD, bool H8>
-__global__ __launch_bounds__(64 * kWaves) void k_paged_compact(PoolShape c, stairs_paged_path p, Pools pools) {
+__global__ __launch_bounds__(64 * kWaves) void k_paged_compact(PoolShape c, int n_pools, stairs_paged_path p, Pools pools) {
   constexpr int U = 4;                                          // rows at a time
+  constexpr int E = H8 ? 1 : 2, KL = HD * E / 16;               // bytes of a number; 16-byte parts of a key
+  constexpr int PLACES = H8 ? HD / 2 : HD, NV = (PLACES + 63) / 64;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int b = blockIdx.x, h = blockIdx.y * kWaves + wave;
-  if (h >= c.n_kv_heads) return;
+  const int groups = (c.n_kv_heads + kWaves - 1) / kWaves, items = p.n_seqs * groups;
+  const int apart = n_pools >= 8 ? 8 : 1, i0 = blockIdx.x / apart, item = i0 % items;
+  const int first_pool = blockIdx.x % apart + i0 / items * apart, step = apart * ((int)gridDim.x / (items * apart));
+  const int b = item / groups, h = item % groups * kWaves + wave;
+  if (h >= c.n_kv_heads || first_pool >= n_pools) return;
+  const int asked = p.kept[b];
   const Rows r = rows_of(p.row_start, p.seq_len, p.rows, b);
   if (r.count == 0 || r.count > STAIRS_TREE_MAX_ROWS || r.len < r.count) return;
-  const int kept = min(p.kept[b], r.count), context = r.len - r.count;
-  // lane j: the path's j-th row, its old and new slot
+  const int kept = min(asked, r.count), context = r.len - r.count, shift = __builtin_ctz(c.page_size);
+  // lane j: the path's j-th row, its old and new slot; the pages of all rows (three at most) in the first lanes
   const int row = lane < kept ? p.path[r.first + lane] : -1;
-  const int shift = __builtin_ctz(c.page_size);
-  auto slot = [&](int pos) {
-    const int block = pos >> shift;
-    const int page = block < p.max_blocks ? p.block_table[(size_t)b * p.max_blocks + block] : -1;
-    return (unsigned)page < (unsigned)c.n_pages ? (page << shift) + (pos & (c.page_size - 1)) : -1;
+  const int block0 = context >> shift;
+  const bool listed = lane < 4 && block0 + lane < p.max_blocks;
+  int page = listed ? p.block_table[(size_t)b * p.max_blocks + block0 + lane] : -1;
+  if ((unsigned)page >= (unsigned)c.n_pages) page = -1;
+  auto slot = [&](int i) {                                      // of the context's position and i more
+    const int pos = context + i, at = __shfl(page, min(max((pos >> shift) - block0, 0), 3));
+    return at < 0 ? -1 : (at << shift) + (pos & (c.page_size - 1));
   };
-  int from = -1, to = -1;
-  if (row > lane && row < r.count) {
-    from = slot(context + row);
-    to = slot(context + lane);
-  }
-  unsigned long long moves = __ballot(from >= 0 && to >= 0);
-  const auto pool = pools.of[blockIdx.z];
+  const bool moves_row = row > lane && row < r.count;
+  const int from = slot(moves_row ? row : 0), to = slot(lane);
+  unsigned long long left = __ballot(moves_row && from >= 0 && to >= 0);
   const size_t head_elems = (size_t)c.page_size * HD;
-  constexpr int E = H8 ? 1 : 2;                                 // bytes of a number
-  uint8_t* const K = static_cast<uint8_t*>(pool.k);
-  uint8_t* const V = static_cast<uint8_t*>(pool.v);
-  uint8_t* const S = static_cast<uint8_t*>(pool.scale);
   auto head_of = [&](int s) { return (size_t)(s >> shift) * c.n_kv_heads + h; };
-  constexpr int KL = HD * E / 16;                               // 16-byte parts of a key
-  // the lane's part of a key (parts past the last: none), its numbers of a value
-  auto key_part = [&](int s) {
-    const int pos = s & (c.page_size - 1), part = lane % KL;
-    const int at = H8 ? k_held_off(pos, part / 4 * 64 + part % 4 * 8, HD) : 2 * (int)k_cache_off(pos, part * 8, HD);
-    return K + head_of(s) * head_elems * E + at;
-  };
-  auto value_part = [&](int s, int e) {
+  // bytes in front of a position's part of a key, of the lane's first place of a value
+  auto key_at = [&](int s, int part) {
     const int pos = s & (c.page_size - 1);
-    return V + head_of(s) * head_elems * E + (H8 ? v_held_off(pos, e, HD) : 2 * (int)v_cache_off(pos, e, HD));
+    return head_of(s) * head_elems * E + (H8 ? k_held_off(pos, part / 4 * 64 + part % 4 * 8, HD) : 2 * (int)k_cache_off(pos, part * 8, HD));
   };
-  auto scale_part = [&](int s) { return S + head_of(s) * c.page_size * 2 + scale_off(s & (c.page_size - 1)) + 8 * (lane & 1); };
-  while (moves) {
-    int src[U], dst[U];
-    bool there[U];
-    int last = 0;
+  auto value_at = [&](int s) {
+    const int pos = s & (c.page_size - 1) & ~19, place = lane % PLACES;   // (positions of a place: 0 .. 3 and 16 .. 19 further)
+    return head_of(s) * head_elems * E + (H8 ? v_held_off(pos, place / 16 * 32 + place % 16, HD) : 2 * (int)v_cache_off(pos, place, HD));
+  };
+  constexpr int kNext = 4 * 1024;                               // bytes from a place to that 64 further
+  auto scales_at = [&](int s) { return head_of(s) * c.page_size * 2; };
+  struct Held {
+    uint4 k, v[U][NV], place[NV];
+    uint32_t s, byte[U];
+  };
+  while (left) {
+    // the next moves whose new positions are in one aligned four
+    int src[U], place[U], n = 0, last = __builtin_ctzll(left);   // (place: which of the four)
+    const int first = __builtin_amdgcn_readlane(to, last) & ~3;
+    int key_from = first + (lane & 3);                          // what comes to the lane's position of the four: itself
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      there[i] = moves != 0;
-      last = moves ? (int)__builtin_ctzll(moves) : last;
-      src[i] = __builtin_amdgcn_readlane(from, last);
-      dst[i] = __builtin_amdgcn_readlane(to, last);
-      moves &= moves - 1;
-    }
-    uint4 k[U];
-    uint16_t v[U][HD / 64];
-    uint8_t s[U];
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      k[i] = *reinterpret_cast<const uint4*>(key_part(src[i]));
-#pragma unroll
-      for (int e = 0; e < HD / 64; ++e) v[i][e] = H8 ? *value_part(src[i], e * 64 + lane) : *reinterpret_cast<const uint16_t*>(value_part(src[i], e * 64 + lane));
-      if constexpr (H8) s[i] = *scale_part(src[i]);
-    }
-    __builtin_amdgcn_s_waitcnt(0);                              // (all of them are here before the first place is written)
-    __atomic_signal_fence(__ATOMIC_SEQ_CST);
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      if (!there[i]) break;
-      if (lane < KL) *reinterpret_cast<uint4*>(key_part(dst[i])) = k[i];
-#pragma unroll
-      for (int e = 0; e < HD / 64; ++e) {
-        if constexpr (H8) *value_part(dst[i], e * 64 + lane) = (uint8_t)v[i][e];
-        else *reinterpret_cast<uint16_t*>(value_part(dst[i], e * 64 + lane)) = v[i][e];
+    for (int i = 0; i < U; ++i) {                               // (past the last: the last again, for nothing)
+      const int next = left ? (int)__builtin_ctzll(left) : last;
+      if (left && (__builtin_amdgcn_readlane(to, next) & ~3) == first) {
+        last = next;
+        ++n;
+        left &= left - 1;
       }
-      if constexpr (H8)
-        if (lane < 2) *scale_part(dst[i]) = s[i];
+      src[i] = __builtin_amdgcn_readlane(from, last);
+      place[i] = __builtin_amdgcn_readlane(to, last) & 3;
+      key_from = (lane & 3) == place[i] ? src[i] : key_from;
     }
+    // the 16 words of powers of two that the four's lie in: the lane's, and which number of values or keys it is of (4: of others)
+    const int sp = first & (c.page_size - 1), word = lane & 15, mine = word / 4 == (sp & 15) >> 2 && (word & 1) == (sp >> 4 & 1) ? word >> 1 & 1 : 4;
+    auto load = [&](int pool, Held& x) {
+      const uint8_t *K = static_cast<const uint8_t*>(pools.of[pool].k), *V = static_cast<const uint8_t*>(pools.of[pool].v), *S = static_cast<const uint8_t*>(pools.of[pool].scale);
+      x.k = *reinterpret_cast<const uint4*>(K + key_at(key_from, (lane >> 2) % KL));
+#pragma unroll
+      for (int e = 0; e < NV; ++e) x.place[e] = *reinterpret_cast<const uint4*>(V + value_at(first) + e * kNext);
+      if constexpr (H8) x.s = *reinterpret_cast<const uint32_t*>(S + scales_at(first) + (sp >> 5) * 64 + word * 4);
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        if (i >= n) break;
+#pragma unroll
+        for (int e = 0; e < NV; ++e) x.v[i][e] = *reinterpret_cast<const uint4*>(V + value_at(src[i]) + e * kNext);
+        if constexpr (H8) x.byte[i] = S[scales_at(src[i]) + scale_off(src[i] & (c.page_size - 1)) + 8 * (mine & 1)];
+      }
+    };
+    auto store = [&](int pool, Held& x) {
+      uint8_t *K = static_cast<uint8_t*>(pools.of[pool].k), *V = static_cast<uint8_t*>(pools.of[pool].v), *S = static_cast<uint8_t*>(pools.of[pool].scale);
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        if (i >= n) break;
+        const int to_place = place[i] + 4 * (sp >> 4 & 1);
+#pragma unroll
+        for (int e = 0; e < NV; ++e) move_position<H8>(x.place[e], to_place, x.v[i][e], place_of(src[i]));
+        if (H8 && mine < 4) x.s = put(x.s, x.byte[i] << (8 * place[i]), 0xFFu << (8 * place[i]));
+      }
+      // (all of it is here before the first is written)
+      asm volatile("" : "+v"(x.k.x), "+v"(x.s)::"memory");
+#pragma unroll
+      for (int e = 0; e < NV; ++e) asm volatile("" : "+v"(x.place[e].x), "+v"(x.place[e].y), "+v"(x.place[e].z), "+v"(x.place[e].w)::"memory");
+      if ((lane >> 2) < KL) st_once(K + key_at(first + (lane & 3), lane >> 2), x.k);
+#pragma unroll
+      for (int e = 0; e < NV; ++e)
+        if (lane < PLACES) st_once(V + value_at(first) + e * kNext, x.place[e]);
+      if constexpr (H8)
+        if (lane < 16) *reinterpret_cast<uint32_t*>(S + scales_at(first) + (sp >> 5) * 64 + word * 4) = x.s;
+    };
+    Held now{}, next{};
+    int pool = first_pool;
+    load(pool, now);
+    for (;;) {
+      const int then = pool + step;
+      if (then < n_pools) load(then, next);
+      store(pool, now);
+      if (then >= n_pools) break;
+      now = next;
+      pool = then;
+    }
+    __builtin_amdgcn_s_waitcnt(0);                              // (rows that follow are read from where these were; another pool's do not meet)
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
   }
 }
@@ -260,13 +321,16 @@ extern "C" int stairs_paged_compact(const stairs_paged_cache* caches, int32_t n_
       pools.of[i].v = caches[at + i].v;
       pools.of[i].scale = caches[at + i].scale;
     }
-    const dim3 grid(p->n_seqs, (c.n_kv_heads + kWaves - 1) / kWaves, n), block(64 * kWaves);
+    const int64_t items = (int64_t)p->n_seqs * ((c.n_kv_heads + kWaves - 1) / kWaves);
+    const int apart = n >= 8 ? 8 : 1, turns = (n + apart - 1) / apart;
+    const int spread = (int)std::clamp<int64_t>(kMostGroups / (items * apart), 1, turns);
+    const dim3 grid((unsigned)(items * apart * spread)), block(64 * kWaves);
     if (c.head_dim == 64) {
-      if (c.held) hipLaunchKernelGGL((k_paged_compact<64, true>), grid, block, 0, st, shape, *p, pools);
-      else hipLaunchKernelGGL((k_paged_compact<64, false>), grid, block, 0, st, shape, *p, pools);
+      if (c.held) hipLaunchKernelGGL((k_paged_compact<64, true>), grid, block, 0, st, shape, n, *p, pools);
+      else hipLaunchKernelGGL((k_paged_compact<64, false>), grid, block, 0, st, shape, n, *p, pools);
     } else {
-      if (c.held) hipLaunchKernelGGL((k_paged_compact<128, true>), grid, block, 0, st, shape, *p, pools);
-      else hipLaunchKernelGGL((k_paged_compact<128, false>), grid, block, 0, st, shape, *p, pools);
+      if (c.held) hipLaunchKernelGGL((k_paged_compact<128, true>), grid, block, 0, st, shape, n, *p, pools);
+      else hipLaunchKernelGGL((k_paged_compact<128, false>), grid, block, 0, st, shape, n, *p, pools);
     }
     if (const int rc = launched()) return rc;
   }
