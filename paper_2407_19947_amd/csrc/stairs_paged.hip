@@ -253,6 +253,8 @@ __device__ __forceinline__ X ld_once_as(const void* p) {
   return __builtin_bit_cast(X, __builtin_nontemporal_load(static_cast<const u32x4*>(p)));
 }
 
+__device__ __forceinline__ void st_once(void* p, uint4 v) { __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), static_cast<u32x4*>(p)); }
+
 // Bound by memory, with few rows by latency.  A work-group has 32 rows and some of the n_heads + 2 n_kv_heads heads (so many
 // groups of them that there are work for all CUs); the rows' rotations are formed once for all its heads.  q and k: a thread takes 8
 // pairs of a row, 16 bytes of either half; in a key tile the same 8 dims of 8 rows are one line.  v: a head's rows go through LDS;
@@ -265,12 +267,13 @@ constexpr int kAppendRows = 32;
 template <typename T, int HD, bool H8>
 __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stairs_paged_rows a, double log2_theta) {
   constexpr int AHEAD = 19, BEHIND = 16;                        // rows around these that decide how theirs are stored
+  constexpr int kHeads = 4;
   __shared__ union {
     float2 cs[kAppendRows][HD / 2];
-    T v[kAppendRows + AHEAD][HD];
-    uint8_t v8[kAppendRows + AHEAD][HD];
+    T v[H8 ? 1 : kAppendRows + AHEAD][HD];
+    uint8_t v8[H8 ? kHeads : 1][kAppendRows + AHEAD][HD];
   } lds;
-  __shared__ uint8_t s_vb[H8 ? kAppendRows + AHEAD : 1];        // the values' powers of two
+  __shared__ uint8_t s_vb[H8 ? kHeads : 1][kAppendRows + AHEAD];   // the values' powers of two
   __shared__ int s_slots[BEHIND + kAppendRows + AHEAD], s_pos[kAppendRows], s_unit[kAppendRows], s_units, s_end;
   const int* const s_slot = s_slots + BEHIND;
   // (an XCD takes rows that follow each other: lines that two work-groups share meet in one L2; 16000 rows of 48 heads 104 -> 101 us)
@@ -337,8 +340,13 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
     x8 lo = ld_once_as<x8>(src), hi = ld_once_as<x8>(src + HD / 2);
     if (rotate) turn(lo, hi, r, e);
     T* dst = static_cast<T*>(a.q_out) + (size_t)(t0 + r) * a.q_out_stride + h * HD + e;
-    *reinterpret_cast<x8*>(dst) = lo;
-    *reinterpret_cast<x8*>(dst + HD / 2) = hi;
+    if constexpr (H8) {                                         // (beside 8-bit pages the streaming hint saves 2 of 50 us)
+      st_once(dst, __builtin_bit_cast(uint4, lo));
+      st_once(dst + HD / 2, __builtin_bit_cast(uint4, hi));
+    } else {
+      *reinterpret_cast<x8*>(dst) = lo;
+      *reinterpret_cast<x8*>(dst + HD / 2) = hi;
+    }
   }
   const size_t head_scales = (size_t)c.page_size * 2;
   uint8_t* const scales = static_cast<uint8_t*>(c.scale);
@@ -400,42 +408,52 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
   }
   const int units = only == 1 ? 0 : s_units, staged = s_end;
   if (units == 0) return;
-  for (int h = k0; h < k1; ++h) {
-    __syncthreads();
-    for (int i = tid; i < staged * (HD / 8); i += 256) {
-      const int r = i / (HD / 8), e = i % (HD / 8) * 8;
-      const x8 in = ld_once_as<x8>(static_cast<const T*>(a.v) + (size_t)(t0 + r) * a.v_stride + h * HD + e);
-      if constexpr (H8) {
-        float x[8];
-        uint32_t top = 0;
+  if constexpr (H8) {
+    // four heads at a time: their rows are all requested before the first is waited for
+    for (int h0 = k0; h0 < k1; h0 += kHeads) {
+      const int nh = min(kHeads, k1 - h0), per_row = nh * (HD / 8);
+      __syncthreads();
+      for (int i0 = tid; i0 < staged * per_row; i0 += 256 * 8) {
+        x8 in[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          x[k] = Elem<T>::up(in[k]);
-          top = max(top, finite_bits(x[k]));
+        for (int j = 0; j < 8; ++j) {
+          const int i = min(i0 + j * 256, staged * per_row - HD / 8 + tid % (HD / 8)), r = i / per_row, e = i % per_row * 8;   // (past the last: the last row's again)
+          in[j] = ld_once_as<x8>(static_cast<const T*>(a.v) + (size_t)(t0 + r) * a.v_stride + h0 * HD + e);
         }
-        if (__is_same(T, _Float16) && top > kHalfTop) top = cut(x, 8);
-        const uint32_t b = scale_byte(group_max(top, HD / 8));
-        const float f = scale_inverse(b);
-        *reinterpret_cast<uint2*>(&lds.v8[r][e]) = make_uint2(codes_of(x[0] * f, x[1] * f, x[2] * f, x[3] * f), codes_of(x[4] * f, x[5] * f, x[6] * f, x[7] * f));
-        if (e == 0) s_vb[r] = (uint8_t)b;
-      } else {
-        *reinterpret_cast<x8*>(&lds.v[r][e]) = in;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int i = i0 + j * 256, r = i / per_row, e = i % per_row * 8;
+          if (i >= staged * per_row) break;
+          float x[8];
+          uint32_t top = 0;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            x[k] = Elem<T>::up(in[j][k]);
+            top = max(top, finite_bits(x[k]));
+          }
+          if (__is_same(T, _Float16) && top > kHalfTop) top = cut(x, 8);
+          const uint32_t b = scale_byte(group_max(top, HD / 8));
+          const float f = scale_inverse(b);
+          *reinterpret_cast<uint2*>(&lds.v8[e / HD][r][e % HD]) = make_uint2(codes_of(x[0] * f, x[1] * f, x[2] * f, x[3] * f), codes_of(x[4] * f, x[5] * f, x[6] * f, x[7] * f));
+          if (e % HD == 0) s_vb[e / HD][r] = (uint8_t)b;
+        }
       }
-    }
-    __syncthreads();
-    if constexpr (H8) {
+      __syncthreads();
       // a place of 16 bytes: dims e and e + 16, eight positions of either
-      for (int i = tid; i < units * (HD / 2); i += 256) {
-        const int j = i % (HD / 2), e = (j >> 4) * 32 + (j & 15), u = s_unit[i / (HD / 2)], r = u >> 2, kind = u & 3, slot = s_slot[r], p = slot & (c.page_size - 1);
-        const size_t head = (size_t)(slot >> ps_shift) * nk + h;
+      for (int i = tid; i < nh * units * (HD / 2); i += 256) {
+        const int j = i % (HD / 2), e = (j >> 4) * 32 + (j & 15), at = i / (HD / 2), hh = at / units, u = s_unit[at - hh * units], r = u >> 2, kind = u & 3, slot = s_slot[r];
+        const int p = slot & (c.page_size - 1);
+        const size_t head = (size_t)(slot >> ps_shift) * nk + h0 + hh;
         uint8_t* dst = static_cast<uint8_t*>(c.v) + head * head_elems + v_held_off(p, e, HD);
         uint8_t* sdst = scales + head * head_scales + scale_off(p) + 8;
-        auto four = [&](int row, int dim) { return lds.v8[row][dim] | lds.v8[row + 1][dim] << 8 | lds.v8[row + 2][dim] << 16 | (uint32_t)lds.v8[row + 3][dim] << 24; };
-        auto bytes = [&](int row) { return s_vb[row] | s_vb[row + 1] << 8 | s_vb[row + 2] << 16 | (uint32_t)s_vb[row + 3] << 24; };
+        const auto& v8 = lds.v8[hh];
+        const auto& vb = s_vb[hh];
+        auto four = [&](int row, int dim) { return v8[row][dim] | v8[row + 1][dim] << 8 | v8[row + 2][dim] << 16 | (uint32_t)v8[row + 3][dim] << 24; };
+        auto bytes = [&](int row) { return vb[row] | vb[row + 1] << 8 | vb[row + 2] << 16 | (uint32_t)vb[row + 3] << 24; };
         if (kind == 1) {
-          dst[0] = lds.v8[r][e];
-          dst[8] = lds.v8[r][e + 16];
-          if (j == 0) *sdst = s_vb[r];
+          dst[0] = v8[r][e];
+          dst[8] = v8[r][e + 16];
+          if (j == 0) *sdst = vb[r];
         } else if (kind == 2) {
           *reinterpret_cast<uint32_t*>(dst) = four(r, e);
           *reinterpret_cast<uint32_t*>(dst + 8) = four(r, e + 16);
@@ -445,7 +463,16 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
           if (j == 0) *reinterpret_cast<uint2*>(sdst) = make_uint2(bytes(r), bytes(r + 16));
         }
       }
-    } else
+    }
+    return;
+  }
+  for (int h = k0; h < k1; ++h) {
+    __syncthreads();
+    for (int i = tid; i < staged * (HD / 8); i += 256) {
+      const int r = i / (HD / 8), e = i % (HD / 8) * 8;
+      *reinterpret_cast<x8*>(&lds.v[r][e]) = ld_once_as<x8>(static_cast<const T*>(a.v) + (size_t)(t0 + r) * a.v_stride + h * HD + e);
+    }
+    __syncthreads();
     for (int i = tid; i < units * HD; i += 256) {
       const int e = i % HD, r = s_unit[i / HD] >> 2, kind = s_unit[i / HD] & 3, slot = s_slot[r];
       T* dst = static_cast<T*>(c.v) + ((size_t)(slot >> ps_shift) * nk + h) * head_elems + v_cache_off(slot & (c.page_size - 1), e, HD);
@@ -532,12 +559,12 @@ __global__ __launch_bounds__(256) void k_paged_read(stairs_paged_cache c, stairs
 #pragma unroll
         for (int t = 0; t < HD / 64; ++t) {
           const uint4 v = *reinterpret_cast<const uint4*>(src + k_held_off(p, 8 * g, HD) + t * 1024);
-          *reinterpret_cast<uint4*>(dst + 64 * t) = plain_row<T>(v.x, v.y, f);
-          *reinterpret_cast<uint4*>(dst + 64 * t + 32) = plain_row<T>(v.z, v.w, f);
+          st_once(dst + 64 * t, plain_row<T>(v.x, v.y, f));
+          st_once(dst + 64 * t + 32, plain_row<T>(v.z, v.w, f));
         }
       } else {
 #pragma unroll
-        for (int j = 0; j < HD / 32; ++j) *reinterpret_cast<uint4*>(dst + 32 * j) = *reinterpret_cast<const uint4*>(src + 2 * k_cache_off(p, 32 * j + 8 * g, HD));
+        for (int j = 0; j < HD / 32; ++j) st_once(dst + 32 * j, *reinterpret_cast<const uint4*>(src + 2 * k_cache_off(p, 32 * j + 8 * g, HD)));
       }
     }
   }
@@ -594,7 +621,7 @@ __global__ __launch_bounds__(256) void k_paged_read(stairs_paged_cache c, stairs
     for (int i = tid; i < n * (HD / 8); i += 256) {
       const int r = i / (HD / 8), e = i % (HD / 8) * 8;
       if (s_slot[r] < 0) continue;
-      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.v) + (size_t)(t0 + r) * a.v_stride + h * HD + e) = *reinterpret_cast<const uint4*>(&s_v[r][e]);
+      st_once(static_cast<uint16_t*>(a.v) + (size_t)(t0 + r) * a.v_stride + h * HD + e, *reinterpret_cast<const uint4*>(&s_v[r][e]));
     }
   }
 }
@@ -705,6 +732,7 @@ struct Span {
   int slots;
   int min_units, whole;       // of a piece; tiles that are not cut (find_piece)
   int first_block;            // the launch's work-groups from here on
+  int start;                  // units that a piece's start and join are worth
   int tickets;                // its first in the workspace
   int64_t partials;           // bytes in front of its partial results there
 };
@@ -744,6 +772,7 @@ __device__ __forceinline__ T wave_scan(T v) {                  // inclusive
 __device__ __forceinline__ int quotient(long long a, int b) {    // a >= 0, b > 0 (a division of 64 bits is over a hundred instructions)
   return (a >> 32) == 0 ? (int)((unsigned)a / (unsigned)b) : (int)min(a / b, (long long)INT32_MAX);
 }
+template <bool WEIGH>
 __device__ __forceinline__ bool find_piece(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, Piece& out) {
   const int lane = threadIdx.x & 63;
   const int block = blockIdx.x - sp.first_block, kvh = block % c.n_kv_heads, item = block / c.n_kv_heads;
@@ -783,7 +812,29 @@ __device__ __forceinline__ bool find_piece(const stairs_paged_cache& c, const st
         if (__builtin_amdgcn_readfirstlane(__float_as_int(wave_sum((float)w.groups * pieces) - fit)) <= 0) hi = mid;
         else lo = mid + 1;
       }
-      if (lo < 4 * per) per = lo;
+      if constexpr (WEIGH) {
+        // ... or more than run at once: what all pieces take, their starts and joins (of so many units each) with them, and half a piece, for
+        // which CUs stand half empty at the end.  (Trees of 61 rows of 32 sequences of 500 .. 6000 keys, 8 heads: one round means whole tiles of up to 94 units.)
+        auto cost = [&](int n) {
+          const float pieces = fmaxf(1.f, floorf(((float)(w.units + n) - 0.5f) * __builtin_amdgcn_rcpf((float)n)));
+          return wave_sum((float)w.groups * pieces) * (float)(c.n_kv_heads * sp.start) * __builtin_amdgcn_rcpf((float)sp.slots) + 0.5f * (float)n;
+        };
+        float least = cost(lo);
+        int best = lo;
+#pragma unroll 1
+        for (int k = 4; k < 12; ++k) {
+          const int n = per * k / 4;
+          if (n >= lo) break;
+          const float x = cost(n);
+          if (x < least) {
+            least = x;
+            best = n;
+          }
+        }
+        per = best;
+      } else if (lo < 4 * per) {
+        per = lo;
+      }
     }
   }
   per = __builtin_amdgcn_readfirstlane(per);
@@ -1002,7 +1053,7 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
   typedef std::conditional_t<H8, uint8_t, T> PT;
   constexpr int KK = HD / 32, ET = HD / 16, NK = H8 ? KK : 2 * KK, NV = H8 ? ET / 2 : ET;
   Piece w;
-  if (!find_piece(c, a, sp, w)) return;
+  if (!find_piece<false>(c, a, sp, w)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j = lane & 15, g = lane >> 4;
   const int G = a.n_heads / c.n_kv_heads, cols = w.rows * G, col0 = w.group * 16 * CT;
   const int limit = a.max_blocks * c.page_size;
@@ -1282,6 +1333,58 @@ struct ChunkLds {
   };
   int last;
 };
+// Pieces of a tile joined two at a time, as the leaves of a binary tree: who comes first to a pair leaves its results there, who comes second adds them to
+// its own, in registers, and goes on; true where that was the last pair.  The last of n pieces reads log2 n others then, not all of them (2 us each for a
+// work-group: trees of 25 rows of 16 sequences, 32 heads on 8, up to 14 pieces: ## us with one work-group that reads all, ## so).  Either order gives the
+// same bits: the sums below are symmetric.  A pair's ticket is that of its right half's first piece.
+template <int HD>
+__device__ __forceinline__ bool join_two_by_two(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, const Piece& w, f32x16 (&o)[HD / 32], float& m, float& l,
+                                                bool here, int* s_last) {
+#pragma clang fp contract(off)
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = wave * (HD / 8) * 256 + lane * 4, at_ml = kChunkCols * HD + wave * 64 + (lane & 31) * 2;
+#pragma unroll 1
+  for (int s = 1; s < w.pieces; s <<= 1) {
+    const int left = w.piece & ~(2 * s - 1), right = left + s;
+    if (right >= w.pieces) continue;
+    const int mine = w.piece & s ? right : left;
+    int* counter = tickets(a, sp) + w.first + right * c.n_kv_heads;
+    auto slot = [&](int piece) { return partials(a, sp) + (size_t)(w.first + piece * c.n_kv_heads) * piece_floats<HD>(kChunkCols); };
+    __syncthreads();
+    if (threadIdx.x == 0) *s_last = __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (*s_last == 0 && here) {                                 // (the other half may still come first: then this was for nothing)
+      float* dst = slot(mine);
+#pragma unroll
+      for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) st_dev4(dst, at + (d * 4 + b) * 256, make_float4(o[d][b * 4], o[d][b * 4 + 1], o[d][b * 4 + 2], o[d][b * 4 + 3]));
+      if (lane < 32) st_dev2(dst + at_ml, m, l);
+    }
+    if (!last_arrival(counter, 2, s_last)) return false;
+    if (here) {
+      const float* src = slot(left + right - mine);
+      const float2 ml = ld_dev2(src + at_ml);
+      float4 x[HD / 8];
+#pragma unroll
+      for (int i = 0; i < HD / 8; ++i) x[i] = ld_dev4(src, at + i * 256);
+      __builtin_amdgcn_sched_barrier(0);                        // (all of them on their way before the first is waited for)
+      const float all = fmaxf(m, ml.x), f = weight_of(m, all), g = weight_of(ml.x, all);
+      m = all;
+      l = l * f + ml.y * g;
+#pragma unroll
+      for (int i = 0; i < HD / 8; ++i) {
+        const int d = i >> 2, b = (i & 3) * 4;
+        o[d][b] = o[d][b] * f + x[i].x * g;
+        o[d][b + 1] = o[d][b + 1] * f + x[i].y * g;
+        o[d][b + 2] = o[d][b + 2] * f + x[i].z * g;
+        o[d][b + 3] = o[d][b + 3] * f + x[i].w * g;
+      }
+    }
+    if (threadIdx.x == 0) *counter = 0;
+  }
+  return true;
+}
+
 template <typename T, int HD, int F>
 __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, float scale2, ChunkLds<HD>& lds) {
   constexpr bool H8 = F & kHeld8, M = F & kMasks;
@@ -1289,7 +1392,7 @@ __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const 
   // (Over 8-bit pages the codes times their powers of two are what lies in LDS: numbers of T, exact but where a half has no steps any more.)
   constexpr int KS = HD / 16, DT = HD / 32;                     // steps of 16 dims, tiles of 32 dims
   Piece w;
-  if (!find_piece(c, a, sp, w)) return;
+  if (!find_piece<M>(c, a, sp, w)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
   const int G = a.n_heads / c.n_kv_heads, cols = w.rows * G, col0 = w.group * kChunkCols, wcol = col0 + wave * 32;
   const int limit = a.max_blocks * c.page_size, pos0 = w.len - w.rows;
@@ -1508,7 +1611,10 @@ __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const 
   }
   l = halves_sum(l);
   m = m == -INFINITY ? m : m * scale2;                          // (what the join works with)
-  if (w.pieces == 1) {
+  if constexpr (M) {
+    if (!join_two_by_two<HD>(c, a, sp, w, o, m, l, wcol < cols, &lds.last)) return;
+  }
+  if (M || w.pieces == 1) {
     if (col < cols) {
       const float f = l == 0.f ? 0.f : 1.f / l;
       T* dst = static_cast<T*>(a.out) + at_row * a.out_stride + at_head + h * 4;
@@ -1524,6 +1630,7 @@ __device__ __forceinline__ void attend_chunk(const stairs_paged_cache& c, const 
     }
     return;
   }
+  if constexpr (M) return;
   float* part = partials(a, sp) + (size_t)(w.first + w.piece * c.n_kv_heads) * piece_floats<HD>(kChunkCols);
   if (col < cols) {
     const int dst = (col - col0) * HD + h * 4;
@@ -1708,12 +1815,12 @@ Launch plan_attention(const stairs_paged_cache* c, const stairs_paged_attn* a) {
     l.work_bytes += most_pieces(s.slots) * (int64_t)(s.tile_cols * (c->head_dim + 2) * sizeof(float));
   };
   if (l.chunk) {
-    l.chunks = Span{l.ct ? kFewCols + 1 : 1, INT32_MAX, kChunkCols, kChunkUnit, kSlots, 8, 400, 0, 0, 0};
+    l.chunks = Span{l.ct ? kFewCols + 1 : 1, INT32_MAX, kChunkCols, kChunkUnit, kSlots, 8, 400, 0, 32, 0, 0};
     add(l.chunks);
   }
   if (l.ct) {
     // pieces of 4 units and more: shorter ones cost more to join than they save (8000 keys of 8 heads alone: 25 us with 2, 19 with 4)
-    l.rows = Span{1, l.chunk ? kFewCols : INT32_MAX, 16 * l.ct, kRowUnit, kSlots, 4, 200, 0, most_pieces(kSlots), 0};
+    l.rows = Span{1, l.chunk ? kFewCols : INT32_MAX, 16 * l.ct, kRowUnit, kSlots, 4, 200, 0, 4, most_pieces(kSlots), 0};
     add(l.rows);
   }
   return l;
