@@ -435,7 +435,7 @@ int stairs_paged_read(const stairs_paged_cache *cache, const stairs_paged_out *o
  *   position[r]   the context's length + parents in front of r: what r's q and k are rotated by, two rows of a tree may share it
  *   sees[r]       bit i: r itself or in front of it on its path (stairs_paged_attn.sees; 0 in a chunk)
  * Rows of a request whose seq_len is smaller than its rows (that got no pages) have position -1 and see none, those behind the last request likewise.
- * 0 <= n_seqs <= STAIRS_PAGED_MAX_SEQS, rows >= 0; position may be NULL. */
+ * 0 <= n_seqs <= STAIRS_PAGED_MAX_SEQS, rows >= 0; position may be NULL, or the array that stairs_paged_plan has written. */
 #define STAIRS_TREE_MAX_ROWS   64
 typedef struct {
   int32_t n_seqs, rows;
@@ -466,10 +466,11 @@ typedef struct {
 } stairs_tree_path;
 int stairs_tree_walk(const stairs_tree_path *walk, void *hip_stream);
 
-/* What the path's rows have in n_caches pools (HOST array; one shape, type and page numbering: a model's layers) to the positions behind the context:
+/* What the path's rows have in n_caches pools (HOST array of different pools; one shape, type and page numbering: a model's layers) to the positions behind the context:
  * position context + path[row_start[b] + j] to context + j, j < kept[b], as they are held.  path ascending from 0 or more (as stairs_tree_walk
- * leaves it; kept and path may be the caller's own); rows that stay, and those whose page or position is none, are not touched.  Requests with more
- * than STAIRS_TREE_MAX_ROWS rows keep all of them: nothing moves.  0 <= n_caches <= 4096. */
+ * leaves it; kept and path may be the caller's own); rows that stay, and those whose page or position is none, keep what they have (what lies in the same
+ * aligned four positions as a moved row is written again as it is).  Requests with more than STAIRS_TREE_MAX_ROWS rows keep
+ * all of them: nothing moves.  0 <= n_caches <= 4096. */
 typedef struct {
   int32_t n_seqs, max_blocks, rows;
   const int32_t *block_table;      /* [n_seqs][max_blocks] */

@@ -28,8 +28,8 @@ __device__ __forceinline__ void rows_behind(const int* row_start, int n_seqs, in
   for (long long t = (long long)from + (blockIdx.x - first) * 256 + threadIdx.x; t < rows; t += (gridDim.x - first) * 256) f((int)t);
 }
 
-// A wave has a request, a lane a row; ancestors by doubling: what a row's ancestors 2^i steps up see, it sees.  Bound by the latency of its
-// three round trips.
+// A wave has a request, a lane a row; ancestors by doubling: what a row's ancestors 2^i steps up see, it sees.  Bound by the latency of
+// two round trips (32 trees of 61 rows 4.6 us, one of 7 rows 1.6).
 __global__ __launch_bounds__(64 * kWaves) void k_tree_plan(stairs_tree t) {
   const int lane = threadIdx.x & 63, b = blockIdx.x * kWaves + (threadIdx.x >> 6);
   if (b < t.n_seqs) {
@@ -66,7 +66,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_tree_plan(stairs_tree t) {
   });
 }
 
-// A wave has a request; each step of the walk is one comparison in all lanes (children are behind their parents, so it ends).
+// A wave has a request; each step of the walk is one comparison in all lanes (children are behind their parents, so it ends; 64 trees
+// of 61 rows 5.2 us).
 __global__ __launch_bounds__(64 * kWaves) void k_tree_walk(stairs_tree_path t) {
   const int lane = threadIdx.x & 63, b = blockIdx.x * kWaves + (threadIdx.x >> 6);
   if (b < t.n_seqs) {
@@ -302,6 +303,8 @@ extern "C" int stairs_paged_compact(const stairs_paged_cache* caches, int32_t n_
   if (!requests_ok(p->n_seqs, p->rows, p->row_start, p->seq_len)) return STAIRS_EINVAL;
   for (int i = 0; i < n_caches; ++i) {
     const stairs_paged_cache &c = caches[i], &first = caches[0];
+    for (int j = 0; j < i; ++j)                                 // (a pool twice would have its rows moved twice)
+      if (caches[j].k == c.k || caches[j].v == c.v || (c.held && caches[j].scale == c.scale)) return STAIRS_EINVAL;
     if (!paged_cache_ok(&c) || c.dtype != first.dtype || c.held != first.held || c.n_pages != first.n_pages || c.page_size != first.page_size ||
         c.n_kv_heads != first.n_kv_heads || c.head_dim != first.head_dim)
       return STAIRS_EINVAL;

@@ -92,7 +92,13 @@ def test_compact_refuses(bad):
 
 @pytest.mark.parametrize("other", [dict(n_pages=9), dict(page_size=32), dict(n_kv_heads=2), dict(head_dim=64), dict(dtype=pkg.DTYPE_FP16), dict(held=0)])
 def test_compact_refuses_pools_of_different_shapes(other):
-    refused(lambda: pkg.stairs_paged_compact([cache(), cache(), cache(**other)], path()))
+    refused(lambda: pkg.stairs_paged_compact([cache(), cache(k=2 * P, v=2 * P, scale=2 * P), cache(**dict(dict(k=3 * P, v=3 * P, scale=3 * P), **other))], path()))
+
+
+@pytest.mark.parametrize("twice", [dict(v=3 * P, scale=3 * P), dict(k=3 * P, scale=3 * P), dict(k=3 * P, v=3 * P), dict()])
+def test_compact_refuses_a_pool_twice(twice):
+    refused(lambda: pkg.stairs_paged_compact([cache(), cache(k=2 * P, v=2 * P, scale=2 * P), cache(**twice)], path()))
+    pkg.stairs_paged_compact([cache(), cache(k=2 * P, v=2 * P, scale=2 * P)], path(rows=0))
 
 
 def test_null_arguments_and_nothing_to_do():
