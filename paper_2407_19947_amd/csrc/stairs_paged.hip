@@ -255,7 +255,8 @@ __device__ __forceinline__ X ld_once_as(const void* p) {
 
 __device__ __forceinline__ void st_once(void* p, uint4 v) { __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), static_cast<u32x4*>(p)); }
 
-// Bound by memory, with few rows by latency.  A work-group has 32 rows and some of the n_heads + 2 n_kv_heads heads (so many
+// Bound by memory, with few rows by latency.  Into 8-bit pages a row's largest magnitude is found by the lanes that share it; values become codes on
+// their way to LDS, four heads at a time (8190 rows of 48 heads 46 us = 3.7 TB/s, a head at a time 49).  A work-group has 32 rows and some of the n_heads + 2 n_kv_heads heads (so many
 // groups of them that there are work for all CUs); the rows' rotations are formed once for all its heads.  q and k: a thread takes 8
 // pairs of a row, 16 bytes of either half; in a key tile the same 8 dims of 8 rows are one line.  v: a head's rows go through LDS;
 // the eight positions of a value tile that are 16 adjacent bytes a dim (two quads, 16 apart) are stored together where they are rows
@@ -498,7 +499,8 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
 // reading rows back
 // ---------------------------------------------------------------------------------------
 // As k_paged_append the other way: a work-group has 32 rows and some of the heads; keys go from a tile's places to the rows directly, values through
-// LDS, the eight positions of a place at once where they are rows of the work-group in that order, four or one otherwise.
+// LDS, the eight positions of a place at once where they are rows of the work-group in that order, four or one otherwise.  Bound by memory (24000 rows
+// of 8 heads of 128 in 8 bits: 29.3 us = 5.2 TB/s, what a copy reaches; 40 without the streaming hint on the stores).
 __device__ __forceinline__ uint16_t half_bits(__bf16, float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 __device__ __forceinline__ uint16_t half_bits(_Float16, float x) {   // (a row's largest half may have been rounded up to 2^16)
   return __builtin_bit_cast(uint16_t, (_Float16)(fabsf(x) > 65504.f && fabsf(x) < INFINITY ? copysignf(65504.f, x) : x));
@@ -732,7 +734,7 @@ struct Span {
   int slots;
   int min_units, whole;       // of a piece; tiles that are not cut (find_piece)
   int first_block;            // the launch's work-groups from here on
-  int start;                  // units that a piece's start and join are worth
+  int start;                  // units that a piece's start and join are worth (where they are weighed)
   int tickets;                // its first in the workspace
   int64_t partials;           // bytes in front of its partial results there
 };
@@ -814,7 +816,8 @@ __device__ __forceinline__ bool find_piece(const stairs_paged_cache& c, const st
       }
       if constexpr (WEIGH) {
         // ... or more than run at once: what all pieces take, their starts and joins (of so many units each) with them, and half a piece, for
-        // which CUs stand half empty at the end.  (Trees of 61 rows of 32 sequences of 500 .. 6000 keys, 8 heads: one round means whole tiles of up to 94 units.)
+        // which CUs stand half empty at the end.  (Trees of 61 rows of 32 sequences of 500 .. 6000 keys, 32 heads on 8 of 128, 8-bit pages: one round means
+        // whole tiles of up to 94 units, 188 us; 153 .. 145 so, for 4 .. 32 units; trees of 25 rows of 16 sequences 70 with 4, 59 with 8 .. 32.)
         auto cost = [&](int n) {
           const float pieces = fmaxf(1.f, floorf(((float)(w.units + n) - 0.5f) * __builtin_amdgcn_rcpf((float)n)));
           return wave_sum((float)w.groups * pieces) * (float)(c.n_kv_heads * sp.start) * __builtin_amdgcn_rcpf((float)sp.slots) + 0.5f * (float)n;
@@ -838,10 +841,25 @@ __device__ __forceinline__ bool find_piece(const stairs_paged_cache& c, const st
     }
   }
   per = __builtin_amdgcn_readfirstlane(per);
+  auto cut = [&](const SeqWork& q) { return min(kMaxPieces, max(1, (int)((unsigned)(q.units + per - 1) / (unsigned)per))); };
+  int seq = lane;
+  if (WEIGH && a.n_seqs <= 64 && all_tiles * 2 > sp.slots) {
+    // Large pieces first (what starts last is short then): the sequences in the order of their pieces' sizes, one behind the other where
+    // they are alike (those trees of 61 rows 145 -> 127 us).
+    const int size = w.groups > 0 ? (int)((unsigned)w.units / (unsigned)cut(w)) : -1;
+    int rank = 0;
+    for (int k = 0; k < a.n_seqs; ++k) {
+      const int other = __builtin_amdgcn_readlane(size, k);
+      rank += other > size || (other == size && k < lane);
+    }
+    if (lane >= a.n_seqs) rank = lane;
+    auto go = [&](int& v) { v = __builtin_amdgcn_ds_permute(rank * 4, v); };
+    go(w.row0); go(w.rows); go(w.len); go(w.groups); go(w.units); go(seq);
+  }
   int before = 0, split_before = 0;
   for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
     if (a.n_seqs > 64) w = seq_work(c, a, sp, b0 + lane);
-    const int pieces = min(kMaxPieces, max(1, (int)((unsigned)(w.units + per - 1) / (unsigned)per)));
+    const int pieces = cut(w);
     const int mine = w.groups * pieces, split = pieces > 1 ? mine : 0;
     const int to = before + wave_scan(mine), split_to = split_before + wave_scan(split);
     const unsigned long long there = __ballot(to > item);
@@ -850,7 +868,7 @@ __device__ __forceinline__ bool find_piece(const stairs_paged_cache& c, const st
       const unsigned at = item - (__builtin_amdgcn_readlane(to, l) - __builtin_amdgcn_readlane(mine, l));
       const unsigned n = __builtin_amdgcn_readlane(pieces, l), group = at / n;
       const int u = __builtin_amdgcn_readlane(w.units, l);
-      out.seq = b0 + l;
+      out.seq = b0 + __builtin_amdgcn_readlane(seq, l);
       out.row0 = __builtin_amdgcn_readlane(w.row0, l);
       out.rows = __builtin_amdgcn_readlane(w.rows, l);
       out.len = __builtin_amdgcn_readlane(w.len, l);
@@ -1035,7 +1053,9 @@ __device__ __forceinline__ uint32_t block_of(const Sees& s, int key0) {   // the
 // wave), no LDS, and are joined at the end.  Values are requested before the scores they wait for, the next block's keys as
 // soon as this block's are used.  (3 sequences of 9 rows and 23456 .. 59999 positions, 32 heads of 128: 300 us = 6.6 TB/s; 32 of 5 rows and
 // 200 .. 8000 positions, 8 key heads: 66.6 us = 4.3 TB/s, the rest goes into starting and joining pieces; 300 positions alone 6.6 us, one sequence of
-// 8000 and 8 key heads 13 us with 1 row, 19 with 5.)
+// 8000 and 8 key heads 13 us with 1 row, 19 with 5.)  Over 8-bit pages the codes become numbers of the matrix unit's type in registers, two an
+// instruction: the same 3 sequences 161 us = 6.2 TB/s, 32 single tokens of 200 .. 8000 positions 32, of which 20 for the bytes (pieces by weight as
+// in chunks, or three and four waves a SIMD with as many pieces, were slower: 201 us, 166 .. 284).
 constexpr int kRowUnit = 32 * 4;
 template <int HD, int CT>
 struct RowsLds {
@@ -1305,7 +1325,9 @@ __global__ __launch_bounds__(256, 2) void k_paged_rows(stairs_paged_cache c, sta
 // lane's 16 scores of 32 keys are two operands of the value product (keys 4 h + i and 16 + 4 h + i, and 8 further, of lane
 // half h), whose other operand is one 16-byte read of a value tile.  (2048 rows that end at 8200, 32 heads of 128 on 8 key heads: 233 ..
 // 249 us by card, 970 .. 1030 TFLOP/s, where a bf16 product of 8192^3 reaches 1181; 2048 rows alone 53.8 us = 640, 256 rows that end at 8000 56.8 =
-// 580: partial results of pieces and their joins.)
+// 580: partial results of pieces and their joins.)  Over 8-bit pages 258 .. 272 us: a work-group turns the codes of the next 64 keys into numbers on
+// their way to LDS, 47 us of the vector units' time, most of it for the values, whose powers of two differ from key to key.  (Requested two units ahead
+// instead of one, in registers, the outputs no longer fit in them: 627 us.)
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mma(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
@@ -1335,8 +1357,9 @@ struct ChunkLds {
 };
 // Pieces of a tile joined two at a time, as the leaves of a binary tree: who comes first to a pair leaves its results there, who comes second adds them to
 // its own, in registers, and goes on; true where that was the last pair.  The last of n pieces reads log2 n others then, not all of them (2 us each for a
-// work-group: trees of 25 rows of 16 sequences, 32 heads on 8, up to 14 pieces: ## us with one work-group that reads all, ## so).  Either order gives the
-// same bits: the sums below are symmetric.  A pair's ticket is that of its right half's first piece.
+// work-group: trees of 25 rows of 16 sequences, 32 heads on 8 of 128, up to 14 pieces: 86 us with one work-group that reads all, 70 so; 59 with the larger
+// pieces that find_piece takes).  Either order gives the same bits: the sums below are symmetric.  A pair's ticket is that of its right half's first piece; a
+// half that sees the other's ticket taken does not leave its results first.
 template <int HD>
 __device__ __forceinline__ bool join_two_by_two(const stairs_paged_cache& c, const stairs_paged_attn& a, const Span& sp, const Piece& w, f32x16 (&o)[HD / 32], float& m, float& l,
                                                 bool here, int* s_last) {
@@ -1820,7 +1843,7 @@ Launch plan_attention(const stairs_paged_cache* c, const stairs_paged_attn* a) {
   }
   if (l.ct) {
     // pieces of 4 units and more: shorter ones cost more to join than they save (8000 keys of 8 heads alone: 25 us with 2, 19 with 4)
-    l.rows = Span{1, l.chunk ? kFewCols : INT32_MAX, 16 * l.ct, kRowUnit, kSlots, 4, 200, 0, 4, most_pieces(kSlots), 0};
+    l.rows = Span{1, l.chunk ? kFewCols : INT32_MAX, 16 * l.ct, kRowUnit, kSlots, 4, 200, 0, 0, most_pieces(kSlots), 0};
     add(l.rows);
   }
   return l;
