@@ -260,6 +260,64 @@ def test_calls_with_and_without_trees_share_a_workspace():
         assert np.array_equal(calls[i].call(workspace=work), alone[i]), i
 
 
+@pytest.mark.parametrize("held", [False, True])
+@pytest.mark.parametrize("lens,n", [([3000], 40), ([12000], 64), ([2500, 700, 9000], 33), ([1100] * 4, 64), ([6000, 64, 64, 64, 64], 64)])
+def test_attention_of_trees_whose_tiles_are_cut_into_any_number_of_pieces(lens, n, held):
+    """Pieces are joined two at a time: 2 and more of them, powers of two and others; twice on one workspace with the same bits, every
+    ticket 0 again."""
+    import torch
+    rng = np.random.default_rng(n)
+    for dtype, heads in (("bf16", (4, 1, 128)), ("fp16", (6, 2, 64))):
+        a = tu.Attend(dtype, lens, [n] * len(lens), *heads, 64, held=held, sees=tree_masks(rng, [n] * len(lens)), seed=n)
+        out = a.call()
+        a.check(out)
+        work = torch.zeros_like(a.dev["work"])
+        for _ in range(3):
+            assert np.array_equal(a.call(workspace=work), out)
+        assert int(work[:8192].sum()) == 0
+
+
+@pytest.mark.parametrize("held", [False, True])
+@pytest.mark.parametrize("B", [2, 63, 64, 65, 130, 1000])
+def test_attention_of_trees_of_many_sequences(B, held):
+    """Long ones among short ones, before and behind the first 64; sequences without rows."""
+    rng = np.random.default_rng([B, held])
+    fresh = rng.integers(0, 4, B)
+    lens = fresh + rng.integers(0, 60, B)
+    for at, n, f in ((0, 3000, 64), (B // 2, 900, 40), (B - 1, 5000, 20), (B * 3 // 4, 2000, 3)):
+        lens[at], fresh[at] = n, f
+    a = tu.Attend("bf16", lens.tolist(), fresh.tolist(), 4, 2, 64, 32, held=held, sees=tree_masks(rng, fresh.tolist()), seed=B)
+    a.check(a.call())
+
+
+def test_two_calls_at_once_with_a_workspace_each():
+    import torch
+    rng = np.random.default_rng(6)
+    a = tu.Attend("bf16", [9000, 3000], [64, 33], 8, 2, 128, 64, held=False, sees=tree_masks(rng, [64, 33]))
+    b = tu.Attend("fp16", [2000, 6000], [60, 64], 8, 2, 128, 64, held=True, sees=tree_masks(rng, [60, 64]))
+    first = [a.call(), b.call()]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for x in (a, b):
+        x.dev["out"].fill_(7.0)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for x, st in zip((a, b), streams):
+            pkg.stairs_paged_attention(x.cache, x.args, st.cuda_stream)
+    torch.cuda.synchronize()
+    for x, want in zip((a, b), first):
+        assert np.array_equal(x.result(), want)
+
+
+def test_plans_walks_and_moves_on_a_stream_of_the_callers():
+    import torch
+    side = torch.cuda.Stream()
+    t = Trees([7, 64, 1], [70, 64, 5])
+    one, two = t.plan(), t.plan(stream=side.cuda_stream)
+    assert all(np.array_equal(x, y) for x, y in zip(one, two))
+    L = Layers("bf16", 2, 4, 32, 2, 64, False)
+    L.check(np.array([[2, 0, 3, 1]], np.int32), [0, 40], [100], paths(np.random.default_rng(3), [40])[0], [12], stream=side.cuda_stream)
+
+
 # ---- the caches in line with a path ----------------------------------------------------------------------------------------
 class Layers:
     def __init__(self, dtype, layers, n_pages, page, Hkv, hd, held, seed=0):
