@@ -180,15 +180,19 @@ def test_attention_of_trees_beside_chunks_and_single_rows(Hq, Hkv, hd, held):
 @pytest.mark.parametrize("held", [False, True])
 @pytest.mark.parametrize("n", [5, 40])
 def test_a_chain_is_what_causal_rows_see(n, held):
+    """Within what both may be off by (the sums' order is the launch's); bits behind a sequence's rows say nothing."""
     lens = [n, 100, 333]
     chain = [(2 << i) - 1 for _ in lens for i in range(n)]
     for dtype, heads in (("bf16", (8, 2, 128)), ("fp16", (2, 2, 64))):
         a = tu.Attend(dtype, lens, [n] * 3, *heads, 64, held=held, seed=n)
-        causal = a.call()
+        a.check(a.call())
+        want, tol = a.reference()
         a.sees = chain
-        assert np.array_equal(a.call(), causal)
-        a.sees = [s | ~((1 << n) - 1) & (2 ** 64 - 1) for s in chain]     # bits behind the sequence's rows say nothing
-        assert np.array_equal(a.call(), causal)
+        out = a.call()
+        live = a.row_start[-1]
+        ou.check_close(out[:live], want[:live], tol[:live])
+        a.sees = [s | ~((1 << n) - 1) & (2 ** 64 - 1) for s in chain]
+        assert np.array_equal(a.call(), out)
 
 
 @pytest.mark.parametrize("held", [False, True])
@@ -244,7 +248,7 @@ def test_trees_with_strides_hints_and_a_scale():
     fresh = [30, 3, 5, 64]
     a = tu.Attend("bf16", [300, 64, 5, 900], fresh, 8, 2, 128, 64, held=True, sees=tree_masks(rng, fresh))
     a.check(a.call(scale=0.3), scale=0.3)
-    for hint in (0, 1, 5000):
+    for hint in (0, 1, 10, 5000):
         a.check(a.call(max_fresh=hint))
 
 
