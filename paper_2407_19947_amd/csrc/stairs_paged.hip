@@ -500,7 +500,8 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
 // ---------------------------------------------------------------------------------------
 // As k_paged_append the other way: a work-group has 32 rows and some of the heads; keys go from a tile's places to the rows directly, values through
 // LDS, the eight positions of a place at once where they are rows of the work-group in that order, four or one otherwise.  Bound by memory (24000 rows
-// of 8 heads of 128 in 8 bits: 29.3 us = 5.2 TB/s, what a copy reaches; 40 without the streaming hint on the stores).
+// of 8 heads of 128 in 8 bits: 29.3 us = 5.2 TB/s, what a copy reaches; 40 without the streaming hint on the stores; in 16 bits 49 = 4.1 TB/s; several
+// heads at a time, as in k_paged_append, 1 .. 5 us slower).
 __device__ __forceinline__ uint16_t half_bits(__bf16, float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 __device__ __forceinline__ uint16_t half_bits(_Float16, float x) {   // (a row's largest half may have been rounded up to 2^16)
   return __builtin_bit_cast(uint16_t, (_Float16)(fabsf(x) > 65504.f && fabsf(x) < INFINITY ? copysignf(65504.f, x) : x));
@@ -1801,7 +1802,7 @@ extern "C" int stairs_paged_read(const stairs_paged_cache* c, const stairs_paged
   if (a->v && (!aligned16(a->v) || !stride_ok(a->v_stride, c->n_kv_heads, c->head_dim))) return STAIRS_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (const int rc = check_stream(st)) return rc;
-  const int tiles = (a->rows - 1) / kAppendRows + 1, groups = std::max(1, std::min((4 * kCus + tiles - 1) / tiles, c->n_kv_heads));
+  const int tiles = (a->rows - 1) / kAppendRows + 1, groups = std::max(1, std::min((8 * kCus + tiles - 1) / tiles, c->n_kv_heads));
   by_pages(c, [&](auto type, auto hd, auto h8) {
     hipLaunchKernelGGL((k_paged_read<decltype(type), decltype(hd)::value, decltype(h8)::value>), dim3(tiles, groups, a->k && a->v ? 2 : 1), dim3(256), 0, st, *c, *a);
   });
