@@ -842,12 +842,12 @@ __device__ __forceinline__ bool find_piece(const stairs_paged_cache& c, const st
     }
   }
   per = __builtin_amdgcn_readfirstlane(per);
-  auto cut = [&](const SeqWork& q) { return min(kMaxPieces, max(1, (int)((unsigned)(q.units + per - 1) / (unsigned)per))); };
+  auto pieces_of = [&](const SeqWork& q) { return min(kMaxPieces, max(1, (int)((unsigned)(q.units + per - 1) / (unsigned)per))); };
   int seq = lane;
   if (WEIGH && a.n_seqs <= 64 && all_tiles * 2 > sp.slots) {
     // Large pieces first (what starts last is short then): the sequences in the order of their pieces' sizes, one behind the other where
     // they are alike (those trees of 61 rows 145 -> 127 us).
-    const int size = w.groups > 0 ? (int)((unsigned)w.units / (unsigned)cut(w)) : -1;
+    const int size = w.groups > 0 ? (int)((unsigned)w.units / (unsigned)pieces_of(w)) : -1;
     int rank = 0;
     for (int k = 0; k < a.n_seqs; ++k) {
       const int other = __builtin_amdgcn_readlane(size, k);
@@ -860,7 +860,7 @@ __device__ __forceinline__ bool find_piece(const stairs_paged_cache& c, const st
   int before = 0, split_before = 0;
   for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
     if (a.n_seqs > 64) w = seq_work(c, a, sp, b0 + lane);
-    const int pieces = cut(w);
+    const int pieces = pieces_of(w);
     const int mine = w.groups * pieces, split = pieces > 1 ? mine : 0;
     const int to = before + wave_scan(mine), split_to = split_before + wave_scan(split);
     const unsigned long long there = __ballot(to > item);
