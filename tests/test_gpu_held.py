@@ -317,6 +317,13 @@ def test_masked_positions_may_hold_any_bytes(rows, byte):
         assert np.isnan(out[last]).all() and np.array_equal(out[others], clean[others])
 
 
+def test_attention_with_strides_scale_and_a_hint_that_is_too_small():
+    a = tu.Attend("bf16", [300, 64, 5, 900], [70, 3, 5, 300], 8, 2, 128, 64)
+    a.check(a.call(scale=0.3, q_pad=40, out_pad=8), scale=0.3)
+    for hint in (0, 1, 5000):
+        a.check(a.call(max_fresh=hint))
+
+
 def test_pages_that_are_none_and_rows_that_see_nothing():
     for rows in (1, 5, 140):
         a = tu.Attend("bf16", [rows + 40, rows + 100, rows + 300], [rows] * 3, 8, 2, 128, 32)

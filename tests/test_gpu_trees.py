@@ -247,7 +247,7 @@ def test_trees_with_strides_hints_and_a_scale():
     rng = np.random.default_rng(4)
     fresh = [30, 3, 5, 64]
     a = tu.Attend("bf16", [300, 64, 5, 900], fresh, 8, 2, 128, 64, held=True, sees=tree_masks(rng, fresh))
-    a.check(a.call(scale=0.3), scale=0.3)
+    a.check(a.call(scale=0.3, q_pad=40, out_pad=8), scale=0.3)
     for hint in (0, 1, 10, 5000):
         a.check(a.call(max_fresh=hint))
 
@@ -419,6 +419,34 @@ def test_compact_of_more_pools_than_a_launch_has_addresses_for():
     rng = np.random.default_rng(0)
     L = Layers("fp16", 131, 4, 32, 2, 64, False)
     L.check(np.array([[2, 0, 3, 1]], np.int32), [0, 40], [100], paths(rng, [40])[0], [12])
+
+
+@pytest.mark.parametrize("held", [False, True])
+def test_compact_beyond_32_bit_offsets(held):
+    """The last pages of pools of more than 2^32 bytes each; rows stored there, moved, and read back."""
+    import torch
+    page, hd, n_pages = 256, 128, 140000 if held else 70000
+    bytes_ = [page * hd * (1 if held else 2)] * 2 + [page * 2]
+    pools = [torch.zeros(n_pages, n, dtype=torch.uint8, device="cuda") for n in bytes_]
+    cache = pkg.StairsPagedCache(k=pools[0].data_ptr(), v=pools[1].data_ptr(), dtype=pkg.DTYPE_BF16, n_pages=n_pages, page_size=page, n_kv_heads=1, head_dim=hd,
+                                 held=pkg.DTYPE_E4M3 if held else 0, scale=pools[2].data_ptr())
+    n, context = 20, 250                                         # across a page's end
+    table = np.array([[n_pages - 1, n_pages - 2]], np.int32)
+    pos = context + np.arange(n)
+    slot = i32(table[0, pos // page] * page + pos % page)
+    x = torch.randn(2, n, hd, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).cuda()
+    pkg.stairs_paged_append(cache, pkg.StairsPagedRows(rows=n, n_heads=0, k=x[0].data_ptr(), v=x[1].data_ptr(), k_stride=hd, v_stride=hd, slot=slot.data_ptr(), rope_theta=0.0), None)
+    got = [torch.zeros(2, n, hd, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    reads = [pkg.StairsPagedRead(rows=n, k=g[0].data_ptr(), v=g[1].data_ptr(), k_stride=hd, v_stride=hd, slot=slot.data_ptr()) for g in got]
+    pkg.stairs_paged_read(cache, reads[0], None)
+    path = [0, 3, 7, 8, 13, 14, 15, 19]
+    p = dict(block_table=i32(table), row_start=i32([0, n]), seq_len=i32([context + n]), path=i32(path + [-1] * (n - len(path))), kept=i32([len(path)]))
+    pkg.stairs_paged_compact([cache], pkg.StairsPagedPath(n_seqs=1, max_blocks=2, rows=n, **{k: v.data_ptr() for k, v in p.items()}), None)
+    pkg.stairs_paged_read(cache, reads[1], None)
+    torch.cuda.synchronize()
+    want = got[0].clone()
+    want[:, :len(path)] = got[0][:, path]
+    assert torch.equal(got[1], want) and bool((got[0] != 0).any(2).all())
 
 
 def test_compact_with_paths_that_make_no_sense_stays_in_its_pages():

@@ -187,11 +187,13 @@ class Attend(ou.Attend):
             return self.K.double().numpy(), self.V.double().numpy()
         return values_of(self.kc, self.kb), values_of(self.vc, self.vb)
 
-    def call(self, scale=0.0, stream=None, max_fresh=None, workspace=None, poison=7.0, run=True):
+    def call(self, scale=0.0, stream=None, max_fresh=None, workspace=None, poison=7.0, q_pad=0, out_pad=0):
         import torch
         hd, Hq = self.hd, self.Hq
         dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
-        d = self.dev = dict(q=self.q.view(self.rows, -1).cuda(), out=torch.full((self.rows, Hq * hd), poison, dtype=self.dt).cuda(), table=dev(self.table),
+        q = torch.full((self.rows, Hq * hd + q_pad), float("nan"), dtype=self.dt)
+        q[:, :Hq * hd] = self.q.view(self.rows, -1)
+        d = self.dev = dict(q=q.cuda(), out=torch.full((self.rows, Hq * hd + out_pad), poison, dtype=self.dt).cuda(), table=dev(self.table),
                             row_start=dev(self.row_start), seq_len=torch.tensor(self.lens, dtype=torch.int32).cuda())
         if self.held:
             d.update(k=dev(ou.rows_to_pages(self.kc, held_key_at)), v=dev(ou.rows_to_pages(self.vc, held_value_at)), scale=dev(scales_to_pages(self.kb, self.vb)))
@@ -205,18 +207,16 @@ class Attend(ou.Attend):
         self.cache = pkg.StairsPagedCache(k=at("k"), v=at("v"), dtype=ou.CODE[self.dtype], n_pages=self.n_pages, page_size=self.page, n_kv_heads=self.Hkv,
                                           head_dim=hd, held=pkg.DTYPE_E4M3 if self.held else 0, scale=at("scale"))
         a = self.args = pkg.StairsPagedAttention(n_seqs=len(self.lens), max_blocks=self.max_blocks, rows=self.rows, n_heads=Hq,
-                                                 max_fresh=max(self.fresh) if max_fresh is None else max_fresh, q=at("q"), out=at("out"), q_stride=Hq * hd,
-                                                 out_stride=Hq * hd, block_table=at("table"), row_start=at("row_start"), seq_len=at("seq_len"), scale=scale,
+                                                 max_fresh=max(self.fresh) if max_fresh is None else max_fresh, q=at("q"), out=at("out"), q_stride=Hq * hd + q_pad,
+                                                 out_stride=Hq * hd + out_pad, block_table=at("table"), row_start=at("row_start"), seq_len=at("seq_len"), scale=scale,
                                                  sees=at("sees"))
         need = pkg.stairs_paged_attention_workspace(self.cache, a)
         d["work"] = torch.zeros(max(need, 16), dtype=torch.uint8).cuda() if workspace is None else workspace
         a.workspace, a.workspace_bytes = d["work"].data_ptr(), d["work"].numel()
         torch.cuda.synchronize()
-        if not run:
-            return None
         pkg.stairs_paged_attention(self.cache, a, torch.cuda.current_stream().cuda_stream if stream is None else stream)
         torch.cuda.synchronize()
-        return self.result(0, poison)
+        return self.result(out_pad, poison)
 
     def reference(self, scale=None):
         K, V = self.numbers()
