@@ -119,21 +119,23 @@ struct Pools {
 constexpr int kMostGroups = 2048;                               // work-groups of four waves that run at once
 struct PoolShape { int n_pages, page_size, n_kv_heads; };
 
-// a place of 16 bytes of a value tile: eight positions of one dim, or in 8 bits of each of two; position k of it
+// A place of 16 bytes of a value tile: eight positions of one dim, or in 8 bits of each of two.  An aligned four of positions is one half of
+// it (`high`: the four 16 behind the others): 8 bytes, in 8 bits 4 and 4 more 8 further; its two words
 __device__ __forceinline__ uint32_t of_four(uint4 v, int i) {   // (i: the same in all lanes)
   const uint32_t a = i & 1 ? v.y : v.x, b = i & 1 ? v.w : v.z;
   return i & 2 ? b : a;
 }
 __device__ __forceinline__ uint32_t put(uint32_t there, uint32_t value, uint32_t mask) { return (there & ~mask) | (value & mask); }
+// position kf of a place to position kt of a half
 template <bool H8>
-__device__ __forceinline__ void move_position(uint4& to, int kt, const uint4& from, int kf) {
+__device__ __forceinline__ void move_position(uint2& to, int kt, uint4 from, int kf) {
   if constexpr (H8) {
-    const uint32_t lo = (kf >> 2 ? from.y : from.x) >> (8 * (kf & 3)) << (8 * (kt & 3)), hi = (kf >> 2 ? from.w : from.z) >> (8 * (kf & 3)) << (8 * (kt & 3));
-    const uint32_t mask = 0xFFu << (8 * (kt & 3)), first = kt >> 2 ? 0 : mask, second = kt >> 2 ? mask : 0;
-    to = make_uint4(put(to.x, lo, first), put(to.y, lo, second), put(to.z, hi, first), put(to.w, hi, second));
+    const uint2 v = kf >> 2 ? make_uint2(from.y, from.w) : make_uint2(from.x, from.z);
+    const uint32_t mask = 0xFFu << (8 * kt);
+    to = make_uint2(put(to.x, v.x >> (8 * (kf & 3)) << (8 * kt), mask), put(to.y, v.y >> (8 * (kf & 3)) << (8 * kt), mask));
   } else {
     const uint32_t v = of_four(from, kf >> 1) >> (16 * (kf & 1)) << (16 * (kt & 1)), mask = 0xFFFFu << (16 * (kt & 1));
-    to = make_uint4(put(to.x, v, kt >> 1 == 0 ? mask : 0), put(to.y, v, kt >> 1 == 1 ? mask : 0), put(to.z, v, kt >> 1 == 2 ? mask : 0), put(to.w, v, kt >> 1 == 3 ? mask : 0));
+    to = make_uint2(put(to.x, v, kt >> 1 ? 0 : mask), put(to.y, v, kt >> 1 ? mask : 0));
   }
 }
 // (streaming hint: a launch that leaves thousands of changed lines behind in the L2s ends only when they have been written back; 31 rows of 12 heads in
@@ -142,12 +144,28 @@ __device__ __forceinline__ void st_once(void* p, uint4 v) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
   __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), static_cast<u32x4*>(p));
 }
+template <bool H8>
+__device__ __forceinline__ uint2 ld_half(const uint8_t* place, bool high) {
+  if constexpr (H8) return make_uint2(*reinterpret_cast<const uint32_t*>(place + 4 * high), *reinterpret_cast<const uint32_t*>(place + 8 + 4 * high));
+  else return *reinterpret_cast<const uint2*>(place + 8 * high);
+}
+template <bool H8>
+__device__ __forceinline__ void st_half(uint8_t* place, bool high, uint2 v) {
+  if constexpr (H8) {
+    __builtin_nontemporal_store(v.x, reinterpret_cast<uint32_t*>(place + 4 * high));
+    __builtin_nontemporal_store(v.y, reinterpret_cast<uint32_t*>(place + 8 + 4 * high));
+  } else {
+    __builtin_nontemporal_store(__builtin_bit_cast(uint64_t, v), reinterpret_cast<uint64_t*>(place + 8 * high));
+  }
+}
 __device__ __forceinline__ int place_of(int pos) { return (pos & 3) + 4 * ((pos >> 4) & 1); }
 
 // A wave has a request and a head in some of the pools: where its rows lie is found once, and the next pool's rows are requested before this one's are
 // written.  Paths ascend: what moves is the path's end, to positions one behind the other, none behind its old one, so no row that is still to
 // move lies where one has moved to.  Four positions at a time, aligned: all that comes there and what stays there is read before the
-// first is written, and written in runs of 64 bytes and more.  (Bound by the memory's granularity: a key is pieces of 16 bytes 256 apart, a value
+// first is written, and nothing beside the four is: other positions of a page may be another stream's meanwhile.  (Keys are written in runs of 64 bytes;
+// of a value's places, whose other half is the four 16 further, only the half: whole places took the same time.  64 trees of 61 rows in 32 pools of 8
+// heads of 128, with the walk: 87 us, in 8 bits 45.)  (Bound by the memory's granularity: a key is pieces of 16 bytes 256 apart, a value
 // numbers 16 apart, so that eight times what moves is read.)
 template <int HD, bool H8>
 __global__ __launch_bounds__(64 * kWaves) void k_paged_compact(PoolShape c, int n_pools, stairs_paged_path p, Pools pools) {
@@ -191,7 +209,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_paged_compact(PoolShape c, int 
   constexpr int kNext = 4 * 1024;                               // bytes from a place to that 64 further
   auto scales_at = [&](int s) { return head_of(s) * c.page_size * 2; };
   struct Held {
-    uint4 k, v[U][NV], place[NV];
+    uint4 k, v[U][NV];
+    uint2 place[NV];
     uint32_t s, byte[U];
   };
   while (left) {
@@ -212,12 +231,14 @@ __global__ __launch_bounds__(64 * kWaves) void k_paged_compact(PoolShape c, int 
       key_from = (lane & 3) == place[i] ? src[i] : key_from;
     }
     // the 16 words of powers of two that the four's lie in: the lane's, and which number of values or keys it is of (4: of others)
-    const int sp = first & (c.page_size - 1), word = lane & 15, mine = word / 4 == (sp & 15) >> 2 && (word & 1) == (sp >> 4 & 1) ? word >> 1 & 1 : 4;
+    const int sp = first & (c.page_size - 1);
+    const bool high = sp >> 4 & 1;
+    const int word = lane & 15, mine = word / 4 == (sp & 15) >> 2 && (word & 1) == (sp >> 4 & 1) ? word >> 1 & 1 : 4;
     auto load = [&](int pool, Held& x) {
       const uint8_t *K = static_cast<const uint8_t*>(pools.of[pool].k), *V = static_cast<const uint8_t*>(pools.of[pool].v), *S = static_cast<const uint8_t*>(pools.of[pool].scale);
       x.k = *reinterpret_cast<const uint4*>(K + key_at(key_from, (lane >> 2) % KL));
 #pragma unroll
-      for (int e = 0; e < NV; ++e) x.place[e] = *reinterpret_cast<const uint4*>(V + value_at(first) + e * kNext);
+      for (int e = 0; e < NV; ++e) x.place[e] = ld_half<H8>(V + value_at(first) + e * kNext, high);
       if constexpr (H8) x.s = *reinterpret_cast<const uint32_t*>(S + scales_at(first) + (sp >> 5) * 64 + word * 4);
 #pragma unroll
       for (int i = 0; i < U; ++i) {
@@ -232,21 +253,20 @@ __global__ __launch_bounds__(64 * kWaves) void k_paged_compact(PoolShape c, int 
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         if (i >= n) break;
-        const int to_place = place[i] + 4 * (sp >> 4 & 1);
 #pragma unroll
-        for (int e = 0; e < NV; ++e) move_position<H8>(x.place[e], to_place, x.v[i][e], place_of(src[i]));
+        for (int e = 0; e < NV; ++e) move_position<H8>(x.place[e], place[i], x.v[i][e], place_of(src[i]));
         if (H8 && mine < 4) x.s = put(x.s, x.byte[i] << (8 * place[i]), 0xFFu << (8 * place[i]));
       }
       // (all of it is here before the first is written)
       asm volatile("" : "+v"(x.k.x), "+v"(x.s)::"memory");
 #pragma unroll
-      for (int e = 0; e < NV; ++e) asm volatile("" : "+v"(x.place[e].x), "+v"(x.place[e].y), "+v"(x.place[e].z), "+v"(x.place[e].w)::"memory");
+      for (int e = 0; e < NV; ++e) asm volatile("" : "+v"(x.place[e].x), "+v"(x.place[e].y)::"memory");
       if ((lane >> 2) < KL) st_once(K + key_at(first + (lane & 3), lane >> 2), x.k);
 #pragma unroll
       for (int e = 0; e < NV; ++e)
-        if (lane < PLACES) st_once(V + value_at(first) + e * kNext, x.place[e]);
+        if (lane < PLACES) st_half<H8>(V + value_at(first) + e * kNext, high, x.place[e]);
       if constexpr (H8)
-        if (lane < 16) *reinterpret_cast<uint32_t*>(S + scales_at(first) + (sp >> 5) * 64 + word * 4) = x.s;
+        if (lane < 16 && mine < 4) *reinterpret_cast<uint32_t*>(S + scales_at(first) + (sp >> 5) * 64 + word * 4) = x.s;
     };
     Held now{}, next{};
     int pool = first_pool;

@@ -661,3 +661,42 @@ def test_steps_of_a_server_that_verifies_trees_captured_and_replayed(dtype, held
                 rows = pos * server.vocab + np.array(seqs[b][:cached[b]])
                 assert np.array_equal(k, server.of[layer][1][rows]) and np.array_equal(v, server.of[layer][2][rows]), (it, b, layer)
     assert longest > 3                                           # some paths were long
+
+
+# ---- what a call leaves alone ----------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("held", [False, True])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_compact_writes_the_aligned_fours_that_rows_move_to_and_nothing_else(hd, held):
+    """Four requests with a page, each at eight positions of its own, and rows stored by another stream at the last of them: whoever wrote more than
+    the four positions that its rows move to would undo what the others do."""
+    import torch
+    page, Hkv, layers, n_pages = 32, 6, 20, 40
+    L = Layers("bf16", layers, n_pages, page, Hkv, hd, held, seed=hd)
+    table = np.repeat(np.arange(n_pages, dtype=np.int32)[::-1].copy(), 4)[:, None]
+    B = len(table)
+    seq_len = [8 * (b % 4) + 7 for b in range(B)]                # seven new rows each, behind 0, 8, 16 and 24 positions
+    path, kept = [0, 2, 4, 5, -1, -1, -1] * B, [4, 3, 4, 2] * n_pages
+    slots = i32(np.arange(n_pages) * page + 31)
+    x = torch.randn(n_pages, 2 * Hkv * hd, generator=torch.Generator().manual_seed(hd)).to(torch.bfloat16).cuda()
+    rows = pkg.StairsPagedRows(rows=n_pages, n_heads=0, k=x.data_ptr(), v=x[:, Hkv * hd:].data_ptr(), k_stride=2 * Hkv * hd, v_stride=2 * Hkv * hd, slot=slots.data_ptr(),
+                               rope_theta=0.0)
+    p = dict(block_table=i32(table), row_start=i32(range(0, 7 * B + 1, 7)), seq_len=i32(seq_len), path=i32(path), kept=i32(kept))
+    a = pkg.StairsPagedPath(n_seqs=B, max_blocks=1, rows=7 * B, **{k: v.data_ptr() for k, v in p.items()})
+    start = [t.clone() for t in L.dev]
+    for c in L.caches:                                           # what the stored rows are alone
+        pkg.stairs_paged_append(c, rows, None)
+    torch.cuda.synchronize()
+    L.k, L.v, L.s = (t.cpu().numpy() for t in L.dev)
+    want = L.moved(table, [7 * b for b in range(B + 1)], seq_len, path, kept)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for t, first in zip(L.dev, start):
+            t.copy_(first)
+        torch.cuda.synchronize()
+        pkg.stairs_paged_compact(L.caches, a, streams[0].cuda_stream)
+        for c in L.caches:
+            pkg.stairs_paged_append(c, rows, streams[1].cuda_stream)
+        torch.cuda.synchronize()
+        for got, w in zip(L.dev, want):
+            got = got.cpu().numpy()
+            assert np.array_equal(got, w), np.argwhere(got != w)[:4]
