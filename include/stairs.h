@@ -325,7 +325,8 @@ int stairs_get_tokens(stairs_ctx *ctx, int32_t *out, int32_t cap, int32_t *len);
  *
  * held = STAIRS_DTYPE_E4M3: rows go in and come out in dtype, pages hold them in 8 bits; a row of a head (its keys; its values) is codes times
  * one power of two, 2^(b - 127) with a byte b, as it is stored the smallest from 1 to 254 for which the row's largest finite magnitude is at
- * most 448 * 2^(b - 127), codes rounded to nearest even; infinities and NaN become NaN; in FP16, magnitudes past 61440 count as 61440.  A page is n_kv_heads * page_size * head_dim bytes; inside
+ * most 448 * 2^(b - 127), codes rounded to nearest even; infinities and NaN become NaN; in FP16, magnitudes past 61440 count as 61440; in BF16,
+ * those from 1.9375 * 2^127 on are rounded to 2^128, a number past the type's largest.  A page is n_kv_heads * page_size * head_dim bytes; inside
  * a head, element (p, e) of
  *   keys   is at ((p / 16) * (head_dim / 64) + e / 64) * 1024 + (p % 16 + 16 * (e % 32 / 8)) * 16 + e % 64 / 32 * 8 + e % 8
  *   values is at ((p / 32) * (head_dim / 32) + e / 32) * 1024 + (e % 16 + 16 * (p % 16 / 4)) * 16 + e % 32 / 16 * 8 + p % 4 + 4 * (p % 32 / 16)
@@ -418,8 +419,8 @@ int64_t stairs_paged_attention_workspace(const stairs_paged_cache *cache, const 
 int stairs_paged_attention(const stairs_paged_cache *cache, const stairs_paged_attn *attn, void *hip_stream);
 
 /* Rows out of their pages, what stairs_paged_append stored: k, v [rows][n_kv_heads][head_dim] in the cache's dtype, rows *_stride elements
- * apart.  8-bit rows come back as the numbers they stand for (in FP16 those past 65504 as 65504).  A row whose slot is outside the pool is left as it was;
- * slots may come more than once.  k or v may be NULL.  Pointers 16-byte aligned, strides multiples of 8; 0 <= rows <= 2^29 - 32. */
+ * apart.  8-bit rows come back as the numbers they stand for, those past the type's largest as the largest.  A row whose slot is outside the pool
+ * is left as it was; slots may come more than once.  k or v may be NULL.  Pointers 16-byte aligned, strides multiples of 8; 0 <= rows <= 2^29 - 32. */
 typedef struct {
   int32_t rows;
   void *k, *v;

@@ -502,22 +502,14 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
 // LDS, the eight positions of a place at once where they are rows of the work-group in that order, four or one otherwise.  Bound by memory (24000 rows
 // of 8 heads of 128 in 8 bits: 29.3 us = 5.2 TB/s, what a copy reaches; 40 without the streaming hint on the stores; in 16 bits 49 = 4.1 TB/s; several
 // heads at a time, as in k_paged_append, 1 .. 5 us slower).
-__device__ __forceinline__ uint16_t half_bits(__bf16, float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
-__device__ __forceinline__ uint16_t half_bits(_Float16, float x) {   // (a row's largest half may have been rounded up to 2^16)
-  return __builtin_bit_cast(uint16_t, (_Float16)(fabsf(x) > 65504.f && fabsf(x) < INFINITY ? copysignf(65504.f, x) : x));
-}
-// eight codes times powers of two, as bits of the type
+// What is past the type's largest comes back as that (a bfloat16 from 1.9375 * 2^127 on is stored as 2^128; halves as large are in pages alone that others
+// have filled).  Codes have no infinities, so an infinity is such a number, its bits one more than the largest's: one is taken off whatever has all
+// exponent bits (of a NaN, too: it stays one).  (24000 rows of bfloat16 30.2 us, without it 29.7; every number compared as a float 32.0.)
+template <typename T> __device__ __forceinline__ uint32_t odd_bits(uint32_t u);
 template <typename T>
-__device__ __forceinline__ uint4 plain_row(uint32_t lo, uint32_t hi, float f) {
-  uint32_t out[4];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t u = i ? hi : lo;
-    const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8(u, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
-    out[2 * i] = half_bits(T{}, a.x * f) | (uint32_t)half_bits(T{}, a.y * f) << 16;
-    out[2 * i + 1] = half_bits(T{}, b.x * f) | (uint32_t)half_bits(T{}, b.y * f) << 16;
-  }
-  return make_uint4(out[0], out[1], out[2], out[3]);
+__device__ __forceinline__ uint4 no_infinities(uint4 v) {
+  auto less = [](uint32_t u) { return u - (odd_bits<T>(u) >> 15); };
+  return make_uint4(less(v.x), less(v.y), less(v.z), less(v.w));
 }
 template <typename T, int HD, bool H8>
 __global__ __launch_bounds__(256) void k_paged_read(stairs_paged_cache c, stairs_paged_out a) {
@@ -562,8 +554,8 @@ __global__ __launch_bounds__(256) void k_paged_read(stairs_paged_cache c, stairs
 #pragma unroll
         for (int t = 0; t < HD / 64; ++t) {
           const uint4 v = *reinterpret_cast<const uint4*>(src + k_held_off(p, 8 * g, HD) + t * 1024);
-          st_once(dst + 64 * t, plain_row<T>(v.x, v.y, f));
-          st_once(dst + 64 * t + 32, plain_row<T>(v.z, v.w, f));
+          st_once(dst + 64 * t, no_infinities<T>(widen<T>(v.x, v.y, f)));
+          st_once(dst + 64 * t + 32, no_infinities<T>(widen<T>(v.z, v.w, f)));
         }
       } else {
 #pragma unroll
@@ -583,11 +575,11 @@ __global__ __launch_bounds__(256) void k_paged_read(stairs_paged_cache c, stairs
         const uint8_t* src = static_cast<const uint8_t*>(c.v) + head * head_bytes + v_held_off(p, e, HD);
         const uint8_t* sc = scales + head * head_scales + scale_off(p) + 8;
         auto put = [&](int row, uint32_t codes, uint32_t bytes, int dim, int count) {
-          const f32x2_t x = __builtin_amdgcn_cvt_pk_f32_fp8(codes, false), y = __builtin_amdgcn_cvt_pk_f32_fp8(codes, true);
-          const float v[4] = {x.x, x.y, y.x, y.y};
+          const uint32_t v[4] = {Wide<T>::template pair<false>(codes, scale_of(bytes, 0)), Wide<T>::template pair<false>(codes, scale_of(bytes, 1)) >> 16,
+                                 Wide<T>::template pair<true>(codes, scale_of(bytes, 2)), Wide<T>::template pair<true>(codes, scale_of(bytes, 3)) >> 16};
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            if (k < count) s_v[row + k][dim] = half_bits(T{}, v[k] * scale_of(bytes, k));
+            if (k < count) s_v[row + k][dim] = (uint16_t)v[k];
         };
         if (kind == 3) {
           const uint4 v = *reinterpret_cast<const uint4*>(src);
@@ -624,7 +616,8 @@ __global__ __launch_bounds__(256) void k_paged_read(stairs_paged_cache c, stairs
     for (int i = tid; i < n * (HD / 8); i += 256) {
       const int r = i / (HD / 8), e = i % (HD / 8) * 8;
       if (s_slot[r] < 0) continue;
-      st_once(static_cast<uint16_t*>(a.v) + (size_t)(t0 + r) * a.v_stride + h * HD + e, *reinterpret_cast<const uint4*>(&s_v[r][e]));
+      const uint4 v = *reinterpret_cast<const uint4*>(&s_v[r][e]);
+      st_once(static_cast<uint16_t*>(a.v) + (size_t)(t0 + r) * a.v_stride + h * HD + e, H8 ? no_infinities<T>(v) : v);
     }
   }
 }

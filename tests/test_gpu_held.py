@@ -388,3 +388,37 @@ def test_calls_on_a_stream_of_the_callers():
     pool = Pool("bf16", 4, 64, 2, 128)
     one, two = read(pool, list(range(200))), read(pool, list(range(200)), stream=side.cuda_stream)
     assert all(np.array_equal(x, y) for x, y in zip(one, two))
+
+
+# ---- the largest numbers -----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_the_largest_rows_come_back_finite(dtype):
+    """Rows up to the type's largest, stored and read: within half a step of the 8-bit numbers (2^-4) and never infinite, though a code may stand for
+    the next number past the type's largest."""
+    import torch
+    Hkv, hd, page = 2, 64, 32
+    pool = Pool(dtype, 3, page, Hkv, hd)
+    top = float(torch.finfo(pool.dt).max)
+    x = torch.randn(40, 2 * Hkv * hd, generator=torch.Generator().manual_seed(4)).clamp(-4, 4) / 4
+    x[:, ::3] = torch.linspace(0.9, 1.0, 40)[:, None]            # (0.9 .. 1 of the largest: on both sides of where rounding goes up past it)
+    x[1::2] *= -1
+    x = (x.double() * top).to(pool.dt)
+    assert bool(torch.isfinite(x).all())
+    append(pool, range(40), 0, 0.0, x, range(40))
+    for got, want in zip(read(pool, range(40)), x.double().numpy().reshape(40, 2, -1).swapaxes(0, 1)):
+        ou.check_close(got, want, np.maximum(np.abs(want) * 2.0 ** -4, top * 2.0 ** -17))
+
+
+def test_read_of_numbers_past_the_types_largest():
+    """All codes with the largest powers of two: what is past the type's largest comes back as that."""
+    import torch
+    for dtype, powers in (("bf16", [246, 247, 248, 250, 253, 254]), ("fp16", [134, 135, 143, 200, 247, 254])):
+        pool = Pool(dtype, 2, 32, 2, 128)
+        codes = np.arange(2 * 2 * 32 * 128).reshape(2, 2, -1) % 256
+        pool.k.copy_(pool.k.new_tensor(codes.astype(np.uint8).tolist()))
+        pool.v.copy_(pool.v.new_tensor(codes[..., ::-1].astype(np.uint8).tolist()))
+        pool.s.copy_(pool.s.new_tensor(np.resize(np.array(powers, np.uint8), (2, 2, 64)).tolist()))
+        top = float(torch.finfo(pool.dt).max)
+        for got, num in zip(read(pool, list(range(64))), pool.numbers()):
+            want = np.where(np.isnan(num), num, np.clip(num, -top, top)).swapaxes(1, 2).reshape(64, -1)
+            assert np.array_equal(got, torch.from_numpy(want).to(pool.dt).double().numpy(), equal_nan=True), dtype
