@@ -398,8 +398,8 @@ int stairs_paged_append(const stairs_paged_cache *cache, const stairs_paged_rows
  * zeros before its first use, left fit for the next call, of other sizes and types too; calls that may overlap need one each.
  * 0 <= n_seqs <= STAIRS_PAGED_MAX_SEQS; row_start ascending; n_heads a multiple of n_kv_heads; rows * n_heads / n_kv_heads at most
  * 2^24, work-groups (a tile of 16, 32 or 128 such columns and a key head) fewer than 2^24; pointers 16-byte aligned, strides multiples of 8.
- * Over E4M3 pages keys and values count as the numbers they stand for, in FP16 those past 65504 as infinite; where the probabilities are sums of two numbers,
- * those are bfloat16.
+ * Over E4M3 pages keys and values count as the numbers they stand for, those past the type's largest as infinite; where the probabilities are sums of
+ * two numbers, those are bfloat16.
  * sees (8-byte aligned, or NULL): what the rows of a sequence with up to STAIRS_TREE_MAX_ROWS of them see of each other: bit i of a row's, the i-th new
  * row of its sequence.  All positions in front of the new rows are seen.  Sequences with more rows are not trees: each row sees the positions up to its own. */
 typedef struct {

@@ -188,6 +188,10 @@ __device__ __forceinline__ float scale_inverse(uint32_t b) { return __uint_as_fl
 __device__ __forceinline__ float scale_of(uint32_t bytes, int i) {                                           // byte i of four
   return __uint_as_float((i < 3 ? bytes << (23 - 8 * i) : bytes >> 1) & 0x7F800000u);
 }
+// the largest byte with which all codes are numbers of the type: 448 * 2^(b - 127) is; of four bytes those past it, as their top bits
+template <typename T> constexpr uint32_t kMostByte = __is_same(T, __bf16) ? 246 : 134;
+template <typename T>
+__device__ __forceinline__ uint32_t bytes_past(uint32_t u) { return ((u & 0x7F7F7F7Fu) + (255 - kMostByte<T>) * 0x01010101u) & u & 0x80808080u; }
 __device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
@@ -711,6 +715,19 @@ __device__ __forceinline__ uint32_t odd_kinds(uint32_t v) {
   }
   return kinds;
 }
+// a pair of bfloat16s, those past the largest number of type T as infinities (a bfloat16 past its own is one; 65536 is the next number of 4 bits behind
+// 65504)
+template <typename T>
+__device__ __forceinline__ uint32_t infinite_past(uint32_t v) {
+  if constexpr (__is_same(T, __bf16)) return v;
+  uint32_t out = 0;
+#pragma unroll
+  for (int h = 0; h < 32; h += 16) {
+    const uint32_t x = (v >> h) & 0xFFFFu, m = x & 0x7FFFu;
+    out |= (m >= 0x4780u && m <= 0x7F80u ? 0x7F80u | (x ^ m) : x) << h;
+  }
+  return out;
+}
 __device__ __forceinline__ float odd_value(float n) {
   const int c = (int)n;
   return (c & 63 ? INFINITY : 0.f) + (c & (63 << 6) ? -INFINITY : 0.f) + (c >> 12 ? __uint_as_float(0x7FC00000u) : 0.f);
@@ -1151,14 +1168,6 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
   while (u < u1) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) vf[i] = ld_once_as<uint4>(V + at + (i * 64 + lane) * PER);
-    float ks[8], vs[8];
-    if constexpr (H8) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        ks[i] = scale_of(i < 4 ? scales.x : scales.y, i & 3) * scale2;
-        vs[i] = scale_of(i < 4 ? scales.z : scales.w, i & 3);
-      }
-    }
     f32x4 s[CT][2];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
@@ -1180,11 +1189,55 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
     const int key0 = u * kRowUnit + wave * 32;
     const int un = next_block(u + 1);
     const size_t at_here = at;
+    uint4 powers = scales;
     if (un < u1) {
       at = block_at(un);
       load_keys(at);
     }
-    const bool full = key0 + 31 <= first_last;
+    bool past = false;
+    if constexpr (H8) {
+      // Powers of two with which a code may be past the type's largest number (of rows that others have stored, or of the largest bfloat16s): such
+      // numbers are infinite, as they are in attend_chunk, where numbers of the type are what is multiplied: scores by this, values as odd_values.  Looking for
+      // them costs 0 .. 1 % (32 verifications of 8 rows 43.4 us, 42.7 without).  Of keys that a column sees:
+      const uint32_t far[2] = {bytes_past<T>(powers.x), bytes_past<T>(powers.y)};
+      if (__any((far[0] | far[1] | bytes_past<T>(powers.z) | bytes_past<T>(powers.w)) != 0)) {
+        auto seen = [&](int i) {
+          const int n = last_last - (key0 + i * 16 + g * 4) + 1;
+          return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1;
+        };
+        past = __any((((far[0] | bytes_past<T>(powers.z)) & seen(0)) | ((far[1] | bytes_past<T>(powers.w)) & seen(1))) != 0);
+        if (past) {
+          // scores again, such keys as numbers of the type in the product and their scores multiplied by 1
+          auto one = [](uint32_t u, uint32_t bits) { return (u & ~((bits >> 7) * 255u)) | (bits >> 7) * 127u; };
+          powers.x = one(powers.x, far[0]);
+          powers.y = one(powers.y, far[1]);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const uint32_t b = S[at_here / (HD / 2) + scale_off(t * 16 + j)];
+            const float f = b > kMostByte<T> ? __uint_as_float(b << 23) : 1.f;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) s[ct][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+              const uint2 codes = *reinterpret_cast<const uint2*>(K + at_here + ((t * (KK / 2) + kk / 2) * 64 + lane) * PER + kk % 2 * 8);
+              const x8 k = __builtin_bit_cast(x8, widen<T>(codes.x, codes.y, f));
+#pragma unroll
+              for (int ct = 0; ct < CT; ++ct) s[ct][t] = mma(k, q[ct][kk], s[ct][t]);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
+        }
+      }
+    }
+    float ks[8], vs[8];
+    if constexpr (H8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        ks[i] = scale_of(i < 4 ? powers.x : powers.y, i & 3) * scale2;
+        vs[i] = scale_of(i < 4 ? powers.z : powers.w, i & 3);
+      }
+    }
+    const bool full = key0 + 31 <= first_last && !past;
     vx8 p[CT], rest[CT];
     uint32_t seen_bits[CT];                                     // of the lane's keys: (i >> 2) * 16 + (i & 3) for the i-th
     if constexpr (M)
@@ -1206,7 +1259,8 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
         for (int i = 0; i < 8; ++i) x[i] = sees_key(ct, i) ? x[i] : -INFINITY;
       }
       float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-      if (__any(mx - m[ct] > Headroom<VT>::slack)) {            // (the difference is exact where the scores are far from 0)
+      if (__any(mx - m[ct] > (past ? 0.f : Headroom<VT>::slack))) {   // (the difference is exact where the scores are far
+                                                                // from 0; past: probabilities times 2^127 are floats)
         const float mn = fmaxf(m[ct], groups_max(mx));
         const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[ct] - mn);
         m[ct] = mn;
@@ -1254,7 +1308,7 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
         if constexpr (H8) add_value(et, v);
         __builtin_amdgcn_sched_barrier(0);                      // (one tile after the other: their temporaries share registers)
       }
-      if (__any(odd != 0)) {
+      if (past || __any(odd != 0)) {
         if (!had_odd)
           for (int i = lane; i < 16 * CT * (HD + 4); i += 64) (&lds.o[wave][0][0])[i] = 0.f;
         had_odd = true;
@@ -1266,7 +1320,18 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
 #pragma unroll 1
         for (int et = 0; et < ET; ++et) {
           uint4 v = *reinterpret_cast<const uint4*>(V + at_here + ((H8 ? et / 2 : et) * 64 + lane) * PER);
-          if constexpr (H8) v = et & 1 ? widen<VT>(v.z, v.w, 1.f) : widen<VT>(v.x, v.y, 1.f);
+          if constexpr (H8) {
+            const uint2 b = *reinterpret_cast<const uint2*>(S + at_here / (HD / 2) + g * 16 + 8), codes = et & 1 ? make_uint2(v.z, v.w) : make_uint2(v.x, v.y);
+            auto pair = [&](uint32_t lo, uint32_t hi) {
+              __builtin_amdgcn_sched_barrier(0);
+              return infinite_past<T>(low_high(lo, hi));
+            };
+            typedef Wide<VT> W;
+            v.x = pair(W::template pair<false>(codes.x, scale_of(b.x, 0)), W::template pair<false>(codes.x, scale_of(b.x, 1)));
+            v.y = pair(W::template pair<true>(codes.x, scale_of(b.x, 2)), W::template pair<true>(codes.x, scale_of(b.x, 3)));
+            v.z = pair(W::template pair<false>(codes.y, scale_of(b.y, 0)), W::template pair<false>(codes.y, scale_of(b.y, 1)));
+            v.w = pair(W::template pair<true>(codes.y, scale_of(b.y, 2)), W::template pair<true>(codes.y, scale_of(b.y, 3)));
+          }
           v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
           const uint4 kinds = make_uint4(odd_kinds<VT>(v.x), odd_kinds<VT>(v.y), odd_kinds<VT>(v.z), odd_kinds<VT>(v.w));
 #pragma unroll

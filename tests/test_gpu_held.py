@@ -422,3 +422,63 @@ def test_read_of_numbers_past_the_types_largest():
         for got, num in zip(read(pool, list(range(64))), pool.numbers()):
             want = np.where(np.isnan(num), num, np.clip(num, -top, top)).swapaxes(1, 2).reshape(64, -1)
             assert np.array_equal(got, torch.from_numpy(want).to(pool.dt).double().numpy(), equal_nan=True), dtype
+
+
+def past_reference(a):
+    """As trees_util's for causal rows, with numbers past the type's largest as infinities; a score of +infinity makes a row NaN, a key with -infinity
+    is as if not seen."""
+    import torch
+    top = float(torch.finfo(a.dt).max)
+    K, V = (np.where(np.abs(x) > top, np.copysign(np.inf, x), x) for x in a.numbers())
+    half, q = ou.HALF_STEP[a.dtype], a.q.double().numpy()
+    want, tol = np.full((a.rows, a.Hq, a.hd), np.nan), np.zeros((a.rows, a.Hq, a.hd))
+    for b, (n, f) in enumerate(zip(a.lens, a.fresh)):
+        hp = tu.TWO["bf16"] if f * a.Hq // a.Hkv <= 32 else half
+        pages = a.table[b, :-(-n // a.page)]
+        for h in range(a.Hq):
+            k, v = (x[pages, h // (a.Hq // a.Hkv)].reshape(-1, a.hd)[:n] for x in (K, V))
+            for i in range(f):
+                t = a.row_start[b] + i
+                see = np.arange(n) <= n - f + i
+                with np.errstate(invalid="ignore"):
+                    x = k[see] @ q[t, h] * a.scale
+                    if not (x < np.inf).all():
+                        continue                                 # (NaN)
+                    on = x > -np.inf
+                    x, ks, vs = x[on], k[see][on], v[see][on]
+                    p = np.exp(x - x.max())
+                    p /= p.sum()
+                    want[t, h] = p @ vs
+                    d = 2 * ((a.hd + 2) * 2.0 ** -24 * (np.abs(ks) @ np.abs(q[t, h])).max() * a.scale + 2.0 ** -22 * (x.max() - x).max()
+                             + 2.0 ** -25 * np.abs(q[t, h]).sum() * a.scale) + 2 * (len(x) + 64) * 2.0 ** -24
+                    tol[t, h] = half * np.abs(want[t, h]) + (p @ np.abs(vs)) * (hp + d) + 2 * ou.SMALLEST[a.dtype]
+    return want, tol
+
+
+@pytest.mark.parametrize("what", ["values", "keys"])
+@pytest.mark.parametrize("rows", [1, 5, 8, 9, 40])
+@pytest.mark.parametrize("dtype,byte", [("fp16", 135), ("fp16", 137), ("fp16", 200), ("bf16", 247), ("bf16", 248), ("bf16", 254)])
+def test_numbers_past_the_types_largest_are_infinite_in_few_rows_and_in_many(dtype, byte, rows, what):
+    """In pages that the caller has filled: one such row in front of all new rows, one that the last two see (32 columns of a key head are 8 rows)."""
+    for Hq, Hkv, hd in ((8, 2, 128), (4, 1, 64)):
+        a = tu.Attend(dtype, [rows + 45, rows + 200], [rows, rows], Hq, Hkv, hd, 64, seed=byte)
+        a.check(a.call())
+        rng = np.random.default_rng(rows)
+        codes, scale = (a.vc, a.vb) if what == "values" else (a.kc, a.kb)
+        for b, n in enumerate(a.lens):
+            for at in (13, n - 2):
+                page, p = a.table[b, at // 64], at % 64
+                scale[page, :, p] = byte
+                if what == "values":                             # +-448 and numbers of the type that sums have room for
+                    codes[page, :, p] = rng.choice(np.array([0x7E, 0xFE, 0x08, 0x88, 0x00], np.uint8), (Hkv, hd))
+                else:                                            # one dim that says which infinity the score is
+                    codes[page, :, p] = 0
+                    codes[page, :, p, 7] = 0x7E
+        out = a.call()
+        want, tol = past_reference(a)
+        live = np.arange(a.rows) < a.row_start[-1]
+        assert (out[~live] == 7).all()
+        with np.errstate(invalid="ignore"):
+            fine = (np.isnan(want) & np.isnan(out)) | (out == want) | (np.abs(out - want) <= tol)
+        assert fine[live].all(), (int((~fine[live]).sum()), np.argwhere(~fine & live[:, None, None])[:4].tolist())
+        assert np.isnan(want[live]).any() if what == "keys" else np.isinf(want).any()
