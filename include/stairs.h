@@ -451,8 +451,9 @@ int stairs_tree_plan(const stairs_tree *tree, void *hip_stream);
 /* Validation of a tree: predicted[r] is the token the model says comes behind row r (the argmax of its logits, say).  From row 0 on, a row
  * whose token is the one predicted for its parent is kept, and so on from that row; of several such children the first.  A row with a
  * negative token goes with its parent whatever is predicted (a prompt's rows).  A chain of parents is the stairs validation.
- *   kept[b]       rows of the path, 1 and more (0: the request has none, or got no pages)
- *   cached[b]     the context's length + kept: the next plan's (which may be the same array); left as it was if the request got no pages
+ *   kept[b]       rows of the path, 1 and more (0: the request has none, or got no pages, or has rows outside the buffers)
+ *   cached[b]     the context's length + kept: the next plan's (which may be the same array); left as it was if the request has rows that got no
+ *                 pages or are outside the buffers.  Without rows: its seq_len (0, too, where what it has cached got no pages)
  *   path[row_start[b] + j], emitted[...]   the path's j-th row, ascending, and the token predicted for it; -1 behind the path and behind the
  *                 last request
  * All rows of a chunk are kept. */

@@ -11,12 +11,16 @@ namespace {
 static_assert(STAIRS_TREE_MAX_ROWS == 64, "a lane for each row of a tree");
 constexpr int kWaves = 4;                                       // of a work-group, a request each
 
-// a request's rows: none where row_start makes no sense
-struct Rows { int first, count, len; };
+// a request's rows: none where row_start makes no sense (lost then)
+struct Rows {
+  int first, count, len;
+  bool lost;
+};
 __device__ __forceinline__ Rows rows_of(const int* row_start, const int* seq_len, int rows, int b) {
-  Rows r{row_start[b], 0, seq_len[b]};
+  Rows r{row_start[b], 0, seq_len[b], false};
   const int n = row_start[b + 1] - r.first;
   if (r.first >= 0 && n > 0 && n <= rows - r.first) r.count = n;
+  r.lost = n != r.count;
   return r;
 }
 // rows behind the last request's; work-groups from `first` on
@@ -72,7 +76,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_tree_walk(stairs_tree_path t) {
   const int lane = threadIdx.x & 63, b = blockIdx.x * kWaves + (threadIdx.x >> 6);
   if (b < t.n_seqs) {
     const Rows r = rows_of(t.row_start, t.seq_len, t.rows, b);
-    const bool there = r.len >= r.count;
+    const bool there = r.len >= r.count && !r.lost;
     int kept = 0;
     if (r.count <= STAIRS_TREE_MAX_ROWS) {
       const bool here = lane < r.count;

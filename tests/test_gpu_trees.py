@@ -700,3 +700,17 @@ def test_compact_writes_the_aligned_fours_that_rows_move_to_and_nothing_else(hd,
         for got, w in zip(L.dev, want):
             got = got.cpu().numpy()
             assert np.array_equal(got, w), np.argwhere(got != w)[:4]
+
+
+@pytest.mark.parametrize("counts", [[5, 9, 3], [5, 70, 3], [5, 0, 40]])
+def test_the_walk_keeps_nothing_of_requests_whose_rows_the_buffers_do_not_hold(counts):
+    """A step with more rows than the buffers have: those requests' counts of cached positions stay, so the next step brings their rows again."""
+    t = Trees(counts, [300, 200, 100])
+    t.rows = 7
+    got = t.walk()
+    r0 = [0, 5, 5 + counts[1]]
+    kept, cached, path, emitted = tu.walk_reference(r0[:2], [300], t.parent, t.token, t.predicted, 7, [100])
+    whole = counts[1] == 0                                       # (no rows: all that is cached is its length)
+    assert got["kept"].tolist() == kept + [0, 0, -9] and got["cached"].tolist() == cached + [200 if whole else 101, 102, 103]
+    assert got["path"].tolist()[:5] == path[:5].tolist() and got["emitted"].tolist()[:5] == emitted[:5].tolist()
+    assert (got["path"][7:] == -9).all() and (got["emitted"][7:] == -9).all()
