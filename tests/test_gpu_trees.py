@@ -714,3 +714,63 @@ def test_the_walk_keeps_nothing_of_requests_whose_rows_the_buffers_do_not_hold(c
     assert got["kept"].tolist() == kept + [0, 0, -9] and got["cached"].tolist() == cached + [200 if whole else 101, 102, 103]
     assert got["path"].tolist()[:5] == path[:5].tolist() and got["emitted"].tolist()[:5] == emitted[:5].tolist()
     assert (got["path"][7:] == -9).all() and (got["emitted"][7:] == -9).all()
+
+
+@pytest.mark.parametrize("value", [0x7F, 0xFF])
+@pytest.mark.parametrize("n,Hq,Hkv,hd", [(6, 8, 2, 128), (6, 4, 4, 64), (50, 8, 2, 128)])
+def test_rows_of_other_branches_may_hold_anything_in_8_bit_pages(n, Hq, Hkv, hd, value):
+    """Codes that are no number show in the rows that see them alone, and so do numbers past the type's largest."""
+    parent = [-1] + [0, 0, 1, 2, 2] + list(range(5, n - 1))
+    sees = [sum(1 << j for j in tu.path_of(parent, i)) for i in range(n)] * 2
+    off = np.array([sees[i] >> 1 & 1 for i in range(n)] * 2, bool)
+    assert off.sum() == 4
+    for dtype, past in (("bf16", 250), ("fp16", 137)):
+        a = tu.Attend(dtype, [n + 70, n + 3], [n, n], Hq, Hkv, hd, 32, sees=sees)
+        clean = a.call()
+        a.check(clean)
+        want, tol = a.reference()
+        keep = a.kc.copy(), a.vc.copy(), a.vb.copy()
+        for kind in ("keys", "values", "past"):
+            a.kc, a.vc, a.vb = (x.copy() for x in keep)
+            for b, m in enumerate(a.lens):
+                at = m - n + 1                                   # row 1 and, behind it, row 3
+                page, p = a.table[b, at // 32], at % 32
+                if kind == "past":
+                    a.vc[page, :, p], a.vb[page, :, p] = 0x7E, past
+                else:
+                    (a.kc if kind == "keys" else a.vc)[page, :, p] = value
+            out = a.call()
+            assert not np.isfinite(out[:2 * n][off]).any(), (dtype, kind)
+            if kind == "past":                                   # (maxima follow at once there: the same but for the sums' order)
+                assert np.isposinf(out[:2 * n][off]).all()
+                ou.check_close(out[:2 * n][~off], want[:2 * n][~off], tol[:2 * n][~off], dtype)
+            else:
+                assert np.array_equal(out[:2 * n][~off], clean[:2 * n][~off]), (dtype, kind)
+
+
+@pytest.mark.parametrize("held", [False, True])
+def test_paths_that_make_no_sense_touch_no_page_of_others(held):
+    """Keys, values and powers of two of the page nobody has, and whatever lies in front of the new rows' first aligned four."""
+    for path, kept, lens in (([0, 70, -3, 2 ** 31 - 1, 4, 5], [6], [40]), ([0] * 6, [2 ** 31 - 1], [64]), ([0, 2, 4, 5, -1, -1], [-4], [64]),
+                             ([0, 2, 3, 4, 5, -1], [5], [2 ** 31 - 1]), ([0, 2, 3, 4, 5, -1], [5], [66]), ([5, 4, 3, 2, 1, 0], [6], [40])):
+        L = Layers("bf16", 2, 3, 32, 2, 64, held)
+        table = np.array([[2, 0]], np.int32)
+        p = dict(block_table=i32(table), row_start=i32([0, 6]), seq_len=i32(lens), path=i32(path), kept=i32(kept))
+        a = pkg.StairsPagedPath(n_seqs=1, max_blocks=2, rows=6, **{k: v.data_ptr() for k, v in p.items()})
+        import torch
+        torch.cuda.synchronize()
+        pkg.stairs_paged_compact(L.caches, a, None)
+        torch.cuda.synchronize()
+        front = (lens[0] - 6) // 4 * 4
+        for i, (got, was) in enumerate(zip(L.dev, (L.k, L.v, L.s))):
+            got = got.cpu().numpy()
+            assert np.array_equal(got[:, 1], was[:, 1]), (path, i)
+            places = L.places()[i]
+            if places is None:
+                assert np.array_equal(got, was)
+                continue
+            w = 1 if held else 2
+            pages = [x.reshape(*x.shape[:3], -1, w)[..., places, :] for x in (got, was)]     # [layer, page, head, position, ...]
+            for block, page in enumerate(table[0]):
+                mine = np.arange(32) + 32 * block < front
+                assert np.array_equal(pages[0][:, page][:, :, mine], pages[1][:, page][:, :, mine]), (path, i, block)
