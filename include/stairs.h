@@ -309,7 +309,9 @@ int stairs_get_tokens(stairs_ctx *ctx, int32_t *out, int32_t cap, int32_t *len);
  *   stairs_tree_walk        the path of each tree that the model's own predictions follow
  *   stairs_paged_compact    the path's rows to the positions behind the context, in the pools of all layers
  * All pointers inside the structures are DEVICE pointers the caller owns, on the device that is current and that hip_stream
- * (a hipStream_t or NULL) belongs to; the structures themselves are host memory and may go after the call.  Calls allocate
+ * (a hipStream_t or NULL) belongs to; the structures themselves are host memory and may go after the call.  A structure begins as
+ * zeros (= {0}, memset) and a program is built with the header of its library: structures grow at their ends, and a member added
+ * there means what was before it where it is 0 (stairs_paged_cache: held, scale; stairs_paged_attn: sees).  Calls allocate
  * nothing, keep nothing from one call to the next, and do not wait: results are valid once the stream has reached the end of
  * them.  All may be captured into a HIP graph.  What the device finds in index arrays is checked there: a page or slot
  * outside the pool is neither read nor written, rows outside the buffers likewise.

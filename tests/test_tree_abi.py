@@ -1,5 +1,7 @@
 """CPU: what the operators on trees and on 8-bit pages refuse, before anything reaches a GPU; page addressing and plain
 implementations by hand."""
+import ctypes as C
+
 import numpy as np
 import pytest
 
@@ -155,3 +157,25 @@ def test_the_trees_references_by_hand():
     assert position.tolist() == [10, 11, 11, 12, 12, 10, -1] and sees.tolist() == [1, 3, 5, 11, 21, 32, 0]
     kept, cached, path, emitted = tu.walk_reference([0, 6], [16], parent, [9, 4, 5, 6, 7, 8], [5, 0, 7, 0, 3, 0], 7, [10])
     assert kept == [3] and cached == [13] and path.tolist() == [0, 2, 4, -1, -1, -1, -1] and emitted.tolist() == [5, 7, 3, -1, -1, -1, -1]
+
+
+def test_structures_lie_as_the_header_has_them(tmp_path):
+    """Sizes and offsets of the operators' structures, by a C compiler; built from zeros, members that were added last mean what was before them."""
+    import os
+    import subprocess
+    include = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+    classes = [pkg.StairsPagedCache, pkg.StairsPagePlan, pkg.StairsPagedRows, pkg.StairsPagedAttention, pkg.StairsPagedRead, pkg.StairsTree, pkg.StairsTreeWalk,
+               pkg.StairsPagedPath, pkg.StairsSampling]
+    lines, want = [], []
+    for c in classes:
+        name = c.__doc__.split(":")[0]
+        lines.append(f'printf("{name} %zu\\n", sizeof({name}));')
+        want.append(f"{name} {C.sizeof(c)}")
+        for field, _ in c._fields_:
+            lines.append(f'printf("{name}.{field} %zu\\n", offsetof({name}, {field}));')
+            want.append(f"{name}.{field} {getattr(c, field).offset}")
+    zeros = "stairs_paged_cache c = {0}; stairs_paged_attn a = {0}; if (c.held || c.scale || a.sees) return 1;"
+    (tmp_path / "layout.c").write_text("#include <stddef.h>\n#include <stdio.h>\n#include <string.h>\n#include \"stairs.h\"\nint main(void) {" + zeros + "\n".join(lines) + "return 0; }\n")
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-I", include, "-o", tmp_path / "layout", tmp_path / "layout.c"], check=True)
+    out = subprocess.run([tmp_path / "layout"], check=True, capture_output=True, text=True).stdout
+    assert out.split("\n")[:-1] == want
