@@ -504,7 +504,7 @@ __global__ __launch_bounds__(256) void k_paged_append(stairs_paged_cache c, stai
 // ---------------------------------------------------------------------------------------
 // As k_paged_append the other way: a work-group has 32 rows and some of the heads; keys go from a tile's places to the rows directly, values through
 // LDS, the eight positions of a place at once where they are rows of the work-group in that order, four or one otherwise.  Bound by memory (24000 rows
-// of 8 heads of 128 in 8 bits: 29.3 us = 5.2 TB/s, what a copy reaches; 40 without the streaming hint on the stores; in 16 bits 49 = 4.1 TB/s; several
+// of 8 heads of 128 in 8 bits: 29.4 .. 30.2 us = 5.0 .. 5.2 TB/s, what a copy reaches; 40 without the streaming hint on the stores; in 16 bits 49 = 4.1 TB/s; several
 // heads at a time, as in k_paged_append, 1 .. 5 us slower).
 // What is past the type's largest comes back as that (a bfloat16 from 1.9375 * 2^127 on is stored as 2^128; halves as large are in pages alone that others
 // have filled).  Codes have no infinities, so an infinity is such a number, its bits one more than the largest's: one is taken off whatever has all
@@ -1078,7 +1078,8 @@ __device__ __forceinline__ void attend_rows(const stairs_paged_cache& c, const s
   constexpr bool H8 = F & kHeld8, M = F & kMasks;
   typedef typename Elem<T>::x8 x8;
   // Codes are numbers of either type.  A score is multiplied by its key's power of two, a probability by its value's: in bfloat16, so that whatever
-  // power of two that is stays in range; two numbers of it are as exact as half's two.
+  // power of two that is stays in range; two numbers of it are as exact as half's two.  (But for values of less than 2^-112: times their power
+  // the probabilities are then below the normal bfloat16s and lose bits, to 0.3 % of the largest at 2^-116.)
   typedef std::conditional_t<H8, __bf16, T> VT;
   typedef typename Elem<VT>::x8 vx8;
   typedef std::conditional_t<H8, uint8_t, T> PT;

@@ -71,7 +71,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_tree_plan(stairs_tree t) {
 }
 
 // A wave has a request; each step of the walk is one comparison in all lanes (children are behind their parents, so it ends; 64 trees
-// of 61 rows 5.2 us).
+// of 61 rows 4.7 us).
 __global__ __launch_bounds__(64 * kWaves) void k_tree_walk(stairs_tree_path t) {
   const int lane = threadIdx.x & 63, b = blockIdx.x * kWaves + (threadIdx.x >> 6);
   if (b < t.n_seqs) {
@@ -120,11 +120,11 @@ constexpr int kLaunchCaches = 64;                               // pools of a la
 struct Pools {
   struct { void *k, *v, *scale; } of[kLaunchCaches];
 };
-constexpr int kMostGroups = 2048;                               // work-groups of four waves that run at once
+constexpr int kMostGroups = 2048;                               // work-groups past which a wave takes several pools (1024 .. 1536 run at once, by form)
 struct PoolShape { int n_pages, page_size, n_kv_heads; };
 
 // A place of 16 bytes of a value tile: eight positions of one dim, or in 8 bits of each of two.  An aligned four of positions is one half of
-// it (`high`: the four 16 behind the others): 8 bytes, in 8 bits 4 and 4 more 8 further; its two words
+// it (`high`: the four 16 behind the others): 8 bytes, in 8 bits 4 and 4 more 8 further
 __device__ __forceinline__ uint32_t of_four(uint4 v, int i) {   // (i: the same in all lanes)
   const uint32_t a = i & 1 ? v.y : v.x, b = i & 1 ? v.w : v.z;
   return i & 2 ? b : a;
